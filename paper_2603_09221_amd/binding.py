@@ -1,4 +1,4 @@
-"""ctypes binding of the C-ABI library (include/ttc_lqr.h): argument marshalling only.
+"""ctypes binding of the C-ABI library (include/ttc_lqr.h, include/ttc_attention.h): argument marshalling only.
 
 PyTorch is used for device memory and streams; every step of the path runs in the HIP library.
 The library must have been built (``python -c "import __graft_entry__ as g; g.build()"``); there is
@@ -7,6 +7,7 @@ no fallback: a missing library raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from ctypes import c_char_p, c_int, c_int32, c_int64, c_size_t, c_void_p
 
@@ -28,6 +29,8 @@ EXPORTS = ("ttc_lqr_workspace_bytes", "ttc_lqr_solve", "ttc_lqr_solve_squares", 
            "ttc_lqr_backward", "ttc_lqr_backward_workspace_bytes",
            "ttc_lqr_backward_tv", "ttc_lqr_backward_tv_workspace_bytes", "ttc_lqr_backward_cxt", "ttc_lqr_backward_cxt_workspace_bytes", "ttc_block_workspace_bytes", "ttc_block_forward",
            "ttc_status_string", "ttc_version")
+ATTENTION_EXPORTS = ("ttc_rope", "ttc_rope_backward", "ttc_rope_table", "ttc_kv_page_bytes", "ttc_kv_append", "ttc_kv_read",
+                     "ttc_attention_workspace_bytes", "ttc_attention")
 
 
 class Problem(ctypes.Structure):
@@ -78,6 +81,32 @@ CXT_GRADS = ("gsA", "gsB", "gsQ", "gsQf", "grinv", "glgA", "glgB", "glgQ", "gx0"
 
 class CxtGrads(ctypes.Structure):
     _fields_ = [(k, c_void_p) for k in CXT_GRADS]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("tokens", c_int64), ("heads", c_int32), ("d", c_int32), ("rot", c_int32), ("dtype", c_int32),
+                ("layout", c_int32), ("x", c_void_p), ("y", c_void_p), ("x_token", c_int64), ("x_head", c_int64),
+                ("y_token", c_int64), ("y_head", c_int64), ("positions", c_void_p), ("table", c_void_p), ("table_rows", c_int64)]
+
+
+class KvCache(ctypes.Structure):
+    _fields_ = [("data", c_void_p), ("pages", c_int64), ("heads", c_int32), ("d", c_int32), ("page", c_int32)]
+
+
+class KvAppend(ctypes.Structure):
+    _fields_ = [("cache", KvCache), ("tokens", c_int64), ("dtype", c_int32), ("rot", c_int32), ("layout", c_int32),
+                ("k", c_void_p), ("v", c_void_p), ("k_token", c_int64), ("k_head", c_int64), ("v_token", c_int64),
+                ("v_head", c_int64), ("slots", c_void_p), ("positions", c_void_p), ("table", c_void_p), ("table_rows", c_int64),
+                ("q", c_void_p), ("q_out", c_void_p), ("heads_q", c_int32), ("q_token", c_int64), ("q_head", c_int64),
+                ("q_out_token", c_int64), ("q_out_head", c_int64)]
+
+
+class Attention(ctypes.Structure):
+    _fields_ = [("cache", KvCache), ("sequences", c_int64), ("tokens", c_int64), ("heads_q", c_int32), ("dtype", c_int32),
+                ("causal", c_int32), ("window", c_int32), ("scale", ctypes.c_float), ("max_q", c_int32), ("max_kv", c_int32),
+                ("q", c_void_p), ("out", c_void_p), ("lse", c_void_p), ("q_token", c_int64), ("q_head", c_int64),
+                ("out_token", c_int64), ("out_head", c_int64), ("cu_q", c_void_p), ("kv_len", c_void_p),
+                ("block_table", c_void_p), ("table_stride", c_int64)]
 
 
 class TtcError(RuntimeError):
@@ -153,6 +182,22 @@ def load():
     lib.ttc_block_forward.restype = c_int
     lib.ttc_block_forward.argtypes = [ctypes.POINTER(Block), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                       c_size_t, c_void_p]
+    lib.ttc_rope.restype = c_int
+    lib.ttc_rope.argtypes = [ctypes.POINTER(Rope), c_void_p]
+    lib.ttc_rope_backward.restype = c_int
+    lib.ttc_rope_backward.argtypes = [ctypes.POINTER(Rope), c_void_p]
+    lib.ttc_rope_table.restype = c_int
+    lib.ttc_rope_table.argtypes = [c_void_p, c_int64, c_int32, c_void_p, ctypes.c_double, c_void_p]
+    lib.ttc_kv_page_bytes.restype = c_size_t
+    lib.ttc_kv_page_bytes.argtypes = [c_int32, c_int32]
+    lib.ttc_kv_append.restype = c_int
+    lib.ttc_kv_append.argtypes = [ctypes.POINTER(KvAppend), c_void_p]
+    lib.ttc_kv_read.restype = c_int
+    lib.ttc_kv_read.argtypes = [ctypes.POINTER(KvCache), c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_void_p]
+    lib.ttc_attention_workspace_bytes.restype = c_size_t
+    lib.ttc_attention_workspace_bytes.argtypes = [ctypes.POINTER(Attention)]
+    lib.ttc_attention.restype = c_int
+    lib.ttc_attention.argtypes = [ctypes.POINTER(Attention), c_void_p, c_size_t, c_void_p]
     lib.ttc_status_string.restype = c_char_p
     lib.ttc_status_string.argtypes = [c_int]
     lib.ttc_version.restype = c_int
@@ -554,4 +599,259 @@ def ttc_block_forward(x_in, weights, T, *, eps=1e-5, want_h0=False, want_o=False
         workspace = _scratch(need, dev, stream)
     _check(lib.ttc_block_forward(ctypes.byref(blk), _ptr(x_in), _ptr(out["x_out"]), _ptr(out.get("h0")), _ptr(out.get("o")),
                                  _ptr(out["info"]), c_void_p(workspace.data_ptr()), workspace.numel(), _stream_ptr(stream)))
+    return out
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# rotary positions, the cache in 4 bits, attention over it (include/ttc_attention.h)
+
+_ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+
+
+def _rope_layout(layout):
+    code = _ROPE_LAYOUTS.get(layout)
+    if code is None:
+        raise ValueError("layout must be 'half' or 'interleaved'")
+    return code
+
+
+def _heads_strides(t, name, tokens=None, heads=None, d=None, dtype=None):
+    """(token stride, head stride) of a (tokens, heads, d) tensor whose heads are contiguous, after its shape and type were checked."""
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name}: expected (tokens, heads, d) with contiguous heads")
+    for have, want, what in ((t.shape[0], tokens, "tokens"), (t.shape[1], heads, "heads"), (t.shape[2], d, "entries a head")):
+        if want is not None and have != want:
+            raise ValueError(f"{name}: {have} {what}, expected {want}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name}: expected {dtype}")
+    return t.stride(0), t.stride(1)
+
+
+def _vector(t, n, dtype, name):
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of {n}")
+    return t.data_ptr()
+
+
+def _same_device(dev, *tensors):
+    for t in tensors:
+        if t is not None and t.device != dev:
+            raise ValueError("all tensors must be on one device")
+
+
+def _rope_table(table, d):
+    if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+        raise ValueError("table: expected a contiguous float32 (rows, rot / 2, 2) tensor")
+    if 2 * table.shape[1] > d:
+        raise ValueError("table: more entries rotated than a head has")
+    return table.data_ptr(), table.shape[0], 2 * table.shape[1]
+
+
+def _new(shape, dtype, dev, stream):
+    """A result tensor, from the memory of the stream that the kernels run on."""
+    if stream is None or stream == torch.cuda.current_stream():
+        return torch.empty(shape, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=dev)
+
+
+def rope_frequencies(rot, *, base=10000.0, scaling=None, factor=1.0, trained=None, fast=32.0, slow=1.0):
+    """(frequencies, scale) for ttc_rope_table: rot / 2 angles per position, float64 on the host, and the factor on cos and sin.
+
+    scaling None: base^(-2i/rot).  For contexts `factor` times as long as the `trained` one:
+      "linear"  positions are compressed: every frequency divided by factor.
+      "base"    the base grows to base * factor^(rot/(rot-2)): the highest frequency stays, the lowest is divided by factor.
+      "bands"   frequencies that turn more than `fast` times within `trained` positions stay, those that turn less than `slow`
+                times are divided by factor, those in between are mixed linearly over their index; the scale is 0.1 ln(factor) + 1."""
+    if rot < 2 or rot % 2 or factor < 1.0 or not base > 1.0:
+        raise ValueError("rot must be even and positive, factor >= 1, base > 1")
+    i = torch.arange(rot // 2, dtype=torch.float64)
+    if scaling == "base":
+        if rot < 4:
+            raise ValueError("scaling 'base' needs rot >= 4")
+        base = base * factor ** (rot / (rot - 2))
+    freqs = torch.tensor(base, dtype=torch.float64) ** (-2.0 * i / rot)
+    if scaling in (None, "base"):
+        return freqs, 1.0
+    if scaling == "linear":
+        return freqs / factor, 1.0
+    if scaling != "bands":
+        raise ValueError("scaling must be None, 'linear', 'base' or 'bands'")
+    if not trained or not fast > slow > 0:
+        raise ValueError("scaling 'bands' needs the trained length, and fast > slow > 0")
+
+    def index(turns):  # of the frequency that turns so often within the trained length
+        return rot * math.log(trained / (2.0 * math.pi * turns)) / (2.0 * math.log(base))
+
+    lo, hi = max(0, math.floor(index(fast))), min(rot // 2 - 1, math.ceil(index(slow)))
+    mix = ((i - lo) / max(hi - lo, 0.001)).clamp(0.0, 1.0)
+    return freqs * (1.0 - mix) + freqs / factor * mix, 0.1 * math.log(factor) + 1.0
+
+
+def ttc_rope_table(rows, freqs, *, scale=1.0, device="cuda", out=None, stream=None):
+    """float32 table (rows, pairs, 2) of scale * cos and scale * sin of position * freqs (pairs, float64; see rope_frequencies)."""
+    freqs = freqs.to(device=device, dtype=torch.float64).contiguous()
+    pairs = freqs.shape[0]
+    if out is None:
+        out = _new((rows, pairs, 2), torch.float32, freqs.device, stream)
+    elif tuple(out.shape) != (rows, pairs, 2) or out.dtype != torch.float32 or not out.is_contiguous() or out.device != freqs.device:
+        raise ValueError("out: expected a contiguous float32 (rows, pairs, 2) tensor on the frequencies' device")
+    if stream is not None and stream != torch.cuda.current_stream():
+        stream.wait_stream(torch.cuda.current_stream())  # the frequencies were copied there
+        freqs.record_stream(stream)
+    _check(load().ttc_rope_table(out.data_ptr(), rows, pairs, freqs.data_ptr(), scale, _stream_ptr(stream)))
+    return out
+
+
+def _rope(call, x, positions, table, layout, out, stream):
+    dtype = _in_dtype(x)
+    x_token, x_head = _heads_strides(x, "x")
+    tokens, heads, d = x.shape
+    table_ptr, rows, rot = _rope_table(table, d)
+    pos = _vector(positions, tokens, torch.int64, "positions")
+    _same_device(x.device, positions, table, out)
+    if out is None:
+        out = _new((tokens, heads, d), x.dtype, x.device, stream)
+    y_token, y_head = _heads_strides(out, "out", tokens, heads, d, x.dtype)
+    if tokens and heads and d:
+        _check(call(Rope(tokens, heads, d, rot, dtype, _rope_layout(layout), x.data_ptr(), out.data_ptr(), x_token, x_head, y_token,
+                         y_head, pos, table_ptr, rows), _stream_ptr(stream)))
+    return out
+
+
+def ttc_rope(x, positions, table, *, layout="half", out=None, stream=None):
+    """x (tokens, heads, d) with the first 2 * table.shape[1] entries of each head turned to the tokens' positions (int64); float32 or
+    bfloat16, any strides with contiguous heads (so also a part of a fused projection).  out may be x."""
+    return _rope(load().ttc_rope, x, positions, table, layout, out, stream)
+
+
+def ttc_rope_backward(grad, positions, table, *, layout="half", out=None, stream=None):
+    """The gradient of a loss with respect to ttc_rope's x, from grad, the one with respect to its result."""
+    return _rope(load().ttc_rope_backward, grad, positions, table, layout, out, stream)
+
+
+def ttc_kv_page_bytes(d, page):
+    """Bytes of one head of one page of `page` tokens; 0 if d or page is not supported."""
+    return load().ttc_kv_page_bytes(d, page)
+
+
+def make_kv_cache(pages, heads, d, page, device="cuda"):
+    """An empty cache: (pages, heads, ttc_kv_page_bytes(d, page)) bytes, all zero.  What describes a cache everywhere is this tensor and d."""
+    nbytes = ttc_kv_page_bytes(d, page)
+    if not nbytes:
+        raise ValueError("d must be 64, 128 or 256, page 16, 32, 64, 128 or 256")
+    return torch.zeros((pages, heads, nbytes), dtype=torch.uint8, device=device)
+
+
+def _kv_cache(cache, d):
+    if cache.dtype != torch.uint8 or cache.dim() != 3 or not cache.is_contiguous():
+        raise ValueError("cache: expected a contiguous uint8 (pages, heads, bytes) tensor")
+    pages, heads, nbytes = cache.shape
+    page = nbytes // (d + d // 16)
+    if page * (d + d // 16) != nbytes:
+        raise ValueError("cache: its pages are not of heads of %d" % d)
+    return KvCache(cache.data_ptr(), pages, heads, d, page)
+
+
+def ttc_kv_append(cache, k, v, slots, positions=None, table=None, *, layout="half", q=None, q_out=None, stream=None):
+    """New tokens' keys (turned to their positions, unless table is None) and values into the cache at slots (int64; page number *
+    tokens a page + token of the page; -1 leaves a token out); all of k, v (tokens, heads, d) and q (tokens, heads_q, d) float32 or
+    bfloat16.  Returns the turned queries (q_out, which may be q; None without q)."""
+    dtype = _in_dtype(k, v, q, q_out)
+    k_token, k_head = _heads_strides(k, "k")
+    tokens, heads, d = k.shape
+    v_token, v_head = _heads_strides(v, "v", tokens, heads, d)
+    kv = _kv_cache(cache, d)
+    if kv.heads != heads:
+        raise ValueError("cache: %d heads, expected %d" % (kv.heads, heads))
+    at = _vector(slots, tokens, torch.int64, "slots")
+    pos, table_ptr, rows, rot = None, None, 0, 0
+    if table is not None:
+        table_ptr, rows, rot = _rope_table(table, d)
+        pos = _vector(positions, tokens, torch.int64, "positions")
+    _same_device(cache.device, k, v, slots, positions, table, q, q_out)
+    heads_q = q_token = q_head = qo_token = qo_head = 0
+    if q is not None:
+        q_token, q_head = _heads_strides(q, "q", tokens, None, d)
+        heads_q = q.shape[1]
+        if q_out is None:
+            q_out = _new(q.shape, q.dtype, q.device, stream)
+        qo_token, qo_head = _heads_strides(q_out, "q_out", tokens, heads_q, d)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if tokens:
+        _check(load().ttc_kv_append(KvAppend(kv, tokens, dtype, rot, _rope_layout(layout), k.data_ptr(), v.data_ptr(), k_token, k_head,
+                                             v_token, v_head, at, pos, table_ptr, rows, _ptr(q), _ptr(q_out), heads_q, q_token, q_head,
+                                             qo_token, qo_head), _stream_ptr(stream)))
+    return q_out
+
+
+def ttc_kv_read(cache, slots, d, *, dtype=torch.bfloat16, out=None, stream=None):
+    """(k, v), each (n, heads, d): the numbers that the cache holds at n slots (int64); zeros for a slot outside the cache."""
+    kv = _kv_cache(cache, d)
+    at = _vector(slots, slots.shape[0], torch.int64, "slots")
+    code = _IN_DTYPES.get(dtype)
+    if code is None:
+        raise ValueError("dtype must be float32 or bfloat16")
+    shape = (slots.shape[0], kv.heads, d)
+    k, v = out if out is not None else (_new(shape, dtype, cache.device, stream), _new(shape, dtype, cache.device, stream))
+    for t in (k, v):
+        if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+            raise ValueError("out: expected two contiguous %s tensors of %s" % (dtype, shape))
+    _same_device(cache.device, slots, k, v)
+    if shape[0]:
+        _check(load().ttc_kv_read(kv, at, shape[0], code, k.data_ptr(), v.data_ptr(), _stream_ptr(stream)))
+    return k, v
+
+
+def ttc_attention(q, cache, block_table, kv_len, *, cu_q=None, max_q=None, max_kv=None, scale=None, causal=True, window=0,
+                  want_lse=True, out=None, workspace=None, stream=None):
+    """{"out": (tokens, heads_q, d) like q, "lse": (tokens, heads_q) float32} of the queries of new tokens over a cache in 4 bits.
+
+    Sequence s has kv_len[s] tokens in the cache (int32), the new ones the last of them, on the pages block_table[s] (int32), and the
+    rows cu_q[s] .. cu_q[s+1]-1 of q (int32; without cu_q one row each).  max_q and max_kv bound the sequences' numbers of new and of all
+    tokens (with cu_q max_q is needed; max_kv defaults to what block_table has room for): the work is shared out by them.  scale
+    defaults to d^-1/2.  `out` may carry tensors under the same names; `workspace` a uint8 tensor."""
+    lib = load()
+    dtype = _in_dtype(q)
+    q_token, q_head = _heads_strides(q, "q")
+    tokens, heads_q, d = q.shape
+    kv = _kv_cache(cache, d)
+    if block_table.dtype != torch.int32 or block_table.dim() != 2 or (block_table.shape[1] > 1 and block_table.stride(1) != 1):
+        raise ValueError("block_table: expected an int32 (sequences, pages) tensor with contiguous rows")
+    sequences, width = block_table.shape
+    lens = _vector(kv_len, sequences, torch.int32, "kv_len")
+    room = width * kv.page
+    if max_kv is None:
+        max_kv = room
+    elif max_kv > room:
+        raise ValueError("max_kv: block_table has room for %d tokens" % room)
+    cu = None
+    if cu_q is not None:
+        cu = _vector(cu_q, sequences + 1, torch.int32, "cu_q")
+        if max_q is None:
+            raise ValueError("max_q is needed with cu_q")
+    else:
+        if tokens != sequences:
+            raise ValueError("q: %d rows for %d sequences" % (tokens, sequences))
+        max_q = 1
+    _same_device(cache.device, q, block_table, kv_len, cu_q, workspace)
+    out = dict(out or {})
+    if "out" not in out:
+        out["out"] = _new(q.shape, q.dtype, q.device, stream)
+    y = out["out"]
+    out_token, out_head = _heads_strides(y, "out", tokens, heads_q, d, q.dtype)
+    if want_lse and "lse" not in out:
+        out["lse"] = _new((tokens, heads_q), torch.float32, q.device, stream)
+    lse = out.get("lse")
+    if lse is not None and (tuple(lse.shape) != (tokens, heads_q) or lse.dtype != torch.float32 or not lse.is_contiguous()):
+        raise ValueError("lse: expected a contiguous float32 (tokens, heads_q) tensor")
+    _same_device(cache.device, y, lse)
+    att = Attention(kv, sequences, tokens, heads_q, dtype, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, max_q, max_kv,
+                    q.data_ptr(), y.data_ptr(), _ptr(lse), q_token, q_head, out_token, out_head, cu, lens, block_table.data_ptr(),
+                    block_table.stride(0))
+    need = lib.ttc_attention_workspace_bytes(att)
+    if need and workspace is None:
+        workspace = _scratch(need, q.device, stream)
+    _check(lib.ttc_attention(att, _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream)))
     return out

@@ -40,7 +40,11 @@ UNITS = [("ttc_api.hip", None),
          ("k_tv_small.hip", None),
          ("k_cxt.hip", None),
          ("k_cxt_bwd.hip", None),
-         ("k_block.hip", None)]
+         ("k_block.hip", None),
+         ("ttc_api_attention.hip", None),
+         ("k_rope.hip", None),
+         ("k_kv.hip", None),
+         ("k_attention.hip", (64, 128, 256))]
 
 # Per (source, state size) compile flags: wavefronts of one 16-wide block each (twice as many per problem) instead of
 # two, where measured faster.  The Riccati and squaring kernels own matrices by columns: at d = 64 one column tile a wavefront

@@ -1,0 +1,20 @@
+// attention_kernel, attention_join_kernel (ttc_attention), for heads of TTC_D entries.
+#include "ttc_attention.hpp"
+#include "ttc_serve_launch.hpp"
+
+namespace ttc {
+
+template <typename T>
+static hipError_t launch(const AttentionArgs& p, hipStream_t st) {
+  hipLaunchKernelGGL((attention_kernel<T, TTC_D>), dim3((unsigned)(p.items * p.spans)), dim3(64 * ATT_WAVES), 0, st, p);
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess || p.spans <= 1) return e;
+  hipLaunchKernelGGL((attention_join_kernel<T, TTC_D>), dim3((unsigned)p.items), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
+template <>
+hipError_t launch_attention<TTC_D>(const AttentionArgs& p, bool bf16, hipStream_t st) {
+  return bf16 ? launch<unsigned short>(p, st) : launch<float>(p, st);
+}
+
+}  // namespace ttc
