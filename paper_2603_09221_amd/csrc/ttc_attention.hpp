@@ -12,6 +12,9 @@
 
 namespace ttc {
 
+#ifndef ATT_OCC
+#define ATT_OCC 3
+#endif
 // The row tile of a workgroup: its sequence's numbers and this lane's row
 struct AttTile {
   int len;          // tokens in the cache
@@ -19,6 +22,7 @@ struct AttTile {
   int64_t first_q;  // row of q of its first new token
   int first, last;  // tokens that the lane's row sees: first .. last (none where last < first)
   int lo, hi;       // all that the tile's rows see lies in lo .. hi-1
+  int all_lo, all_hi;  // and every one of them sees all of all_lo .. all_hi-1
 };
 
 __device__ __forceinline__ AttTile att_tile(const AttentionArgs& p, int64_t seq, int tile, int row) {
@@ -42,12 +46,15 @@ __device__ __forceinline__ AttTile att_tile(const AttentionArgs& p, int64_t seq,
     t.last = min(shift + r / p.group, t.len - 1);
     t.first = a.window ? max(t.last - a.window + 1, 0) : 0;
     t.hi = min(shift + r1 / p.group, t.len - 1) + 1;
-    t.lo = a.window ? max(min(shift + tile * ATT_ROWS / p.group, t.len - 1) - a.window + 1, 0) : 0;
+    const int first = min(shift + tile * ATT_ROWS / p.group, t.len - 1);  // what the first row sees last
+    t.lo = a.window ? max(first - a.window + 1, 0) : 0;
+    t.all_lo = a.window ? max(t.hi - a.window, 0) : 0;
+    t.all_hi = first + 1;
   } else {
     t.last = t.len - 1;
     t.first = 0;
-    t.hi = t.len;
-    t.lo = 0;
+    t.hi = t.all_hi = t.len;
+    t.lo = t.all_lo = 0;
   }
   if (r >= t.rows) t.last = -1;
   if (r1 < tile * ATT_ROWS) t.hi = 0;
@@ -75,17 +82,84 @@ __device__ __forceinline__ srv_bf16x8 att_widen(uint32_t code, float scale) {
 // 128 in every byte that is 255
 __device__ __forceinline__ uint32_t att_full_bytes(uint32_t x) { return x & ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
+// What a workgroup reads the cache with, the same for all of its lanes
+struct AttSource {
+  const unsigned char* cache;  // the workgroup's head of page 0
+  const int32_t* pages;        // the sequence's
+  int64_t page_stride;
+  uint32_t page_count;
+  int page_tokens, log_page, end;
+  // the pages of the four sixteens from token n0 on; those at or behind `end` are none
+  __device__ __forceinline__ void look_up(int n0, int (&page)[4]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int n = n0 + 16 * i;
+      const int at = pages[min(n, end - 1) >> log_page];
+      page[i] = n < end && (uint32_t)at < page_count ? at : -1;
+    }
+  }
+  __device__ __forceinline__ const unsigned char* base(int page) const { return cache + max(page, 0) * page_stride; }
+};
+
+// A wavefront's share of one step of 64 tokens, as it lies in the cache: lane (c, g) has the entries g*D/4 .. of the keys of token c of each
+// sixteen, and entries c*D/16 .. of the values of tokens 4g .. 4g+3.  `there`: bit i is set if the page of sixteen i is in the cache.
+template <int D>
+struct AttKeys {
+  typedef KvParts<D> P;
+  typedef uint32_t word_t __attribute__((ext_vector_type(D / 32)));
+  word_t code[4];
+  uint32_t exp[4];
+  int there;
+  __device__ __forceinline__ void load(const AttSource& s, const int (&page)[4], int n0, int c, int g) {
+    there = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      there |= page[i] >= 0 ? 1 << i : 0;
+      const unsigned char* base = s.base(page[i]);
+      const uint32_t token = ((n0 + 16 * i) & (s.page_tokens - 1)) + c;
+      code[i] = *reinterpret_cast<const word_t*>(base + (token * P::TOKEN + g * (D / 8)));
+      const uint32_t at = P::key_exps(s.page_tokens) + token * P::BLOCKS;
+      exp[i] = D == 256 ? *reinterpret_cast<const unsigned short*>(base + (at + 2 * g)) : base[at + (D == 64 ? g / 2 : g)];
+    }
+  }
+};
+template <int D>
+struct AttValues {
+  typedef KvParts<D> P;
+  typedef uint32_t word_t __attribute__((ext_vector_type(D / 32)));
+  word_t code[4];
+  uint32_t exp[4];
+  __device__ __forceinline__ void load(const AttSource& s, const int (&page)[4], int n0, int c, int g) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned char* base = s.base(page[i]);
+      const uint32_t four = ((n0 + 16 * i) & (s.page_tokens - 1)) / 4 + g;
+      code[i] = *reinterpret_cast<const word_t*>(base + (P::values(s.page_tokens) + (four * 16 + c) * (4 * P::LANE)));
+      exp[i] = *reinterpret_cast<const uint32_t*>(base + (P::value_exps(s.page_tokens) + (four * P::BLOCKS + c * (D / 16) / 32) * 4));
+    }
+  }
+};
+
+// entries e, e+1 of token k of the four whose codes a lane holds: E/2 bytes a token
+template <int E, typename W>
+__device__ __forceinline__ srv_bf16x2 att_value_pair(const W& code, int k, int e, float scale) {
+  const int byte = k * (E / 2) + e / 2;
+  const uint32_t word = code[byte / 4];
+  switch (byte % 4) {
+    case 0: return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 0);
+    case 1: return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 1);
+    case 2: return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 2);
+    default: return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 3);
+  }
+}
+
 template <typename T, int D>
-__global__ void __launch_bounds__(64 * ATT_WAVES) attention_kernel(const AttentionArgs p) {
+__global__ void __launch_bounds__(64 * ATT_WAVES, ATT_OCC) attention_kernel(const AttentionArgs p) {
   constexpr bool BF16 = sizeof(T) == 2;
   constexpr int TERMS = BF16 ? 1 : 3;   // bfloat16 parts of a query and of a weight
   constexpr int KS = D / 32;            // products of 32 entries that a score takes
-  constexpr int KW = D / 32;            // words of codes of a lane's share of a key: D/4 entries
   constexpr int E = D / 16;             // entries of a value that a lane holds
-  constexpr int VW = D / 32;            // words of four tokens' values of one lane
   typedef KvParts<D> P;
-  typedef uint32_t kw_t __attribute__((ext_vector_type(KW)));
-  typedef uint32_t vw_t __attribute__((ext_vector_type(VW)));
   const ttc_attention_t& a = p.a;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
   const int span = blockIdx.x % p.spans;
@@ -119,63 +193,80 @@ __global__ void __launch_bounds__(64 * ATT_WAVES) attention_kernel(const Attenti
   srv_floatx4 o[E] = {};
   float m = -INFINITY, l = 0.f;
   const float to_log2 = a.scale * 1.44269504088896340736f;
-  const int log_page = __builtin_ctz(a.cache.page), page_bytes = P::bytes(a.cache.page);
-  const int32_t* pages = a.block_table + seq * a.table_stride;
-  const unsigned char* cache = static_cast<const unsigned char*>(a.cache.data);
+  AttSource src;
+  const int page_bytes = P::bytes(a.cache.page);
+  src.cache = static_cast<const unsigned char*>(a.cache.data) + (int64_t)head * page_bytes;
+  src.pages = a.block_table + seq * a.table_stride;
+  src.page_stride = (int64_t)a.cache.heads * page_bytes;
+  src.page_count = (uint32_t)min(a.cache.pages, (int64_t)INT32_MAX);
+  src.page_tokens = a.cache.page;
+  src.log_page = __builtin_ctz(a.cache.page);
+  src.end = end;
 
-  for (int n0 = begin + wave * ATT_STEP; n0 < end; n0 += ATT_STEP * ATT_WAVES) {
-    const unsigned char* base[4];
-    int in[4];      // token of the page that the sixteen begin with
-    bool there[4];  // whether the sixteen are in the cache at all
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int n = n0 + 16 * i;
-      const int page = n < end ? pages[n >> log_page] : -1;
-      there[i] = page >= 0 && page < a.cache.pages;
-      in[i] = n & (a.cache.page - 1);
-      base[i] = cache + ((int64_t)(there[i] ? page : 0) * a.cache.heads + head) * page_bytes;
-    }
+  // Keys and values of the next step are read into the registers that this step has just done with, and the page numbers of the step
+  // after it: the reads are under way during the other product and the softmax, and while other wavefronts of the SIMD work.
+  constexpr int STRIDE = ATT_STEP * ATT_WAVES;
+  AttKeys<D> keys;
+  AttValues<D> values;
+  int page[4], n0 = begin + wave * ATT_STEP;
+  if (n0 < end) {
+    src.look_up(n0, page);
+    keys.load(src, page, n0, c, g);
+    values.load(src, page, n0, c, g);
+    src.look_up(n0 + STRIDE, page);
+  }
+  for (; n0 < end; n0 += STRIDE) {
+    const bool more = n0 + STRIDE < end;
+    const int there = keys.there;
     // scores: S^T = K Q^T, sixteen tokens at a time
-    float s[4][4];
+    srv_floatx4 z[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int token = in[i] + c;
-      const kw_t code = *reinterpret_cast<const kw_t*>(base[i] + token * P::TOKEN + g * (D / 8));
-      const unsigned char* ke = base[i] + P::key_exps(a.cache.page) + token * P::BLOCKS;
-      srv_floatx4 z = {};
+      z[i] = srv_floatx4{};
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        const float scale = srv_scale(ke[(g * (D / 4) + 8 * k) / 32]);
-        const srv_bf16x8 key = att_widen(code[k], scale);
+        const srv_bf16x8 key = att_widen(keys.code[i][k], srv_scale((keys.exp[i] >> (D == 256 ? 8 * (k / 4) : 0)) & 255));
 #pragma unroll
-        for (int x = TERMS - 1; x >= 0; --x) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[x][k], z, 0, 0, 0);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int n = n0 + 16 * i + 4 * g + j;
-        s[i][j] = there[i] && n >= t.first && n <= t.last ? z[j] * to_log2 : -INFINITY;
+        for (int x = TERMS - 1; x >= 0; --x) z[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[x][k], z[i], 0, 0, 0);
       }
     }
-    // running maximum and sum of the row: the lane's sixteen tokens, then the four lanes that share the row
-    float top = m;
+    if (more) keys.load(src, page, n0 + STRIDE, c, g);
+    if (n0 < t.all_lo || n0 + ATT_STEP > t.all_hi || there != 15) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int n = n0 + 16 * i + 4 * g + j;
+          z[i][j] = (there >> i & 1) && n >= t.first && n <= t.last ? z[i][j] * to_log2 : -INFINITY;
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z[i] *= to_log2;
+    }
+    // The maximum that weights are relative to moves only when a score passes it by 8 (weights stay below 2^8, which costs float32 sums
+    // nothing): most steps need no exchange between lanes and no rescaling.
+    float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) top = fmaxf(top, s[i][j]);
-    top = fmaxf(top, __shfl_xor(top, 16, 64));
-    top = fmaxf(top, __shfl_xor(top, 32, 64));
-    const float zero = top == -INFINITY ? 0.f : top;  // (a row that has seen nothing yet)
-    const float shrink = __builtin_amdgcn_exp2f(m - zero);
-    m = top;
-    l *= shrink;
+      for (int j = 0; j < 4; ++j) top = fmaxf(top, z[i][j]);
+    if (__builtin_amdgcn_ballot_w64(top > m + 8.f)) {
+      top = fmaxf(m, top);
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float shrink = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));  // (a row that has seen nothing yet)
+      m = top;
+      l *= shrink;
 #pragma unroll
-    for (int i = 0; i < E; ++i) o[i] *= shrink;
+      for (int i = 0; i < E; ++i) o[i] *= shrink;
+    }
+    const float zero = m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        s[i][j] = __builtin_amdgcn_exp2f(s[i][j] - zero);
-        l += s[i][j];
+        z[i][j] = __builtin_amdgcn_exp2f(z[i][j] - zero);
+        l += z[i][j];
       }
     // O^T += V^T P^T, 32 tokens at a time: lane (c, g) has tokens 4g .. 4g+3 of two sixteens
 #pragma unroll
@@ -184,18 +275,11 @@ __global__ void __launch_bounds__(64 * ATT_WAVES) attention_kernel(const Attenti
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         __bf16 part[TERMS];
-        att_split<TERMS>(s[2 * h + k / 4][k % 4], part);
+        att_split<TERMS>(z[2 * h + k / 4][k % 4], part);
 #pragma unroll
         for (int x = 0; x < TERMS; ++x) w[x][k] = part[x];
       }
-      vw_t code[2];
-      uint32_t exps[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int four = in[2 * h + i] / 4 + g;
-        code[i] = *reinterpret_cast<const vw_t*>(base[2 * h + i] + P::values(a.cache.page) + (four * 16 + c) * (4 * P::LANE));
-        exps[i] = *reinterpret_cast<const uint32_t*>(base[2 * h + i] + P::value_exps(a.cache.page) + (four * P::BLOCKS + c * E / 32) * 4);
-      }
+      uint32_t exps[2] = {values.exp[2 * h], values.exp[2 * h + 1]};
       // A weight of 0 takes out any number, but not NaN.  Blocks of NaN are rare: they are read as numbers, and what the rows that
       // see them get is made NaN by a product of its own.
       const uint32_t nan0 = att_full_bytes(exps[0]), nan1 = att_full_bytes(exps[1]);
@@ -205,7 +289,7 @@ __global__ void __launch_bounds__(64 * ATT_WAVES) attention_kernel(const Attenti
         for (int k = 0; k < 8; ++k) {
           const int i = 2 * h + k / 4, n = n0 + 16 * i + 4 * g + k % 4;
           bad[k] = static_cast<__bf16>((k < 4 ? nan0 : nan1) >> (8 * (k % 4)) & 128 ? 1.f : 0.f);
-          seen[k] = static_cast<__bf16>(there[i] && n >= t.first && n <= t.last ? 1.f : 0.f);
+          seen[k] = static_cast<__bf16>((there >> i & 1) && n >= t.first && n <= t.last ? 1.f : 0.f);
         }
         const srv_floatx4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bad, seen, srv_floatx4{}, 0, 0, 0);
 #pragma unroll
@@ -215,30 +299,25 @@ __global__ void __launch_bounds__(64 * ATT_WAVES) attention_kernel(const Attenti
         exps[0] ^= nan0;
         exps[1] ^= nan1;
       }
-      srv_bf16x8 v[E];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float scale = srv_scale((exps[k / 4] >> (8 * (k % 4))) & 255);
+      for (int e = 0; e < E; e += 2) {
+        srv_bf16x8 v0, v1;
 #pragma unroll
-        for (int e = 0; e < E; e += 2) {
-          // token k % 4 of the four: E/2 bytes of codes each
-          const int byte = (k % 4) * (E / 2) + e / 2;
-          const uint32_t word = code[k / 4][byte / 4];
-          srv_bf16x2 two;
-          switch (byte % 4) {
-            case 0: two = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 0); break;
-            case 1: two = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 1); break;
-            case 2: two = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 2); break;
-            default: two = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, scale, 3); break;
-          }
-          v[e][k] = two[0];
-          v[e + 1][k] = two[1];
+        for (int k = 0; k < 8; ++k) {
+          const srv_bf16x2 two = att_value_pair<E>(values.code[2 * h + k / 4], k % 4, e, srv_scale((exps[k / 4] >> (8 * (k % 4))) & 255));
+          v0[k] = two[0];
+          v1[k] = two[1];
+        }
+#pragma unroll
+        for (int x = TERMS - 1; x >= 0; --x) {
+          o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, w[x], o[e], 0, 0, 0);
+          o[e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, w[x], o[e + 1], 0, 0, 0);
         }
       }
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-#pragma unroll
-        for (int x = TERMS - 1; x >= 0; --x) o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[e], w[x], o[e], 0, 0, 0);
+    }
+    if (more) {
+      values.load(src, page, n0 + STRIDE, c, g);
+      src.look_up(n0 + 2 * STRIDE, page);
     }
   }
   l += __shfl_xor(l, 16, 64);
@@ -268,6 +347,8 @@ __global__ void __launch_bounds__(64 * ATT_WAVES) attention_kernel(const Attenti
 #pragma unroll
     for (int e = 0; e < E; ++e) sum[e] += f * part_o[w][row][e0 + e];
   }
+  const int r = tile * ATT_ROWS + row;
+  if (r >= t.rows) return;
   if (p.spans > 1) {
     float* stat = p.part_stat + (item * p.spans + span) * (2 * ATT_ROWS);
     float* out = p.part_out + ((item * p.spans + span) * ATT_ROWS + row) * D + e0;
@@ -279,47 +360,72 @@ __global__ void __launch_bounds__(64 * ATT_WAVES) attention_kernel(const Attenti
     for (int e = 0; e < E; e += 4) *reinterpret_cast<srv_floatx4*>(out + e) = srv_floatx4{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
     return;
   }
-  const int r = tile * ATT_ROWS + row;
-  if (r >= t.rows) return;
+  const float f = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
   const int64_t token = t.first_q + r / p.group;
   const int h = head * p.group + r % p.group;
-  const float f = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
   T* y = static_cast<T*>(a.out) + token * a.out_token + (int64_t)h * a.out_head + e0;
 #pragma unroll
   for (int e = 0; e < E; ++e) y[e] = srv_narrow<T>(f * sum[e]);
   if (a.lse && threadIdx.x % 16 == 0) a.lse[token * a.heads_q + h] = (mm + __builtin_log2f(ll)) * 0.69314718055994530942f;
 }
 
-// The spans' results of one row tile
+// The spans' results of one row: a workgroup to a row of a tile, four entries to a thread, the spans dealt out among the threads that have the
+// same entries
 template <typename T, int D>
 __global__ void __launch_bounds__(256) attention_join_kernel(const AttentionArgs p) {
-  constexpr int E = D / 16;
+  constexpr int Q = D / 4, PARTS = 256 / Q;
   const ttc_attention_t& a = p.a;
-  const int64_t item = blockIdx.x;
+  const int row = blockIdx.x % p.join_rows;
+  const int64_t item = blockIdx.x / p.join_rows;
   const int tile = (int)(item % p.row_tiles), head = (int)(item / p.row_tiles % a.cache.heads);
   const int64_t seq = item / p.row_tiles / a.cache.heads;
   const AttTile t = att_tile(p, seq, tile, 0);
-  const int row = threadIdx.x / 16, e0 = (threadIdx.x % 16) * E, r = tile * ATT_ROWS + row;
+  const int r = tile * ATT_ROWS + row;
   if (r >= t.rows) return;
   const int used = t.hi > t.lo ? (t.hi - t.lo + p.span - 1) / p.span : 0;
-  const float* stat = p.part_stat + item * p.spans * (2 * ATT_ROWS);
-  const float* part = p.part_out + item * p.spans * ATT_ROWS * D;
-  float mm = -INFINITY, ll = 0.f, sum[E] = {};
-  for (int s = 0; s < used; ++s) mm = fmaxf(mm, stat[s * 2 * ATT_ROWS + row]);
-  const float zero = mm == -INFINITY ? 0.f : mm;
-  for (int s = 0; s < used; ++s) {
-    const float f = __builtin_amdgcn_exp2f(stat[s * 2 * ATT_ROWS + row] - zero);
-    ll += f * stat[s * 2 * ATT_ROWS + ATT_ROWS + row];
+  const int part = threadIdx.x / Q, e = threadIdx.x % Q * 4;
+  const float* stat = p.part_stat + item * p.spans * (2 * ATT_ROWS) + row;
+  const float* out = p.part_out + (item * p.spans * ATT_ROWS + row) * D + e;
+  // each part keeps a maximum of its own; rescaling happens once per span and thread
+  float m = -INFINITY, l = 0.f;
+  srv_floatx4 sum = {};
+#pragma unroll 4
+  for (int s = part; s < used; s += PARTS) {
+    const float ms = stat[s * 2 * ATT_ROWS], ls = stat[s * 2 * ATT_ROWS + ATT_ROWS];
+    const srv_floatx4 x = *reinterpret_cast<const srv_floatx4*>(out + (int64_t)s * ATT_ROWS * D);
+    const float top = fmaxf(m, ms), zero = top == -INFINITY ? 0.f : top;
+    const float f = __builtin_amdgcn_exp2f(m - zero), h = __builtin_amdgcn_exp2f(ms - zero);
+    m = top;
+    l = f * l + h * ls;
+    sum = f * sum + h * x;
+  }
+  __shared__ float part_m[PARTS], part_l[PARTS];
+  __shared__ srv_floatx4 part_o[PARTS][Q];
+  part_o[part][threadIdx.x % Q] = sum;
+  if (threadIdx.x % Q == 0) {
+    part_m[part] = m;
+    part_l[part] = l;
+  }
+  __syncthreads();
+  if (part) return;
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum[e] += f * part[(s * ATT_ROWS + row) * D + e0 + e];
+  for (int i = 1; i < PARTS; ++i) m = fmaxf(m, part_m[i]);
+  const float zero = m == -INFINITY ? 0.f : m;
+  l = 0.f;
+  sum = srv_floatx4{};
+#pragma unroll
+  for (int i = 0; i < PARTS; ++i) {
+    const float f = __builtin_amdgcn_exp2f(part_m[i] - zero);
+    l += f * part_l[i];
+    sum += f * part_o[i][threadIdx.x];
   }
   const int64_t token = t.first_q + r / p.group;
   const int h = head * p.group + r % p.group;
-  const float f = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
-  T* y = static_cast<T*>(a.out) + token * a.out_token + (int64_t)h * a.out_head + e0;
+  const float f = l > 0.f || l != l ? 1.f / l : 0.f;
+  T* y = static_cast<T*>(a.out) + token * a.out_token + (int64_t)h * a.out_head + e;
 #pragma unroll
-  for (int e = 0; e < E; ++e) y[e] = srv_narrow<T>(f * sum[e]);
-  if (a.lse && threadIdx.x % 16 == 0) a.lse[token * a.heads_q + h] = (mm + __builtin_log2f(ll)) * 0.69314718055994530942f;
+  for (int i = 0; i < 4; ++i) y[i] = srv_narrow<T>(f * sum[i]);
+  if (a.lse && threadIdx.x == 0) a.lse[token * a.heads_q + h] = (m + __builtin_log2f(l)) * 0.69314718055994530942f;
 }
 
 }  // namespace ttc

@@ -18,6 +18,7 @@ struct AttentionArgs {
   int32_t span;        // tokens of the context that one workgroup takes
   int32_t spans;       // for the longest context; with 1 the workgroup writes out itself
   int64_t items;       // sequences * heads * row_tiles
+  int32_t join_rows;   // rows of a tile that can be real
   float *part_out;     // (items, spans, ATT_ROWS, d) sums of exp2(s - m) v
   float *part_stat;    // (items, spans, 2, ATT_ROWS): m, sum of exp2(s - m)
 };
@@ -38,13 +39,14 @@ inline void plan_attention(AttentionArgs& p, int cus) {
   p.items = a.sequences * a.cache.heads * p.row_tiles;
   const int64_t most = visible_at_most(a, p.group), unit = ATT_STEP * ATT_WAVES;
   const int64_t units = (most + unit - 1) / unit;
-  // about four workgroups to a compute unit, as long as each has a step for every wavefront
-  int64_t spans = p.items > 0 ? (4 * cus + p.items - 1) / p.items : 1;
+  // about sixteen workgroups to a compute unit, as long as each has a step for every wavefront
+  int64_t spans = p.items > 0 ? (16 * cus + p.items - 1) / p.items : 1;
   spans = spans < 1 ? 1 : spans > units ? units : spans;
   const int64_t per = spans ? (units + spans - 1) / spans : 1;
   p.span = (int32_t)((per < 1 ? 1 : per) * unit);
   p.spans = (int32_t)((most + p.span - 1) / p.span);
   if (p.spans < 1) p.spans = 1;
+  p.join_rows = (int32_t)(rows < ATT_ROWS ? rows : ATT_ROWS);
   p.part_out = p.part_stat = nullptr;
 }
 
