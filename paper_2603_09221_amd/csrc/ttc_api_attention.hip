@@ -137,7 +137,7 @@ ttc_status_t ttc_attention(const ttc_attention_t* a, void* workspace, size_t wor
   if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return TTC_ERR_WORKSPACE;
   if (need) {
     p.part_out = static_cast<float*>(workspace);
-    p.part_stat = p.part_out + (uint64_t)p.items * p.spans * ttc::ATT_ROWS * a->cache.d;
+    p.part_stat = p.part_out + 2 * (uint64_t)p.workgroups * ttc::ATT_ROWS * a->cache.d;
   }
   const bool bf16 = a->dtype == TTC_BF16;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);

@@ -12,9 +12,6 @@
 
 namespace ttc {
 
-#ifndef ATT_OCC
-#define ATT_OCC 3
-#endif
 // The row tile of a workgroup: its sequence's numbers and this lane's row
 struct AttTile {
   int len;          // tokens in the cache
@@ -62,6 +59,41 @@ __device__ __forceinline__ AttTile att_tile(const AttentionArgs& p, int64_t seq,
   return t;
 }
 
+// units of 256 tokens of one item
+__device__ __forceinline__ uint32_t att_units(const AttTile& t) { return t.hi > t.lo ? (uint32_t)(t.hi - t.lo + ATT_UNIT - 1) / ATT_UNIT : 0; }
+
+// The entries (sequence, row tile) in their order, each of `heads` items of its number of units: all threads of a workgroup of 256
+// add them up, a run of entries to a thread.
+struct AttShares {
+  uint32_t total;   // units of all items
+  uint32_t before;  // of the entries before this thread's run
+  uint32_t own;     // of this thread's run
+  int first, last;  // the run: first .. last-1
+  __device__ __forceinline__ AttShares(const AttentionArgs& p, uint32_t (&wave_sum)[4]) {
+    const int run = (p.entries + 255) / 256;
+    first = min((int)threadIdx.x * run, p.entries);
+    last = min(first + run, p.entries);
+    own = 0;
+    for (int i = first; i < last; ++i) own += att_units(att_tile(p, i / p.row_tiles, i % p.row_tiles, 0));
+    own *= p.a.cache.heads;
+    uint32_t sum = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t x = __shfl_up(sum, o, 64);
+      sum += (int)(threadIdx.x & 63) >= o ? x : 0;
+    }
+    if ((threadIdx.x & 63) == 63) wave_sum[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    total = 0;
+    before = sum - own;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      before += w < (int)(threadIdx.x >> 6) ? wave_sum[w] : 0;
+      total += wave_sum[w];
+    }
+  }
+};
+
 // A float32 number as the sum of TERMS bfloat16 ones: one, rounded, or three that give every bit
 template <int TERMS>
 __device__ __forceinline__ void att_split(float x, __bf16 (&t)[TERMS]) {
@@ -85,20 +117,23 @@ __device__ __forceinline__ uint32_t att_full_bytes(uint32_t x) { return x & ((x 
 // What a workgroup reads the cache with, the same for all of its lanes
 struct AttSource {
   const unsigned char* cache;  // the workgroup's head of page 0
-  const int32_t* pages;        // the sequence's
+  const __attribute__((address_space(4))) int32_t* pages;  // the sequence's, through the scalar cache: nothing writes them meanwhile
   int64_t page_stride;
   uint32_t page_count;
   int page_tokens, log_page, end;
-  // the pages of the four sixteens from token n0 on; those at or behind `end` are none
+  // What the table says of the four sixteens from token n0 on, not yet looked at (whoever looks waits for it)
   __device__ __forceinline__ void look_up(int n0, int (&page)[4]) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int n = n0 + 16 * i;
-      const int at = pages[min(n, end - 1) >> log_page];
-      page[i] = n < end && (uint32_t)at < page_count ? at : -1;
-    }
+    for (int i = 0; i < 4; ++i) page[i] = pages[min(n0 + 16 * i, end - 1) >> log_page];
   }
-  __device__ __forceinline__ const unsigned char* base(int page) const { return cache + max(page, 0) * page_stride; }
+  // bit i is set if the page of sixteen i is in the cache
+  __device__ __forceinline__ int there(int n0, const int (&page)[4]) const {
+    int bits = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bits |= n0 + 16 * i < end && (uint32_t)page[i] < page_count ? 1 << i : 0;
+    return bits;
+  }
+  __device__ __forceinline__ const unsigned char* base(int page) const { return cache + ((uint32_t)page < page_count ? page : 0) * page_stride; }
 };
 
 // A wavefront's share of one step of 64 tokens, as it lies in the cache: lane (c, g) has the entries g*D/4 .. of the keys of token c of each
@@ -111,10 +146,9 @@ struct AttKeys {
   uint32_t exp[4];
   int there;
   __device__ __forceinline__ void load(const AttSource& s, const int (&page)[4], int n0, int c, int g) {
-    there = 0;
+    there = s.there(n0, page);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      there |= page[i] >= 0 ? 1 << i : 0;
       const unsigned char* base = s.base(page[i]);
       const uint32_t token = ((n0 + 16 * i) & (s.page_tokens - 1)) + c;
       code[i] = *reinterpret_cast<const word_t*>(base + (token * P::TOKEN + g * (D / 8)));
@@ -154,7 +188,7 @@ __device__ __forceinline__ srv_bf16x2 att_value_pair(const W& code, int k, int e
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(64 * ATT_WAVES, ATT_OCC) attention_kernel(const AttentionArgs p) {
+__global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(sizeof(T) == 2, D)) attention_kernel(const AttentionArgs p) {
   constexpr bool BF16 = sizeof(T) == 2;
   constexpr int TERMS = BF16 ? 1 : 3;   // bfloat16 parts of a query and of a weight
   constexpr int KS = D / 32;            // products of 32 entries that a score takes
@@ -162,13 +196,56 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, ATT_OCC) attention_kernel(cons
   typedef KvParts<D> P;
   const ttc_attention_t& a = p.a;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  const int span = blockIdx.x % p.spans;
-  const int64_t item = blockIdx.x / p.spans;
-  const int tile = (int)(item % p.row_tiles), head = (int)(item / p.row_tiles % a.cache.heads);
-  const int64_t seq = item / p.row_tiles / a.cache.heads;
+  __shared__ float part_o[ATT_WAVES][ATT_ROWS][D + 4];
+  __shared__ float part_m[ATT_WAVES][ATT_ROWS], part_l[ATT_WAVES][ATT_ROWS];
+  __shared__ uint32_t wave_sum[4], found[2];
+
+  // The workgroup's units: unit .. stop-1 of all; of entry `entry` from its unit `rest` on (the entry's heads one after the other)
+  uint32_t unit = 0, stop = 1, rest = 0;
+  int entry = 0, head = 0;
+  if (p.shared) {
+    const AttShares all(p, wave_sum);
+    const uint32_t used = min(all.total, gridDim.x);  // workgroups with any unit
+    if (blockIdx.x >= used) return;
+    unit = (uint32_t)((uint64_t)all.total * blockIdx.x / used);
+    stop = (uint32_t)((uint64_t)all.total * (blockIdx.x + 1) / used);
+    if (unit >= all.before && unit < all.before + all.own) {
+      uint32_t at = all.before;
+      for (int i = all.first; i < all.last; ++i) {
+        const uint32_t n = att_units(att_tile(p, i / p.row_tiles, i % p.row_tiles, 0)) * a.cache.heads;
+        if (unit < at + n) {
+          found[0] = i;
+          found[1] = unit - at;
+          break;
+        }
+        at += n;
+      }
+    }
+    __syncthreads();
+    entry = __builtin_amdgcn_readfirstlane(found[0]);
+    rest = __builtin_amdgcn_readfirstlane(found[1]);
+  } else {
+    entry = (int)(blockIdx.x / a.cache.heads);
+    head = (int)(blockIdx.x % a.cache.heads);
+  }
+  bool first_item = true;
+  while (unit < stop) {
+  const int64_t seq = entry / p.row_tiles;
+  const int tile = entry % p.row_tiles;
   const AttTile t = att_tile(p, seq, tile, c);
-  const int begin = t.lo + span * p.span, end = min(t.hi, begin + p.span);
-  if (span > 0 && begin >= end) return;  // (the whole workgroup: nothing reads what this span would have written)
+  const uint32_t units = att_units(t);
+  uint32_t take = units, from = 0;
+  if (p.shared) {
+    if (rest >= units * a.cache.heads) {  // the next entry (the first one found is not done yet)
+      ++entry;
+      rest = 0;
+      continue;
+    }
+    head = (int)(rest / units);
+    from = rest % units;
+    take = min(units - from, stop - unit);
+  }
+  const int begin = t.lo + (int)from * ATT_UNIT, end = min(t.hi, begin + (int)take * ATT_UNIT);
 
   // the lane's share of its row: entries g*D/4 .. of every part
   srv_bf16x8 q[TERMS][KS];
@@ -196,7 +273,7 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, ATT_OCC) attention_kernel(cons
   AttSource src;
   const int page_bytes = P::bytes(a.cache.page);
   src.cache = static_cast<const unsigned char*>(a.cache.data) + (int64_t)head * page_bytes;
-  src.pages = a.block_table + seq * a.table_stride;
+  src.pages = (const __attribute__((address_space(4))) int32_t*)(a.block_table + seq * a.table_stride);
   src.page_stride = (int64_t)a.cache.heads * page_bytes;
   src.page_count = (uint32_t)min(a.cache.pages, (int64_t)INT32_MAX);
   src.page_tokens = a.cache.page;
@@ -324,8 +401,6 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, ATT_OCC) attention_kernel(cons
   l += __shfl_xor(l, 32, 64);
 
   // the wavefronts' results join: lane (c, g) holds entries (4g + j)*E + e of row c
-  __shared__ float part_o[ATT_WAVES][ATT_ROWS][D + 4];
-  __shared__ float part_m[ATT_WAVES][ATT_ROWS], part_l[ATT_WAVES][ATT_ROWS];
 #pragma unroll
   for (int j = 0; j < 4; ++j)
 #pragma unroll
@@ -348,51 +423,77 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, ATT_OCC) attention_kernel(cons
     for (int e = 0; e < E; ++e) sum[e] += f * part_o[w][row][e0 + e];
   }
   const int r = tile * ATT_ROWS + row;
-  if (r >= t.rows) return;
-  if (p.spans > 1) {
-    float* stat = p.part_stat + (item * p.spans + span) * (2 * ATT_ROWS);
-    float* out = p.part_out + ((item * p.spans + span) * ATT_ROWS + row) * D + e0;
-    if (threadIdx.x % 16 == 0) {
-      stat[row] = mm;
-      stat[ATT_ROWS + row] = ll;
+  if (r < t.rows) {
+    if (take < units) {
+      // of the items that a workgroup does only a part of one can be its first and another its last
+      const int64_t slot = 2 * (int64_t)blockIdx.x + (first_item ? 0 : 1);
+      float* stat = p.part_stat + slot * (2 * ATT_ROWS);
+      float* out = p.part_out + (slot * ATT_ROWS + row) * D + e0;
+      if (threadIdx.x % 16 == 0) {
+        stat[row] = mm;
+        stat[ATT_ROWS + row] = ll;
+      }
+#pragma unroll
+      for (int e = 0; e < E; e += 4) *reinterpret_cast<srv_floatx4*>(out + e) = srv_floatx4{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
+    } else {
+      const float f = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
+      const int64_t token = t.first_q + r / p.group;
+      const int h = head * p.group + r % p.group;
+      T* y = static_cast<T*>(a.out) + token * a.out_token + (int64_t)h * a.out_head + e0;
+#pragma unroll
+      for (int e = 0; e < E; ++e) y[e] = srv_narrow<T>(f * sum[e]);
+      if (a.lse && threadIdx.x % 16 == 0) a.lse[token * a.heads_q + h] = (mm + __builtin_log2f(ll)) * 0.69314718055994530942f;
     }
-#pragma unroll
-    for (int e = 0; e < E; e += 4) *reinterpret_cast<srv_floatx4*>(out + e) = srv_floatx4{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
-    return;
   }
-  const float f = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
-  const int64_t token = t.first_q + r / p.group;
-  const int h = head * p.group + r % p.group;
-  T* y = static_cast<T*>(a.out) + token * a.out_token + (int64_t)h * a.out_head + e0;
-#pragma unroll
-  for (int e = 0; e < E; ++e) y[e] = srv_narrow<T>(f * sum[e]);
-  if (a.lse && threadIdx.x % 16 == 0) a.lse[token * a.heads_q + h] = (mm + __builtin_log2f(ll)) * 0.69314718055994530942f;
+  if (!p.shared) return;
+  unit += take;
+  rest += take;
+  first_item = false;
+  __syncthreads();  // before the next item's results
+  }
 }
 
-// The spans' results of one row: a workgroup to a row of a tile, four entries to a thread, the spans dealt out among the threads that have the
-// same entries
+// One row of an item that several workgroups had units of: four entries to a thread, the workgroups' results dealt out among the threads
+// that have the same entries.  Rows that nobody had units of, because they see nothing, are written here too.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) attention_join_kernel(const AttentionArgs p) {
   constexpr int Q = D / 4, PARTS = 256 / Q;
   const ttc_attention_t& a = p.a;
   const int row = blockIdx.x % p.join_rows;
   const int64_t item = blockIdx.x / p.join_rows;
-  const int tile = (int)(item % p.row_tiles), head = (int)(item / p.row_tiles % a.cache.heads);
-  const int64_t seq = item / p.row_tiles / a.cache.heads;
-  const AttTile t = att_tile(p, seq, tile, 0);
+  const int entry = (int)(item / a.cache.heads), head = (int)(item % a.cache.heads), tile = entry % p.row_tiles;
+  const AttTile t = att_tile(p, entry / p.row_tiles, tile, 0);
   const int r = tile * ATT_ROWS + row;
   if (r >= t.rows) return;
-  const int used = t.hi > t.lo ? (t.hi - t.lo + p.span - 1) / p.span : 0;
+  const uint32_t units = att_units(t);
+  __shared__ uint32_t wave_sum[4], found;
+  const AttShares all(p, wave_sum);
+  if (entry >= all.first && entry < all.last) {
+    uint32_t at = all.before;
+    for (int i = all.first; i < entry; ++i) at += att_units(att_tile(p, i / p.row_tiles, i % p.row_tiles, 0)) * a.cache.heads;
+    found = at + head * units;
+  }
+  __syncthreads();
+  // workgroup w has the units from total * w / workgroups on
+  uint32_t w0 = 0;
+  int used = 0, slot0 = 0;
+  if (units) {
+    const uint64_t workgroups = min((int64_t)all.total, p.workgroups);
+    const uint32_t u0 = found;
+    w0 = (uint32_t)(((u0 + 1) * workgroups - 1) / all.total);
+    used = (int)((uint32_t)(((u0 + units) * workgroups - 1) / all.total) - w0) + 1;
+    if (used == 1) return;  // that workgroup wrote the row
+    slot0 = (uint32_t)((uint64_t)all.total * w0 / workgroups) < u0 ? 1 : 0;
+  }
   const int part = threadIdx.x / Q, e = threadIdx.x % Q * 4;
-  const float* stat = p.part_stat + item * p.spans * (2 * ATT_ROWS) + row;
-  const float* out = p.part_out + (item * p.spans * ATT_ROWS + row) * D + e;
   // each part keeps a maximum of its own; rescaling happens once per span and thread
   float m = -INFINITY, l = 0.f;
   srv_floatx4 sum = {};
 #pragma unroll 4
   for (int s = part; s < used; s += PARTS) {
-    const float ms = stat[s * 2 * ATT_ROWS], ls = stat[s * 2 * ATT_ROWS + ATT_ROWS];
-    const srv_floatx4 x = *reinterpret_cast<const srv_floatx4*>(out + (int64_t)s * ATT_ROWS * D);
+    const int64_t slot = 2 * ((int64_t)w0 + s) + (s == 0 ? slot0 : 0);
+    const float ms = p.part_stat[slot * (2 * ATT_ROWS) + row], ls = p.part_stat[slot * (2 * ATT_ROWS) + ATT_ROWS + row];
+    const srv_floatx4 x = *reinterpret_cast<const srv_floatx4*>(p.part_out + (slot * ATT_ROWS + row) * D + e);
     const float top = fmaxf(m, ms), zero = top == -INFINITY ? 0.f : top;
     const float f = __builtin_amdgcn_exp2f(m - zero), h = __builtin_amdgcn_exp2f(ms - zero);
     m = top;

@@ -1,5 +1,5 @@
-// How the attention over the cache is shared between workgroups: row tiles, spans of the context, and the workspace where the spans'
-// results meet.  Host code; the kernels read the same numbers.
+// How the attention over the cache is shared between workgroups, and the workspace where their results meet.  Host code; the kernels read
+// the same numbers.
 #pragma once
 #include <stdint.h>
 
@@ -7,20 +7,28 @@
 
 namespace ttc {
 
-constexpr int ATT_ROWS = 16;   // query rows (new tokens x query heads of one cache head) of a workgroup
+constexpr int ATT_ROWS = 16;   // query rows (new tokens x query heads of one cache head) of a tile
 constexpr int ATT_STEP = 64;   // tokens that a wavefront takes at a time
 constexpr int ATT_WAVES = 4;   // wavefronts of a workgroup, side by side along the context
+constexpr int ATT_UNIT = ATT_STEP * ATT_WAVES;
+
+// workgroups of a compute unit, by the registers that a wavefront takes
+#ifndef ATT_ROUNDS
+#define ATT_ROUNDS 1
+#endif
+constexpr int att_resident(bool bf16, int d) { return d == 64 || (bf16 && d == 128) ? 3 : 2; }
 
 struct AttentionArgs {
   ttc_attention_t a;
   int32_t group;       // query heads of one cache head
   int32_t row_tiles;   // of ATT_ROWS rows, for the longest sequence
-  int32_t span;        // tokens of the context that one workgroup takes
-  int32_t spans;       // for the longest context; with 1 the workgroup writes out itself
-  int64_t items;       // sequences * heads * row_tiles
+  int32_t entries;     // sequences * row_tiles
+  int64_t items;       // entries * heads: what one workgroup would do by itself
   int32_t join_rows;   // rows of a tile that can be real
-  float *part_out;     // (items, spans, ATT_ROWS, d) sums of exp2(s - m) v
-  float *part_stat;    // (items, spans, 2, ATT_ROWS): m, sum of exp2(s - m)
+  int32_t shared;      // whether the workgroups share the items' units evenly; else each does an item
+  int64_t workgroups;
+  float *part_out;     // (2 * workgroups, ATT_ROWS, d) sums of exp2(s - m) v
+  float *part_stat;    // (2 * workgroups, 2, ATT_ROWS): m, sum of exp2(s - m)
 };
 
 // Tokens of the context that the rows of one tile can see between them, at most
@@ -31,27 +39,27 @@ inline int64_t visible_at_most(const ttc_attention_t& a, int group) {
   return n < a.max_kv ? n : a.max_kv;
 }
 
+// Shared: the contexts are cut into units of 256 tokens and every workgroup that the device holds at once gets the same number of
+// them, whatever the sequences' lengths; an item whose units several workgroups have is joined by a second launch.  Each workgroup finds its
+// share from all lengths (a few per thread), and every row of the second launch does so too, so many short items are better off with
+// a workgroup each, which the device deals out as others end.
 inline void plan_attention(AttentionArgs& p, int cus) {
   const ttc_attention_t& a = p.a;
   p.group = a.heads_q / a.cache.heads;
   const int64_t rows = (int64_t)a.max_q * p.group;
   p.row_tiles = (int32_t)((rows + ATT_ROWS - 1) / ATT_ROWS);
-  p.items = a.sequences * a.cache.heads * p.row_tiles;
-  const int64_t most = visible_at_most(a, p.group), unit = ATT_STEP * ATT_WAVES;
-  const int64_t units = (most + unit - 1) / unit;
-  // about sixteen workgroups to a compute unit, as long as each has a step for every wavefront
-  int64_t spans = p.items > 0 ? (16 * cus + p.items - 1) / p.items : 1;
-  spans = spans < 1 ? 1 : spans > units ? units : spans;
-  const int64_t per = spans ? (units + spans - 1) / spans : 1;
-  p.span = (int32_t)((per < 1 ? 1 : per) * unit);
-  p.spans = (int32_t)((most + p.span - 1) / p.span);
-  if (p.spans < 1) p.spans = 1;
+  p.entries = (int32_t)(a.sequences * p.row_tiles);
+  p.items = (int64_t)p.entries * a.cache.heads;
   p.join_rows = (int32_t)(rows < ATT_ROWS ? rows : ATT_ROWS);
+  const int64_t slots = (int64_t)att_resident(a.dtype == TTC_BF16, a.cache.d) * cus * ATT_ROUNDS;
+  const int64_t units = (visible_at_most(a, p.group) + ATT_UNIT - 1) / ATT_UNIT;
+  p.shared = units > 1 && p.entries <= 2048 && p.items < 8 * slots && (double)units * p.items < 1e9;
+  p.workgroups = !p.shared ? p.items : units * p.items < slots ? units * p.items : slots;
   p.part_out = p.part_stat = nullptr;
 }
 
 inline uint64_t attention_workspace(const AttentionArgs& p) {
-  return p.spans <= 1 ? 0 : (uint64_t)p.items * p.spans * ATT_ROWS * (p.a.cache.d + 2) * sizeof(float);
+  return p.shared ? 2 * (uint64_t)p.workgroups * ATT_ROWS * (p.a.cache.d + 2) * sizeof(float) : 0;
 }
 
 }  // namespace ttc
