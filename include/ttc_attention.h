@@ -131,8 +131,8 @@ typedef struct {
 } ttc_attention_t;
 
 /* workspace: DEVICE, 16-byte aligned, at least ttc_attention_workspace_bytes(attention) bytes (0: none needed, may be NULL),
- * which depends on sequences, heads, heads_q, d, max_q, max_kv, window and the device's compute units only.  Long contexts are
- * shared between workgroups and joined by a second launch. */
+ * which depends on sequences, heads, heads_q, d, max_q, max_kv, window and the device's compute units only.  One launch; the workspace
+ * need not be cleared and may be used again by the next call on the same stream. */
 size_t ttc_attention_workspace_bytes(const ttc_attention_t *attention);
 ttc_status_t ttc_attention(const ttc_attention_t *attention, void *workspace, size_t workspace_bytes, void *hip_stream);
 

@@ -1,4 +1,4 @@
-// attention_kernel, attention_join_kernel (ttc_attention), for heads of TTC_D entries.
+// attention_kernel (ttc_attention), for heads of TTC_D entries.
 #include "ttc_attention.hpp"
 #include "ttc_serve_launch.hpp"
 
@@ -7,8 +7,6 @@ namespace ttc {
 template <typename T>
 static hipError_t launch(const AttentionArgs& p, hipStream_t st) {
   hipLaunchKernelGGL((attention_kernel<T, TTC_D>), dim3((unsigned)p.workgroups), dim3(64 * ATT_WAVES), 0, st, p);
-  if (const hipError_t e = hipGetLastError(); e != hipSuccess || !p.shared) return e;
-  hipLaunchKernelGGL((attention_join_kernel<T, TTC_D>), dim3((unsigned)(p.items * p.join_rows)), dim3(256), 0, st, p);
   return hipGetLastError();
 }
 

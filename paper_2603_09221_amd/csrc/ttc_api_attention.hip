@@ -2,7 +2,9 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
+#include <time.h>
 
+#include <atomic>
 #include <mutex>
 
 #include "../../include/ttc_attention.h"
@@ -34,6 +36,16 @@ int compute_units() {
     count[dev] = n;
   });
   return count[dev];
+}
+
+// 64 bits that what lies in a workspace has by chance only: a counter from a starting point of the process's own, mixed
+uint64_t next_mark() {
+  static std::atomic<uint64_t> calls{(uint64_t)time(nullptr) * 0x9e3779b97f4a7c15ull ^ (uint64_t)&calls ^ (uint64_t)clock()};
+  uint64_t x = calls.fetch_add(0x9e3779b97f4a7c15ull, std::memory_order_relaxed);
+  x = (x ^ (x >> 30)) * 0xbf58476d1ce4e5b9ull;
+  x = (x ^ (x >> 27)) * 0x94d049bb133111ebull;
+  x ^= x >> 31;
+  return x ? x : 1;  // (a mark taken away is 0)
 }
 
 ttc_status_t check_rope(int32_t d, int32_t rot, int32_t layout, const int64_t* positions, const float* table, int64_t table_rows) {
@@ -135,10 +147,7 @@ ttc_status_t ttc_attention(const ttc_attention_t* a, void* workspace, size_t wor
   ttc::plan_attention(p, compute_units());
   const uint64_t need = ttc::attention_workspace(p);
   if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return TTC_ERR_WORKSPACE;
-  if (need) {
-    p.part_out = static_cast<float*>(workspace);
-    p.part_stat = p.part_out + 2 * (uint64_t)p.workgroups * ttc::ATT_ROWS * a->cache.d;
-  }
+  ttc::place_workspace(p, workspace, next_mark());
   const bool bf16 = a->dtype == TTC_BF16;
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   hipError_t e = hipErrorInvalidValue;

@@ -20,6 +20,7 @@ struct AttTile {
   int first, last;  // tokens that the lane's row sees: first .. last (none where last < first)
   int lo, hi;       // all that the tile's rows see lies in lo .. hi-1
   int all_lo, all_hi;  // and every one of them sees all of all_lo .. all_hi-1
+  int real;         // rows of the tile
 };
 
 __device__ __forceinline__ AttTile att_tile(const AttentionArgs& p, int64_t seq, int tile, int row) {
@@ -53,25 +54,28 @@ __device__ __forceinline__ AttTile att_tile(const AttentionArgs& p, int64_t seq,
     t.hi = t.all_hi = t.len;
     t.lo = t.all_lo = 0;
   }
+  t.real = max(r1 - tile * ATT_ROWS + 1, 0);
   if (r >= t.rows) t.last = -1;
-  if (r1 < tile * ATT_ROWS) t.hi = 0;
+  if (!t.real) t.hi = 0;
   t.lo = t.lo / ATT_STEP * ATT_STEP;
   return t;
 }
 
-// units of 256 tokens of one item
-__device__ __forceinline__ uint32_t att_units(const AttTile& t) { return t.hi > t.lo ? (uint32_t)(t.hi - t.lo + ATT_UNIT - 1) / ATT_UNIT : 0; }
+// units of 256 tokens of one item; one for rows that see nothing, whose results somebody has to write
+__device__ __forceinline__ uint32_t att_units(const AttTile& t) {
+  return t.hi > t.lo ? (uint32_t)(t.hi - t.lo + ATT_UNIT - 1) / ATT_UNIT : t.real ? 1 : 0;
+}
 
-// The entries (sequence, row tile) in their order, each of `heads` items of its number of units: all threads of a workgroup of 256
-// add them up, a run of entries to a thread.
+// The entries (sequence, row tile) in their order, each of `heads` items of its number of units: every wavefront adds them up for
+// itself, a run of entries to a lane.
 struct AttShares {
   uint32_t total;   // units of all items
-  uint32_t before;  // of the entries before this thread's run
-  uint32_t own;     // of this thread's run
+  uint32_t before;  // of the entries before this lane's run
+  uint32_t own;     // of this lane's run
   int first, last;  // the run: first .. last-1
-  __device__ __forceinline__ AttShares(const AttentionArgs& p, uint32_t (&wave_sum)[4]) {
-    const int run = (p.entries + 255) / 256;
-    first = min((int)threadIdx.x * run, p.entries);
+  __device__ __forceinline__ explicit AttShares(const AttentionArgs& p) {
+    const int lane = threadIdx.x & 63, run = (p.entries + 63) / 64;
+    first = min(lane * run, p.entries);
     last = min(first + run, p.entries);
     own = 0;
     for (int i = first; i < last; ++i) own += att_units(att_tile(p, i / p.row_tiles, i % p.row_tiles, 0));
@@ -80,16 +84,22 @@ struct AttShares {
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const uint32_t x = __shfl_up(sum, o, 64);
-      sum += (int)(threadIdx.x & 63) >= o ? x : 0;
+      sum += lane >= o ? x : 0;
     }
-    if ((threadIdx.x & 63) == 63) wave_sum[threadIdx.x >> 6] = sum;
-    __syncthreads();
-    total = 0;
+    total = __builtin_amdgcn_readlane(sum, 63);
     before = sum - own;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      before += w < (int)(threadIdx.x >> 6) ? wave_sum[w] : 0;
-      total += wave_sum[w];
+  }
+  // the entry that unit u of all is of (u < total), and the entry's units before it
+  __device__ __forceinline__ int find(const AttentionArgs& p, uint32_t u, uint32_t& rest) const {
+    const int lane = __builtin_ctzll(__builtin_amdgcn_ballot_w64(u >= before && u < before + own));
+    uint32_t at = __builtin_amdgcn_readlane(before, lane);
+    for (int i = __builtin_amdgcn_readlane(first, lane);; ++i) {
+      const uint32_t n = __builtin_amdgcn_readfirstlane(att_units(att_tile(p, i / p.row_tiles, i % p.row_tiles, 0))) * p.a.cache.heads;
+      if (u < at + n || i + 1 >= p.entries) {
+        rest = u - at;
+        return i;
+      }
+      at += n;
     }
   }
 };
@@ -187,6 +197,124 @@ __device__ __forceinline__ srv_bf16x2 att_value_pair(const W& code, int k, int e
   }
 }
 
+// A workgroup had some of an item's units: its result goes to a slot of the workspace, and whoever finds that all have arrived joins them, in
+// the order of the units, so that equal calls give equal bits.  True for the threads that then hold entries e0 .. of row `row` of the whole.
+//
+// Arrival is a mark in the slot, of 64 bits that no earlier contents of the workspace have but by chance (1 in 2^64); the caller need
+// not clear anything.  Every workgroup sets its own mark and then looks at the others', so the last one sees all; two may, and then both
+// write the same.  The marks are taken away again, for a captured launch comes back with the same one.  Nobody waits for another workgroup.
+// The workgroups may be on different XCDs, whose caches do not see each other's lines: results and marks go past them, in stores and loads
+// of device scope.  Each wavefront waits for its stores, the workgroup for its wavefronts, and only then the mark is set.
+// Fences of device scope instead write back and empty whole caches: a call over 4 x 131072 tokens took 282 us with them.  A count of
+// arrivals, which all workgroups of an item change one after the other, took 26 us where the marks take REPLACE (17 workgroups, 4099 tokens).
+__device__ __forceinline__ void att_put2(float* p, float a, float b) {
+  __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), (unsigned long long)__float_as_uint(b) << 32 | __float_as_uint(a), __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void att_get2(const float* p, float& a, float& b) {
+  const unsigned long long x = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  a = __uint_as_float((uint32_t)x);
+  b = __uint_as_float((uint32_t)(x >> 32));
+}
+template <int D>
+__device__ __forceinline__ bool att_join(const AttentionArgs& p, const AttTile& t, uint32_t first_unit, uint32_t units, uint32_t total, uint32_t used,
+                                         uint32_t slot, int& row, int e0, float& mm, float& ll, float (&sum)[D / 16], float* part_o,
+                                         float* part_m, int* joins) {
+  constexpr int E = D / 16;
+  if (row < t.real) {
+    float* stat = p.part_stat + ((int64_t)slot * ATT_ROWS + row) * 2;
+    float* out = p.part_out + ((int64_t)slot * ATT_ROWS + row) * D + e0;
+    if (threadIdx.x % 16 == 0) att_put2(stat, mm, ll);
+#pragma unroll
+    for (int e = 0; e < E; e += 2) att_put2(out + e, sum[e], sum[e + 1]);
+  }
+  // workgroup w has the units from total * w / used on; the item's first may have begun with another item
+  const uint32_t w0 = (uint32_t)(((uint64_t)(first_unit + 1) * used - 1) / total);
+  const uint32_t parts = (uint32_t)(((uint64_t)(first_unit + units) * used - 1) / total) - w0 + 1;
+  const uint32_t slot0 = (uint32_t)((uint64_t)total * w0 / used) < first_unit ? 1 : 0;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    if (threadIdx.x == 0) (void)__hip_atomic_exchange(p.marks + slot, p.mark, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    bool all = true;
+    for (uint32_t s = threadIdx.x; s < parts; s += 64)
+      all &= __hip_atomic_load(p.marks + 2 * ((int64_t)w0 + s) + (s == 0 ? slot0 : 0), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == p.mark;
+    if (threadIdx.x == 0) *joins = 1;
+    if (!all) *joins = 0;
+  }
+  __syncthreads();
+  if (!*joins) return false;
+  asm volatile("" ::: "memory");
+  for (uint32_t s = threadIdx.x; s < parts; s += 64 * ATT_WAVES)
+    __hip_atomic_store(p.marks + 2 * ((int64_t)w0 + s) + (s == 0 ? slot0 : 0), 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  // 16 threads to a row, and as many groups of them to the same row as there are rows to spare; each group takes every so many-th part
+  int rows = 1;
+  while (rows < t.real) rows <<= 1;
+  const int group = threadIdx.x / 16, groups = ATT_ROWS / rows, first = group / rows;
+  row = group % rows;
+  mm = -INFINITY;
+  ll = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) sum[e] = 0.f;
+  if (row < t.real) {
+    // four parts' loads under way before the first is used
+    for (uint32_t s0 = first; s0 < parts; s0 += 4 * groups) {
+      float ms[4], ls[4], x[4][E];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t s = s0 + k * groups < parts ? s0 + k * groups : s0;
+        const int64_t at = (2 * ((int64_t)w0 + s) + (s == 0 ? slot0 : 0)) * ATT_ROWS + row;
+        att_get2(p.part_stat + at * 2, ms[k], ls[k]);
+#pragma unroll
+        for (int e = 0; e < E; e += 2) att_get2(p.part_out + at * D + e0 + e, x[k][e], x[k][e + 1]);
+      }
+      float top = mm;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        ms[k] = s0 + k * groups < parts ? ms[k] : -INFINITY;
+        top = fmaxf(top, ms[k]);
+      }
+      const float zero = top == -INFINITY ? 0.f : top, f = __builtin_amdgcn_exp2f(mm - zero);
+      mm = top;
+      ll *= f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) sum[e] *= f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (s0 + k * groups >= parts) break;
+        const float h = __builtin_amdgcn_exp2f(ms[k] - zero);
+        ll += h * ls[k];
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] += h * x[k][e];
+      }
+    }
+  }
+  if (groups == 1) return row < t.real;
+  float* const o = part_o + group * (D + 4) + e0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = sum[e];
+  if (threadIdx.x % 16 == 0) {
+    part_m[2 * group] = mm;
+    part_m[2 * group + 1] = ll;
+  }
+  __syncthreads();
+  if (first || row >= t.real) return false;
+  for (int i = 1; i < groups; ++i) mm = fmaxf(mm, part_m[2 * (i * rows + row)]);
+  const float zero = mm == -INFINITY ? 0.f : mm;
+  ll = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) sum[e] = 0.f;
+  for (int i = 0; i < groups; ++i) {
+    const int at = i * rows + row;
+    const float f = __builtin_amdgcn_exp2f(part_m[2 * at] - zero);
+    ll += f * part_m[2 * at + 1];
+#pragma unroll
+    for (int e = 0; e < E; ++e) sum[e] += f * part_o[at * (D + 4) + e0 + e];
+  }
+  return true;
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(sizeof(T) == 2, D)) attention_kernel(const AttentionArgs p) {
   constexpr bool BF16 = sizeof(T) == 2;
@@ -198,32 +326,19 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(sizeof(T) == 2, D
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
   __shared__ float part_o[ATT_WAVES][ATT_ROWS][D + 4];
   __shared__ float part_m[ATT_WAVES][ATT_ROWS], part_l[ATT_WAVES][ATT_ROWS];
-  __shared__ uint32_t wave_sum[4], found[2];
+  __shared__ int joins;
 
   // The workgroup's units: unit .. stop-1 of all; of entry `entry` from its unit `rest` on (the entry's heads one after the other)
-  uint32_t unit = 0, stop = 1, rest = 0;
+  uint32_t unit = 0, stop = 1, rest = 0, total = 0, used = 0;
   int entry = 0, head = 0;
   if (p.shared) {
-    const AttShares all(p, wave_sum);
-    const uint32_t used = min(all.total, gridDim.x);  // workgroups with any unit
+    const AttShares all(p);
+    total = all.total;
+    used = min(total, gridDim.x);  // workgroups with any unit
     if (blockIdx.x >= used) return;
-    unit = (uint32_t)((uint64_t)all.total * blockIdx.x / used);
-    stop = (uint32_t)((uint64_t)all.total * (blockIdx.x + 1) / used);
-    if (unit >= all.before && unit < all.before + all.own) {
-      uint32_t at = all.before;
-      for (int i = all.first; i < all.last; ++i) {
-        const uint32_t n = att_units(att_tile(p, i / p.row_tiles, i % p.row_tiles, 0)) * a.cache.heads;
-        if (unit < at + n) {
-          found[0] = i;
-          found[1] = unit - at;
-          break;
-        }
-        at += n;
-      }
-    }
-    __syncthreads();
-    entry = __builtin_amdgcn_readfirstlane(found[0]);
-    rest = __builtin_amdgcn_readfirstlane(found[1]);
+    unit = (uint32_t)((uint64_t)total * blockIdx.x / used);
+    stop = (uint32_t)((uint64_t)total * (blockIdx.x + 1) / used);
+    entry = all.find(p, unit, rest);
   } else {
     entry = (int)(blockIdx.x / a.cache.heads);
     head = (int)(blockIdx.x % a.cache.heads);
@@ -233,7 +348,7 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(sizeof(T) == 2, D
   const int64_t seq = entry / p.row_tiles;
   const int tile = entry % p.row_tiles;
   const AttTile t = att_tile(p, seq, tile, c);
-  const uint32_t units = att_units(t);
+  const uint32_t units = __builtin_amdgcn_readfirstlane(att_units(t));
   uint32_t take = units, from = 0;
   if (p.shared) {
     if (rest >= units * a.cache.heads) {  // the next entry (the first one found is not done yet)
@@ -410,7 +525,8 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(sizeof(T) == 2, D
     part_l[wave][c] = l;
   }
   __syncthreads();
-  const int row = threadIdx.x / 16, e0 = (threadIdx.x % 16) * E;
+  int row = threadIdx.x / 16;
+  const int e0 = (threadIdx.x % 16) * E;
   float mm = -INFINITY, ll = 0.f, sum[E] = {};
 #pragma unroll
   for (int w = 0; w < ATT_WAVES; ++w) mm = fmaxf(mm, part_m[w][row]);
@@ -422,28 +538,18 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(sizeof(T) == 2, D
 #pragma unroll
     for (int e = 0; e < E; ++e) sum[e] += f * part_o[w][row][e0 + e];
   }
-  const int r = tile * ATT_ROWS + row;
-  if (r < t.rows) {
-    if (take < units) {
-      // of the items that a workgroup does only a part of one can be its first and another its last
-      const int64_t slot = 2 * (int64_t)blockIdx.x + (first_item ? 0 : 1);
-      float* stat = p.part_stat + slot * (2 * ATT_ROWS);
-      float* out = p.part_out + (slot * ATT_ROWS + row) * D + e0;
-      if (threadIdx.x % 16 == 0) {
-        stat[row] = mm;
-        stat[ATT_ROWS + row] = ll;
-      }
+  bool writes = row < t.real;
+  if (take < units) writes = att_join<D>(p, t, unit - from, units, total, used, 2 * blockIdx.x + (first_item ? 0 : 1), row, e0,
+                                         mm, ll, sum, &part_o[0][0][0], &part_m[0][0], &joins);
+  if (writes) {
+    const float f = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
+    const int r = tile * ATT_ROWS + row;
+    const int64_t token = t.first_q + r / p.group;
+    const int h = head * p.group + r % p.group;
+    T* y = static_cast<T*>(a.out) + token * a.out_token + (int64_t)h * a.out_head + e0;
 #pragma unroll
-      for (int e = 0; e < E; e += 4) *reinterpret_cast<srv_floatx4*>(out + e) = srv_floatx4{sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
-    } else {
-      const float f = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
-      const int64_t token = t.first_q + r / p.group;
-      const int h = head * p.group + r % p.group;
-      T* y = static_cast<T*>(a.out) + token * a.out_token + (int64_t)h * a.out_head + e0;
-#pragma unroll
-      for (int e = 0; e < E; ++e) y[e] = srv_narrow<T>(f * sum[e]);
-      if (a.lse && threadIdx.x % 16 == 0) a.lse[token * a.heads_q + h] = (mm + __builtin_log2f(ll)) * 0.69314718055994530942f;
-    }
+    for (int e = 0; e < E; ++e) y[e] = srv_narrow<T>(f * sum[e]);
+    if (a.lse && threadIdx.x % 16 == 0) a.lse[token * a.heads_q + h] = (mm + __builtin_log2f(ll)) * 0.69314718055994530942f;
   }
   if (!p.shared) return;
   unit += take;
@@ -451,82 +557,6 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(sizeof(T) == 2, D
   first_item = false;
   __syncthreads();  // before the next item's results
   }
-}
-
-// One row of an item that several workgroups had units of: four entries to a thread, the workgroups' results dealt out among the threads
-// that have the same entries.  Rows that nobody had units of, because they see nothing, are written here too.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) attention_join_kernel(const AttentionArgs p) {
-  constexpr int Q = D / 4, PARTS = 256 / Q;
-  const ttc_attention_t& a = p.a;
-  const int row = blockIdx.x % p.join_rows;
-  const int64_t item = blockIdx.x / p.join_rows;
-  const int entry = (int)(item / a.cache.heads), head = (int)(item % a.cache.heads), tile = entry % p.row_tiles;
-  const AttTile t = att_tile(p, entry / p.row_tiles, tile, 0);
-  const int r = tile * ATT_ROWS + row;
-  if (r >= t.rows) return;
-  const uint32_t units = att_units(t);
-  __shared__ uint32_t wave_sum[4], found;
-  const AttShares all(p, wave_sum);
-  if (entry >= all.first && entry < all.last) {
-    uint32_t at = all.before;
-    for (int i = all.first; i < entry; ++i) at += att_units(att_tile(p, i / p.row_tiles, i % p.row_tiles, 0)) * a.cache.heads;
-    found = at + head * units;
-  }
-  __syncthreads();
-  // workgroup w has the units from total * w / workgroups on
-  uint32_t w0 = 0;
-  int used = 0, slot0 = 0;
-  if (units) {
-    const uint64_t workgroups = min((int64_t)all.total, p.workgroups);
-    const uint32_t u0 = found;
-    w0 = (uint32_t)(((u0 + 1) * workgroups - 1) / all.total);
-    used = (int)((uint32_t)(((u0 + units) * workgroups - 1) / all.total) - w0) + 1;
-    if (used == 1) return;  // that workgroup wrote the row
-    slot0 = (uint32_t)((uint64_t)all.total * w0 / workgroups) < u0 ? 1 : 0;
-  }
-  const int part = threadIdx.x / Q, e = threadIdx.x % Q * 4;
-  // each part keeps a maximum of its own; rescaling happens once per span and thread
-  float m = -INFINITY, l = 0.f;
-  srv_floatx4 sum = {};
-#pragma unroll 4
-  for (int s = part; s < used; s += PARTS) {
-    const int64_t slot = 2 * ((int64_t)w0 + s) + (s == 0 ? slot0 : 0);
-    const float ms = p.part_stat[slot * (2 * ATT_ROWS) + row], ls = p.part_stat[slot * (2 * ATT_ROWS) + ATT_ROWS + row];
-    const srv_floatx4 x = *reinterpret_cast<const srv_floatx4*>(p.part_out + (slot * ATT_ROWS + row) * D + e);
-    const float top = fmaxf(m, ms), zero = top == -INFINITY ? 0.f : top;
-    const float f = __builtin_amdgcn_exp2f(m - zero), h = __builtin_amdgcn_exp2f(ms - zero);
-    m = top;
-    l = f * l + h * ls;
-    sum = f * sum + h * x;
-  }
-  __shared__ float part_m[PARTS], part_l[PARTS];
-  __shared__ srv_floatx4 part_o[PARTS][Q];
-  part_o[part][threadIdx.x % Q] = sum;
-  if (threadIdx.x % Q == 0) {
-    part_m[part] = m;
-    part_l[part] = l;
-  }
-  __syncthreads();
-  if (part) return;
-#pragma unroll
-  for (int i = 1; i < PARTS; ++i) m = fmaxf(m, part_m[i]);
-  const float zero = m == -INFINITY ? 0.f : m;
-  l = 0.f;
-  sum = srv_floatx4{};
-#pragma unroll
-  for (int i = 0; i < PARTS; ++i) {
-    const float f = __builtin_amdgcn_exp2f(part_m[i] - zero);
-    l += f * part_l[i];
-    sum += f * part_o[i][threadIdx.x];
-  }
-  const int64_t token = t.first_q + r / p.group;
-  const int h = head * p.group + r % p.group;
-  const float f = l > 0.f || l != l ? 1.f / l : 0.f;
-  T* y = static_cast<T*>(a.out) + token * a.out_token + (int64_t)h * a.out_head + e;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) y[i] = srv_narrow<T>(f * sum[i]);
-  if (a.lse && threadIdx.x == 0) a.lse[token * a.heads_q + h] = (m + __builtin_log2f(l)) * 0.69314718055994530942f;
 }
 
 }  // namespace ttc

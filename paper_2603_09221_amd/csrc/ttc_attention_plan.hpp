@@ -13,9 +13,6 @@ constexpr int ATT_WAVES = 4;   // wavefronts of a workgroup, side by side along 
 constexpr int ATT_UNIT = ATT_STEP * ATT_WAVES;
 
 // workgroups of a compute unit, by the registers that a wavefront takes
-#ifndef ATT_ROUNDS
-#define ATT_ROUNDS 1
-#endif
 constexpr int att_resident(bool bf16, int d) { return d == 64 || (bf16 && d == 128) ? 3 : 2; }
 
 struct AttentionArgs {
@@ -24,11 +21,12 @@ struct AttentionArgs {
   int32_t row_tiles;   // of ATT_ROWS rows, for the longest sequence
   int32_t entries;     // sequences * row_tiles
   int64_t items;       // entries * heads: what one workgroup would do by itself
-  int32_t join_rows;   // rows of a tile that can be real
   int32_t shared;      // whether the workgroups share the items' units evenly; else each does an item
   int64_t workgroups;
   float *part_out;     // (2 * workgroups, ATT_ROWS, d) sums of exp2(s - m) v
-  float *part_stat;    // (2 * workgroups, 2, ATT_ROWS): m, sum of exp2(s - m)
+  float *part_stat;    // (2 * workgroups, ATT_ROWS, 2): m, sum of exp2(s - m)
+  unsigned long long *marks;  // (2 * workgroups): which slots are written
+  unsigned long long mark;    // the call's own
 };
 
 // Tokens of the context that the rows of one tile can see between them, at most
@@ -40,9 +38,9 @@ inline int64_t visible_at_most(const ttc_attention_t& a, int group) {
 }
 
 // Shared: the contexts are cut into units of 256 tokens and every workgroup that the device holds at once gets the same number of
-// them, whatever the sequences' lengths; an item whose units several workgroups have is joined by a second launch.  Each workgroup finds its
-// share from all lengths (a few per thread), and every row of the second launch does so too, so many short items are better off with
-// a workgroup each, which the device deals out as others end.
+// them, whatever the sequences' lengths; an item whose units several workgroups have is joined by the last of them.  Each wavefront finds its
+// share from all lengths (a few per lane), so many short items are better off with a workgroup each, which the device deals out as others
+// end.
 inline void plan_attention(AttentionArgs& p, int cus) {
   const ttc_attention_t& a = p.a;
   p.group = a.heads_q / a.cache.heads;
@@ -50,16 +48,25 @@ inline void plan_attention(AttentionArgs& p, int cus) {
   p.row_tiles = (int32_t)((rows + ATT_ROWS - 1) / ATT_ROWS);
   p.entries = (int32_t)(a.sequences * p.row_tiles);
   p.items = (int64_t)p.entries * a.cache.heads;
-  p.join_rows = (int32_t)(rows < ATT_ROWS ? rows : ATT_ROWS);
-  const int64_t slots = (int64_t)att_resident(a.dtype == TTC_BF16, a.cache.d) * cus * ATT_ROUNDS;
+  const int64_t slots = (int64_t)att_resident(a.dtype == TTC_BF16, a.cache.d) * cus;
   const int64_t units = (visible_at_most(a, p.group) + ATT_UNIT - 1) / ATT_UNIT;
-  p.shared = units > 1 && p.entries <= 2048 && p.items < 8 * slots && (double)units * p.items < 1e9;
+  p.shared = units > 1 && p.entries <= 1024 && p.items < 8 * slots && (double)units * p.items < 1e9;
   p.workgroups = !p.shared ? p.items : units * p.items < slots ? units * p.items : slots;
   p.part_out = p.part_stat = nullptr;
+  p.marks = nullptr;
+  p.mark = 0;
 }
 
 inline uint64_t attention_workspace(const AttentionArgs& p) {
-  return p.shared ? 2 * (uint64_t)p.workgroups * ATT_ROWS * (p.a.cache.d + 2) * sizeof(float) : 0;
+  return p.shared ? 2 * (uint64_t)p.workgroups * (ATT_ROWS * (p.a.cache.d + 2) * sizeof(float) + sizeof(*p.marks)) : 0;
+}
+
+inline void place_workspace(AttentionArgs& p, void* workspace, uint64_t mark) {
+  if (!p.shared) return;
+  p.part_out = static_cast<float*>(workspace);
+  p.part_stat = p.part_out + 2 * (uint64_t)p.workgroups * ATT_ROWS * p.a.cache.d;
+  p.marks = reinterpret_cast<unsigned long long*>(p.part_stat + 2 * (uint64_t)p.workgroups * ATT_ROWS * 2);
+  p.mark = mark;
 }
 
 }  // namespace ttc
