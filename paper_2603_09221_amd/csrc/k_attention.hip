@@ -1,12 +1,13 @@
-// attention_kernel (ttc_attention), for heads of TTC_D entries.
-#include "ttc_attention.hpp"
+// attention_kernel, attention_prompt_kernel (ttc_attention), for heads of TTC_D entries.
+#include "ttc_attention_prompt.hpp"
 #include "ttc_serve_launch.hpp"
 
 namespace ttc {
 
 template <typename T>
 static hipError_t launch(const AttentionArgs& p, hipStream_t st) {
-  hipLaunchKernelGGL((attention_kernel<T, TTC_D>), dim3((unsigned)p.workgroups), dim3(64 * ATT_WAVES), 0, st, p);
+  if (p.prompt) hipLaunchKernelGGL((attention_prompt_kernel<T, TTC_D>), dim3((unsigned)p.workgroups), dim3(64 * PROMPT_WAVES), 0, st, p);
+  else hipLaunchKernelGGL((attention_kernel<T, TTC_D>), dim3((unsigned)p.workgroups), dim3(64 * ATT_WAVES), 0, st, p);
   return hipGetLastError();
 }
 

@@ -23,6 +23,7 @@ struct AttTile {
   int real;         // rows of the tile
 };
 
+template <int ROWS = ATT_ROWS>
 __device__ __forceinline__ AttTile att_tile(const AttentionArgs& p, int64_t seq, int tile, int row) {
   const ttc_attention_t& a = p.a;
   AttTile t;
@@ -37,14 +38,14 @@ __device__ __forceinline__ AttTile att_tile(const AttentionArgs& p, int64_t seq,
   t.len = len < 0 ? 0 : len > a.max_kv ? a.max_kv : len;
   t.rows = (int)m * p.group;
   t.first_q = q0;
-  const int r = tile * ATT_ROWS + row;
-  const int r1 = min(t.rows, (tile + 1) * ATT_ROWS) - 1;  // last row of the tile
+  const int r = tile * ROWS + row;
+  const int r1 = min(t.rows, (tile + 1) * ROWS) - 1;  // last row of the tile
   const int shift = t.len - (int)all;                     // token number of the first new one
   if (a.causal) {
     t.last = min(shift + r / p.group, t.len - 1);
     t.first = a.window ? max(t.last - a.window + 1, 0) : 0;
     t.hi = min(shift + r1 / p.group, t.len - 1) + 1;
-    const int first = min(shift + tile * ATT_ROWS / p.group, t.len - 1);  // what the first row sees last
+    const int first = min(shift + tile * ROWS / p.group, t.len - 1);  // what the first row sees last
     t.lo = a.window ? max(first - a.window + 1, 0) : 0;
     t.all_lo = a.window ? max(t.hi - a.window, 0) : 0;
     t.all_hi = first + 1;
@@ -54,7 +55,7 @@ __device__ __forceinline__ AttTile att_tile(const AttentionArgs& p, int64_t seq,
     t.hi = t.all_hi = t.len;
     t.lo = t.all_lo = 0;
   }
-  t.real = max(r1 - tile * ATT_ROWS + 1, 0);
+  t.real = max(r1 - tile * ROWS + 1, 0);
   if (r >= t.rows) t.last = -1;
   if (!t.real) t.hi = 0;
   t.lo = t.lo / ATT_STEP * ATT_STEP;
@@ -131,6 +132,16 @@ struct AttSource {
   int64_t page_stride;
   uint32_t page_count;
   int page_tokens, log_page, end;
+  __device__ __forceinline__ AttSource(const AttentionArgs& p, int64_t seq, int head, int end_) : end(end_) {
+    const ttc_kv_cache_t& c = p.a.cache;
+    const int64_t bytes = (int64_t)c.page * (c.d + c.d / 16);
+    cache = static_cast<const unsigned char*>(c.data) + head * bytes;
+    pages = (const __attribute__((address_space(4))) int32_t*)(p.a.block_table + seq * p.a.table_stride);
+    page_stride = c.heads * bytes;
+    page_count = (uint32_t)min(c.pages, (int64_t)INT32_MAX);
+    page_tokens = c.page;
+    log_page = __builtin_ctz(c.page);
+  }
   // What the table says of the four sixteens from token n0 on, not yet looked at (whoever looks waits for it)
   __device__ __forceinline__ void look_up(int n0, int (&page)[4]) const {
 #pragma unroll
@@ -321,7 +332,6 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(sizeof(T) == 2, D
   constexpr int TERMS = BF16 ? 1 : 3;   // bfloat16 parts of a query and of a weight
   constexpr int KS = D / 32;            // products of 32 entries that a score takes
   constexpr int E = D / 16;             // entries of a value that a lane holds
-  typedef KvParts<D> P;
   const ttc_attention_t& a = p.a;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
   __shared__ float part_o[ATT_WAVES][ATT_ROWS][D + 4];
@@ -385,15 +395,7 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(sizeof(T) == 2, D
   srv_floatx4 o[E] = {};
   float m = -INFINITY, l = 0.f;
   const float to_log2 = a.scale * 1.44269504088896340736f;
-  AttSource src;
-  const int page_bytes = P::bytes(a.cache.page);
-  src.cache = static_cast<const unsigned char*>(a.cache.data) + (int64_t)head * page_bytes;
-  src.pages = (const __attribute__((address_space(4))) int32_t*)(a.block_table + seq * a.table_stride);
-  src.page_stride = (int64_t)a.cache.heads * page_bytes;
-  src.page_count = (uint32_t)min(a.cache.pages, (int64_t)INT32_MAX);
-  src.page_tokens = a.cache.page;
-  src.log_page = __builtin_ctz(a.cache.page);
-  src.end = end;
+  const AttSource src(p, seq, head, end);
 
   // Keys and values of the next step are read into the registers that this step has just done with, and the page numbers of the step
   // after it: the reads are under way during the other product and the softmax, and while other wavefronts of the SIMD work.

@@ -12,6 +12,9 @@ constexpr int ATT_STEP = 64;   // tokens that a wavefront takes at a time
 constexpr int ATT_WAVES = 4;   // wavefronts of a workgroup, side by side along the context
 constexpr int ATT_UNIT = ATT_STEP * ATT_WAVES;
 
+constexpr int PROMPT_WAVES = 4;  // wavefronts of a workgroup of the kernel for many rows, 32 rows each
+constexpr int prompt_waves_per_simd(bool bf16, int d) { return d == 256 ? 1 : 2; }
+
 // workgroups of a compute unit, by the registers that a wavefront takes
 constexpr int att_resident(bool bf16, int d) { return d == 64 || (bf16 && d == 128) ? 3 : 2; }
 
@@ -21,6 +24,7 @@ struct AttentionArgs {
   int32_t row_tiles;   // of ATT_ROWS rows, for the longest sequence
   int32_t entries;     // sequences * row_tiles
   int64_t items;       // entries * heads: what one workgroup would do by itself
+  int32_t prompt;      // whether the kernel for many rows is taken; row_tiles are its own then
   int32_t shared;      // whether the workgroups share the items' units evenly; else each does an item
   int64_t workgroups;
   float *part_out;     // (2 * workgroups, ATT_ROWS, d) sums of exp2(s - m) v
@@ -45,12 +49,17 @@ inline void plan_attention(AttentionArgs& p, int cus) {
   const ttc_attention_t& a = p.a;
   p.group = a.heads_q / a.cache.heads;
   const int64_t rows = (int64_t)a.max_q * p.group;
-  p.row_tiles = (int32_t)((rows + ATT_ROWS - 1) / ATT_ROWS);
+#ifndef PROMPT_MIN
+#define PROMPT_MIN 65
+#endif
+  p.prompt = rows >= PROMPT_MIN;
+  const int tile = p.prompt ? 32 * PROMPT_WAVES : ATT_ROWS;
+  p.row_tiles = (int32_t)((rows + tile - 1) / tile);
   p.entries = (int32_t)(a.sequences * p.row_tiles);
   p.items = (int64_t)p.entries * a.cache.heads;
   const int64_t slots = (int64_t)att_resident(a.dtype == TTC_BF16, a.cache.d) * cus;
   const int64_t units = (visible_at_most(a, p.group) + ATT_UNIT - 1) / ATT_UNIT;
-  p.shared = units > 1 && p.entries <= 1024 && p.items < 8 * slots && (double)units * p.items < 1e9;
+  p.shared = !p.prompt && units > 1 && p.entries <= 1024 && p.items < 8 * slots && (double)units * p.items < 1e9;
   p.workgroups = !p.shared ? p.items : units * p.items < slots ? units * p.items : slots;
   p.part_out = p.part_stat = nullptr;
   p.marks = nullptr;
