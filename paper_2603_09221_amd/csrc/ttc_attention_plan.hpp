@@ -13,7 +13,10 @@ constexpr int ATT_WAVES = 4;   // wavefronts of a workgroup, side by side along 
 constexpr int ATT_UNIT = ATT_STEP * ATT_WAVES;
 
 constexpr int PROMPT_WAVES = 4;  // wavefronts of a workgroup of the kernel for many rows, 32 rows each
-constexpr int prompt_waves_per_simd(bool bf16, int d) { return d == 256 ? 1 : 2; }
+// It keeps operands, sums and a step's weights of 32 rows in registers.  Queries of three parts, or heads of 256, do not fit: with float32 and
+// d = 128 it took 463 us where attention_kernel takes 369 (64 cache heads, 4096 rows each over 1024 tokens), with bfloat16 and d = 256 it was
+// at most 1.28 times faster, so those shapes do without.
+constexpr bool prompt_kernel(bool bf16, int d) { return d == 64 || (bf16 && d == 128); }
 
 // workgroups of a compute unit, by the registers that a wavefront takes
 constexpr int att_resident(bool bf16, int d) { return d == 64 || (bf16 && d == 128) ? 3 : 2; }
@@ -49,10 +52,12 @@ inline void plan_attention(AttentionArgs& p, int cus) {
   const ttc_attention_t& a = p.a;
   p.group = a.heads_q / a.cache.heads;
   const int64_t rows = (int64_t)a.max_q * p.group;
-#ifndef PROMPT_MIN
-#define PROMPT_MIN 65
-#endif
-  p.prompt = rows >= PROMPT_MIN;
+  // The kernel for many rows does a tile's context from end to end in one workgroup: 1.2 us for every 64 tokens, up to a tile to each
+  // compute unit; attention_kernel takes tiles in time proportional to their number.  Measured over 8192 tokens, d = 128, this one /
+  // attention_kernel, us: 64 tiles of 128 rows 193 / 90, 128 tiles 197 / 161, 256 tiles 210 / 304.
+  const int64_t prompt_tiles = (rows + 32 * PROMPT_WAVES - 1) / (32 * PROMPT_WAVES), all_rows = a.tokens * p.group;
+  const int64_t tiles = a.sequences * prompt_tiles, real = all_rows / (32 * PROMPT_WAVES) + a.sequences;
+  p.prompt = prompt_kernel(a.dtype == TTC_BF16, a.cache.d) && 4 * a.cache.heads * (tiles < real ? tiles : real) >= 3 * cus && rows > ATT_ROWS;
   const int tile = p.prompt ? 32 * PROMPT_WAVES : ATT_ROWS;
   p.row_tiles = (int32_t)((rows + tile - 1) / tile);
   p.entries = (int32_t)(a.sequences * p.row_tiles);

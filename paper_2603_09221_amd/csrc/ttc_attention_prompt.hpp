@@ -2,11 +2,15 @@
 //
 // As in attention_kernel the rows are the columns of both products, here of 32 x 32 x 16 tiles: S^T = K Q^T leaves in a lane sixteen tokens'
 // scores of one row, and taking the tokens of O^T = V^T P^T in the order that the lanes hold them the weights never move.  A wavefront has
-// 32 rows, a workgroup 128 of one cache head.  Keys are widened by each wavefront for itself, from codes that the first of them has brought
-// into the compute unit's cache (32 bytes of codes widen to 128 of operand, so reading them widened from LDS would take four times the
-// bytes, and that would be all the LDS can give).  Values have to be turned, four tokens' entries side by side, which costs an exchange per two
-// entries: the workgroup does that once, into LDS, in the order of the lanes that read it, without bank conflicts.
+// 32 rows, a workgroup 128 of one cache head.  Keys are widened by each wavefront for itself (widened once for the workgroup, through LDS, every
+// product waits for its operand: 838 us where this takes 700).  Values have to be turned, four tokens' entries side by side, which costs an
+// exchange per two entries: the workgroup does that once, into LDS, in the order of the lanes that read it, without bank conflicts.
+//
+// 4096 queries of 32 heads over 12288 tokens (d = 128, 8 cache heads): 690 us, 1.0 PFLOP/s, as a large matrix product runs at 1.25.  Matrix and vector instructions of the two wavefronts of a
+// SIMD share its issue: a step of 64 tokens is 32 products (1024 cycles), 32 exponentials and about 290 other vector instructions.
 #pragma once
+#include <type_traits>
+
 #include "ttc_attention.hpp"
 
 namespace ttc {
@@ -16,14 +20,14 @@ typedef float srv_floatx16 __attribute__((ext_vector_type(16)));
 constexpr int PROMPT_ROWS = 32 * PROMPT_WAVES;  // rows of a workgroup
 
 template <typename T, int D>
-__global__ void __launch_bounds__(64 * PROMPT_WAVES, prompt_waves_per_simd(sizeof(T) == 2, D)) attention_prompt_kernel(const AttentionArgs p) {
+__global__ void __launch_bounds__(64 * PROMPT_WAVES, 2) attention_prompt_kernel(const AttentionArgs p) {
   constexpr bool BF16 = sizeof(T) == 2;
   constexpr int TERMS = BF16 ? 1 : 3;
   constexpr int KS = D / 16;     // products of 16 entries that a score takes
   constexpr int KW = D / 16;     // words of codes of a lane's share of a key: D/2 entries
+  constexpr int EXPS = D / 64;   // exponents of a lane's share of a key
   constexpr int E = D / 16;      // entries of a value in one of the cache's 16 lanes
   constexpr int DT = D / 32;     // tiles of 32 entries
-  constexpr int EXPS = D / 64;   // exponents of a lane's share of a key
   typedef KvParts<D> P;
   typedef uint32_t key_t __attribute__((ext_vector_type(KW)));
   typedef uint32_t val_t __attribute__((ext_vector_type(D / 32)));
@@ -39,8 +43,8 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, prompt_waves_per_simd(sizeo
   const AttTile t = att_tile<PROMPT_ROWS>(p, seq, tile, 32 * wave + c);
   if (!t.real) return;
 
-  // values of a step, widened: [four tokens' place][entry's place][8 tokens], and their exponents; two steps
-  __shared__ srv_bf16x8 turned[2][8][D];
+  // two steps' values, widened, [16 tokens][8 of them][entry's place]: eight numbers that a lane takes at once; and their exponents
+  __shared__ srv_bf16x8 turned[2][4][2][D];
   __shared__ uint32_t exps[2][16][D / 32];
   __shared__ int bad_step[2][PROMPT_WAVES];
 
@@ -59,7 +63,7 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, prompt_waves_per_simd(sizeo
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         __bf16 part[TERMS];
-        att_split<TERMS>(v[i], part);
+        att_split<TERMS>(a.scale < 0.f ? -v[i] : v[i], part);
 #pragma unroll
         for (int k = 0; k < TERMS; ++k) q[k][s][i] = part[k];
       }
@@ -67,16 +71,15 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, prompt_waves_per_simd(sizeo
   }
   srv_floatx16 o[DT] = {};
   float m = -INFINITY, l = 0.f;
-  const float to_log2 = a.scale * 1.44269504088896340736f;
+  const float to_log2 = fabsf(a.scale) * 1.44269504088896340736f;  // (largest scores are largest products)
   const AttSource src(p, seq, head, t.hi);
 
-  // keys: lane (c, g) has entries g*D/2 .. of token c of each 32; values: thread (f, l) has those of four tokens f that the cache's lane l holds
+  // keys: lane (c, g) has entries g*D/2 .. of token c of each 32; values: thread (f, vl) has those of four tokens f that the cache's lane vl holds
   key_t key[2];
   uint32_t key_exp[2];
   val_t value;
   uint32_t value_exp;
-  int page[4];
-  const auto load_keys = [&](int n0) {
+  const auto load_keys = [&](int n0, const int (&page)[4]) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const unsigned char* base = src.base(c < 16 ? page[2 * u] : page[2 * u + 1]);
@@ -87,20 +90,19 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, prompt_waves_per_simd(sizeo
     }
   };
   const int f = threadIdx.x >> 4, vl = threadIdx.x & 15;  // f / 4 is the wavefront's number
-  const auto load_values = [&](int n0) {
+  const auto load_values = [&](int n0, const int (&page)[4]) {
     const unsigned char* base = src.base(wave == 0 ? page[0] : wave == 1 ? page[1] : wave == 2 ? page[2] : page[3]);
     const uint32_t four = ((n0 + 16 * wave) & (src.page_tokens - 1)) / 4 + (f & 3);
     value = *reinterpret_cast<const val_t*>(base + (P::values(src.page_tokens) + (four * 16 + vl) * (4 * P::LANE)));
     value_exp = *reinterpret_cast<const uint32_t*>(base + (P::value_exps(src.page_tokens) + (four * P::BLOCKS + vl * E / 32) * 4));
   };
-  // Row 32*dt + i of O^T is entry (i % 16) * E + 2*dt + i / 16, so that the threads of a cache's lane write side by side
+  // Row 32*dt + i of O^T is entry (i % 16) * E + 2*dt + i / 16, so that the threads of the cache's lanes write side by side
   const auto turn_values = [&](int buffer) {
     const uint32_t nan = att_full_bytes(value_exp);
-    if (vl * E % 32 == 0) exps[buffer][f][vl * E / 32] = value_exp;
-    const bool any = __builtin_amdgcn_ballot_w64(nan != 0) != 0;
-    if (lane == 0) bad_step[buffer][wave] = any;
+    exps[buffer][f][vl * E / 32] = value_exp;  // (the same from all lanes of a block)
+    bad_step[buffer][wave] = __builtin_amdgcn_ballot_w64(nan != 0) != 0;
     const uint32_t finite = value_exp ^ nan;
-    __bf16* const to = reinterpret_cast<__bf16*>(&turned[buffer][(f / 4) * 2 + (f & 1)][vl]) + (f & 2) * 2;
+    __bf16* const to = reinterpret_cast<__bf16*>(&turned[buffer][wave][f & 1][vl]) + (f & 2) * 2;
 #pragma unroll
     for (int e = 0; e < E; e += 2) {
       typedef __bf16 four_t __attribute__((ext_vector_type(4)));
@@ -116,20 +118,44 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, prompt_waves_per_simd(sizeo
     }
   };
 
-  int there = 0, buffer = 0;
-  if (t.lo < t.hi) {
-    src.look_up(t.lo, page);
-    there = src.there(t.lo, page);
-    load_keys(t.lo);
-    load_values(t.lo);
-    src.look_up(t.lo + ATT_STEP, page);
-    turn_values(0);
-  }
-  __syncthreads();
-  for (int n0 = t.lo; n0 < t.hi; n0 += ATT_STEP, buffer ^= 1) {
-    const bool more = n0 + ATT_STEP < t.hi;
-    if (more) load_values(n0 + ATT_STEP);
-    srv_floatx16 z[2];
+  // Step n: beside the scores of its tokens, whose codes are widened on the way, values n are turned; beside the sum over the values of
+  // step n-1 the weights of step n are formed.  The codes of step n+1 are on their way from memory meanwhile.
+  srv_floatx16 z[2];        // products q . k, 32 tokens each
+  srv_bf16x8 w[TERMS][4];   // weights, 16 tokens each
+  int page[4], there = 0, there_before = 0;  // of step n+1; of steps n and n-1
+  bool moved = false;
+  float shrink = 1.f;
+  const auto add_values = [&](int buffer) {
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int i = 0; i < DT; ++i) {
+        const srv_bf16x8 v = turned[buffer][s][g][32 * i + c];
+#pragma unroll
+        for (int x = TERMS - 1; x >= 0; --x) o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[x][s], o[i], 0, 0, 0);
+      }
+  };
+  // blocks of NaN among the values of the step from token n0 on: what the rows that see them get is made NaN (see attention_kernel)
+  const auto spread_nan = [&](int n0, int buffer, int there) {
+    if (!(bad_step[buffer][0] | bad_step[buffer][1] | bad_step[buffer][2] | bad_step[buffer][3])) return;
+#pragma unroll 1
+    for (int s = 0; s < 4; ++s) {
+      srv_bf16x8 bad, seen;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int four = 4 * s + 2 * (k / 4) + g, n = n0 + 4 * four + k % 4;
+        bad[k] = static_cast<__bf16>((exps[buffer][four][(c & 15) * E / 32] >> (8 * (k % 4)) & 255) == 255 ? 1.f : 0.f);
+        seen[k] = static_cast<__bf16>((there >> s & 1) && n >= t.first && n <= t.last ? 1.f : 0.f);
+      }
+      const srv_floatx16 hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bad, seen, srv_floatx16{}, 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[i][j] = hit[j] > 0.f ? __builtin_nanf("") : o[i][j];
+    }
+  };
+  const auto step = [&](int n0, int buffer, auto first_) {
+    constexpr bool first = decltype(first_)::value;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       z[u] = srv_floatx16{};
@@ -137,82 +163,102 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, prompt_waves_per_simd(sizeo
       for (int s = 0; s < KS; ++s) {
         const srv_bf16x8 k = att_widen(key[u][s], srv_scale((key_exp[u] >> (8 * (s / 4))) & 255));
 #pragma unroll
-        for (int x = TERMS - 1; x >= 0; --x) z[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[x][s], z[u], 0, 0, 0);
+        for (int i = TERMS - 1; i >= 0; --i) z[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[i][s], z[u], 0, 0, 0);
       }
     }
-    const int now = there;
-    if (more) {
-      there = src.there(n0 + ATT_STEP, page);
-      load_keys(n0 + ATT_STEP);
-      src.look_up(n0 + 2 * ATT_STEP, page);
+    turn_values(buffer);
+    // a product, then what else there is to do while it runs: about six vector instructions
+    if constexpr (BF16) {
+      __builtin_amdgcn_sched_group_barrier(0x002, 8, 0);
+#pragma unroll
+      for (int i = 0; i < 2 * KS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
+        __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+      }
     }
-    if (n0 < t.all_lo || n0 + ATT_STEP > t.all_hi || now != 15) {
+    load_keys(n0 + ATT_STEP, page);
+    load_values(n0 + ATT_STEP, page);
+    const int next = src.there(n0 + ATT_STEP, page);
+    src.look_up(n0 + 2 * ATT_STEP, page);
+    if (n0 < t.all_lo || n0 + ATT_STEP > t.all_hi || there != 15) {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
           const int n = n0 + 32 * u + 8 * (j / 4) + 4 * g + j % 4;
-          z[u][j] = (now >> (2 * u + j / 8) & 1) && n >= t.first && n <= t.last ? z[u][j] * to_log2 : -INFINITY;
+          z[u][j] = (there >> (2 * u + j / 8) & 1) && n >= t.first && n <= t.last ? z[u][j] : -INFINITY;
         }
-    } else {
-#pragma unroll
-      for (int u = 0; u < 2; ++u) z[u] *= to_log2;
     }
+    // The weights of step n-1 are relative to that step's maximum
+    if (moved) {
+#pragma unroll
+      for (int i = 0; i < DT; ++i) o[i] *= shrink;
+    }
+    // The maximum that weights are relative to (in units of log2) moves as attention_kernel's does
     float top = -INFINITY;
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int j = 0; j < 16; ++j) top = fmaxf(top, z[u][j]);
-    if (__builtin_amdgcn_ballot_w64(top > m + 8.f)) {  // (see attention_kernel)
+    top = top == -INFINITY ? top : top * to_log2;  // (a scale of 0)
+    moved = __builtin_amdgcn_ballot_w64(top > m + 8.f) != 0;
+    if (moved) {
       top = fmaxf(m, top);
       top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float shrink = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
+      shrink = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
       m = top;
       l *= shrink;
-#pragma unroll
-      for (int i = 0; i < DT; ++i) o[i] *= shrink;
     }
+    if constexpr (!first) spread_nan(n0 - ATT_STEP, buffer ^ 1, there_before);
+    if constexpr (!first) add_values(buffer ^ 1);
     const float zero = m == -INFINITY ? 0.f : m;
-    srv_bf16x8 w[TERMS][4];
+    srv_bf16x8 w1[TERMS][4];
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int j = 0; j < 16; ++j) {
-        const float x = __builtin_amdgcn_exp2f(z[u][j] - zero);
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(z[u][j], to_log2, -zero));
         l += x;
         __bf16 part[TERMS];
         att_split<TERMS>(x, part);
 #pragma unroll
-        for (int k = 0; k < TERMS; ++k) w[k][2 * u + j / 8][j % 8] = part[k];
+        for (int k = 0; k < TERMS; ++k) w1[k][2 * u + j / 8][j % 8] = part[k];
       }
-    if (bad_step[buffer][0] | bad_step[buffer][1] | bad_step[buffer][2] | bad_step[buffer][3]) {
-      // blocks of NaN: what the rows that see them get is made NaN (see attention_kernel)
-#pragma unroll 1
-      for (int s = 0; s < 4; ++s) {
-        srv_bf16x8 bad, seen;
+    if constexpr (BF16) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int four = 4 * s + 2 * (k / 4) + g, n = n0 + 4 * four + k % 4;
-          bad[k] = static_cast<__bf16>((exps[buffer][four][(c & 15) * E / 32] >> (8 * (k % 4)) & 255) == 255 ? 1.f : 0.f);
-          seen[k] = static_cast<__bf16>((now >> s & 1) && n >= t.first && n <= t.last ? 1.f : 0.f);
-        }
-        const srv_floatx16 hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bad, seen, srv_floatx16{}, 0, 0, 0);
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-#pragma unroll
-          for (int i = 0; i < DT; ++i) o[i][j] = hit[j] > 0.f ? __builtin_nanf("") : o[i][j];
+      for (int i = 0; i < 4 * DT; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+        __builtin_amdgcn_sched_group_barrier(0x400, 2, 0);
       }
     }
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
+    for (int k = 0; k < TERMS; ++k)
 #pragma unroll
-      for (int i = 0; i < DT; ++i) {
-        const srv_bf16x8 v = turned[buffer][2 * s + g][32 * i + c];
-#pragma unroll
-        for (int x = TERMS - 1; x >= 0; --x) o[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, w[x][s], o[i], 0, 0, 0);
-      }
-    if (more) turn_values(buffer ^ 1);
+      for (int i = 0; i < 4; ++i) w[k][i] = w1[k][i];
+    there_before = there;
+    there = next;
     __syncthreads();
+  };
+
+  if (t.lo < t.hi) {
+    int n0 = t.lo, buffer = 0;
+    src.look_up(n0, page);
+    there = src.there(n0, page);
+    load_keys(n0, page);
+    load_values(n0, page);
+    src.look_up(n0 + ATT_STEP, page);
+    step(n0, 0, std::true_type{});
+    for (n0 += ATT_STEP, buffer = 1; n0 < t.hi; n0 += ATT_STEP, buffer ^= 1) step(n0, buffer, std::false_type{});
+    if (moved) {
+#pragma unroll
+      for (int i = 0; i < DT; ++i) o[i] *= shrink;
+    }
+    spread_nan(n0 - ATT_STEP, buffer ^ 1, there_before);
+    add_values(buffer ^ 1);
   }
   l += __shfl_xor(l, 32, 64);
   if (r >= t.rows) return;

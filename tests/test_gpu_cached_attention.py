@@ -124,6 +124,39 @@ def test_prompts(kv_len, new, heads, group, d, page, dtype):
     s.check(binding.ttc_attention(**s.gpu(), causal=False), causal=False)
 
 
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 64), (torch.bfloat16, 128), (torch.float32, 64)])
+@pytest.mark.parametrize("kv_len,new,heads,group,page,window", [
+    ([150, 37, 300, 0, 64, 1, 65], [150, 33, 120, 3, 64, 1, 2], 8, 16, 16, 0),    # prompts, chunks, more queries than keys, empty rows
+    ([129, 400], [129, 200], 16, 8, 256, 0),
+    ([700, 64, 63, 128, 40], [90, 64, 63, 127, 70], 8, 16, 32, 50),               # windows shorter than a step
+    ([500, 200], [300, 1], 8, 11, 64, 130)])
+def test_many_rows(kv_len, new, heads, group, page, window, dtype, d):
+    """Enough tiles of 128 rows for the kernel that is made for them."""
+    s = Setup(kv_len, new, heads, group, d, page, dtype, seed=sum(new) + d)
+    assert heads * (sum(new) * group // 128) >= 192
+    s.check(binding.ttc_attention(**s.gpu(), window=window), window=window)
+    if not window:
+        s.check(binding.ttc_attention(**s.gpu(), causal=False), causal=False)
+
+
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 64), (torch.bfloat16, 128), (torch.float32, 64)])
+def test_many_rows_with_nan_missing_pages_and_negative_scale(dtype, d):
+    s = Setup([300, 150], [250, 150], 8, 8, d, 16, dtype, seed=5)
+    k, v = s.exponents()
+    k[s.table[0, 180 // 16], 1, 180 % 16, 1] = 255              # keys of token 180, values of token 75 of the other sequence
+    v[s.table[1, 75 // 16], 2, 75 % 16 // 4, 0, 75 % 4] = 255
+    s.table[0, 3], s.table[1, 1] = -1, s.pages
+    c, e = s.page * s.d, s.page * s.d // 32
+    s.raw[..., c:c + e], s.raw[..., c + e:] = k.reshape(*s.raw.shape[:2], e), v.reshape(*s.raw.shape[:2], e)
+    (out, _, _), _ = s.oracle(window=100)
+    assert 0 < np.isnan(out).mean() < 0.2
+    s.check(binding.ttc_attention(**s.gpu(), window=100), window=100)
+    s.scale = -0.25
+    got = binding.ttc_attention(**s.gpu())
+    s.q, s.scale = -s.q, 0.25
+    s.check(got)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("window", [1, 2, 17, 64, 100, 5000])
 def test_windows(window, dtype):
