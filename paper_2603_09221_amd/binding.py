@@ -649,7 +649,7 @@ def _rope_table(table, d):
 def _new(like, shape, dtype, stream):
     """A result tensor on the device of `like`, from the memory of the stream that the kernels run on."""
     if stream is None or stream == torch.cuda.current_stream():
-        return like.new_empty(shape, dtype=dtype)
+        return torch.empty_like(like) if shape is like.shape and dtype is like.dtype and like.is_contiguous() else like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
         return like.new_empty(shape, dtype=dtype)
 

@@ -112,9 +112,10 @@ ttc_status_t ttc_kv_append(const ttc_kv_append_t* a, void* hip_stream) {
   if (!a->k || !a->v || !a->slots || !aligned(a->k, n) || !aligned(a->v, n) || !aligned(a->slots, 8)) return TTC_ERR_INVALID_ARG;
   if (!a->q != !a->q_out || (a->q && (a->heads_q < 1 || !aligned(a->q, n) || !aligned(a->q_out, n)))) return TTC_ERR_INVALID_ARG;
   if (a->q && a->q == a->q_out && (a->q_token != a->q_out_token || a->q_head != a->q_out_head)) return TTC_ERR_INVALID_ARG;
-  // a launch has fewer than 2^32 threads along the tokens and 2^16 workgroups along the heads
-  if (a->tokens > (1 << 26) || (a->q ? (int64_t)a->heads_q : 0) + 2ll * a->cache.heads > 65535) return TTC_ERR_UNSUPPORTED;
-  return ttc::launch_kv_append(*a, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? TTC_OK : TTC_ERR_DEVICE;
+  // a launch has fewer than 2^32 threads, one to eight entries
+  if (a->tokens > (1 << 26) || (a->q ? (int64_t)a->heads_q : 0) + 2ll * a->cache.heads > 65535 ||
+      (double)a->tokens * ((a->q ? a->heads_q : 0) + 2. * a->cache.heads) * a->cache.d >= 8. * 4e9) return TTC_ERR_UNSUPPORTED;
+  return ttc::launch_kv_append(*a, compute_units(), static_cast<hipStream_t>(hip_stream)) == hipSuccess ? TTC_OK : TTC_ERR_DEVICE;
 }
 
 ttc_status_t ttc_kv_read(const ttc_kv_cache_t* c, const int64_t* slots, int64_t n, int32_t out_dtype, void* k_out, void* v_out, void* hip_stream) {
@@ -122,7 +123,7 @@ ttc_status_t ttc_kv_read(const ttc_kv_cache_t* c, const int64_t* slots, int64_t 
   if (const ttc_status_t s = check_cache(*c); s != TTC_OK) return s;
   if (!n || (!k_out && !v_out)) return TTC_OK;
   if (!slots || !aligned(slots, 8) || !aligned(k_out, 16) || !aligned(v_out, 16)) return TTC_ERR_INVALID_ARG;
-  if (n > (1 << 26) || c->heads > 65535) return TTC_ERR_UNSUPPORTED;
+  if (n > (1 << 26) || c->heads > 65535) return TTC_ERR_UNSUPPORTED;  // (fewer than 2^32 threads along the tokens, 2^16 workgroups along the heads)
   return ttc::launch_kv_read(*c, slots, n, out_dtype == TTC_BF16, k_out, v_out, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? TTC_OK : TTC_ERR_DEVICE;
 }
 

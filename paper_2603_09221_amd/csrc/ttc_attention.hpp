@@ -12,6 +12,9 @@
 
 namespace ttc {
 
+// What nothing writes during the launch: read through the scalar cache where all lanes want the same
+typedef __attribute__((address_space(4))) int32_t att_const_int;
+
 // The row tile of a workgroup: its sequence's numbers and this lane's row
 struct AttTile {
   int len;          // tokens in the cache
@@ -28,13 +31,17 @@ __device__ __forceinline__ AttTile att_tile(const AttentionArgs& p, int64_t seq,
   const ttc_attention_t& a = p.a;
   AttTile t;
   int64_t q0 = seq, q1 = seq + 1;
-  if (a.cu_q) { q0 = a.cu_q[seq]; q1 = a.cu_q[seq + 1]; }
+  if (a.cu_q) {
+    const att_const_int* const cu = (const att_const_int*)a.cu_q;
+    q0 = cu[seq];
+    q1 = cu[seq + 1];
+  }
   q0 = q0 < 0 ? 0 : q0;
   q1 = q1 > a.tokens ? a.tokens : q1;
   int64_t m = q1 - q0;
   const int64_t all = m;  // (positions count every new token, also those behind max_q)
   m = m < 0 ? 0 : m > a.max_q ? a.max_q : m;
-  int len = a.kv_len[seq];
+  const int len = ((const att_const_int*)a.kv_len)[seq];
   t.len = len < 0 ? 0 : len > a.max_kv ? a.max_kv : len;
   t.rows = (int)m * p.group;
   t.first_q = q0;
@@ -94,6 +101,10 @@ struct AttShares {
   __device__ __forceinline__ int find(const AttentionArgs& p, uint32_t u, uint32_t& rest) const {
     const int lane = __builtin_ctzll(__builtin_amdgcn_ballot_w64(u >= before && u < before + own));
     uint32_t at = __builtin_amdgcn_readlane(before, lane);
+    if (p.entries <= 64) {  // a run is one entry
+      rest = u - at;
+      return lane;
+    }
     for (int i = __builtin_amdgcn_readlane(first, lane);; ++i) {
       const uint32_t n = __builtin_amdgcn_readfirstlane(att_units(att_tile(p, i / p.row_tiles, i % p.row_tiles, 0))) * p.a.cache.heads;
       if (u < at + n || i + 1 >= p.entries) {
@@ -128,7 +139,7 @@ __device__ __forceinline__ uint32_t att_full_bytes(uint32_t x) { return x & ((x 
 // What a workgroup reads the cache with, the same for all of its lanes
 struct AttSource {
   const unsigned char* cache;  // the workgroup's head of page 0
-  const __attribute__((address_space(4))) int32_t* pages;  // the sequence's, through the scalar cache: nothing writes them meanwhile
+  const att_const_int* pages;  // the sequence's
   int64_t page_stride;
   uint32_t page_count;
   int page_tokens, log_page, end;
@@ -136,7 +147,7 @@ struct AttSource {
     const ttc_kv_cache_t& c = p.a.cache;
     const int64_t bytes = (int64_t)c.page * (c.d + c.d / 16);
     cache = static_cast<const unsigned char*>(c.data) + head * bytes;
-    pages = (const __attribute__((address_space(4))) int32_t*)(p.a.block_table + seq * p.a.table_stride);
+    pages = (const att_const_int*)(p.a.block_table + seq * p.a.table_stride);
     page_stride = c.heads * bytes;
     page_count = (uint32_t)min(c.pages, (int64_t)INT32_MAX);
     page_tokens = c.page;
@@ -372,8 +383,15 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(sizeof(T) == 2, D
   }
   const int begin = t.lo + (int)from * ATT_UNIT, end = min(t.hi, begin + (int)take * ATT_UNIT);
 
+  // page numbers, queries and the first step's codes are on their way together
+  const AttSource src(p, seq, head, end);
+  constexpr int STRIDE = ATT_STEP * ATT_WAVES;
+  int page[4], n0 = begin + wave * ATT_STEP;
+  if (n0 < end) src.look_up(n0, page);
+
   // the lane's share of its row: entries g*D/4 .. of every part
   srv_bf16x8 q[TERMS][KS];
+  float query[BF16 ? 1 : KS][8];
   {
     const int r = tile * ATT_ROWS + c;
     const bool real = r < t.rows;
@@ -381,33 +399,38 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(sizeof(T) == 2, D
     const bool vec = (uint64_t)a.q % 16 == 0 && (a.q_token | a.q_head) % (16 / (int)sizeof(T)) == 0;
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      float v[8] = {};
-      if (real) srv_ld8(x + 8 * s, vec, v);
+      if constexpr (BF16) {
+        q[0][s] = srv_bf16x8{};
+        if (real) q[0][s] = srv_ld8_bf16(x + 8 * s, vec);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        __bf16 part[TERMS];
-        att_split<TERMS>(v[i], part);
-#pragma unroll
-        for (int k = 0; k < TERMS; ++k) q[k][s][i] = part[k];
+        for (int i = 0; i < 8; ++i) query[s][i] = 0.f;
+        if (real) srv_ld8(x + 8 * s, vec, query[s]);
       }
     }
   }
   srv_floatx4 o[E] = {};
   float m = -INFINITY, l = 0.f;
   const float to_log2 = a.scale * 1.44269504088896340736f;
-  const AttSource src(p, seq, head, end);
-
   // Keys and values of the next step are read into the registers that this step has just done with, and the page numbers of the step
   // after it: the reads are under way during the other product and the softmax, and while other wavefronts of the SIMD work.
-  constexpr int STRIDE = ATT_STEP * ATT_WAVES;
   AttKeys<D> keys;
   AttValues<D> values;
-  int page[4], n0 = begin + wave * ATT_STEP;
   if (n0 < end) {
-    src.look_up(n0, page);
     keys.load(src, page, n0, c, g);
     values.load(src, page, n0, c, g);
     src.look_up(n0 + STRIDE, page);
+  }
+  if constexpr (!BF16) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        __bf16 part[TERMS];
+        att_split<TERMS>(query[s][i], part);
+#pragma unroll
+        for (int k = 0; k < TERMS; ++k) q[k][s][i] = part[k];
+      }
   }
   for (; n0 < end; n0 += STRIDE) {
     const bool more = n0 + STRIDE < end;

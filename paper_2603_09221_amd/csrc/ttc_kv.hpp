@@ -9,8 +9,8 @@ namespace ttc {
 
 struct KvAppendArgs {
   ttc_kv_append_t a;
-  int q_pieces;                      // workgroups along the query heads, each of q_heads of them
-  int q_heads;
+  uint32_t cache_workgroups;         // that write the cache, ahead of those of the queries
+  int q_pieces;                      // workgroups along the query heads: number i takes heads i, i + q_pieces, ..
   bool k_vec, v_vec, q_vec, qo_vec;  // rows that allow 16-byte accesses
   bool t_vec;                        // and the table's
 };
@@ -46,10 +46,31 @@ __device__ __forceinline__ KvTurn kv_turn(const float* row, int rot, int e, bool
   return t;
 }
 
-// entries e .. e+7 of the head at x, turned
+// entries e .. e+7 of the head at x and, where the pairs are a multiple of eight entries apart, their partners, as they lie in memory
+template <typename T>
+struct KvRaw {
+  float own[8], partner[8];
+};
+template <>
+struct KvRaw<unsigned short> {
+  srv_u16x8 own, partner;
+};
+__device__ __forceinline__ void kv_load8(const float* p, bool vec, float (&x)[8]) { srv_ld8(p, vec, x); }
+__device__ __forceinline__ void kv_load8(const unsigned short* p, bool vec, srv_u16x8& x) {
+  x = __builtin_bit_cast(srv_u16x8, srv_ld8_bf16(p, vec));
+}
 template <typename T, bool HALF>
-__device__ __forceinline__ void kv_load_turned(const T* x, int rot, int e, bool vec, const KvTurn& t, float (&y)[8]) {
-  srv_ld8(x + e, vec, y);
+__device__ __forceinline__ void kv_load(const T* x, int rot, int e, bool vec, KvRaw<T>& raw) {
+  kv_load8(x + e, vec, raw.own);
+  const int half = rot / 2;
+  if (HALF && half % 8 == 0 && e < rot) kv_load8(x + (e < half ? e + half : e - half), vec, raw.partner);
+}
+
+// the entries turned
+template <typename T, bool HALF>
+__device__ __forceinline__ void kv_turned(const KvRaw<T>& raw, const T* x, int rot, int e, const KvTurn& t, float (&y)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = srv_widen(raw.own[i]);
   if (e >= rot) return;
   const int half = rot / 2;
   if constexpr (!HALF) {
@@ -62,14 +83,13 @@ __device__ __forceinline__ void kv_load_turned(const T* x, int rot, int e, bool 
         y[2 * i + 1] = b;
       }
   } else if (half % 8 == 0) {
-    float w[8], other;
-    srv_ld8(x + (e < half ? e + half : e - half), vec, w);
+    float other;
     if (e < half) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) srv_turn(y[i], w[i], t.c[i], t.s[i], y[i], other);
+      for (int i = 0; i < 8; ++i) srv_turn(y[i], srv_widen(raw.partner[i]), t.c[i], t.s[i], y[i], other);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) srv_turn(w[i], y[i], t.c[i], t.s[i], other, y[i]);
+      for (int i = 0; i < 8; ++i) srv_turn(srv_widen(raw.partner[i]), y[i], t.c[i], t.s[i], other, y[i]);
     }
   } else {
 #pragma unroll
@@ -124,63 +144,91 @@ struct KvPlace {  // of entries 8u .. 8u+7 of one token in one head of one page
   }
 };
 
-template <typename T, int D, bool HALF>
+constexpr int KV_MANY = 4;  // query heads, or tokens of a cache head, that a thread takes where there is enough work for it
+
+// Workgroups first of the cache's heads, then of the queries'.  Of the cache a workgroup takes N * 256/U tokens of one head; neighbouring workgroups
+// take other heads, so that (with a multiple of eight of them) a head's pages are all written through one XCD's cache, where the parts of a line
+// that two workgroups write come together.
+template <typename T, int D, bool HALF, int N>
 __global__ void __launch_bounds__(256) kv_append_kernel(const KvAppendArgs p) {
-  constexpr int U = D / 8;
+  constexpr int U = D / 8, TOKENS = 256 / U;
   const ttc_kv_append_t& a = p.a;
-  const int u = threadIdx.x % U, e = 8 * u;
-  const int64_t token = (int64_t)blockIdx.x * (256 / U) + threadIdx.x / U;
-  if (token >= a.tokens) return;
-  const int piece = blockIdx.y, heads = a.cache.heads;
-  const bool value = piece >= p.q_pieces + heads;
-  KvTurn t;
-  bool lost = false;
-  if (!value && a.rot) {
-    const int64_t pos = a.positions[token];
-    lost = (pos < 0 || pos >= a.table_rows) && e < a.rot;
-    if (!lost) t = kv_turn<HALF>(a.table + pos * a.rot, a.rot, e, p.t_vec);
-  }
-  if (piece < p.q_pieces) {
-    for (int i = 0; i < p.q_heads; ++i) {
-      const int h = piece * p.q_heads + i;
+  const int u = threadIdx.x % U, e = 8 * u, heads = a.cache.heads;
+  if (blockIdx.x >= p.cache_workgroups) {
+    const uint32_t b = blockIdx.x - p.cache_workgroups;
+    const int piece = b % p.q_pieces;
+    const int64_t token = (int64_t)(b / p.q_pieces) * TOKENS + threadIdx.x / U;
+    if (token >= a.tokens) return;
+    const int64_t pos = a.rot ? a.positions[token] : 0;
+    const bool lost = (pos < 0 || pos >= a.table_rows) && e < a.rot;
+    const int rot = lost ? 0 : a.rot;
+    // all heads' reads are under way before the first is written: in place a pair's two threads, of one wavefront, read each other's entries
+    KvRaw<T> raw[N];
+    const T* x[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int h = min(piece + i * p.q_pieces, a.heads_q - 1);
+      x[i] = static_cast<const T*>(a.q) + token * a.q_token + (int64_t)h * a.q_head;
+      kv_load<T, HALF>(x[i], rot, e, p.q_vec, raw[i]);
+    }
+    KvTurn t;
+    if (rot) t = kv_turn<HALF>(a.table + pos * a.rot, rot, e, p.t_vec);
+    float y[N][8];
+#pragma unroll
+    for (int i = 0; i < N; ++i) kv_turned<T, HALF>(raw[i], x[i], rot, e, t, y[i]);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int h = piece + i * p.q_pieces;
       if (h >= a.heads_q) break;
-      float y[8];
-      const T* x = static_cast<const T*>(a.q) + token * a.q_token + h * a.q_head;
-      kv_load_turned<T, HALF>(x, lost ? 0 : a.rot, e, p.q_vec, t, y);
-      // in place the partners of a pair are read by two threads of one wavefront: all of its reads come before its writes
-      __builtin_amdgcn_wave_barrier();
       if (lost) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) y[k] = e + k < a.rot ? __builtin_nanf("") : y[k];
+        for (int k = 0; k < 8; ++k) y[i][k] = e + k < a.rot ? __builtin_nanf("") : y[i][k];
       }
-      srv_st8(static_cast<T*>(a.q_out) + token * a.q_out_token + h * a.q_out_head + e, p.qo_vec, y);
+      srv_st8(static_cast<T*>(a.q_out) + token * a.q_out_token + (int64_t)h * a.q_out_head + e, p.qo_vec, y[i]);
     }
     return;
   }
-  const int64_t slot = a.slots[token];
+  const int piece = blockIdx.x % (2 * heads), h = piece >> 1;
+  const bool value = piece & 1;
+  const int64_t first = (int64_t)(blockIdx.x / (2 * heads)) * (N * TOKENS) + threadIdx.x / U;
   const int page = a.cache.page, log_page = __builtin_ctz(page);
-  if (slot < 0 || slot >= a.cache.pages * page) return;
-  const int h = piece - p.q_pieces - (value ? heads : 0);
-  float y[8];
-  if (value) {
-    srv_ld8(static_cast<const T*>(a.v) + token * a.v_token + h * a.v_head + e, p.v_vec, y);
-  } else {
-    kv_load_turned<T, HALF>(static_cast<const T*>(a.k) + token * a.k_token + h * a.k_head, lost ? 0 : a.rot, e, p.k_vec, t, y);
+  KvRaw<T> raw[N];
+  const T* x[N];
+  int64_t slot[N], pos[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int64_t token = min(first + i * TOKENS, a.tokens - 1);
+    slot[i] = first + i * TOKENS < a.tokens ? a.slots[token] : -1;
+    pos[i] = !value && a.rot ? a.positions[token] : 0;
+    x[i] = value ? static_cast<const T*>(a.v) + token * a.v_token + (int64_t)h * a.v_head
+                 : static_cast<const T*>(a.k) + token * a.k_token + (int64_t)h * a.k_head;
+    kv_load<T, HALF>(x[i], value ? 0 : a.rot, e, value ? p.v_vec : p.k_vec, raw[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const bool lost = !value && (pos[i] < 0 || pos[i] >= a.table_rows) && e < a.rot;
+    const int rot = value || lost ? 0 : a.rot;
+    KvTurn t;
+    if (rot) t = kv_turn<HALF>(a.table + pos[i] * a.rot, rot, e, p.t_vec);
+    float y[8];
+    kv_turned<T, HALF>(raw[i], x[i], rot, e, t, y);
     if (lost) y[0] = __builtin_nanf("");
+    uint32_t exp;
+    const uint32_t code = kv_quantise(y, exp);
+    if (slot[i] < 0 || slot[i] >= a.cache.pages * page) continue;
+    unsigned char* base = static_cast<unsigned char*>(a.cache.data) + ((slot[i] >> log_page) * heads + h) * (int64_t)KvParts<D>::bytes(page);
+    const KvPlace<D> at((int)(slot[i] & (page - 1)), u, page);
+    if (!value) {
+      *reinterpret_cast<uint32_t*>(base + at.codes_k) = code;
+    } else if constexpr (D == 64) {  // two lanes' shares of two bytes
+      *reinterpret_cast<unsigned short*>(base + at.codes_v) = (unsigned short)code;
+      *reinterpret_cast<unsigned short*>(base + at.codes_v + 4 * KvParts<D>::LANE) = (unsigned short)(code >> 16);
+    } else {
+      *reinterpret_cast<uint32_t*>(base + at.codes_v) = code;
+    }
+    if (u % 4 == 0) base[value ? at.exp_v : at.exp_k] = (unsigned char)exp;
   }
-  uint32_t exp;
-  const uint32_t code = kv_quantise(y, exp);
-  unsigned char* base = static_cast<unsigned char*>(a.cache.data) + ((slot >> log_page) * heads + h) * (int64_t)KvParts<D>::bytes(page);
-  const KvPlace<D> at((int)(slot & (page - 1)), u, page);
-  if (!value) {
-    *reinterpret_cast<uint32_t*>(base + at.codes_k) = code;
-  } else if constexpr (D == 64) {  // two lanes' shares of two bytes
-    *reinterpret_cast<unsigned short*>(base + at.codes_v) = (unsigned short)code;
-    *reinterpret_cast<unsigned short*>(base + at.codes_v + 4 * KvParts<D>::LANE) = (unsigned short)(code >> 16);
-  } else {
-    *reinterpret_cast<uint32_t*>(base + at.codes_v) = code;
-  }
-  if (u % 4 == 0) base[value ? at.exp_v : at.exp_k] = (unsigned char)exp;
 }
 
 // eight entries from their codes

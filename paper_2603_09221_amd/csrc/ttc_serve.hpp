@@ -48,6 +48,13 @@ __device__ __forceinline__ void srv_ld8(const unsigned short* p, bool vec, float
     for (int i = 0; i < 8; ++i) x[i] = srv_widen(p[i]);
   }
 }
+__device__ __forceinline__ srv_bf16x8 srv_ld8_bf16(const unsigned short* p, bool vec) {
+  if (vec) return *reinterpret_cast<const srv_bf16x8*>(p);
+  srv_u16x8 x;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = p[i];
+  return __builtin_bit_cast(srv_bf16x8, x);
+}
 __device__ __forceinline__ void srv_st8(float* p, bool vec, const float (&x)[8]) {
   if (vec) {
     *reinterpret_cast<srv_floatx4*>(p) = srv_floatx4{x[0], x[1], x[2], x[3]};
