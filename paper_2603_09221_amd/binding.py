@@ -632,26 +632,35 @@ def _vector(t, n, dtype, name):
     return t.data_ptr()
 
 
-def _same_device(dev, *tensors):
+def _same_device(first, *tensors):
+    at = first.get_device()
     for t in tensors:
-        if t is not None and t.device != dev:
+        if t is not None and t.get_device() != at:
             raise ValueError("all tensors must be on one device")
 
 
 def _rope_table(table, d):
-    if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+    rows, pairs, two = table.shape if table.dim() == 3 else (0, 0, 0)
+    if two != 2 or table.dtype is not torch.float32 or not table.is_contiguous():
         raise ValueError("table: expected a contiguous float32 (rows, rot / 2, 2) tensor")
-    if 2 * table.shape[1] > d:
+    if 2 * pairs > d:
         raise ValueError("table: more entries rotated than a head has")
-    return table.data_ptr(), table.shape[0], 2 * table.shape[1]
+    return table.data_ptr(), rows, 2 * pairs
 
 
 def _new(like, shape, dtype, stream):
     """A result tensor on the device of `like`, from the memory of the stream that the kernels run on."""
     if stream is None or stream == torch.cuda.current_stream():
-        return torch.empty_like(like) if shape is like.shape and dtype is like.dtype and like.is_contiguous() else like.new_empty(shape, dtype=dtype)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
         return like.new_empty(shape, dtype=dtype)
+
+
+def _new_like(t, stream):
+    """A contiguous tensor of the shape and type of t, likewise."""
+    if stream is None and t.is_contiguous():
+        return torch.empty_like(t)  # (half the time of new_empty)
+    return _new(t, t.shape, t.dtype, stream)
 
 
 def rope_frequencies(rot, *, base=10000.0, scaling=None, factor=1.0, trained=None, fast=32.0, slow=1.0):
@@ -708,9 +717,9 @@ def _rope(call, x, positions, table, layout, out, stream):
     tokens, heads, d = x.shape
     table_ptr, rows, rot = _rope_table(table, d)
     pos = _vector(positions, tokens, torch.int64, "positions")
-    _same_device(x.device, positions, table, out)
+    _same_device(x, positions, table, out)
     if out is None:
-        out = _new(x, x.shape, x.dtype, stream)
+        out = _new_like(x, stream)
     y_token, y_head = _heads_strides(out, "out", x.shape, x.dtype)
     if tokens and heads and d:
         _check(call(Rope(tokens, heads, d, rot, dtype, _rope_layout(layout), x.data_ptr(), out.data_ptr(), x_token, x_head, y_token,
@@ -768,7 +777,7 @@ def ttc_kv_append(cache, k, v, slots, positions=None, table=None, *, layout="hal
     if table is not None:
         table_ptr, rows, rot = _rope_table(table, d)
         pos = _vector(positions, tokens, torch.int64, "positions")
-    _same_device(cache.device, k, v, slots, positions, table, q, q_out)
+    _same_device(cache, k, v, slots, positions, table, q, q_out)
     heads_q = q_token = q_head = qo_token = qo_head = 0
     if q is not None:
         q_token, q_head = _heads_strides(q, "q")
@@ -776,7 +785,7 @@ def ttc_kv_append(cache, k, v, slots, positions=None, table=None, *, layout="hal
             raise ValueError("q: expected (%d, heads_q, %d)" % (tokens, d))
         heads_q = q.shape[1]
         if q_out is None:
-            q_out = _new(q, q.shape, q.dtype, stream)
+            q_out = _new_like(q, stream)
         qo_token, qo_head = _heads_strides(q_out, "q_out", q.shape)
     elif q_out is not None:
         raise ValueError("q_out without q")
@@ -799,7 +808,7 @@ def ttc_kv_read(cache, slots, d, *, dtype=torch.bfloat16, out=None, stream=None)
     for t in (k, v):
         if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
             raise ValueError("out: expected two contiguous %s tensors of %s" % (dtype, shape))
-    _same_device(cache.device, slots, k, v)
+    _same_device(cache, slots, k, v)
     if shape[0]:
         _check(load().ttc_kv_read(kv, at, shape[0], code, k.data_ptr(), v.data_ptr(), _stream_ptr(stream)))
     return k, v
@@ -818,9 +827,12 @@ def ttc_attention(q, cache, block_table, kv_len, *, cu_q=None, max_q=None, max_k
     q_token, q_head = _heads_strides(q, "q")
     tokens, heads_q, d = q.shape
     kv = _kv_cache(cache, d)
-    if block_table.dtype != torch.int32 or block_table.dim() != 2 or (block_table.shape[1] > 1 and block_table.stride(1) != 1):
-        raise ValueError("block_table: expected an int32 (sequences, pages) tensor with contiguous rows")
+    if block_table.dtype is not torch.int32 or block_table.dim() != 2:
+        raise ValueError("block_table: expected an int32 (sequences, pages) tensor")
     sequences, width = block_table.shape
+    table_stride, step = block_table.stride()
+    if step != 1 and width > 1:
+        raise ValueError("block_table: expected contiguous rows")
     lens = _vector(kv_len, sequences, torch.int32, "kv_len")
     room = width * kv.page
     if max_kv is None:
@@ -836,21 +848,20 @@ def ttc_attention(q, cache, block_table, kv_len, *, cu_q=None, max_q=None, max_k
         if tokens != sequences:
             raise ValueError("q: %d rows for %d sequences" % (tokens, sequences))
         max_q = 1
-    _same_device(cache.device, q, block_table, kv_len, cu_q, workspace)
-    out = dict(out or {})
-    if "out" not in out:
-        out["out"] = _new(q, q.shape, q.dtype, stream)
-    y = out["out"]
-    out_token, out_head = _heads_strides(y, "out", q.shape, q.dtype)
-    if want_lse and "lse" not in out:
-        out["lse"] = _new(q, (tokens, heads_q), torch.float32, stream)
-    lse = out.get("lse")
-    if lse is not None and (tuple(lse.shape) != (tokens, heads_q) or lse.dtype != torch.float32 or not lse.is_contiguous()):
+    _same_device(cache, q, block_table, kv_len, cu_q, workspace)
+    out = dict(out) if out else {}
+    y, lse = out.get("out"), out.get("lse")
+    if lse is not None and (lse.shape != (tokens, heads_q) or lse.dtype is not torch.float32 or not lse.is_contiguous()):
         raise ValueError("lse: expected a contiguous float32 (tokens, heads_q) tensor")
-    _same_device(cache.device, y, lse)
+    _same_device(cache, y, lse)
+    if y is None:
+        y = out["out"] = _new_like(q, stream)
+    out_token, out_head = _heads_strides(y, "out", q.shape, q.dtype)
+    if want_lse and lse is None:
+        lse = out["lse"] = _new(q, (tokens, heads_q), torch.float32, stream)
     att = Attention(kv, sequences, tokens, heads_q, dtype, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, max_q, max_kv,
                     q.data_ptr(), y.data_ptr(), _ptr(lse), q_token, q_head, out_token, out_head, cu, lens, block_table.data_ptr(),
-                    block_table.stride(0))
+                    table_stride)
     need = lib.ttc_attention_workspace_bytes(att)
     if need and workspace is None:
         workspace = _new(q, (need,), torch.uint8, stream)

@@ -48,8 +48,12 @@ hipError_t launch_kv_append(const ttc_kv_append_t& a, int cus, hipStream_t st) {
 template <typename T, int D>
 static void read(const ttc_kv_cache_t& c, const int64_t* slots, int64_t n, void* k, void* v, hipStream_t st) {
   constexpr int TOKENS = 256 / (D / 8);
-  hipLaunchKernelGGL((kv_read_kernel<T, D>), dim3((unsigned)((n + TOKENS - 1) / TOKENS), (unsigned)c.heads), dim3(256), 0, st, c, slots, n,
-                     static_cast<T*>(k), static_cast<T*>(v));
+  const dim3 grid((unsigned)((n + TOKENS - 1) / TOKENS), (unsigned)c.heads);
+  // from 16 MiB of results on they are written past the caches: 16384 tokens of 8 heads of 128 take 16 us instead of 22
+  if (2 * n * c.heads * D * (int64_t)sizeof(T) >= (16ll << 20))
+    hipLaunchKernelGGL((kv_read_kernel<T, D, true>), grid, dim3(256), 0, st, c, slots, n, static_cast<T*>(k), static_cast<T*>(v));
+  else
+    hipLaunchKernelGGL((kv_read_kernel<T, D, false>), grid, dim3(256), 0, st, c, slots, n, static_cast<T*>(k), static_cast<T*>(v));
 }
 
 hipError_t launch_kv_read(const ttc_kv_cache_t& c, const int64_t* slots, int64_t n, bool bf16, void* k, void* v, hipStream_t st) {

@@ -136,6 +136,15 @@ __device__ __forceinline__ srv_bf16x8 att_widen(uint32_t code, float scale) {
 // 128 in every byte that is 255
 __device__ __forceinline__ uint32_t att_full_bytes(uint32_t x) { return x & ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
+// Codes of a wavefront's step, which nobody else reads soon: past the caches' replacement, 114 us a call instead of 131 over 4 x 131072 tokens,
+// 122 instead of 136 over 64 sequences of 257 to 16384 (d = 128; where row tiles share a context it costs up to 8 %).  With heads of 256 a
+// lane's 32 bytes take two reads of the same lines, and the second would miss (16 x 4096 tokens 63 us instead of 51).
+template <int D, typename W>
+__device__ __forceinline__ W att_stream(const W* p) {
+  if constexpr (D <= 128) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+
 // What a workgroup reads the cache with, the same for all of its lanes
 struct AttSource {
   const unsigned char* cache;  // the workgroup's head of page 0
@@ -183,7 +192,7 @@ struct AttKeys {
     for (int i = 0; i < 4; ++i) {
       const unsigned char* base = s.base(page[i]);
       const uint32_t token = ((n0 + 16 * i) & (s.page_tokens - 1)) + c;
-      code[i] = *reinterpret_cast<const word_t*>(base + (token * P::TOKEN + g * (D / 8)));
+      code[i] = att_stream<D>(reinterpret_cast<const word_t*>(base + (token * P::TOKEN + g * (D / 8))));
       const uint32_t at = P::key_exps(s.page_tokens) + token * P::BLOCKS;
       exp[i] = D == 256 ? *reinterpret_cast<const unsigned short*>(base + (at + 2 * g)) : base[at + (D == 64 ? g / 2 : g)];
     }
@@ -200,7 +209,7 @@ struct AttValues {
     for (int i = 0; i < 4; ++i) {
       const unsigned char* base = s.base(page[i]);
       const uint32_t four = ((n0 + 16 * i) & (s.page_tokens - 1)) / 4 + g;
-      code[i] = *reinterpret_cast<const word_t*>(base + (P::values(s.page_tokens) + (four * 16 + c) * (4 * P::LANE)));
+      code[i] = att_stream<D>(reinterpret_cast<const word_t*>(base + (P::values(s.page_tokens) + (four * 16 + c) * (4 * P::LANE))));
       exp[i] = *reinterpret_cast<const uint32_t*>(base + (P::value_exps(s.page_tokens) + (four * P::BLOCKS + c * (D / 16) / 32) * 4));
     }
   }
@@ -338,7 +347,7 @@ __device__ __forceinline__ bool att_join(const AttentionArgs& p, const AttTile& 
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(sizeof(T) == 2, D)) attention_kernel(const AttentionArgs p) {
+__global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(D)) attention_kernel(const AttentionArgs p) {
   constexpr bool BF16 = sizeof(T) == 2;
   constexpr int TERMS = BF16 ? 1 : 3;   // bfloat16 parts of a query and of a weight
   constexpr int KS = D / 32;            // products of 32 entries that a score takes

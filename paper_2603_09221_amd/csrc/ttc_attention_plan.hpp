@@ -18,8 +18,10 @@ constexpr int PROMPT_WAVES = 4;  // wavefronts of a workgroup of the kernel for 
 // at most 1.28 times faster, so those shapes do without.
 constexpr bool prompt_kernel(bool bf16, int d) { return d == 64 || (bf16 && d == 128); }
 
-// workgroups of a compute unit, by the registers that a wavefront takes
-constexpr int att_resident(bool bf16, int d) { return d == 64 || (bf16 && d == 128) ? 3 : 2; }
+// Workgroups that a compute unit holds at once, by the registers that a wavefront needs; d = 64 / 128 / 256.  Measured with one / two / three (us;
+// with three, d = 128 spills, as d = 256 does with two): bfloat16, 64 sequences of 257 to 16384 tokens at d = 64 140 / 95 / 77, four of 65536
+// at d = 128 73 / 55 / 68, four of 32768 at d = 256 61 / 98 / 97.
+constexpr int att_resident(int d) { return d == 64 ? 3 : d == 128 ? 2 : 1; }
 
 struct AttentionArgs {
   ttc_attention_t a;
@@ -62,7 +64,7 @@ inline void plan_attention(AttentionArgs& p, int cus) {
   p.row_tiles = (int32_t)((rows + tile - 1) / tile);
   p.entries = (int32_t)(a.sequences * p.row_tiles);
   p.items = (int64_t)p.entries * a.cache.heads;
-  const int64_t slots = (int64_t)att_resident(a.dtype == TTC_BF16, a.cache.d) * cus;
+  const int64_t slots = (int64_t)att_resident(a.cache.d) * cus;
   const int64_t units = (visible_at_most(a, p.group) + ATT_UNIT - 1) / ATT_UNIT;
   p.shared = !p.prompt && units > 1 && p.entries <= 1024 && p.items < 8 * slots && (double)units * p.items < 1e9;
   p.workgroups = !p.shared ? p.items : units * p.items < slots ? units * p.items : slots;

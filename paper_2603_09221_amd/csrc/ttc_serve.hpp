@@ -76,6 +76,26 @@ __device__ __forceinline__ void srv_st8(unsigned short* p, bool vec, const float
   }
 }
 
+// eight entries of a large result, past the caches' replacement
+__device__ __forceinline__ void srv_stream8(float* p, bool vec, const float (&x)[8]) {
+  if (vec) {
+    __builtin_nontemporal_store(srv_floatx4{x[0], x[1], x[2], x[3]}, reinterpret_cast<srv_floatx4*>(p));
+    __builtin_nontemporal_store(srv_floatx4{x[4], x[5], x[6], x[7]}, reinterpret_cast<srv_floatx4*>(p + 4));
+  } else {
+    srv_st8(p, false, x);
+  }
+}
+__device__ __forceinline__ void srv_stream8(unsigned short* p, bool vec, const float (&x)[8]) {
+  if (vec) {
+    srv_u16x8 v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = srv_narrow<unsigned short>(x[i]);
+    __builtin_nontemporal_store(v, reinterpret_cast<srv_u16x8*>(p));
+  } else {
+    srv_st8(p, false, x);
+  }
+}
+
 // Two entries of a pair turned by (cos, sin): each product and the sum rounded on its own, so that the key that the cache takes is
 // the same number, to the last bit, as the rotation gives by itself (a contracted multiply-add would round differently, and
 // entries that lie between two codes would go the other way).
