@@ -375,221 +375,222 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(D)) attention_ker
   }
   bool first_item = true;
   while (unit < stop) {
-  const int64_t seq = entry / p.row_tiles;
-  const int tile = entry % p.row_tiles;
-  const AttTile t = att_tile(p, seq, tile, c);
-  const uint32_t units = __builtin_amdgcn_readfirstlane(att_units(t));
-  uint32_t take = units, from = 0;
-  if (p.shared) {
-    if (rest >= units * a.cache.heads) {  // the next entry (the first one found is not done yet)
-      ++entry;
-      rest = 0;
-      continue;
+    const int64_t seq = entry / p.row_tiles;
+    const int tile = entry % p.row_tiles;
+    const AttTile t = att_tile(p, seq, tile, c);
+    const uint32_t units = __builtin_amdgcn_readfirstlane(att_units(t));
+    uint32_t take = units, from = 0;
+    if (p.shared) {
+      if (rest >= units * a.cache.heads) {  // the next entry (the first one found is not done yet)
+        ++entry;
+        rest = 0;
+        continue;
+      }
+      head = (int)(rest / units);
+      from = rest % units;
+      take = min(units - from, stop - unit);
     }
-    head = (int)(rest / units);
-    from = rest % units;
-    take = min(units - from, stop - unit);
-  }
-  const int begin = t.lo + (int)from * ATT_UNIT, end = min(t.hi, begin + (int)take * ATT_UNIT);
+    const int begin = t.lo + (int)from * ATT_UNIT, end = min(t.hi, begin + (int)take * ATT_UNIT);
 
-  // page numbers, queries and the first step's codes are on their way together
-  const AttSource src(p, seq, head, end);
-  constexpr int STRIDE = ATT_STEP * ATT_WAVES;
-  int page[4], n0 = begin + wave * ATT_STEP;
-  if (n0 < end) src.look_up(n0, page);
+    // page numbers, queries and the first step's codes are on their way together
+    const AttSource src(p, seq, head, end);
+    constexpr int STRIDE = ATT_STEP * ATT_WAVES;
+    int page[4], n0 = begin + wave * ATT_STEP;
+    if (n0 < end) src.look_up(n0, page);
 
-  // the lane's share of its row: entries g*D/4 .. of every part
-  srv_bf16x8 q[TERMS][KS];
-  float query[BF16 ? 1 : KS][8];
-  {
-    const int r = tile * ATT_ROWS + c;
-    const bool real = r < t.rows;
-    const T* x = static_cast<const T*>(a.q) + (real ? (t.first_q + r / p.group) * a.q_token + (int64_t)(head * p.group + r % p.group) * a.q_head : 0) + g * (D / 4);
-    const bool vec = (uint64_t)a.q % 16 == 0 && (a.q_token | a.q_head) % (16 / (int)sizeof(T)) == 0;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      if constexpr (BF16) {
-        q[0][s] = srv_bf16x8{};
-        if (real) q[0][s] = srv_ld8_bf16(x + 8 * s, vec);
+    // the lane's share of its row: entries g*D/4 .. of every part
+    srv_bf16x8 q[TERMS][KS];
+    float query[BF16 ? 1 : KS][8];
+    {
+      const int r = tile * ATT_ROWS + c;
+      const bool real = r < t.rows;
+      const int64_t at = real ? (t.first_q + r / p.group) * a.q_token + (int64_t)(head * p.group + r % p.group) * a.q_head : 0;
+      const T* x = static_cast<const T*>(a.q) + at + g * (D / 4);
+      const bool vec = (uint64_t)a.q % 16 == 0 && (a.q_token | a.q_head) % (16 / (int)sizeof(T)) == 0;
+  #pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        if constexpr (BF16) {
+          q[0][s] = srv_bf16x8{};
+          if (real) q[0][s] = srv_ld8_bf16(x + 8 * s, vec);
+        } else {
+  #pragma unroll
+          for (int i = 0; i < 8; ++i) query[s][i] = 0.f;
+          if (real) srv_ld8(x + 8 * s, vec, query[s]);
+        }
+      }
+    }
+    srv_floatx4 o[E] = {};
+    float m = -INFINITY, l = 0.f;
+    const float to_log2 = a.scale * 1.44269504088896340736f;
+    // Keys and values of the next step are read into the registers that this step has just done with, and the page numbers of the step
+    // after it: the reads are under way during the other product and the softmax, and while other wavefronts of the SIMD work.
+    AttKeys<D> keys;
+    AttValues<D> values;
+    if (n0 < end) {
+      keys.load(src, page, n0, c, g);
+      values.load(src, page, n0, c, g);
+      src.look_up(n0 + STRIDE, page);
+    }
+    if constexpr (!BF16) {
+  #pragma unroll
+      for (int s = 0; s < KS; ++s)
+  #pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          __bf16 part[TERMS];
+          att_split<TERMS>(query[s][i], part);
+  #pragma unroll
+          for (int k = 0; k < TERMS; ++k) q[k][s][i] = part[k];
+        }
+    }
+    for (; n0 < end; n0 += STRIDE) {
+      const bool more = n0 + STRIDE < end;
+      const int there = keys.there;
+      // scores: S^T = K Q^T, sixteen tokens at a time
+      srv_floatx4 z[4];
+  #pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        z[i] = srv_floatx4{};
+  #pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          const srv_bf16x8 key = att_widen(keys.code[i][k], srv_scale((keys.exp[i] >> (D == 256 ? 8 * (k / 4) : 0)) & 255));
+  #pragma unroll
+          for (int x = TERMS - 1; x >= 0; --x) z[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[x][k], z[i], 0, 0, 0);
+        }
+      }
+      if (more) keys.load(src, page, n0 + STRIDE, c, g);
+      if (n0 < t.all_lo || n0 + ATT_STEP > t.all_hi || there != 15) {
+  #pragma unroll
+        for (int i = 0; i < 4; ++i)
+  #pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int n = n0 + 16 * i + 4 * g + j;
+            z[i][j] = (there >> i & 1) && n >= t.first && n <= t.last ? z[i][j] * to_log2 : -INFINITY;
+          }
       } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) query[s][i] = 0.f;
-        if (real) srv_ld8(x + 8 * s, vec, query[s]);
+  #pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] *= to_log2;
       }
-    }
-  }
-  srv_floatx4 o[E] = {};
-  float m = -INFINITY, l = 0.f;
-  const float to_log2 = a.scale * 1.44269504088896340736f;
-  // Keys and values of the next step are read into the registers that this step has just done with, and the page numbers of the step
-  // after it: the reads are under way during the other product and the softmax, and while other wavefronts of the SIMD work.
-  AttKeys<D> keys;
-  AttValues<D> values;
-  if (n0 < end) {
-    keys.load(src, page, n0, c, g);
-    values.load(src, page, n0, c, g);
-    src.look_up(n0 + STRIDE, page);
-  }
-  if constexpr (!BF16) {
-#pragma unroll
-    for (int s = 0; s < KS; ++s)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        __bf16 part[TERMS];
-        att_split<TERMS>(query[s][i], part);
-#pragma unroll
-        for (int k = 0; k < TERMS; ++k) q[k][s][i] = part[k];
-      }
-  }
-  for (; n0 < end; n0 += STRIDE) {
-    const bool more = n0 + STRIDE < end;
-    const int there = keys.there;
-    // scores: S^T = K Q^T, sixteen tokens at a time
-    srv_floatx4 z[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      z[i] = srv_floatx4{};
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        const srv_bf16x8 key = att_widen(keys.code[i][k], srv_scale((keys.exp[i] >> (D == 256 ? 8 * (k / 4) : 0)) & 255));
-#pragma unroll
-        for (int x = TERMS - 1; x >= 0; --x) z[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[x][k], z[i], 0, 0, 0);
-      }
-    }
-    if (more) keys.load(src, page, n0 + STRIDE, c, g);
-    if (n0 < t.all_lo || n0 + ATT_STEP > t.all_hi || there != 15) {
-#pragma unroll
+      // The maximum that weights are relative to moves only when a score passes it by 8 (weights stay below 2^8, which costs float32 sums
+      // nothing): most steps need no exchange between lanes and no rescaling.
+      float top = -INFINITY;
+  #pragma unroll
       for (int i = 0; i < 4; ++i)
-#pragma unroll
+  #pragma unroll
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, z[i][j]);
+      if (__builtin_amdgcn_ballot_w64(top > m + 8.f)) {
+        top = fmaxf(m, top);
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float shrink = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));  // (a row that has seen nothing yet)
+        m = top;
+        l *= shrink;
+  #pragma unroll
+        for (int i = 0; i < E; ++i) o[i] *= shrink;
+      }
+      const float zero = m == -INFINITY ? 0.f : m;
+  #pragma unroll
+      for (int i = 0; i < 4; ++i)
+  #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int n = n0 + 16 * i + 4 * g + j;
-          z[i][j] = (there >> i & 1) && n >= t.first && n <= t.last ? z[i][j] * to_log2 : -INFINITY;
+          z[i][j] = __builtin_amdgcn_exp2f(z[i][j] - zero);
+          l += z[i][j];
         }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) z[i] *= to_log2;
-    }
-    // The maximum that weights are relative to moves only when a score passes it by 8 (weights stay below 2^8, which costs float32 sums
-    // nothing): most steps need no exchange between lanes and no rescaling.
-    float top = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) top = fmaxf(top, z[i][j]);
-    if (__builtin_amdgcn_ballot_w64(top > m + 8.f)) {
-      top = fmaxf(m, top);
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
-      const float shrink = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));  // (a row that has seen nothing yet)
-      m = top;
-      l *= shrink;
-#pragma unroll
-      for (int i = 0; i < E; ++i) o[i] *= shrink;
-    }
-    const float zero = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        z[i][j] = __builtin_amdgcn_exp2f(z[i][j] - zero);
-        l += z[i][j];
-      }
-    // O^T += V^T P^T, 32 tokens at a time: lane (c, g) has tokens 4g .. 4g+3 of two sixteens
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      srv_bf16x8 w[TERMS];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        __bf16 part[TERMS];
-        att_split<TERMS>(z[2 * h + k / 4][k % 4], part);
-#pragma unroll
-        for (int x = 0; x < TERMS; ++x) w[x][k] = part[x];
-      }
-      uint32_t exps[2] = {values.exp[2 * h], values.exp[2 * h + 1]};
-      // A weight of 0 takes out any number, but not NaN.  Blocks of NaN are rare: they are read as numbers, and what the rows that
-      // see them get is made NaN by a product of its own.
-      const uint32_t nan0 = att_full_bytes(exps[0]), nan1 = att_full_bytes(exps[1]);
-      if (__builtin_amdgcn_ballot_w64((nan0 | nan1) != 0)) {
-        srv_bf16x8 bad, seen;
-#pragma unroll
+      // O^T += V^T P^T, 32 tokens at a time: lane (c, g) has tokens 4g .. 4g+3 of two sixteens
+  #pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        srv_bf16x8 w[TERMS];
+  #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const int i = 2 * h + k / 4, n = n0 + 16 * i + 4 * g + k % 4;
-          bad[k] = static_cast<__bf16>((k < 4 ? nan0 : nan1) >> (8 * (k % 4)) & 128 ? 1.f : 0.f);
-          seen[k] = static_cast<__bf16>((there >> i & 1) && n >= t.first && n <= t.last ? 1.f : 0.f);
+          __bf16 part[TERMS];
+          att_split<TERMS>(z[2 * h + k / 4][k % 4], part);
+  #pragma unroll
+          for (int x = 0; x < TERMS; ++x) w[x][k] = part[x];
         }
-        const srv_floatx4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bad, seen, srv_floatx4{}, 0, 0, 0);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int e = 0; e < E; ++e) o[e][j] = hit[j] > 0.f ? __builtin_nanf("") : o[e][j];
-        exps[0] ^= nan0;
-        exps[1] ^= nan1;
+        uint32_t exps[2] = {values.exp[2 * h], values.exp[2 * h + 1]};
+        // A weight of 0 takes out any number, but not NaN.  Blocks of NaN are rare: they are read as numbers, and what the rows that
+        // see them get is made NaN by a product of its own.
+        const uint32_t nan0 = att_full_bytes(exps[0]), nan1 = att_full_bytes(exps[1]);
+        if (__builtin_amdgcn_ballot_w64((nan0 | nan1) != 0)) {
+          srv_bf16x8 bad, seen;
+  #pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int i = 2 * h + k / 4, n = n0 + 16 * i + 4 * g + k % 4;
+            bad[k] = static_cast<__bf16>((k < 4 ? nan0 : nan1) >> (8 * (k % 4)) & 128 ? 1.f : 0.f);
+            seen[k] = static_cast<__bf16>((there >> i & 1) && n >= t.first && n <= t.last ? 1.f : 0.f);
+          }
+          const srv_floatx4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bad, seen, srv_floatx4{}, 0, 0, 0);
+  #pragma unroll
+          for (int j = 0; j < 4; ++j)
+  #pragma unroll
+            for (int e = 0; e < E; ++e) o[e][j] = hit[j] > 0.f ? __builtin_nanf("") : o[e][j];
+          exps[0] ^= nan0;
+          exps[1] ^= nan1;
+        }
+  #pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          srv_bf16x8 v0, v1;
+  #pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const srv_bf16x2 two = att_value_pair<E>(values.code[2 * h + k / 4], k % 4, e, srv_scale((exps[k / 4] >> (8 * (k % 4))) & 255));
+            v0[k] = two[0];
+            v1[k] = two[1];
+          }
+  #pragma unroll
+          for (int x = TERMS - 1; x >= 0; --x) {
+            o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, w[x], o[e], 0, 0, 0);
+            o[e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, w[x], o[e + 1], 0, 0, 0);
+          }
+        }
       }
-#pragma unroll
-      for (int e = 0; e < E; e += 2) {
-        srv_bf16x8 v0, v1;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const srv_bf16x2 two = att_value_pair<E>(values.code[2 * h + k / 4], k % 4, e, srv_scale((exps[k / 4] >> (8 * (k % 4))) & 255));
-          v0[k] = two[0];
-          v1[k] = two[1];
-        }
-#pragma unroll
-        for (int x = TERMS - 1; x >= 0; --x) {
-          o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, w[x], o[e], 0, 0, 0);
-          o[e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, w[x], o[e + 1], 0, 0, 0);
-        }
+      if (more) {
+        values.load(src, page, n0 + STRIDE, c, g);
+        src.look_up(n0 + 2 * STRIDE, page);
       }
     }
-    if (more) {
-      values.load(src, page, n0 + STRIDE, c, g);
-      src.look_up(n0 + 2 * STRIDE, page);
-    }
-  }
-  l += __shfl_xor(l, 16, 64);
-  l += __shfl_xor(l, 32, 64);
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
 
-  // the wavefronts' results join: lane (c, g) holds entries (4g + j)*E + e of row c
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int e = 0; e < E; ++e) part_o[wave][c][(4 * g + j) * E + e] = o[e][j];
-  if (g == 0) {
-    part_m[wave][c] = m;
-    part_l[wave][c] = l;
-  }
-  __syncthreads();
-  int row = threadIdx.x / 16;
-  const int e0 = (threadIdx.x % 16) * E;
-  float mm = -INFINITY, ll = 0.f, sum[E] = {};
-#pragma unroll
-  for (int w = 0; w < ATT_WAVES; ++w) mm = fmaxf(mm, part_m[w][row]);
-  const float zero = mm == -INFINITY ? 0.f : mm;
-#pragma unroll
-  for (int w = 0; w < ATT_WAVES; ++w) {
-    const float f = __builtin_amdgcn_exp2f(part_m[w][row] - zero);
-    ll += f * part_l[w][row];
-#pragma unroll
-    for (int e = 0; e < E; ++e) sum[e] += f * part_o[w][row][e0 + e];
-  }
-  bool writes = row < t.real;
-  if (take < units) writes = att_join<D>(p, t, unit - from, units, total, used, 2 * blockIdx.x + (first_item ? 0 : 1), row, e0,
-                                         mm, ll, sum, &part_o[0][0][0], &part_m[0][0], &joins);
-  if (writes) {
-    const float f = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
-    const int r = tile * ATT_ROWS + row;
-    const int64_t token = t.first_q + r / p.group;
-    const int h = head * p.group + r % p.group;
-    T* y = static_cast<T*>(a.out) + token * a.out_token + (int64_t)h * a.out_head + e0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) y[e] = srv_narrow<T>(f * sum[e]);
-    if (a.lse && threadIdx.x % 16 == 0) a.lse[token * a.heads_q + h] = (mm + __builtin_log2f(ll)) * 0.69314718055994530942f;
-  }
-  if (!p.shared) return;
-  unit += take;
-  rest += take;
-  first_item = false;
-  __syncthreads();  // before the next item's results
+    // the wavefronts' results join: lane (c, g) holds entries (4g + j)*E + e of row c
+  #pragma unroll
+    for (int j = 0; j < 4; ++j)
+  #pragma unroll
+      for (int e = 0; e < E; ++e) part_o[wave][c][(4 * g + j) * E + e] = o[e][j];
+    if (g == 0) {
+      part_m[wave][c] = m;
+      part_l[wave][c] = l;
+    }
+    __syncthreads();
+    int row = threadIdx.x / 16;
+    const int e0 = (threadIdx.x % 16) * E;
+    float mm = -INFINITY, ll = 0.f, sum[E] = {};
+  #pragma unroll
+    for (int w = 0; w < ATT_WAVES; ++w) mm = fmaxf(mm, part_m[w][row]);
+    const float zero = mm == -INFINITY ? 0.f : mm;
+  #pragma unroll
+    for (int w = 0; w < ATT_WAVES; ++w) {
+      const float f = __builtin_amdgcn_exp2f(part_m[w][row] - zero);
+      ll += f * part_l[w][row];
+  #pragma unroll
+      for (int e = 0; e < E; ++e) sum[e] += f * part_o[w][row][e0 + e];
+    }
+    bool writes = row < t.real;
+    if (take < units) writes = att_join<D>(p, t, unit - from, units, total, used, 2 * blockIdx.x + (first_item ? 0 : 1), row, e0,
+                                           mm, ll, sum, &part_o[0][0][0], &part_m[0][0], &joins);
+    if (writes) {
+      const float f = ll > 0.f || ll != ll ? 1.f / ll : 0.f;
+      const int r = tile * ATT_ROWS + row;
+      const int64_t token = t.first_q + r / p.group;
+      const int h = head * p.group + r % p.group;
+      T* y = static_cast<T*>(a.out) + token * a.out_token + (int64_t)h * a.out_head + e0;
+  #pragma unroll
+      for (int e = 0; e < E; ++e) y[e] = srv_narrow<T>(f * sum[e]);
+      if (a.lse && threadIdx.x % 16 == 0) a.lse[token * a.heads_q + h] = (mm + __builtin_log2f(ll)) * 0.69314718055994530942f;
+    }
+    if (!p.shared) return;
+    unit += take;
+    rest += take;
+    first_item = false;
+    __syncthreads();  // before the next item's results
   }
 }
 

@@ -175,6 +175,19 @@ def test_long_contexts_are_shared_and_joined(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("heads,group,d,page", [(1, 5, 64, 16), (2, 16, 128, 64), (1, 3, 256, 32)])
+def test_many_sequences_share_a_long_context(heads, group, d, page, dtype):
+    """More sequences and row tiles than a wavefront has lanes, some of them empty, beside contexts that several workgroups divide; and the short
+    ones alone, which take a workgroup each."""
+    lengths = [37 * i % 301 for i in range(70)]
+    s = Setup(lengths[:35] + [2900] + lengths[35:] + [0, 1500], [(i + 1) % 4 for i in range(73)], heads, group, d, page, dtype, seed=d)
+    s.check(binding.ttc_attention(**s.gpu()))
+    s.check(binding.ttc_attention(**s.gpu(), window=1900), window=1900)
+    s = Setup(lengths, [i % 4 for i in range(70)], heads, group, d, page, dtype, seed=d)
+    s.check(binding.ttc_attention(**s.gpu()))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_nan_reaches_the_rows_that_see_it_only(dtype):
     """A token whose keys (or values) are NaN: earlier tokens' rows, and rows whose window has passed it, have no trace of it."""
     for part, window in (("key", 0), ("key", 9), ("value", 0), ("value", 9)):
