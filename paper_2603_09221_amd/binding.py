@@ -720,7 +720,9 @@ def _rope(call, x, positions, table, layout, out, stream):
     _same_device(x, positions, table, out)
     if out is None:
         out = _new_like(x, stream)
-    y_token, y_head = _heads_strides(out, "out", x.shape, x.dtype)
+        y_token, y_head = heads * d, d
+    else:
+        y_token, y_head = _heads_strides(out, "out", x.shape, x.dtype)
     if tokens and heads and d:
         _check(call(Rope(tokens, heads, d, rot, dtype, _rope_layout(layout), x.data_ptr(), out.data_ptr(), x_token, x_head, y_token,
                          y_head, pos, table_ptr, rows), _stream_ptr(stream)))
@@ -786,7 +788,9 @@ def ttc_kv_append(cache, k, v, slots, positions=None, table=None, *, layout="hal
         heads_q = q.shape[1]
         if q_out is None:
             q_out = _new_like(q, stream)
-        qo_token, qo_head = _heads_strides(q_out, "q_out", q.shape)
+            qo_token, qo_head = heads_q * d, d
+        else:
+            qo_token, qo_head = _heads_strides(q_out, "q_out", q.shape)
     elif q_out is not None:
         raise ValueError("q_out without q")
     if tokens:
@@ -804,11 +808,16 @@ def ttc_kv_read(cache, slots, d, *, dtype=torch.bfloat16, out=None, stream=None)
     if code is None:
         raise ValueError("dtype must be float32 or bfloat16")
     shape = (slots.shape[0], kv.heads, d)
-    k, v = out if out is not None else (_new(cache, shape, dtype, stream), _new(cache, shape, dtype, stream))
-    for t in (k, v):
-        if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
-            raise ValueError("out: expected two contiguous %s tensors of %s" % (dtype, shape))
-    _same_device(cache, slots, k, v)
+    if out is None:
+        k = _new(cache, shape, dtype, stream)
+        v = _new_like(k, stream)
+        _same_device(cache, slots)
+    else:
+        k, v = out
+        for t in (k, v):
+            if tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+                raise ValueError("out: expected two contiguous %s tensors of %s" % (dtype, shape))
+        _same_device(cache, slots, k, v)
     if shape[0]:
         _check(load().ttc_kv_read(kv, at, shape[0], code, k.data_ptr(), v.data_ptr(), _stream_ptr(stream)))
     return k, v
@@ -849,14 +858,18 @@ def ttc_attention(q, cache, block_table, kv_len, *, cu_q=None, max_q=None, max_k
             raise ValueError("q: %d rows for %d sequences" % (tokens, sequences))
         max_q = 1
     _same_device(cache, q, block_table, kv_len, cu_q, workspace)
+    y = lse = None
+    if out:
+        y, lse = out.get("out"), out.get("lse")
+        if lse is not None and (lse.shape != (tokens, heads_q) or lse.dtype is not torch.float32 or not lse.is_contiguous()):
+            raise ValueError("lse: expected a contiguous float32 (tokens, heads_q) tensor")
+        _same_device(cache, y, lse)
     out = dict(out) if out else {}
-    y, lse = out.get("out"), out.get("lse")
-    if lse is not None and (lse.shape != (tokens, heads_q) or lse.dtype is not torch.float32 or not lse.is_contiguous()):
-        raise ValueError("lse: expected a contiguous float32 (tokens, heads_q) tensor")
-    _same_device(cache, y, lse)
     if y is None:
         y = out["out"] = _new_like(q, stream)
-    out_token, out_head = _heads_strides(y, "out", q.shape, q.dtype)
+        out_token, out_head = heads_q * d, d
+    else:
+        out_token, out_head = _heads_strides(y, "out", q.shape, q.dtype)
     if want_lse and lse is None:
         lse = out["lse"] = _new(q, (tokens, heads_q), torch.float32, stream)
     att = Attention(kv, sequences, tokens, heads_q, dtype, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, max_q, max_kv,
