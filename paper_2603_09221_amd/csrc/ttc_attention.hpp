@@ -583,7 +583,8 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(D)) attention_ker
       const int h = head * p.group + r % p.group;
       T* y = static_cast<T*>(a.out) + token * a.out_token + (int64_t)h * a.out_head + e0;
   #pragma unroll
-      for (int e = 0; e < E; ++e) y[e] = srv_narrow<T>(f * sum[e]);
+      for (int e = 0; e < E; ++e) sum[e] *= f;
+      srv_st(y, (uint64_t)a.out % 16 == 0 && (a.out_token | a.out_head) % (16 / (int)sizeof(T)) == 0, sum);
       if (a.lse && threadIdx.x % 16 == 0) a.lse[token * a.heads_q + h] = (mm + __builtin_log2f(ll)) * 0.69314718055994530942f;
     }
     if (!p.shared) return;

@@ -71,7 +71,7 @@ inline void plan_attention(AttentionArgs& p, int cus) {
   const int64_t units = (visible_at_most(a, p.group) + ATT_UNIT - 1) / ATT_UNIT;
   const int64_t own = 4 * p.items / cus;
   p.shared = !p.prompt && units > (own > 4 ? own : 4) && p.entries <= 1024 && (double)units * p.items < 1e9;
-  p.workgroups = !p.shared ? p.items : units * p.items < slots ? units * p.items : slots;
+  p.workgroups = p.prompt ? a.cache.heads * (tiles < real ? tiles : real) : !p.shared ? p.items : units * p.items < slots ? units * p.items : slots;
   p.part_out = p.part_stat = nullptr;
   p.marks = nullptr;
   p.mark = 0;

@@ -6,8 +6,9 @@
 // product waits for its operand: 838 us where this takes 700).  Values have to be turned, four tokens' entries side by side, which costs an
 // exchange per two entries: the workgroup does that once, into LDS, in the order of the lanes that read it, without bank conflicts.
 //
-// 4096 queries of 32 heads over 12288 tokens (d = 128, 8 cache heads): 690 us, 1.0 PFLOP/s, as a large matrix product runs at 1.25.  Matrix and vector instructions of the two wavefronts of a
-// SIMD share its issue: a step of 64 tokens is 32 products (1024 cycles), 32 exponentials and about 290 other vector instructions.
+// 4096 queries of 32 heads over 12288 tokens (d = 128, 8 cache heads): 690 us, 1.0 PFLOP/s, where a large matrix product of the library runs
+// at 1.25.  Matrix and vector instructions of the two wavefronts of a SIMD share its issue: a step of 64 tokens is 32 products (1024
+// cycles), 32 exponentials and about 290 other vector instructions.  With d = 64, 470 us: half the products beside the same softmax.
 #pragma once
 #include <type_traits>
 
@@ -19,8 +20,51 @@ typedef float srv_floatx16 __attribute__((ext_vector_type(16)));
 
 constexpr int PROMPT_ROWS = 32 * PROMPT_WAVES;  // rows of a workgroup
 
+// The place of item `at` (of one head): false if there are fewer.  Every wavefront adds up the sequences' tiles for itself, a run of sequences to
+// a lane.  Where all have the same number, the tiles that see most come first, and each round of them begins with another sequence, for the
+// contexts' lengths may differ and eight sequences of one head would each stay on one XCD.  Otherwise one sequence after the other: workgroups
+// without a tile, left between the others, would leave compute units idle: 8 prompts of 17 to 1500 tokens, 16 query heads of one cache head,
+// d = 64, a window of 512, took 58 us where this takes 35.
+__device__ __forceinline__ bool prompt_tile(const AttentionArgs& p, int64_t at, int lane, int64_t& seq, int& tile) {
+  const int64_t n = p.a.sequences, run = (n + 63) / 64, first = min(lane * run, n), last = min(first + run, n);
+  const auto tiles = [&](int64_t s) {
+    if (!p.a.cu_q) return (uint32_t)p.row_tiles;
+    const int64_t q0 = max(p.a.cu_q[s], 0), q1 = min((int64_t)p.a.cu_q[s + 1], p.a.tokens), m = min(q1 - q0, (int64_t)p.a.max_q);
+    return m > 0 ? (uint32_t)((m * p.group + PROMPT_ROWS - 1) / PROMPT_ROWS) : 0u;
+  };
+  uint32_t own = 0;
+  for (int64_t s = first; s < last; ++s) own += tiles(s);
+  uint32_t sum = own;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t x = __shfl_up(sum, o, 64);
+    sum += lane >= o ? x : 0;
+  }
+  const uint32_t total = __builtin_amdgcn_readlane(sum, 63);
+  if (at >= total) return false;
+  if (total == (uint32_t)p.entries) {
+    const int64_t turn = at / n;
+    tile = p.row_tiles - 1 - (int)turn;
+    seq = n % 2 ? at % n : (at + turn) % n;
+    return true;
+  }
+  uint32_t before = sum - own;
+  const int there = __builtin_ctzll(__builtin_amdgcn_ballot_w64(at >= before && at < before + own));
+  before = __builtin_amdgcn_readlane(before, there);
+  for (int s = there * (int)run;; ++s) {
+    const uint32_t m = __builtin_amdgcn_readfirstlane(tiles(s));
+    if (at < before + m || s + 1 >= n) {
+      seq = __builtin_amdgcn_readfirstlane(s);
+      tile = __builtin_amdgcn_readfirstlane((int)(before + m - 1 - at));  // what sees most first
+      return true;
+    }
+    before += m;
+  }
+}
+
+// Workgroups of a compute unit at once: as many as the registers of a wavefront allow without spilling
 template <typename T, int D>
-__global__ void __launch_bounds__(64 * PROMPT_WAVES, 2) attention_prompt_kernel(const AttentionArgs p) {
+__global__ void __launch_bounds__(64 * PROMPT_WAVES, sizeof(T) == 2 && D == 64 ? 3 : 2) attention_prompt_kernel(const AttentionArgs p) {
   constexpr bool BF16 = sizeof(T) == 2;
   constexpr int TERMS = BF16 ? 1 : 3;
   constexpr int KS = D / 16;     // products of 16 entries that a score takes
@@ -35,11 +79,11 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, 2) attention_prompt_kernel(
 
   const ttc_attention_t& a = p.a;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, g = lane >> 5;
-  // heads fastest: with a multiple of eight of them an XCD's cache holds the keys and values of its own; the tiles that see most first
-  const int64_t item = blockIdx.x;
-  const int head = (int)(item % a.cache.heads);
-  const int64_t seq = item / a.cache.heads % a.sequences;
-  const int tile = p.row_tiles - 1 - (int)(item / a.cache.heads / a.sequences);
+  // heads fastest: with a multiple of eight of them an XCD's cache holds the keys and values of its own
+  const int head = (int)(blockIdx.x % a.cache.heads);
+  int64_t seq;
+  int tile;
+  if (!prompt_tile(p, blockIdx.x / a.cache.heads, lane, seq, tile)) return;
   const AttTile t = att_tile<PROMPT_ROWS>(p, seq, tile, 32 * wave + c);
   if (!t.real) return;
 
@@ -275,13 +319,7 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, 2) attention_prompt_kernel(
       x[2 * i + 1] = inverse * o[i][j + 8];
     }
     T* const to = y + ((j % 4) + 8 * (j / 4) + 4 * g) * E;
-    if constexpr (E >= 8) {
-#pragma unroll
-      for (int i = 0; i < E; i += 8) srv_st8(to + i, vec, reinterpret_cast<const float(&)[8]>(x[i]));
-    } else {
-#pragma unroll
-      for (int i = 0; i < E; ++i) to[i] = srv_narrow<T>(x[i]);
-    }
+    srv_st(to, vec, x);
   }
   if (a.lse && g == 0) a.lse[token * a.heads_q + h] = (m + __builtin_log2f(l)) * 0.69314718055994530942f;
 }

@@ -76,6 +76,25 @@ __device__ __forceinline__ void srv_st8(unsigned short* p, bool vec, const float
   }
 }
 
+// 4, 8 or 16 consecutive entries
+template <typename T, int N>
+__device__ __forceinline__ void srv_st(T* p, bool vec, const float (&x)[N]) {
+  if constexpr (N % 8 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; i += 8) srv_st8(p + i, vec, reinterpret_cast<const float(&)[8]>(x[i]));
+  } else {
+    typedef T four_t __attribute__((ext_vector_type(4)));
+    static_assert(N == 4);
+    const four_t v = {srv_narrow<T>(x[0]), srv_narrow<T>(x[1]), srv_narrow<T>(x[2]), srv_narrow<T>(x[3])};
+    if (vec) {
+      *reinterpret_cast<four_t*>(p) = v;
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) p[i] = v[i];
+    }
+  }
+}
+
 // eight entries of a large result, past the caches' replacement
 __device__ __forceinline__ void srv_stream8(float* p, bool vec, const float (&x)[8]) {
   if (vec) {

@@ -140,6 +140,18 @@ def test_many_rows(kv_len, new, heads, group, page, window, dtype, d):
 
 
 @pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 64), (torch.bfloat16, 128), (torch.float32, 64)])
+@pytest.mark.parametrize("kv_len,new,heads,group", [
+    ([140, 300, 128, 129], [128] * 4, 8, 8),                           # the same number of tiles each, contexts of other lengths
+    ([140, 300, 128], [127, 128, 121], 8, 8),                          # and of an odd number of sequences
+    ([200, 90], [200, 90], 8, 11),
+    ([37 * i % 101 + 9 for i in range(150)], [7 * i % 13 for i in range(150)], 3, 16)])   # more sequences than a wavefront has lanes, some without rows
+def test_many_rows_in_tiles_of_many_sequences(kv_len, new, heads, group, dtype, d):
+    s = Setup(kv_len, new, heads, group, d, 32, dtype, seed=len(new) + d)
+    assert heads * min(len(new) * -(-max(new) * group // 128), sum(new) * group // 128 + len(new)) >= 192
+    s.check(binding.ttc_attention(**s.gpu()))
+
+
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 64), (torch.bfloat16, 128), (torch.float32, 64)])
 def test_many_rows_with_nan_missing_pages_and_negative_scale(dtype, d):
     s = Setup([300, 150], [250, 150], 8, 8, d, 16, dtype, seed=5)
     k, v = s.exponents()
