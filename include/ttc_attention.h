@@ -60,8 +60,8 @@ ttc_status_t ttc_rope_table(float *table, int64_t rows, int32_t pairs, const dou
  *     values' codes    [token/4][16][token%4][d/32]       lane l of 16 holds entries l*d/16 ..  of four tokens side by side
  *     keys' exponents  [token][d/32]
  *     values' exponents [token/4][d/32][token%4]
- * which is the order the attention's matrix operands are read in: 16 consecutive bytes of keys are one row's share of a
- * 16 x 16 x 128 product, four tokens' values of one lane become its columns without an exchange between lanes. */
+ * which is the order the attention's matrix operands are read in: d/8 consecutive bytes of a token's keys are one lane's share
+ * of its products, four tokens' values of one lane become its columns without an exchange between lanes. */
 typedef struct {
   void *data;                  /* (pages, heads, page*(d + d/16)) bytes, 16-byte aligned */
   int64_t pages;
@@ -107,7 +107,8 @@ ttc_status_t ttc_kv_read(const ttc_kv_cache_t *cache, const int64_t *slots, int6
  * Causal: it sees tokens j <= p, with a window w > 0 only p - w < j <= p.  Otherwise all n.  A query that sees nothing gets
  * out = 0 and lse = -inf.  What a query does not see has no influence on it, NaN included.
  * Queries of float32 are worked on as exact sums of parts, sums and statistics are float32; for bfloat16 the weights
- * exp(s_j - max) are rounded to bfloat16 for their product with the values. */
+ * exp(s_j - max) are rounded to bfloat16 for their product with the values.  Equal calls give equal bits; the last bits of a
+ * sequence's result may differ with the other sequences of the call, which decide how its context is divided. */
 typedef struct {
   ttc_kv_cache_t cache;
   int64_t sequences;
@@ -131,8 +132,8 @@ typedef struct {
 } ttc_attention_t;
 
 /* workspace: DEVICE, 16-byte aligned, at least ttc_attention_workspace_bytes(attention) bytes (0: none needed, may be NULL),
- * which depends on sequences, heads, heads_q, d, max_q, max_kv, window and the device's compute units only.  One launch; the workspace
- * need not be cleared and may be used again by the next call on the same stream. */
+ * which depends on the sizes, dtype, causal and window and on the device's compute units, on nothing that lies in device memory.  One
+ * launch; the workspace need not be cleared and may be used again by the next call on the same stream. */
 size_t ttc_attention_workspace_bytes(const ttc_attention_t *attention);
 ttc_status_t ttc_attention(const ttc_attention_t *attention, void *workspace, size_t workspace_bytes, void *hip_stream);
 

@@ -5,7 +5,14 @@
 // rows as columns: S^T = K Q^T (16 tokens x 16 rows) leaves in each lane four tokens' scores of one row, and these are what the
 // lane has to hold for O^T = V^T P^T, whose sum runs over the tokens, if the tokens of two such tiles are taken in the order in which the
 // lanes hold them.  So the weights never move between lanes, maxima and sums are the lane's own but for one exchange among four lanes,
-// and rescaling is a product of the lane's own numbers.
+// and rescaling is a product of the lane's own numbers.  The four wavefronts of a workgroup take 64 tokens each in turn and join their sums
+// at the end: with few rows it is the context that has to be divided.
+//
+// What bounds it: 4 sequences of 131072 tokens (8 cache heads of 128, 4 query heads each, bfloat16) are read in 95 us, 6.0 TB/s, where a
+// kernel that only reads reaches 6.7 to 7.2; 64 sequences of 257 to 16384 tokens in 118 us, 5.0 TB/s, the rest being the beginnings and
+// joins of a workgroup's two items or three.  24 sequences of up to 4099 tokens in float32 (16 heads of 64) take 32 us for 10.7 us of
+// bytes: four units a workgroup, and products of three parts.  One sequence of 4099 tokens takes 12 us, a chain of waits (lengths,
+// page numbers, codes, join), none of which the card can shorten by working on more of it.
 #pragma once
 #include "ttc_attention_plan.hpp"
 #include "ttc_serve.hpp"
@@ -136,9 +143,9 @@ __device__ __forceinline__ srv_bf16x8 att_widen(uint32_t code, float scale) {
 // 128 in every byte that is 255
 __device__ __forceinline__ uint32_t att_full_bytes(uint32_t x) { return x & ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
-// Codes of a wavefront's step, which nobody else reads soon: past the caches' replacement, 114 us a call instead of 131 over 4 x 131072 tokens,
-// 122 instead of 136 over 64 sequences of 257 to 16384 (d = 128; where row tiles share a context it costs up to 8 %).  With heads of 256 a
-// lane's 32 bytes take two reads of the same lines, and the second would miss (16 x 4096 tokens 63 us instead of 51).
+// Codes of a wavefront's step, which nobody else reads soon: past the caches' replacement, 97 us a call instead of 110 over 4 x 131072 tokens,
+// 125 instead of 132 over 64 sequences of 257 to 16384 (d = 128).  With heads of 256 a lane's 32 bytes take two reads of the same lines,
+// and the second may miss (16 x 4096 tokens 27.6 us instead of 26.7).
 template <int D, typename W>
 __device__ __forceinline__ W att_stream(const W* p) {
   if constexpr (D <= 128) return __builtin_nontemporal_load(p);
@@ -178,7 +185,7 @@ struct AttSource {
 };
 
 // A wavefront's share of one step of 64 tokens, as it lies in the cache: lane (c, g) has the entries g*D/4 .. of the keys of token c of each
-// sixteen, and entries c*D/16 .. of the values of tokens 4g .. 4g+3.  `there`: bit i is set if the page of sixteen i is in the cache.
+// sixteen, and entries c*D/16 .. of the values of tokens 4g .. 4g+3.  `there` as in AttSource.
 template <int D>
 struct AttKeys {
   typedef KvParts<D> P;
