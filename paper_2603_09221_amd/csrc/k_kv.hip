@@ -20,7 +20,7 @@ static void append_many(KvAppendArgs& p, hipStream_t st) {
 
 // A thread takes four query heads, which share the cosines it reads, or four tokens of a cache head, whose reads are under way together,
 // once there are two workgroups to a compute unit that way.  One / four, us, 32 query and 8 cache heads of 128: 512 tokens 4.8 / 5.8, 1024
-// 8.0 / 6.0, 2048 13.4 / 10.0, 16384 102 / 72; 16 and 16 heads of 64 in float32: 1024 tokens 4.5 / 5.7, 2048 7.7 / 7.5.
+// 8.0 / 6.0, 2048 13.4 / 10.4, 16384 102 / 66; 16 and 16 heads of 64 in float32: 1024 tokens 4.5 / 5.7, 2048 7.7 / 7.5.
 template <typename T, int D>
 static void append(KvAppendArgs& p, int cus, hipStream_t st) {
   const int64_t heads = (p.a.q ? p.a.heads_q : 0) + 2ll * p.a.cache.heads;

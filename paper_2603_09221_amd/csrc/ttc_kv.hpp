@@ -1,6 +1,6 @@
 // The paged key-value cache in 4 bits: new tokens into it with their positions (ttc_kv_append), and tokens out of it as numbers
-// (ttc_kv_read).  Both are bound by memory: 16384 tokens of 32 query and 8 cache heads of 128 in 72 us (370 MB, 5.1 TB/s; 87 with the queries
-// written through the caches).  Eight entries of a head to a thread, so that a thread's codes are one word and a block of 32
+// (ttc_kv_read).  Both are bound by memory: 16384 tokens of 32 query and 8 cache heads of 128 in 66 us (370 MB, 5.6 TB/s; with the
+// queries written through the caches 15 us more), read back in 16 us.  Eight entries of a head to a thread, so that a thread's codes are one word and a block of 32
 // entries is four neighbouring lanes.  A workgroup takes consecutive tokens of one head: the pieces of the cache's lines that
 // consecutive tokens fill (four tokens' values lie side by side) meet in one XCD's cache before they go to memory.
 #pragma once
@@ -47,33 +47,41 @@ __device__ __forceinline__ KvTurn kv_turn(const float* row, int rot, int e, bool
   return t;
 }
 
-// entries e .. e+7 of the head at x and, where the pairs are a multiple of eight entries apart, their partners, as they lie in memory
+// Entries e .. e+7 of a head, as they lie in memory; and, where the pairs are a multiple of eight entries apart, their partners, which
+// another lane of the wavefront has read.  (Past the caches' replacement, as the rotation reads, 16384 tokens took 79 us instead of 66.)
 template <typename T>
 struct KvRaw {
-  float own[8], partner[8];
+  float own[8];
+  __device__ __forceinline__ void load(const float* p, bool vec) { srv_ld8(p, vec, own); }
+  __device__ __forceinline__ void of_lane(int lane, float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = __shfl(own[i], lane, 64);
+  }
 };
 template <>
 struct KvRaw<unsigned short> {
-  srv_u16x8 own, partner;
+  srv_u16x8 own;
+  __device__ __forceinline__ void load(const unsigned short* p, bool vec) { own = __builtin_bit_cast(srv_u16x8, srv_ld8_bf16(p, vec)); }
+  __device__ __forceinline__ void of_lane(int lane, float (&x)[8]) const {
+    typedef int four_t __attribute__((ext_vector_type(4)));
+    four_t v = __builtin_bit_cast(four_t, own);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __shfl(v[i], lane, 64);
+    const srv_u16x8 w = __builtin_bit_cast(srv_u16x8, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = srv_widen(w[i]);
+  }
 };
-__device__ __forceinline__ void kv_load8(const float* p, bool vec, float (&x)[8]) { srv_ld8(p, vec, x); }
-__device__ __forceinline__ void kv_load8(const unsigned short* p, bool vec, srv_u16x8& x) {
-  x = __builtin_bit_cast(srv_u16x8, srv_ld8_bf16(p, vec));
-}
-template <typename T, bool HALF>
-__device__ __forceinline__ void kv_load(const T* x, int rot, int e, bool vec, KvRaw<T>& raw) {
-  kv_load8(x + e, vec, raw.own);
-  const int half = rot / 2;
-  if (HALF && half % 8 == 0 && e < rot) kv_load8(x + (e < half ? e + half : e - half), vec, raw.partner);
-}
 
-// the entries turned
+// The entries turned; `rot` is the same for all lanes, `turns` is false for those whose position is not in the table
 template <typename T, bool HALF>
-__device__ __forceinline__ void kv_turned(const KvRaw<T>& raw, const T* x, int rot, int e, const KvTurn& t, float (&y)[8]) {
+__device__ __forceinline__ void kv_turned(const KvRaw<T>& raw, const T* x, int rot, bool turns, int e, const KvTurn& t, float (&y)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) y[i] = srv_widen(raw.own[i]);
-  if (e >= rot) return;
-  const int half = rot / 2;
+  const int half = rot / 2, lane = threadIdx.x & 63;
+  float partner[8];
+  if (HALF && rot && half % 8 == 0) raw.of_lane(e < half ? lane + half / 8 : e < rot ? lane - half / 8 : lane, partner);
+  if (e >= rot || !turns) return;
   if constexpr (!HALF) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -87,10 +95,10 @@ __device__ __forceinline__ void kv_turned(const KvRaw<T>& raw, const T* x, int r
     float other;
     if (e < half) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) srv_turn(y[i], srv_widen(raw.partner[i]), t.c[i], t.s[i], y[i], other);
+      for (int i = 0; i < 8; ++i) srv_turn(y[i], partner[i], t.c[i], t.s[i], y[i], other);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) srv_turn(srv_widen(raw.partner[i]), y[i], t.c[i], t.s[i], other, y[i]);
+      for (int i = 0; i < 8; ++i) srv_turn(partner[i], y[i], t.c[i], t.s[i], other, y[i]);
     }
   } else {
 #pragma unroll
@@ -156,27 +164,29 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const KvAppendArgs p) {
   const ttc_kv_append_t& a = p.a;
   const int u = threadIdx.x % U, e = 8 * u, heads = a.cache.heads;
   if (blockIdx.x >= p.cache_workgroups) {
-    const uint32_t b = blockIdx.x - p.cache_workgroups;
-    const int piece = b % p.q_pieces;
-    const int64_t token = (int64_t)(b / p.q_pieces) * TOKENS + threadIdx.x / U;
+    // Eight groups of tokens side by side, the pieces of a group one after the other: an XCD reads a token's cosines once (16384 tokens of 32
+    // heads 73 -> 67 us).
+    const uint32_t b = blockIdx.x - p.cache_workgroups, groups = (uint32_t)((a.tokens + TOKENS - 1) / TOKENS);
+    const uint32_t eight = b / (8 * p.q_pieces) * 8, wide = min(8u, groups - eight), r = b - eight * p.q_pieces;
+    const int piece = r / wide;
+    const int64_t token = (int64_t)(eight + r % wide) * TOKENS + threadIdx.x / U;
     if (token >= a.tokens) return;
     const int64_t pos = a.rot ? a.positions[token] : 0;
     const bool lost = (pos < 0 || pos >= a.table_rows) && e < a.rot;
-    const int rot = lost ? 0 : a.rot;
-    // all heads' reads are under way before the first is written: in place a pair's two threads, of one wavefront, read each other's entries
+    // all heads' reads are done before the first is written: in place a pair's two threads, of one wavefront, may read each other's entries
     KvRaw<T> raw[N];
     const T* x[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int h = min(piece + i * p.q_pieces, a.heads_q - 1);
       x[i] = static_cast<const T*>(a.q) + token * a.q_token + (int64_t)h * a.q_head;
-      kv_load<T, HALF>(x[i], rot, e, p.q_vec, raw[i]);
+      raw[i].load(x[i] + e, p.q_vec);
     }
     KvTurn t;
-    if (rot) t = kv_turn<HALF>(a.table + pos * a.rot, rot, e, p.t_vec);
+    if (a.rot && !lost) t = kv_turn<HALF>(a.table + pos * a.rot, a.rot, e, p.t_vec);
     float y[N][8];
 #pragma unroll
-    for (int i = 0; i < N; ++i) kv_turned<T, HALF>(raw[i], x[i], rot, e, t, y[i]);
+    for (int i = 0; i < N; ++i) kv_turned<T, HALF>(raw[i], x[i], a.rot, !lost, e, t, y[i]);
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -206,16 +216,16 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const KvAppendArgs p) {
     pos[i] = !value && a.rot ? a.positions[token] : 0;
     x[i] = value ? static_cast<const T*>(a.v) + token * a.v_token + (int64_t)h * a.v_head
                  : static_cast<const T*>(a.k) + token * a.k_token + (int64_t)h * a.k_head;
-    kv_load<T, HALF>(x[i], value ? 0 : a.rot, e, value ? p.v_vec : p.k_vec, raw[i]);
+    raw[i].load(x[i] + e, value ? p.v_vec : p.k_vec);
   }
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const bool lost = !value && (pos[i] < 0 || pos[i] >= a.table_rows) && e < a.rot;
-    const int rot = value || lost ? 0 : a.rot;
+    const int rot = value ? 0 : a.rot;
     KvTurn t;
-    if (rot) t = kv_turn<HALF>(a.table + pos[i] * a.rot, rot, e, p.t_vec);
+    if (rot && !lost) t = kv_turn<HALF>(a.table + pos[i] * rot, rot, e, p.t_vec);
     float y[8];
-    kv_turned<T, HALF>(raw[i], x[i], rot, e, t, y);
+    kv_turned<T, HALF>(raw[i], x[i], rot, !lost, e, t, y);
     if (lost) y[0] = __builtin_nanf("");
     uint32_t exp;
     const uint32_t code = kv_quantise(y, exp);
