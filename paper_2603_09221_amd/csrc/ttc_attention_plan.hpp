@@ -57,12 +57,18 @@ inline void plan_attention(AttentionArgs& p, int cus) {
   const ttc_attention_t& a = p.a;
   p.group = a.heads_q / a.cache.heads;
   const int64_t rows = (int64_t)a.max_q * p.group;
-  // The kernel for many rows does a tile's context from end to end in one workgroup: 1.2 us for every 64 tokens, up to a tile to each
-  // compute unit; attention_kernel takes tiles in time proportional to their number.  Measured over 8192 tokens, d = 128, this one /
-  // attention_kernel, us: 64 tiles of 128 rows 193 / 90, 128 tiles 197 / 161, 256 tiles 210 / 304.
-  const int64_t prompt_tiles = (rows + 32 * PROMPT_WAVES - 1) / (32 * PROMPT_WAVES), all_rows = a.tokens * p.group;
+  // The kernel for many rows does a tile's context from end to end in one workgroup: 1.2 us for every 64 tokens, however few of its 128
+  // rows there are, up to a tile to each compute unit; attention_kernel takes tiles of 16 in time proportional to their number.  So there have to
+  // be rows for three quarters of the compute units, and half a tile of them to a sequence; with float32 for all, and three quarters of one.
+  // This one / attention_kernel, us: over 8192 tokens, d = 128, one sequence, rows for 64 tiles 193 / 90, 128 197 / 161, 256 210 / 304;
+  // 256 sequences of 8192 tokens, 32 rows each 198 / 101, 64 205 / 203, 96 205 / 296; 1024 of 600 tokens, 32 rows 67 / 47, 64 71 / 86;
+  // the same in float32, d = 64, 64 rows 86 / 74, 96 92 / 106.
+  const bool bf16 = a.dtype == TTC_BF16;
+  const int64_t prompt_tiles = (rows + 32 * PROMPT_WAVES - 1) / (32 * PROMPT_WAVES);
+  const int64_t all_rows = a.tokens * p.group < a.sequences * rows ? a.tokens * p.group : a.sequences * rows;
   const int64_t tiles = a.sequences * prompt_tiles, real = all_rows / (32 * PROMPT_WAVES) + a.sequences;
-  p.prompt = prompt_kernel(a.dtype == TTC_BF16, a.cache.d) && 4 * a.cache.heads * (tiles < real ? tiles : real) >= 3 * cus && rows > ATT_ROWS;
+  p.prompt = prompt_kernel(bf16, a.cache.d) && a.cache.heads * all_rows >= (bf16 ? 96 : 128) * (int64_t)cus &&
+             all_rows >= (bf16 ? 64 : 96) * a.sequences;
   const int tile = p.prompt ? 32 * PROMPT_WAVES : ATT_ROWS;
   p.row_tiles = (int32_t)((rows + tile - 1) / tile);
   p.entries = (int32_t)(a.sequences * p.row_tiles);

@@ -1,8 +1,8 @@
 // The paged key-value cache in 4 bits: new tokens into it with their positions (ttc_kv_append), and tokens out of it as numbers
 // (ttc_kv_read).  Both are bound by memory: 16384 tokens of 32 query and 8 cache heads of 128 in 66 us (370 MB, 5.6 TB/s; with the
-// queries written through the caches 15 us more), read back in 16 us.  Eight entries of a head to a thread, so that a thread's codes are one word and a block of 32
-// entries is four neighbouring lanes.  A workgroup takes consecutive tokens of one head: the pieces of the cache's lines that
-// consecutive tokens fill (four tokens' values lie side by side) meet in one XCD's cache before they go to memory.
+// queries written through the caches 15 us more), read back in 16 us.  Eight entries of a head to a thread, so that a thread's codes are
+// one word and a block of 32 entries is four neighbouring lanes.  A workgroup takes consecutive tokens of one head: the pieces of the
+// cache's lines that consecutive tokens fill (four tokens' values lie side by side) meet in one XCD's cache before they go to memory.
 #pragma once
 #include "ttc_serve.hpp"
 

@@ -143,12 +143,25 @@ def test_many_rows(kv_len, new, heads, group, page, window, dtype, d):
 @pytest.mark.parametrize("kv_len,new,heads,group", [
     ([140, 300, 128, 129], [128] * 4, 8, 8),                           # the same number of tiles each, contexts of other lengths
     ([140, 300, 128], [127, 128, 121], 8, 8),                          # and of an odd number of sequences
+    ([140, 300, 128], [128, 126, 125], 8, 11),
+    ([200, 190], [200, 190], 8, 11),
+    ([37 * i % 101 + 9 for i in range(150)], [9 * i % 14 for i in range(150)], 3, 16),
     ([200, 90], [200, 90], 8, 11),
     ([37 * i % 101 + 9 for i in range(150)], [7 * i % 13 for i in range(150)], 3, 16)])   # more sequences than a wavefront has lanes, some without rows
 def test_many_rows_in_tiles_of_many_sequences(kv_len, new, heads, group, dtype, d):
     s = Setup(kv_len, new, heads, group, d, 32, dtype, seed=len(new) + d)
-    assert heads * min(len(new) * -(-max(new) * group // 128), sum(new) * group // 128 + len(new)) >= 192
     s.check(binding.ttc_attention(**s.gpu()))
+
+
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 128), (torch.float32, 64)])
+@pytest.mark.parametrize("new,group", [(1, 20), (1, 64), (3, 21), (2, 32), (6, 16), (8, 16), (1, 128)])
+def test_a_few_rows_of_each_of_many_sequences(new, group, dtype, d):
+    """Rows for part of a tile, or for one, of 260 sequences."""
+    lengths = [17 * i % 91 for i in range(260)]
+    s = Setup(lengths, [new] * 260, 1, group, d, 16, dtype, seed=new * group)
+    s.check(binding.ttc_attention(**s.gpu()))
+    if new == 1:
+        s.check(binding.ttc_attention(**{k: v for k, v in s.gpu().items() if k not in ("cu_q", "max_q")}))
 
 
 @pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 64), (torch.bfloat16, 128), (torch.float32, 64)])
