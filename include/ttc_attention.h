@@ -54,8 +54,9 @@ ttc_status_t ttc_rope_table(float *table, int64_t rows, int32_t pairs, const dou
 /* ---- the cache ---------------------------------------------------------------------------------------------------------
  * `pages` pages of `page` tokens each (page: 16, 32, 64, 128 or 256; heads of d = 64, 128 or 256).  Token slot s is token
  * s % page of page s / page.  Keys and values are held as blocks of 32 entries of a head: an exponent byte E and 32 codes of
- * 4 bits (bit 3 the sign, magnitudes 0 .5 1 1.5 2 3 4 6); a code c stands for c * 2^(E - 127), E = 255 for NaN.  4.25 bits an
- * entry.  One head of one page is page*(d + d/16) consecutive bytes, four parts:
+ * 4 bits (bit 3 the sign, magnitudes 0 .5 1 1.5 2 3 4 6); a code c stands for c * 2^(E - 127) where E <= 252, for NaN where E is
+ * larger (some codes would pass the largest float32).  4.25 bits an entry.  A cache need not be cleared: bytes that no token was
+ * written to may hold anything.  One head of one page is page*(d + d/16) consecutive bytes, four parts:
  *     keys' codes      [token][d/2]                       entry e: byte e/2, the low half for even e
  *     values' codes    [token/4][16][token%4][d/32]       lane l of 16 holds entries l*d/16 ..  of four tokens side by side
  *     keys' exponents  [token][d/32]

@@ -55,7 +55,7 @@ def quantise(x):
 def numbers(codes, exponents):
     """float64 numbers of codes (.., d) and exponent bytes (.., d / 32)"""
     v = MAGNITUDES[codes & 7] * np.where(codes & 8, -1.0, 1.0)
-    scale = np.where(exponents == 255, np.nan, np.exp2(exponents.astype(np.float64) - 127.0))
+    scale = np.where(exponents > 252, np.nan, np.exp2(exponents.astype(np.float64) - 127.0))
     return v * np.repeat(scale, BLOCK, -1)
 
 

@@ -140,8 +140,8 @@ __device__ __forceinline__ srv_bf16x8 att_widen(uint32_t code, float scale) {
   return srv_bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// 128 in every byte that is 255
-__device__ __forceinline__ uint32_t att_full_bytes(uint32_t x) { return x & ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+// 128 in every byte above 252: the exponents of blocks that are NaN
+__device__ __forceinline__ uint32_t att_nan_bytes(uint32_t x) { return x & ((x & 0x7f7f7f7fu) + (0x7f - (KV_LARGEST & 0x7f)) * 0x01010101u) & 0x80808080u; }
 
 // Codes of a wavefront's step, which nobody else reads soon: past the caches' replacement, 97 us a call instead of 110 over 4 x 131072 tokens,
 // 125 instead of 132 over 64 sequences of 257 to 16384 (d = 128).  With heads of 256 a lane's 32 bytes take two reads of the same lines,
@@ -459,7 +459,7 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(D)) attention_ker
         z[i] = srv_floatx4{};
   #pragma unroll
         for (int k = 0; k < KS; ++k) {
-          const srv_bf16x8 key = att_widen(keys.code[i][k], srv_scale((keys.exp[i] >> (D == 256 ? 8 * (k / 4) : 0)) & 255));
+          const srv_bf16x8 key = att_widen(keys.code[i][k], srv_scale_or_nan((keys.exp[i] >> (D == 256 ? 8 * (k / 4) : 0)) & 255));
   #pragma unroll
           for (int x = TERMS - 1; x >= 0; --x) z[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, q[x][k], z[i], 0, 0, 0);
         }
@@ -514,9 +514,10 @@ __global__ void __launch_bounds__(64 * ATT_WAVES, att_resident(D)) attention_ker
           for (int x = 0; x < TERMS; ++x) w[x][k] = part[x];
         }
         uint32_t exps[2] = {values.exp[2 * h], values.exp[2 * h + 1]};
-        // A weight of 0 takes out any number, but not NaN.  Blocks of NaN are rare: they are read as numbers, and what the rows that
-        // see them get is made NaN by a product of its own.
-        const uint32_t nan0 = att_full_bytes(exps[0]), nan1 = att_full_bytes(exps[1]);
+        // A weight of 0 takes out any number, but neither NaN nor infinity, and what lies behind a sequence's end may be any bytes.  Blocks
+        // whose exponents stand for NaN are rare: they are read as (finite) numbers, and what the rows that see them get is made NaN by a
+        // product of its own.
+        const uint32_t nan0 = att_nan_bytes(exps[0]), nan1 = att_nan_bytes(exps[1]);
         if (__builtin_amdgcn_ballot_w64((nan0 | nan1) != 0)) {
           srv_bf16x8 bad, seen;
   #pragma unroll

@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, sizeof(T) == 2 && D == 64 ?
   };
   // Row 32*dt + i of O^T is entry (i % 16) * E + 2*dt + i / 16, so that the threads of the cache's lanes write side by side
   const auto turn_values = [&](int buffer) {
-    const uint32_t nan = att_full_bytes(value_exp);
+    const uint32_t nan = att_nan_bytes(value_exp);
     exps[buffer][f][vl * E / 32] = value_exp;  // (the same from all lanes of a block)
     bad_step[buffer][wave] = __builtin_amdgcn_ballot_w64(nan != 0) != 0;
     const uint32_t finite = value_exp ^ nan;
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, sizeof(T) == 2 && D == 64 ?
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const int four = 4 * s + 2 * (k / 4) + g, n = n0 + 4 * four + k % 4;
-        bad[k] = static_cast<__bf16>((exps[buffer][four][(c & 15) * E / 32] >> (8 * (k % 4)) & 255) == 255 ? 1.f : 0.f);
+        bad[k] = static_cast<__bf16>((exps[buffer][four][(c & 15) * E / 32] >> (8 * (k % 4)) & 255) > KV_LARGEST ? 1.f : 0.f);
         seen[k] = static_cast<__bf16>((there >> s & 1) && n >= t.first && n <= t.last ? 1.f : 0.f);
       }
       const srv_floatx16 hit = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bad, seen, srv_floatx16{}, 0, 0, 0);
@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, sizeof(T) == 2 && D == 64 ?
       z[u] = srv_floatx16{};
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
-        const srv_bf16x8 k = att_widen(key[u][s], srv_scale((key_exp[u] >> (8 * (s / 4))) & 255));
+        const srv_bf16x8 k = att_widen(key[u][s], srv_scale_or_nan((key_exp[u] >> (8 * (s / 4))) & 255));
 #pragma unroll
         for (int i = TERMS - 1; i >= 0; --i) z[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[i][s], z[u], 0, 0, 0);
       }

@@ -128,7 +128,7 @@ __device__ __forceinline__ uint32_t kv_quantise(const float (&x)[8], uint32_t& e
     m = b > m ? b : m;
   }
   const uint32_t k = (m + 0x200000u) >> 23;  // the exponent, one more from 1.75 on
-  const uint32_t b = k < 2 ? 0u : k - 2 < 252u ? k - 2 : 252u;
+  const uint32_t b = k < 2 ? 0u : k - 2 < KV_LARGEST ? k - 2 : KV_LARGEST;
   const float inverse = __uint_as_float((254u - b) << 23);
   e = m >= 0x7f800000u ? 255u : b;
   uint32_t code = 0;
@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(256) kv_append_kernel(const KvAppendArgs p) {
 
 // eight entries from their codes
 __device__ __forceinline__ void kv_numbers(uint32_t code, uint32_t e, float (&x)[8]) {
-  const float scale = e == 255 ? __builtin_nanf("") : e == 0 ? __uint_as_float(0x00400000u) : srv_scale(e);
+  const float scale = e > KV_LARGEST ? __builtin_nanf("") : e == 0 ? __uint_as_float(0x00400000u) : srv_scale(e);
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint32_t c = (code >> (4 * i)) & 15, m = c & 7;

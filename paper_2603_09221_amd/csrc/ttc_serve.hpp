@@ -139,5 +139,8 @@ struct KvParts {
 
 // an exponent byte as the float32 that the conversion instructions take for a scale (they read its exponent alone)
 __device__ __forceinline__ float srv_scale(uint32_t e) { return __uint_as_float(e << 23); }
+// the same of any byte: above 252, with which some codes would be infinite, a block is NaN
+constexpr uint32_t KV_LARGEST = 252;
+__device__ __forceinline__ float srv_scale_or_nan(uint32_t e) { return srv_scale(e > KV_LARGEST ? 255u : e); }
 
 }  // namespace ttc

@@ -1,0 +1,78 @@
+"""Attention over the cache on the GPU where a call is at an edge: memory that was never written, a scale of 0, a cache without pages, bounds wider
+than the call, replays on a workspace that nobody clears.  Bounds on errors are those of test_gpu_cached_attention; which kernel a case
+takes is asked of the plan."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2603_09221_amd import binding
+from tests.attention_plan import describe, plan
+from tests.test_gpu_cached_attention import DEV, TYPES, Setup, host
+
+pytestmark = pytest.mark.gpu
+MANY = [(torch.bfloat16, 64), (torch.bfloat16, 128), (torch.float32, 64)]   # what the kernel for many rows takes
+FEW = [(t, d) for t in TYPES for d in (64, 128, 256)]
+
+
+def planned(s, window=0, causal=True, max_kv=None):
+    """The plan of the call that Setup `s` makes."""
+    cus = torch.cuda.get_device_properties(0).multi_processor_count
+    heads = s.raw.shape[1]
+    return plan(describe(len(s.kv_len), int(s.cu[-1]), s.q.shape[1], heads, s.d, s.page, s.dtype == torch.bfloat16, max(s.new),
+                         max_kv or s.table.shape[1] * s.page, window, causal, s.pages), cus)
+
+
+def few(dtype, d, seed=11):
+    s = Setup([200, 150, 1, 63], [20, 1, 1, 5], 2, 3, d, 16, dtype, seed=seed)
+    assert not planned(s).prompt
+    return s
+
+
+def many(dtype, d, seed=11):
+    s = Setup([430, 200], [380, 200], 8, 8, d, 16, dtype, seed=seed)
+    assert planned(s).prompt
+    return s
+
+
+CASES = [(few, *c) for c in FEW] + [(many, *c) for c in MANY]
+
+
+def put_exponents(s, k, v):
+    c, e = s.page * s.d, s.page * s.d // 32
+    s.raw[..., c:c + e], s.raw[..., c + e:] = k.reshape(*s.raw.shape[:2], e), v.reshape(*s.raw.shape[:2], e)
+
+
+@pytest.mark.parametrize("make,dtype,d", CASES)
+def test_bytes_that_were_never_written_have_no_influence(make, dtype, d):
+    """Tokens that no row sees hold exponents of 253 to 255 and any codes; so does page 0, which no sequence has, beside a page outside the cache."""
+    s = make(dtype, d)
+    rng = np.random.default_rng(1)
+    s.raw = np.concatenate([s.raw[:1], s.raw])
+    s.raw[0, :, s.page * s.d:] = 254
+    s.table[s.table >= 0] += 1
+    s.pages += 1
+    s.table[0, 2] = -1
+    exps = s.raw[..., s.page * s.d:]
+    unseen = exps == 255
+    exps[unseen] = rng.integers(253, 256, unseen.sum())
+    s.check(binding.ttc_attention(**s.gpu()))
+    s.check(binding.ttc_attention(**s.gpu(), window=70), window=70)
+    s.check(binding.ttc_attention(**s.gpu(), causal=False), causal=False)
+
+
+@pytest.mark.parametrize("exponent", [253, 254])
+@pytest.mark.parametrize("make,dtype,d", CASES)
+def test_exponents_above_252_are_nan_to_the_rows_that_see_them(make, dtype, d, exponent):
+    s = make(dtype, d)
+    k, v = s.exponents()
+    k[s.table[0, 190 // 16], 1, 190 % 16, d // 32 - 1] = exponent       # keys of token 190, values of token 140 of the second sequence
+    v[s.table[1, 140 // 16], 0, 140 % 16 // 4, 1, 140 % 4] = exponent
+    put_exponents(s, k, v)
+    (out, _, _), _ = s.oracle(window=30)
+    assert 0 < np.isnan(out).mean() < 0.2
+    s.check(binding.ttc_attention(**s.gpu(), window=30), window=30)
+    slots = torch.tensor([int(s.table[0, 190 // 16]) * 16 + 190 % 16, int(s.table[1, 140 // 16]) * 16 + 140 % 16], device=DEV)
+    for t in TYPES:
+        rk, rv = (host(x) for x in binding.ttc_kv_read(torch.from_numpy(s.raw).to(DEV), slots, d, dtype=t))
+        assert np.isnan(rk[0, 1, -32:]).all() and np.isnan(rv[1, 0, 32:64]).all()
+        assert np.isnan(rk).sum() == 32 and np.isnan(rv).sum() == 32
