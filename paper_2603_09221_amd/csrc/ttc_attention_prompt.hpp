@@ -96,6 +96,10 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, sizeof(T) == 2 && D == 64 ?
   const int r = tile * PROMPT_ROWS + 32 * wave + c;
   const int64_t token = t.first_q + r / p.group;
   const int h = head * p.group + r % p.group;
+  // Queries take the scale's sign, so that the largest scores are the largest products, and a scale of 0 altogether: masked products are -inf
+  // before they meet to_log2, which therefore must not be 0.
+  const float size = fabsf(a.scale) * 1.44269504088896340736f, to_log2 = size == 0.f ? 1.f : size;
+  const float sign = size == 0.f ? 0.f : a.scale < 0.f ? -1.f : 1.f;
   srv_bf16x8 q[TERMS][KS];
   {
     const bool real = r < t.rows;
@@ -108,7 +112,7 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, sizeof(T) == 2 && D == 64 ?
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         __bf16 part[TERMS];
-        att_split<TERMS>(a.scale < 0.f ? -v[i] : v[i], part);
+        att_split<TERMS>(sign * v[i], part);
 #pragma unroll
         for (int k = 0; k < TERMS; ++k) q[k][s][i] = part[k];
       }
@@ -116,7 +120,6 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, sizeof(T) == 2 && D == 64 ?
   }
   srv_floatx16 o[DT] = {};
   float m = -INFINITY, l = 0.f;
-  const float to_log2 = fabsf(a.scale) * 1.44269504088896340736f;  // (largest scores are largest products)
   const AttSource src(p, seq, head, t.hi);
 
   // keys: lane (c, g) has entries g*D/2 .. of token c of each 32; values: thread (f, vl) has those of four tokens f that the cache's lane vl holds
@@ -246,7 +249,7 @@ __global__ void __launch_bounds__(64 * PROMPT_WAVES, sizeof(T) == 2 && D == 64 ?
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int j = 0; j < 16; ++j) top = fmaxf(top, z[u][j]);
-    top = top == -INFINITY ? top : top * to_log2;  // (a scale of 0)
+    top *= to_log2;
     moved = __builtin_amdgcn_ballot_w64(top > m + 8.f) != 0;
     if (moved) {
       top = fmaxf(m, top);

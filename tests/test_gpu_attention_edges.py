@@ -76,3 +76,31 @@ def test_exponents_above_252_are_nan_to_the_rows_that_see_them(make, dtype, d, e
         rk, rv = (host(x) for x in binding.ttc_kv_read(torch.from_numpy(s.raw).to(DEV), slots, d, dtype=t))
         assert np.isnan(rk[0, 1, -32:]).all() and np.isnan(rv[1, 0, 32:64]).all()
         assert np.isnan(rk).sum() == 32 and np.isnan(rv).sum() == 32
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.0])
+@pytest.mark.parametrize("make,dtype,d", CASES)
+def test_a_scale_of_0_gives_the_mean_of_what_is_seen(make, dtype, d, scale):
+    s = make(dtype, d)
+    s.scale = scale
+    s.table[0, 1] = -1
+    s.check(binding.ttc_attention(**s.gpu()))
+    s.check(binding.ttc_attention(**s.gpu(), window=50), window=50)
+    s.check(binding.ttc_attention(**s.gpu(), causal=False), causal=False)
+
+
+@pytest.mark.parametrize("make,dtype,d", [(few, torch.bfloat16, 128), (many, torch.bfloat16, 128), (many, torch.float32, 64)])
+def test_nan_with_a_scale_of_0(make, dtype, d):
+    """0 times NaN: a query or a key that is NaN makes NaN of the rows that have it or see it."""
+    s = make(dtype, d)
+    s.scale = 0.0
+    k, v = s.exponents()
+    k[s.table[0, 190 // 16], 1, 190 % 16, 1] = 255
+    put_exponents(s, k, v)
+    clean, s.q[3, 2, 5] = s.q.clone(), float("nan")
+    got = binding.ttc_attention(**s.gpu(), window=30)
+    assert torch.isnan(got["out"][3, 2]).all() and torch.isnan(got["lse"][3, 2])
+    s.q = clean     # without the query's NaN: every other row as it is, and this one's from the oracle (bounds are taken from the queries)
+    (out, lse, _), _ = s.oracle(window=30)
+    got["out"][3, 2], got["lse"][3, 2] = torch.from_numpy(out[3, 2]).to(got["out"]), float(lse[3, 2])
+    s.check(got, window=30)
