@@ -54,6 +54,8 @@ inline int64_t visible_at_most(const ttc_attention_t& a, int group) {
 // 0 to 8000 68 / 74; d = 64 float32, 2048 items of 4099 184 / 158.  (Lengths of all sequences but one near 0 would move the balance to sharing:
 // hence 4 units for every item of a compute unit, where even lengths would allow 8.)
 inline void plan_attention(AttentionArgs& p, int cus) {
+  // A cache of no pages holds no tokens, and there is none to read in the place of a page that is missing.
+  if (!p.a.cache.pages) p.a.max_kv = 0;
   const ttc_attention_t& a = p.a;
   p.group = a.heads_q / a.cache.heads;
   const int64_t rows = (int64_t)a.max_q * p.group;

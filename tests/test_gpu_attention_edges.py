@@ -104,3 +104,18 @@ def test_nan_with_a_scale_of_0(make, dtype, d):
     (out, lse, _), _ = s.oracle(window=30)
     got["out"][3, 2], got["lse"][3, 2] = torch.from_numpy(out[3, 2]).to(got["out"]), float(lse[3, 2])
     s.check(got, window=30)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("new", [1, 600])
+def test_a_cache_without_pages_holds_nothing(dtype, new):
+    """Lengths and a table, but no page: what the plan makes of it (lengths of 0) is tested without a GPU."""
+    cache = binding.make_kv_cache(0, 8, 64, 16, device=DEV)
+    q = torch.randn((2 * new, 64, 64), device=DEV).to(dtype)
+    p = plan(describe(2, 2 * new, 64, 8, 64, 16, dtype == torch.bfloat16, new, 160, pages=0))
+    assert p.max_kv == 0 and bool(p.prompt) == (new > 1)
+    cu = torch.tensor([0, new, 2 * new], dtype=torch.int32, device=DEV)
+    for causal in (True, False):
+        got = binding.ttc_attention(q, cache, torch.zeros((2, 10), dtype=torch.int32, device=DEV), torch.tensor([150, 9], dtype=torch.int32, device=DEV),
+                                    cu_q=cu, max_q=new, causal=causal)
+        assert (got["out"] == 0).all() and torch.isneginf(got["lse"]).all()
