@@ -56,6 +56,8 @@ inline int64_t visible_at_most(const ttc_attention_t& a, int group) {
 inline void plan_attention(AttentionArgs& p, int cus) {
   // A cache of no pages holds no tokens, and there is none to read in the place of a page that is missing.
   if (!p.a.cache.pages) p.a.max_kv = 0;
+  // Without cu_q every sequence has one row, however wide the bound: tiles are counted by it, in the grid and in the kernels.
+  if (!p.a.cu_q && p.a.max_q > 1) p.a.max_q = 1;
   const ttc_attention_t& a = p.a;
   p.group = a.heads_q / a.cache.heads;
   const int64_t rows = (int64_t)a.max_q * p.group;

@@ -12,3 +12,14 @@ def test_a_cache_without_pages_is_not_read(new, bf16):
     p = plan(describe(**call, pages=0))
     assert p.max_kv == 0 and not p.shared and p.workspace == 0 and bool(p.prompt) == (new > 1)
     assert plan(describe(**call, pages=1)).max_kv == 100000
+
+
+@pytest.mark.parametrize("bf16,group", [(True, 64), (True, 128), (False, 100)])
+def test_a_bound_wider_than_the_one_row_that_each_sequence_has(bf16, group):
+    """Without cu_q: the same plan as with max_q = 1, and workgroups for every sequence's tiles."""
+    call = dict(sequences=384, tokens=384, heads_q=group, heads=1, d=64, page=16, bf16=bf16, max_kv=80, cu_q=False)
+    one = plan(describe(**call, max_q=1))
+    for max_q in (2, 4, 1000):
+        assert plan(describe(**call, max_q=max_q)) == one
+    assert one.workgroups >= 384 and one.entries == 384 * -(-group // (128 if one.prompt else 16))
+    assert plan(describe(**call, max_q=0)).max_q == 0

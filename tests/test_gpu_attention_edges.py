@@ -107,6 +107,26 @@ def test_nan_with_a_scale_of_0(make, dtype, d):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+def test_rows_without_being_told_and_a_wider_bound(dtype):
+    """Through the C interface: no cu_q, so one row each, with max_q = 4: 384 sequences of 100 rows of a cache head, every one of them answered."""
+    s = Setup([i % 70 for i in range(384)], [1] * 384, 1, 100, 64, 16, dtype, seed=3)
+    a = s.gpu()
+    want = binding.ttc_attention(a["q"], a["cache"], a["block_table"], a["kv_len"], scale=s.scale)
+    s.check(want)
+    lib, tokens, heads_q = binding.load(), *a["q"].shape[:2]
+    for max_q in (4, 1, 37):
+        out, lse = torch.full_like(a["q"], 77.0), torch.full((tokens, heads_q), 77.0, device=DEV)
+        att = binding.Attention(binding.KvCache(a["cache"].data_ptr(), s.pages, 1, s.d, s.page), 384, tokens, heads_q, 1 if dtype == torch.bfloat16 else 0, 1, 0, s.scale, max_q,
+                                a["block_table"].shape[1] * s.page, a["q"].data_ptr(), out.data_ptr(), lse.data_ptr(), heads_q * s.d, s.d,
+                                heads_q * s.d, s.d, None, a["kv_len"].data_ptr(), a["block_table"].data_ptr(), a["block_table"].stride(0))
+        work = torch.empty(max(lib.ttc_attention_workspace_bytes(att), 16), dtype=torch.uint8, device=DEV)
+        assert lib.ttc_attention(att, work.data_ptr(), work.numel(), torch.cuda.current_stream().cuda_stream) == 0
+        torch.cuda.synchronize()
+        assert not (out == 77.0).any() and not (lse == 77.0).any()
+        s.check({"out": out, "lse": lse})
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("new", [1, 600])
 def test_a_cache_without_pages_holds_nothing(dtype, new):
     """Lengths and a table, but no page: what the plan makes of it (lengths of 0) is tested without a GPU."""
