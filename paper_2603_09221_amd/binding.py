@@ -668,9 +668,11 @@ def rope_frequencies(rot, *, base=10000.0, scaling=None, factor=1.0, trained=Non
 
     scaling None: base^(-2i/rot).  For contexts `factor` times as long as the `trained` one:
       "linear"  positions are compressed: every frequency divided by factor.
-      "base"    the base grows to base * factor^(rot/(rot-2)): the highest frequency stays, the lowest is divided by factor.
+      "base"    the base grows to base * factor^(rot/(rot-2)): the highest frequency stays, the lowest is divided by factor (the published
+                method known as NTK-aware scaling).
       "bands"   frequencies that turn more than `fast` times within `trained` positions stay, those that turn less than `slow`
-                times are divided by factor, those in between are mixed linearly over their index; the scale is 0.1 ln(factor) + 1."""
+                times are divided by factor, those in between are mixed linearly over their index (the range between the whole indices that
+                enclose it); the scale is 0.1 ln(factor) + 1.  This is YaRN (Peng et al., arXiv 2309.00071), with its 32, 1 and 0.1."""
     if rot < 2 or rot % 2 or factor < 1.0 or not base > 1.0:
         raise ValueError("rot must be even and positive, factor >= 1, base > 1")
     i = torch.arange(rot // 2, dtype=torch.float64)
@@ -691,7 +693,7 @@ def rope_frequencies(rot, *, base=10000.0, scaling=None, factor=1.0, trained=Non
     def index(turns):  # of the frequency that turns so often within the trained length
         return rot * math.log(trained / (2.0 * math.pi * turns)) / (2.0 * math.log(base))
 
-    lo, hi = max(0, math.floor(index(fast))), min(rot // 2 - 1, math.ceil(index(slow)))
+    lo, hi = max(0, math.floor(index(fast))), math.ceil(index(slow))  # (hi may lie behind the last pair, which then stays mixed)
     mix = ((i - lo) / max(hi - lo, 0.001)).clamp(0.0, 1.0)
     return freqs * (1.0 - mix) + freqs / factor * mix, 0.1 * math.log(factor) + 1.0
 
