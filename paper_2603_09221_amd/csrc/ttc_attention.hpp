@@ -278,8 +278,8 @@ __device__ __forceinline__ bool att_join(const AttentionArgs& p, const AttTile& 
     bool all = true;
     for (uint32_t s = threadIdx.x; s < parts; s += 64)
       all &= __hip_atomic_load(p.marks + 2 * ((int64_t)w0 + s) + (s == 0 ? slot0 : 0), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == p.mark;
-    if (threadIdx.x == 0) *joins = 1;
-    if (!all) *joins = 0;
+    const bool arrived = __builtin_amdgcn_ballot_w64(!all) == 0;
+    if (threadIdx.x == 0) *joins = arrived;
   }
   __syncthreads();
   if (!*joins) return false;

@@ -127,6 +127,32 @@ def test_rows_without_being_told_and_a_wider_bound(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+def test_replays_on_a_workspace_that_nobody_clears(dtype):
+    """A captured call carries the same mark every time: what it left in the workspace must not be taken for this replay's parts.  Behind
+    every replay no mark is left."""
+    s = Setup([3000, 20, 2500], [1, 1, 1], 2, 4, 128, 64, dtype)
+    a = s.gpu()
+    p = planned(s)
+    assert p.shared and p.workgroups > 8
+    work = torch.zeros(p.workspace, dtype=torch.uint8, device=DEV)
+    got = {k: v.clone() for k, v in binding.ttc_attention(**a).items()}
+    binding.ttc_attention(**a, out=got, workspace=work)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        binding.ttc_attention(**a, out=got, workspace=work)
+    for step in range(6):
+        a["q"].copy_(torch.randn(a["q"].shape, device=DEV))
+        a["kv_len"].copy_(torch.tensor([3000 - 400 * step, 20 - step, 2500 - 300 * step], dtype=torch.int32))
+        want = binding.ttc_attention(**a)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got["out"], want["out"]) and torch.equal(got["lse"], want["lse"])
+        assert not work[-2 * 8 * p.workgroups:].any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("new", [1, 600])
 def test_a_cache_without_pages_holds_nothing(dtype, new):
     """Lengths and a table, but no page: what the plan makes of it (lengths of 0) is tested without a GPU."""
