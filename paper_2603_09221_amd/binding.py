@@ -639,6 +639,12 @@ def _same_device(first, *tensors):
             raise ValueError("all tensors must be on one device")
 
 
+def _on_gpu(t):
+    """The last check before a launch: a kernel that is handed host memory faults."""
+    if not t.is_cuda:
+        raise ValueError("tensors must be on a GPU")
+
+
 def _rope_table(table, d):
     rows, pairs, two = table.shape if table.dim() == 3 else (0, 0, 0)
     if two != 2 or table.dtype is not torch.float32 or not table.is_contiguous():
@@ -709,6 +715,7 @@ def ttc_rope_table(rows, freqs, *, scale=1.0, device="cuda", out=None, stream=No
     if stream is not None and stream != torch.cuda.current_stream():
         stream.wait_stream(torch.cuda.current_stream())  # the frequencies were copied there
         freqs.record_stream(stream)
+    _on_gpu(freqs)
     _check(load().ttc_rope_table(out.data_ptr(), rows, pairs, freqs.data_ptr(), scale, _stream_ptr(stream)))
     return out
 
@@ -726,6 +733,7 @@ def _rope(call, x, positions, table, layout, out, stream):
     else:
         y_token, y_head = _heads_strides(out, "out", x.shape, x.dtype)
     if tokens and heads and d:
+        _on_gpu(x)
         _check(call(Rope(tokens, heads, d, rot, dtype, _rope_layout(layout), x.data_ptr(), out.data_ptr(), x_token, x_head, y_token,
                          y_head, pos, table_ptr, rows), _stream_ptr(stream)))
     return out
@@ -796,6 +804,7 @@ def ttc_kv_append(cache, k, v, slots, positions=None, table=None, *, layout="hal
     elif q_out is not None:
         raise ValueError("q_out without q")
     if tokens:
+        _on_gpu(cache)
         _check(load().ttc_kv_append(KvAppend(kv, tokens, dtype, rot, _rope_layout(layout), k.data_ptr(), v.data_ptr(), k_token, k_head,
                                              v_token, v_head, at, pos, table_ptr, rows, _ptr(q), _ptr(q_out), heads_q, q_token, q_head,
                                              qo_token, qo_head), _stream_ptr(stream)))
@@ -821,6 +830,7 @@ def ttc_kv_read(cache, slots, d, *, dtype=torch.bfloat16, out=None, stream=None)
                 raise ValueError("out: expected two contiguous %s tensors of %s" % (dtype, shape))
         _same_device(cache, slots, k, v)
     if shape[0]:
+        _on_gpu(cache)
         _check(load().ttc_kv_read(kv, at, shape[0], code, k.data_ptr(), v.data_ptr(), _stream_ptr(stream)))
     return k, v
 
@@ -877,6 +887,7 @@ def ttc_attention(q, cache, block_table, kv_len, *, cu_q=None, max_q=None, max_k
     att = Attention(kv, sequences, tokens, heads_q, dtype, 1 if causal else 0, window, d ** -0.5 if scale is None else scale, max_q, max_kv,
                     q.data_ptr(), y.data_ptr(), _ptr(lse), q_token, q_head, out_token, out_head, cu, lens, block_table.data_ptr(),
                     table_stride)
+    _on_gpu(cache)
     need = lib.ttc_attention_workspace_bytes(att)
     if need and workspace is None:
         workspace = _new(q, (need,), torch.uint8, stream)
