@@ -639,6 +639,13 @@ def _same_device(first, *tensors):
             raise ValueError("all tensors must be on one device")
 
 
+def _int32(**numbers):
+    """Numbers of the caller that a descriptor holds in 32 bits, where ctypes would cut them off."""
+    for name, value in numbers.items():
+        if not -1 << 31 <= value < 1 << 31:
+            raise ValueError(f"{name}: {value} does not fit in 32 bits")
+
+
 def _on_gpu(t):
     """The last check before a launch: a kernel that is handed host memory faults."""
     if not t.is_cuda:
@@ -857,7 +864,7 @@ def ttc_attention(q, cache, block_table, kv_len, *, cu_q=None, max_q=None, max_k
     lens = _vector(kv_len, sequences, torch.int32, "kv_len")
     room = width * kv.page
     if max_kv is None:
-        max_kv = room
+        max_kv = min(room, 1 << 30)  # (the most that a sequence may have)
     elif max_kv > room:
         raise ValueError("max_kv: block_table has room for %d tokens" % room)
     cu = None
@@ -869,6 +876,7 @@ def ttc_attention(q, cache, block_table, kv_len, *, cu_q=None, max_q=None, max_k
         if tokens != sequences:
             raise ValueError("q: %d rows for %d sequences" % (tokens, sequences))
         max_q = 1
+    _int32(max_q=max_q, max_kv=max_kv, window=window)
     _same_device(cache, q, block_table, kv_len, cu_q, workspace)
     y = lse = None
     if out:

@@ -20,3 +20,12 @@ def test_host_memory_is_not_handed_to_a_kernel():
                     lambda: binding.ttc_rope_backward(k, slots, table, out=k), lambda: binding.ttc_rope_table(8, torch.ones(4), device="cpu")):
         with pytest.raises(ValueError, match="on a GPU"):
             refused()
+
+
+def test_numbers_that_a_descriptor_would_cut_off():
+    """2^32 + 5 is not 5."""
+    cu = torch.zeros(4, dtype=torch.int32)
+    wide = torch.empty((3, 1 << 25), dtype=torch.int32)     # room for 2^31 tokens (never touched)
+    for change in (dict(window=(1 << 32) + 5), dict(window=1 << 31), dict(cu_q=cu, max_q=(1 << 32) + 1), dict(block_table=wide, max_kv=1 << 31)):
+        with pytest.raises(ValueError, match="32 bits"):
+            call(**change)

@@ -152,6 +152,17 @@ def test_replays_on_a_workspace_that_nobody_clears(dtype):
         assert not work[-2 * 8 * p.workgroups:].any()
 
 
+def test_a_table_with_room_for_more_tokens_than_a_sequence_may_have():
+    """max_kv is what the table has room for where the caller names none: 2^32 tokens here, of which a sequence has 300."""
+    s = Setup([300, 64], [1, 1], 1, 4, 64, 256, torch.bfloat16)
+    a = s.gpu()
+    want = binding.ttc_attention(**a)
+    wide = torch.full((2, 1 << 24), -1, dtype=torch.int32, device=DEV)
+    wide[:, :a["block_table"].shape[1]] = a["block_table"]
+    s.check(want)
+    s.check(binding.ttc_attention(**{**a, "block_table": wide}))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("new", [1, 600])
 def test_a_cache_without_pages_holds_nothing(dtype, new):
