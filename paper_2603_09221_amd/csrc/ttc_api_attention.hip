@@ -71,15 +71,14 @@ ttc_status_t run_rope(const ttc_rope_t* r, bool backward, void* hip_stream) {
   return ttc::launch_rope(*r, backward, compute_units(), static_cast<hipStream_t>(hip_stream)) == hipSuccess ? TTC_OK : TTC_ERR_DEVICE;
 }
 
-ttc_status_t check_attention(const ttc_attention_t* a) {
+// Checks what does not depend on tensors, and plans the call
+ttc_status_t check_attention(const ttc_attention_t* a, ttc::AttentionArgs& p) {
   if (!a || a->sequences < 0 || a->tokens < 0 || !known_dtype(a->dtype) || a->max_q < 0 || a->max_kv < 0) return TTC_ERR_INVALID_ARG;
   if ((a->causal != 0 && a->causal != 1) || a->window < 0 || (a->window && !a->causal) || !isfinite(a->scale)) return TTC_ERR_INVALID_ARG;
   if (const ttc_status_t s = check_cache(a->cache); s != TTC_OK) return s;
   if (a->heads_q < 1 || a->heads_q % a->cache.heads) return TTC_ERR_INVALID_ARG;
-  // numbers of tokens and rows are 32-bit inside a sequence; a launch has fewer than 2^24 workgroups
-  if (a->max_kv > (1 << 30) || (int64_t)a->max_q * (a->heads_q / a->cache.heads) > (1 << 30)) return TTC_ERR_UNSUPPORTED;
-  if ((double)a->sequences * a->cache.heads * ((double)a->max_q * (a->heads_q / a->cache.heads) / ttc::ATT_ROWS + 1) >= (1 << 23)) return TTC_ERR_UNSUPPORTED;
-  return TTC_OK;
+  p.a = *a;
+  return ttc::plan_attention(p, compute_units()) ? TTC_OK : TTC_ERR_UNSUPPORTED;
 }
 
 }  // namespace
@@ -128,24 +127,19 @@ ttc_status_t ttc_kv_read(const ttc_kv_cache_t* c, const int64_t* slots, int64_t 
 }
 
 size_t ttc_attention_workspace_bytes(const ttc_attention_t* a) {
-  if (check_attention(a) != TTC_OK) return 0;
   ttc::AttentionArgs p;
-  p.a = *a;
-  ttc::plan_attention(p, compute_units());
-  return ttc::attention_workspace(p);
+  return check_attention(a, p) == TTC_OK ? ttc::attention_workspace(p) : 0;
 }
 
 ttc_status_t ttc_attention(const ttc_attention_t* a, void* workspace, size_t workspace_bytes, void* hip_stream) {
-  if (const ttc_status_t s = check_attention(a); s != TTC_OK) return s;
+  ttc::AttentionArgs p;
+  if (const ttc_status_t s = check_attention(a, p); s != TTC_OK) return s;
   if (!a->sequences || !a->tokens || !a->max_q) return TTC_OK;
   const uint64_t n = bytes_of(a->dtype);
   if (!a->q || !a->out || !aligned(a->q, n) || !aligned(a->out, n) || !aligned(a->lse, 4) || a->q == a->out) return TTC_ERR_INVALID_ARG;
   if (!a->kv_len || !aligned(a->kv_len, 4) || !aligned(a->cu_q, 4)) return TTC_ERR_INVALID_ARG;
   if (a->max_kv && (!a->block_table || !aligned(a->block_table, 4) || a->table_stride < 0)) return TTC_ERR_INVALID_ARG;
   if (!a->cu_q && a->tokens != a->sequences) return TTC_ERR_INVALID_ARG;
-  ttc::AttentionArgs p;
-  p.a = *a;
-  ttc::plan_attention(p, compute_units());
   const uint64_t need = ttc::attention_workspace(p);
   if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return TTC_ERR_WORKSPACE;
   ttc::place_workspace(p, workspace, next_mark());

@@ -53,14 +53,20 @@ inline int64_t visible_at_most(const ttc_attention_t& a, int group) {
 // bfloat16, 32 items of 1000 tokens 15.4 / 13.1, of 4099 17.9 / 36; 512 items of 2000 30 / 29, of 8000 91 / 93, of 0 to 2000 32 / 24, of
 // 0 to 8000 68 / 74; d = 64 float32, 2048 items of 4099 184 / 158.  (Lengths of all sequences but one near 0 would move the balance to sharing:
 // hence 4 units for every item of a compute unit, where even lengths would allow 8.)
-inline void plan_attention(AttentionArgs& p, int cus) {
+// False: more than the kernels' counters or one launch hold (numbers of tokens and rows are 32-bit inside a sequence, and so are tiles of a head; a
+// launch has fewer than 2^24 workgroups).  max_q may be far above what the sequences have: workgroups of the kernel for many rows, and
+// those that share, do not grow with it.
+inline bool plan_attention(AttentionArgs& p, int cus) {
+  p.group = p.a.heads_q / p.a.cache.heads;
+  if (p.a.max_kv > (1 << 30) || (int64_t)p.a.max_q * p.group > (1 << 30)) return false;
   // A cache of no pages holds no tokens, and there is none to read in the place of a page that is missing.
   if (!p.a.cache.pages) p.a.max_kv = 0;
   // Without cu_q every sequence has one row, however wide the bound: tiles are counted by it, in the grid and in the kernels.
   if (!p.a.cu_q && p.a.max_q > 1) p.a.max_q = 1;
   const ttc_attention_t& a = p.a;
-  p.group = a.heads_q / a.cache.heads;
   const int64_t rows = (int64_t)a.max_q * p.group;
+  const double most = (double)a.sequences * ((double)rows / ATT_ROWS + 1);
+  if (most >= 2147483648. || most * a.cache.heads >= 1e15) return false;
   // The kernel for many rows does a tile's context from end to end in one workgroup: 1.2 us for every 64 tokens, however few of its 128
   // rows there are, up to a tile to each compute unit; attention_kernel takes tiles of 16 in time proportional to their number.  So there have to
   // be rows for three quarters of the compute units, and half a tile of them to a sequence; with float32 for all, and three quarters of one.
@@ -69,7 +75,7 @@ inline void plan_attention(AttentionArgs& p, int cus) {
   // the same in float32, d = 64, 64 rows 86 / 74, 96 92 / 106.
   const bool bf16 = a.dtype == TTC_BF16;
   const int64_t prompt_tiles = (rows + 32 * PROMPT_WAVES - 1) / (32 * PROMPT_WAVES);
-  const int64_t all_rows = a.tokens * p.group < a.sequences * rows ? a.tokens * p.group : a.sequences * rows;
+  const int64_t all_rows = (a.tokens < a.sequences * a.max_q ? a.tokens : a.sequences * a.max_q) * p.group;
   const int64_t tiles = a.sequences * prompt_tiles, real = all_rows / (32 * PROMPT_WAVES) + a.sequences;
   p.prompt = prompt_kernel(bf16, a.cache.d) && a.cache.heads * all_rows >= (bf16 ? 96 : 128) * (int64_t)cus &&
              all_rows >= (bf16 ? 64 : 96) * a.sequences;
@@ -85,6 +91,7 @@ inline void plan_attention(AttentionArgs& p, int cus) {
   p.part_out = p.part_stat = nullptr;
   p.marks = nullptr;
   p.mark = 0;
+  return p.workgroups < (1 << 24);
 }
 
 inline uint64_t attention_workspace(const AttentionArgs& p) {

@@ -10,15 +10,16 @@ from types import SimpleNamespace
 from paper_2603_09221_amd import binding
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-FIELDS = ("prompt", "shared", "workgroups", "entries", "items", "max_q", "max_kv", "workspace")
+FIELDS = ("prompt", "shared", "workgroups", "entries", "items", "max_q", "max_kv", "workspace", "fits")
 SOURCE = """
 #include "ttc_attention_plan.hpp"
 extern "C" void plan(const ttc_attention_t *a, int cus, long long *out) {
   ttc::AttentionArgs p;
   p.a = *a;
-  ttc::plan_attention(p, cus);
-  const long long v[] = {p.prompt, p.shared, p.workgroups, p.entries, p.items, p.a.max_q, p.a.max_kv, (long long)ttc::attention_workspace(p)};
-  for (unsigned i = 0; i < sizeof v / sizeof *v; ++i) out[i] = v[i];
+  const bool fits = ttc::plan_attention(p, cus);
+  const long long no[] = {0, 0, 0, 0, 0, 0, 0, 0, 0},
+                  v[] = {p.prompt, p.shared, p.workgroups, p.entries, p.items, p.a.max_q, p.a.max_kv, (long long)ttc::attention_workspace(p), 1};
+  for (unsigned i = 0; i < sizeof v / sizeof *v; ++i) out[i] = fits ? v[i] : no[i];
 }
 """
 

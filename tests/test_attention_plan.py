@@ -23,3 +23,16 @@ def test_a_bound_wider_than_the_one_row_that_each_sequence_has(bf16, group):
         assert plan(describe(**call, max_q=max_q)) == one
     assert one.workgroups >= 384 and one.entries == 384 * -(-group // (128 if one.prompt else 16))
     assert plan(describe(**call, max_q=0)).max_q == 0
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+def test_a_long_bound_on_new_tokens_is_no_reason_to_refuse(bf16):
+    """256 sequences, one with 32768 new tokens beside single ones; a bound far above what there is; and what no launch holds."""
+    call = dict(heads_q=32, heads=8, d=64, page=64, bf16=bf16)
+    p = plan(describe(sequences=256, tokens=32768 + 255, max_q=32768, max_kv=40000, **call))
+    assert p.fits and p.prompt and 8 * (32768 * 4 // 128 + 255) <= p.workgroups < 1 << 24
+    p = plan(describe(sequences=40, tokens=2000, max_q=1 << 19, max_kv=1 << 19, **call))
+    assert p.fits and p.prompt and p.workgroups == 8 * (2000 * 4 // 128 + 40)
+    for sequences, tokens, max_q, max_kv in ((1 << 24, 1 << 24, 1, 64), (1 << 40, 1 << 40, 1, 64), (1, 1 << 29, 1 << 29, 64), (1, 1, 1, (1 << 30) + 1),
+                                             (1 << 20, 1 << 20, 1 << 20, 64), ((1 << 63) - 1, (1 << 63) - 1, 0, 0)):
+        assert not plan(describe(sequences=sequences, tokens=tokens, max_q=max_q, max_kv=max_kv, **call)).fits

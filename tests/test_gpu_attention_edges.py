@@ -126,6 +126,15 @@ def test_rows_without_being_told_and_a_wider_bound(dtype):
         s.check({"out": out, "lse": lse})
 
 
+@pytest.mark.parametrize("dtype,d", MANY)
+def test_a_bound_on_new_tokens_far_above_what_there_is(dtype, d):
+    s = Setup([29 * i % 97 + 3 for i in range(39)] + [1100], [i % 2 for i in range(39)] + [1050], 8, 4, d, 16, dtype, seed=d)
+    a = s.gpu()
+    p = plan(describe(40, int(s.cu[-1]), 32, 8, d, 16, dtype == torch.bfloat16, 1 << 19, s.table.shape[1] * 16))
+    assert p.fits and p.prompt
+    s.check(binding.ttc_attention(**{**a, "max_q": 1 << 19}))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_replays_on_a_workspace_that_nobody_clears(dtype):
     """A captured call carries the same mark every time: what it left in the workspace must not be taken for this replay's parts.  Behind
