@@ -135,6 +135,34 @@ def test_a_bound_on_new_tokens_far_above_what_there_is(dtype, d):
     s.check(binding.ttc_attention(**{**a, "max_q": 1 << 19}))
 
 
+@pytest.mark.parametrize("dtype,d", MANY)
+def test_nan_missing_pages_and_negative_scale_where_rows_are_many(dtype, d):
+    s = many(dtype, d, seed=5)
+    k, v = s.exponents()
+    k[s.table[0, 180 // 16], 1, 180 % 16, 1] = 255
+    v[s.table[1, 75 // 16], 2, 75 % 16 // 4, 0, 75 % 4] = 255
+    s.table[0, 3], s.table[1, 1] = -1, s.pages
+    put_exponents(s, k, v)
+    (out, _, _), _ = s.oracle(window=100)
+    assert 0 < np.isnan(out).mean() < 0.2
+    s.check(binding.ttc_attention(**s.gpu(), window=100), window=100)
+    s.scale = -0.25
+    got = binding.ttc_attention(**s.gpu())
+    s.q, s.scale = -s.q, 0.25
+    s.check(got)
+
+
+@pytest.mark.parametrize("dtype,d", MANY)
+@pytest.mark.parametrize("kv_len,new,group,window", [
+    ([500, 260], [300, 100], 11, 130),
+    ([37 * i % 101 + 9 for i in range(150)], [12 * i % 17 for i in range(150)], 16, 0),     # more sequences than a wavefront has lanes
+    ([140, 300, 128], [128, 126, 125], 11, 0)])
+def test_many_rows_by_the_plan(kv_len, new, group, window, dtype, d):
+    s = Setup(kv_len, new, 8, group, d, 32, dtype, seed=len(new) + d)
+    assert planned(s, window).prompt
+    s.check(binding.ttc_attention(**s.gpu(), window=window), window=window)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_replays_on_a_workspace_that_nobody_clears(dtype):
     """A captured call carries the same mark every time: what it left in the workspace must not be taken for this replay's parts.  Behind
