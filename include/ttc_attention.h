@@ -108,8 +108,10 @@ ttc_status_t ttc_kv_read(const ttc_kv_cache_t *cache, const int64_t *slots, int6
  * Causal: it sees tokens j <= p, with a window w > 0 only p - w < j <= p.  Otherwise all n.  A query that sees nothing gets
  * out = 0 and lse = -inf.  What a query does not see has no influence on it, NaN included.
  * Queries of float32 are worked on as exact sums of parts, sums and statistics are float32; for bfloat16 the weights
- * exp(s_j - max) are rounded to bfloat16 for their product with the values.  Equal calls give equal bits; the last bits of a
- * sequence's result may differ with the other sequences of the call, which decide how its context is divided. */
+ * exp(s_j - max) are rounded to bfloat16 for their product with the values (at most 2^-8 of sum_j exp(s_j - lse) |v_j|).  Values are
+ * summed before they are divided, with weights of up to 2^8: where they are beyond 2^119 / n a sum may pass the largest float32.
+ * Equal calls give equal bits; the last bits of a sequence's result may differ with the other sequences of the call, which decide how
+ * its context is divided. */
 typedef struct {
   ttc_kv_cache_t cache;
   int64_t sequences;

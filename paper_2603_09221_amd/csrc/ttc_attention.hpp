@@ -11,8 +11,13 @@
 // What bounds it: 4 sequences of 131072 tokens (8 cache heads of 128, 4 query heads each, bfloat16) are read in 95 us, 6.0 TB/s, where a
 // kernel that only reads reaches 6.7 to 7.2; 64 sequences of 257 to 16384 tokens in 118 us, 5.0 TB/s, the rest being the beginnings and
 // joins of a workgroup's two items or three.  24 sequences of up to 4099 tokens in float32 (16 heads of 64) take 32 us for 10.7 us of
-// bytes: four units a workgroup, and products of three parts.  One sequence of 4099 tokens takes 12 us, a chain of waits (lengths,
-// page numbers, codes, join), none of which the card can shorten by working on more of it.
+// bytes: four units a workgroup, and products of three parts.  One sequence of 4099 tokens takes 12 us: a chain of waits (lengths,
+// page numbers, codes, join) for 0.9 us of bytes.
+//
+// Roundings: scores, statistics and sums are float32.  With bfloat16 rows a weight is rounded to bfloat16 for its product with the values, one
+// product instead of three and the operand type that the queries came in; the sum that divides is of the unrounded weights.  That moves an
+// entry of the result by 2^-8 of sum weight |value| at most, as much as its own rounding to bfloat16 does.  Rows of float32 round nothing: a number is
+// the sum of three bfloat16 parts, which hold its 24 bits.
 #pragma once
 #include "ttc_attention_plan.hpp"
 #include "ttc_serve.hpp"
@@ -242,7 +247,9 @@ __device__ __forceinline__ srv_bf16x2 att_value_pair(const W& code, int k, int e
 // not clear anything.  Every workgroup sets its own mark and then looks at the others', so the last one sees all; two may, and then both
 // write the same.  The marks are taken away again, for a captured launch comes back with the same one.  Nobody waits for another workgroup.
 // The workgroups may be on different XCDs, whose caches do not see each other's lines: results and marks go past them, in stores and loads
-// of device scope.  Each wavefront waits for its stores, the workgroup for its wavefronts, and only then the mark is set.
+// of device scope.  Each wavefront waits for its stores, the workgroup for its wavefronts, and only then the mark is set.  That order rests on
+// the hardware, whose memory counter (vmcnt) says when a store of device scope has arrived, not on the language, to which relaxed accesses
+// of different addresses have none.
 // Fences of device scope instead write back and empty whole caches: a call over 4 x 131072 tokens took 282 us with them.  A count of
 // arrivals, which all workgroups of an item change one after the other, took 26 us where the marks take 13 (17 workgroups, 4099 tokens).
 __device__ __forceinline__ void att_put2(float* p, float a, float b) {

@@ -69,10 +69,13 @@ inline bool plan_attention(AttentionArgs& p, int cus) {
   if (most >= 2147483648. || most * a.cache.heads >= 1e15) return false;
   // The kernel for many rows does a tile's context from end to end in one workgroup: 1.2 us for every 64 tokens, however few of its 128
   // rows there are, up to a tile to each compute unit; attention_kernel takes tiles of 16 in time proportional to their number.  So there have to
-  // be rows for three quarters of the compute units, and half a tile of them to a sequence; with float32 for all, and three quarters of one.
-  // This one / attention_kernel, us: over 8192 tokens, d = 128, one sequence, rows for 64 tiles 193 / 90, 128 197 / 161, 256 210 / 304;
-  // 256 sequences of 8192 tokens, 32 rows each 198 / 101, 64 205 / 203, 96 205 / 296; 1024 of 600 tokens, 32 rows 67 / 47, 64 71 / 86;
-  // the same in float32, d = 64, 64 rows 86 / 74, 96 92 / 106.
+  // be rows for three quarters of the compute units' tiles, and half a tile of them to a sequence; with float32 for all, and three quarters of one.
+  // This one / attention_kernel, us.  By the first condition, d = 128, one sequence over 8192 tokens, rows for 64 tiles 193 / 90, 128
+  // 197 / 161, 256 210 / 304; 256 sequences of 8192 tokens with 64 rows 205 / 203, 96 205 / 296.  By the second, 1024 items (128 sequences, 8
+  // cache heads) of 600 tokens, 32 rows 67 / 47, 64 72 / 86, 80 75 / 106; d = 64, 512 sequences of 8192 tokens, 64 rows 231 / 242, 92 233 / 355;
+  // float32, d = 64, 1024 items of 600 tokens, 64 rows 86 / 74, 96 92 / 106.  The host knows no lengths: where they are far apart the longest
+  // is this one's time, and 512 sequences of 0 to 8192 tokens with 64 rows take 206 / 160.  One bound and one choice for all sequences of a
+  // call: single tokens beside a long chunk are taken as the chunk is.
   const bool bf16 = a.dtype == TTC_BF16;
   const int64_t prompt_tiles = (rows + 32 * PROMPT_WAVES - 1) / (32 * PROMPT_WAVES);
   const int64_t all_rows = (a.tokens < a.sequences * a.max_q ? a.tokens : a.sequences * a.max_q) * p.group;
@@ -86,6 +89,7 @@ inline bool plan_attention(AttentionArgs& p, int cus) {
   const int64_t slots = (int64_t)att_resident(a.cache.d) * cus;
   const int64_t units = (visible_at_most(a, p.group) + ATT_UNIT - 1) / ATT_UNIT;
   const int64_t own = 4 * p.items / cus;
+  // (entries: every wavefront adds up their units, 16 to a lane at most.  The empty tiles of a long max_q count among them.)
   p.shared = !p.prompt && units > (own > 4 ? own : 4) && p.entries <= 1024 && (double)units * p.items < 1e9;
   p.workgroups = p.prompt ? a.cache.heads * (tiles < real ? tiles : real) : !p.shared ? p.items : units * p.items < slots ? units * p.items : slots;
   p.part_out = p.part_stat = nullptr;

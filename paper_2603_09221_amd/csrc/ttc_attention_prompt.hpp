@@ -6,10 +6,10 @@
 // product waits for its operand: 838 us where this takes 700).  Values have to be turned, four tokens' entries side by side, which costs an
 // exchange per two entries: the workgroup does that once, into LDS, in the order of the lanes that read it (a quarter of LDS's busy cycles are conflicts, of the writes; LDS is busy a quarter of the time).
 //
-// 4096 queries of 32 heads over 12288 tokens (d = 128, 8 cache heads): 695 us, 1.0 PFLOP/s, where a large matrix product of the library runs
-// at 1.25.  Matrix and vector instructions of the two wavefronts of a SIMD share its time, 43 % and 60 % of the cycles: a step of 64 tokens
-// is 32 products (1024 cycles), 32 exponentials and about 290 other vector instructions.  With d = 64, 475 us: half the products beside
-// the same softmax.
+// 4096 queries of 32 heads over 12288 tokens (d = 128, 8 cache heads): 718 us, 0.96 PFLOP/s, where a large matrix product of the library
+// runs at 1.25.  Matrix and vector instructions of the two wavefronts of a SIMD share its time, about 42 % and 62 % of the cycles: a step of 64
+// tokens is 32 products (1024 cycles), 32 exponentials and about 270 other vector instructions.  With d = 64 half the products stand beside
+// the same softmax.  Weights of bfloat16 rows are rounded for their product, as in attention_kernel.
 #pragma once
 #include <type_traits>
 
