@@ -1,6 +1,7 @@
 /*
  * ttc_attention.h -- C ABI of what stands in front of a Test-Time Control block in a decoder layer (the paper's hybrid of
- * memory layers and the block, Sec. 4): rotary positions, a paged key-value cache held in 4 bits, and attention over it.
+ * memory layers and the block, Sec. 4): rotary positions, a paged key-value cache held in 4 bits, the places of new tokens in it, and
+ * attention over it.
  *
  * Conventions are those of ttc_lqr.h: DEVICE pointers, caller-owned outputs and workspaces, no allocation, no
  * synchronisation, asynchronous launches on `hip_stream`; argument errors are reported by the return code and nothing is
@@ -100,6 +101,34 @@ ttc_status_t ttc_kv_append(const ttc_kv_append_t *append, void *hip_stream);
  * number of the cache exactly); a slot outside the cache gives zeros.  k_out or v_out may be NULL. */
 ttc_status_t ttc_kv_read(const ttc_kv_cache_t *cache, const int64_t *slots, int64_t n, int32_t out_dtype, void *k_out,
                          void *v_out, void *hip_stream);
+
+/* ---- new tokens' places ---------------------------------------------------------------------------------------------------
+ * From the sequences' lengths what the calls below take, without the host: whose token each row is, its position and its slot, pages for
+ * tokens that need new ones, and ended sequences' pages back.  Sequence s has past[s] tokens in the cache, on ceil(past[s] / page) pages of its
+ * row of block_table, and gets new_tokens[s] more; new_tokens[s] < 0 says that it has ended: its kv_len becomes 0.
+ * Pages come from a list: free_pages[0 .. *free_count).  First the pages of ended sequences are put behind its end, in the order of sequences and
+ * columns (entries outside 0 .. pages-1 are left out), then every sequence in order takes those it lacks from the end.  Where the list is
+ * empty the entry becomes -1, its tokens' slots too.  Without a list (NULL) the table is taken as it is. */
+typedef struct {
+  int64_t sequences, tokens;   /* tokens: rows of positions, slots, sequence; what the lengths have beyond them is left out.  Both < 2^30 */
+  int64_t pages;               /* of the cache                                                             */
+  int32_t page;                /* tokens a page, 1 .. 65536                                                */
+  int32_t width;               /* columns of block_table; tokens that would need more have the slot -1     */
+  const int32_t *past;         /* (sequences); negative counts as 0, more than 2^30 - 1 as that            */
+  const int32_t *new_tokens;   /* (sequences)                                                              */
+  int32_t *block_table;        /* (sequences, width) by table_stride; new pages are written, nothing else  */
+  int64_t table_stride;
+  int32_t *free_pages;         /* (free_capacity): pages that would pass it are dropped                    */
+  int64_t free_capacity;
+  const int32_t *free_count;
+  int32_t *free_count_out;     /* pages left on the list; may be free_count itself                         */
+  int32_t *missing;            /* pages that were needed and not there, or NULL                            */
+  int32_t *cu_q;               /* (sequences + 1): first rows, as ttc_attention takes them                 */
+  int32_t *kv_len;             /* (sequences): past + new; may be `past` itself                            */
+  int64_t *positions, *slots;  /* (tokens); rows behind the last token: 0 and -1                           */
+  int32_t *sequence;           /* (tokens), -1 behind the last token; or NULL                              */
+} ttc_kv_place_t;
+ttc_status_t ttc_kv_place(const ttc_kv_place_t *place, void *hip_stream);
 
 /* ---- attention over the cache -------------------------------------------------------------------------------------------
  * For every sequence its new tokens' queries over the tokens that the cache holds of it, the new ones included:

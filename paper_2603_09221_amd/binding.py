@@ -1,4 +1,4 @@
-"""ctypes binding of the C-ABI library (include/ttc_lqr.h, include/ttc_attention.h): argument marshalling only.
+"""ctypes binding of the C-ABI library (include/ttc_lqr.h, include/ttc_attention.h, include/ttc_memory.h): argument marshalling only.
 
 PyTorch is used for device memory and streams; every step of the path runs in the HIP library.
 The library must have been built (``python -c "import __graft_entry__ as g; g.build()"``); there is
@@ -30,7 +30,10 @@ EXPORTS = ("ttc_lqr_workspace_bytes", "ttc_lqr_solve", "ttc_lqr_solve_squares", 
            "ttc_lqr_backward_tv", "ttc_lqr_backward_tv_workspace_bytes", "ttc_lqr_backward_cxt", "ttc_lqr_backward_cxt_workspace_bytes", "ttc_block_workspace_bytes", "ttc_block_forward",
            "ttc_status_string", "ttc_version")
 ATTENTION_EXPORTS = ("ttc_rope", "ttc_rope_backward", "ttc_rope_table", "ttc_kv_page_bytes", "ttc_kv_append", "ttc_kv_read",
-                     "ttc_attention_workspace_bytes", "ttc_attention")
+                     "ttc_kv_place", "ttc_attention_workspace_bytes", "ttc_attention")
+MEMORY_EXPORTS = ("ttc_linear_attention_workspace_bytes", "ttc_linear_attention", "ttc_linear_attention_backward_workspace_bytes",
+                  "ttc_linear_attention_backward", "ttc_residual_norm", "ttc_residual_norm_backward_workspace_bytes",
+                  "ttc_residual_norm_backward")
 
 
 class Problem(ctypes.Structure):
@@ -101,12 +104,50 @@ class KvAppend(ctypes.Structure):
                 ("q_out_token", c_int64), ("q_out_head", c_int64)]
 
 
+class KvPlace(ctypes.Structure):
+    _fields_ = [("sequences", c_int64), ("tokens", c_int64), ("pages", c_int64), ("page", c_int32), ("width", c_int32),
+                ("past", c_void_p), ("new_tokens", c_void_p), ("block_table", c_void_p), ("table_stride", c_int64),
+                ("free_pages", c_void_p), ("free_capacity", c_int64), ("free_count", c_void_p), ("free_count_out", c_void_p),
+                ("missing", c_void_p), ("cu_q", c_void_p), ("kv_len", c_void_p), ("positions", c_void_p), ("slots", c_void_p),
+                ("sequence", c_void_p)]
+
+
 class Attention(ctypes.Structure):
     _fields_ = [("cache", KvCache), ("sequences", c_int64), ("tokens", c_int64), ("heads_q", c_int32), ("dtype", c_int32),
                 ("causal", c_int32), ("window", c_int32), ("scale", ctypes.c_float), ("max_q", c_int32), ("max_kv", c_int32),
                 ("q", c_void_p), ("out", c_void_p), ("lse", c_void_p), ("q_token", c_int64), ("q_head", c_int64),
                 ("out_token", c_int64), ("out_head", c_int64), ("cu_q", c_void_p), ("kv_len", c_void_p),
                 ("block_table", c_void_p), ("table_stride", c_int64)]
+
+
+class LinearAttention(ctypes.Structure):
+    _fields_ = [("sequences", c_int64), ("tokens", c_int64), ("heads", c_int32), ("heads_qk", c_int32), ("dk", c_int32), ("dv", c_int32),
+                ("dtype", c_int32), ("max_q", c_int32), ("scale", ctypes.c_float), ("q", c_void_p), ("k", c_void_p), ("v", c_void_p),
+                ("out", c_void_p), ("q_token", c_int64), ("q_head", c_int64), ("k_token", c_int64), ("k_head", c_int64),
+                ("v_token", c_int64), ("v_head", c_int64), ("out_token", c_int64), ("out_head", c_int64), ("log_decay", c_void_p),
+                ("g_token", c_int64), ("g_head", c_int64), ("cu_q", c_void_p), ("state_in", c_void_p), ("state_out", c_void_p),
+                ("state_rows", c_int64), ("state_row", c_void_p), ("kv_len", c_void_p)]
+
+
+class LinearAttentionBackward(ctypes.Structure):
+    _fields_ = [("forward", LinearAttention), ("gout", c_void_p), ("gout_token", c_int64), ("gout_head", c_int64),
+                ("gstate_out", c_void_p), ("gq", c_void_p), ("gk", c_void_p), ("gv", c_void_p), ("glog_decay", c_void_p),
+                ("gstate", c_void_p)]
+
+
+NORM_VECTORS = ("post_gain", "post_offset", "residual_gain", "pre_gain", "pre_offset")
+
+
+class ResidualNorm(ctypes.Structure):
+    _fields_ = [("tokens", c_int64), ("features", c_int32), ("groups", c_int32), ("dtype", c_int32), ("post", c_int32), ("pre", c_int32),
+                ("act", c_int32), ("post_eps", ctypes.c_float), ("pre_eps", ctypes.c_float), ("scale", ctypes.c_float), ("y", c_void_p),
+                ("gate", c_void_p), ("residual", c_void_p), ("r", c_void_p), ("h", c_void_p), ("y_token", c_int64), ("gate_token", c_int64),
+                ("residual_token", c_int64), ("r_token", c_int64), ("h_token", c_int64)] + [(k, c_void_p) for k in NORM_VECTORS]
+
+
+class ResidualNormBackward(ctypes.Structure):
+    _fields_ = [("forward", ResidualNorm), ("gr", c_void_p), ("gh", c_void_p), ("gr_token", c_int64), ("gh_token", c_int64), ("gy", c_void_p),
+                ("ggate", c_void_p), ("gresidual", c_void_p)] + [("g" + k, c_void_p) for k in NORM_VECTORS]
 
 
 class TtcError(RuntimeError):
@@ -194,10 +235,19 @@ def load():
     lib.ttc_kv_append.argtypes = [ctypes.POINTER(KvAppend), c_void_p]
     lib.ttc_kv_read.restype = c_int
     lib.ttc_kv_read.argtypes = [ctypes.POINTER(KvCache), c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_void_p]
+    lib.ttc_kv_place.restype = c_int
+    lib.ttc_kv_place.argtypes = [ctypes.POINTER(KvPlace), c_void_p]
     lib.ttc_attention_workspace_bytes.restype = c_size_t
     lib.ttc_attention_workspace_bytes.argtypes = [ctypes.POINTER(Attention)]
     lib.ttc_attention.restype = c_int
     lib.ttc_attention.argtypes = [ctypes.POINTER(Attention), c_void_p, c_size_t, c_void_p]
+    for name, descriptor in (("ttc_linear_attention", LinearAttention), ("ttc_linear_attention_backward", LinearAttentionBackward),
+                             ("ttc_residual_norm_backward", ResidualNormBackward)):
+        call, size = getattr(lib, name), getattr(lib, name + "_workspace_bytes")
+        call.restype, call.argtypes = c_int, [ctypes.POINTER(descriptor), c_void_p, c_size_t, c_void_p]
+        size.restype, size.argtypes = c_size_t, [ctypes.POINTER(descriptor)]
+    lib.ttc_residual_norm.restype = c_int
+    lib.ttc_residual_norm.argtypes = [ctypes.POINTER(ResidualNorm), c_void_p]
     lib.ttc_status_string.restype = c_char_p
     lib.ttc_status_string.argtypes = [c_int]
     lib.ttc_version.restype = c_int
@@ -603,7 +653,7 @@ def ttc_block_forward(x_in, weights, T, *, eps=1e-5, want_h0=False, want_o=False
 
 
 # ---------------------------------------------------------------------------------------------------------------
-# rotary positions, the cache in 4 bits, attention over it (include/ttc_attention.h)
+# rotary positions, the cache in 4 bits, new tokens' places in it, attention over it (include/ttc_attention.h)
 
 _ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 
@@ -644,6 +694,14 @@ def _int32(**numbers):
     for name, value in numbers.items():
         if not -1 << 31 <= value < 1 << 31:
             raise ValueError(f"{name}: {value} does not fit in 32 bits")
+
+
+def _here(t, stream):
+    """The last check before a launch, which goes to the current device (or the stream's): that device holds the tensors."""
+    _on_gpu(t)
+    at = torch.cuda.current_device()
+    if t.get_device() != at or (stream is not None and stream.device_index != at):
+        raise ValueError("tensors and stream must be on the current device")
 
 
 def _on_gpu(t):
@@ -842,6 +900,52 @@ def ttc_kv_read(cache, slots, d, *, dtype=torch.bfloat16, out=None, stream=None)
     return k, v
 
 
+PLACE_OUTPUTS = {"cu_q": torch.int32, "kv_len": torch.int32, "positions": torch.int64, "slots": torch.int64, "sequence": torch.int32,
+                 "free_count": torch.int32, "missing": torch.int32}
+
+
+def ttc_kv_place(past, new_tokens, block_table, page, tokens, *, pages, free=None, free_count=None, out=None, stream=None):
+    """Where the new tokens of all sequences go, from lengths that lie on the device: {"cu_q" (sequences + 1), "kv_len" (sequences), "positions",
+    "slots" (tokens, int64), "sequence" (tokens)} and, with a list of free pages, {"free_count", "missing"} (1 each).
+
+    Sequence s has past[s] tokens (int32) on the pages of block_table[s] (int32; `pages` in the whole cache, of `page` tokens) and gets
+    new_tokens[s] more; -1: it has ended and its pages go back.  `free` (int32) and `free_count` (int32, 1 entry): the list that pages are taken
+    from, changed in place as block_table is; without it the table is taken as it is.  `tokens` is the number of rows: those behind the last
+    token get the slot -1, tokens beyond them are left out.  `out` may carry tensors under the same names: kv_len may be `past`, free_count
+    the list's."""
+    if block_table.dtype is not torch.int32 or block_table.dim() != 2:
+        raise ValueError("block_table: expected an int32 (sequences, pages) tensor")
+    sequences, width = block_table.shape
+    table_stride, step = block_table.stride()
+    if step != 1 and width > 1:
+        raise ValueError("block_table: expected contiguous rows")
+    _int32(page=page, tokens=tokens, pages=pages)
+    if tokens < 0 or page < 1 or pages < 0:
+        raise ValueError("tokens and pages must not be negative, page must be positive")
+    before, new = _vector(past, sequences, torch.int32, "past"), _vector(new_tokens, sequences, torch.int32, "new_tokens")
+    listed = capacity = count = None
+    if free is not None:
+        capacity = free.shape[0] if free.dim() == 1 else -1
+        listed, count = _vector(free, capacity, torch.int32, "free"), _vector(free_count, 1, torch.int32, "free_count")
+    elif free_count is not None:
+        raise ValueError("free_count without free")
+    sizes = {"cu_q": sequences + 1, "kv_len": sequences, "positions": tokens, "slots": tokens, "sequence": tokens}
+    if free is not None:
+        sizes.update(free_count=1, missing=1)
+    out = dict(out) if out else {}
+    at = {}
+    for name, n in sizes.items():
+        if out.get(name) is None:
+            out[name] = _new(past, (n,), PLACE_OUTPUTS[name], stream)
+        at[name] = _vector(out[name], n, PLACE_OUTPUTS[name], name)
+    _same_device(past, new_tokens, block_table, free, free_count, *(out[name] for name in sizes))
+    _here(past, stream)
+    _check(load().ttc_kv_place(KvPlace(sequences, tokens, pages, page, width, before, new, block_table.data_ptr(), table_stride, listed,
+                                       capacity or 0, count, at.get("free_count"), at.get("missing"), at["cu_q"], at["kv_len"],
+                                       at["positions"], at["slots"], at["sequence"]), _stream_ptr(stream)))
+    return out
+
+
 def ttc_attention(q, cache, block_table, kv_len, *, cu_q=None, max_q=None, max_kv=None, scale=None, causal=True, window=0,
                   want_lse=True, out=None, workspace=None, stream=None):
     """{"out": (tokens, heads_q, d) like q, "lse": (tokens, heads_q) float32} of the queries of new tokens over a cache in 4 bits.
@@ -900,4 +1004,218 @@ def ttc_attention(q, cache, block_table, kv_len, *, cu_q=None, max_q=None, max_k
     if need and workspace is None:
         workspace = _new(q, (need,), torch.uint8, stream)
     _check(lib.ttc_attention(att, _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream)))
+    return out
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# memory layers: linear attention with decays, and the norms around a block (include/ttc_memory.h)
+
+def _linear_attention(q, k, v, log_decay, cu_q, max_q, state, state_row, kv_len, scale, backward):
+    """The descriptor without out, state_out and state_rows, after all that it is made of was checked."""
+    dtype = _in_dtype(q, k, v)
+    q_token, q_head = _heads_strides(q, "q")
+    tokens, heads_qk, dk = q.shape
+    k_token, k_head = _heads_strides(k, "k", q.shape)
+    v_token, v_head = _heads_strides(v, "v")
+    if v.shape[0] != tokens:
+        raise ValueError("v: expected %d tokens" % tokens)
+    heads, dv = v.shape[1:]
+    if not heads_qk or not heads or heads % heads_qk:
+        raise ValueError("v: its heads must be a multiple of those of q and k")
+    if log_decay.dtype is not torch.float32 or log_decay.shape not in ((heads,), (tokens, heads)):
+        raise ValueError("log_decay: expected a float32 tensor (tokens, heads) or (heads)")
+    g_token, g_head = log_decay.stride() if log_decay.dim() == 2 else (0, log_decay.stride(0))
+    if log_decay.dim() == 2 and not g_token and backward:
+        if tokens > 1:
+            raise ValueError("log_decay: a decay for all tokens is given as (heads), which is what its gradient is")
+        g_token = 1
+    cu = None
+    if cu_q is not None:
+        sequences = cu_q.shape[0] - 1 if cu_q.dim() == 1 else -1
+        if sequences < 0:
+            raise ValueError("cu_q: expected an int32 tensor (sequences + 1)")
+        cu = _vector(cu_q, sequences + 1, torch.int32, "cu_q")
+        if max_q is None:
+            raise ValueError("max_q is needed with cu_q")
+    else:
+        sequences, max_q = tokens, 1
+    _int32(max_q=max_q)
+    row = None if state_row is None else _vector(state_row, sequences, torch.int32, "state_row")
+    lens = None if kv_len is None else _vector(kv_len, sequences, torch.int32, "kv_len")
+    if state is not None:
+        _states(state, "state", None if state_row is not None else sequences, heads, dk, dv)
+    return LinearAttention(sequences, tokens, heads, heads_qk, dk, dv, dtype, max_q, dk ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(),
+                           v.data_ptr(), None, q_token, q_head, k_token, k_head, v_token, v_head, 0, 0, log_decay.data_ptr(), g_token, g_head, cu,
+                           _ptr(state), None, 0 if state is None else state.shape[0], row, lens)
+
+
+def _states(t, name, rows, heads, dk, dv):
+    """Checks a tensor of states (rows, heads, dk, dv); rows None: any number."""
+    if t.dtype is not torch.float32 or t.dim() != 4 or t.shape[1:] != (heads, dk, dv) or (rows is not None and t.shape[0] != rows) or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous float32 tensor of {'rows' if rows is None else rows} x {(heads, dk, dv)}")
+
+
+def ttc_linear_attention(q, k, v, log_decay, *, cu_q=None, max_q=None, state=None, state_row=None, kv_len=None, want_state=False, scale=None, out=None,
+                         workspace=None, stream=None):
+    """{"out": (tokens, heads, dv) like v} of linear attention whose states fade: S = exp(log_decay) S + k v^T, out = scale S^T q.
+
+    q, k (tokens, heads_qk, dk), v (tokens, heads, dv): float32 or bfloat16, any strides with contiguous heads; log_decay float32 (tokens, heads),
+    or (heads) for decays that do not change.  Sequences are the rows cu_q[s] .. cu_q[s+1]-1 (int32; without cu_q one token each); with cu_q
+    max_q, the most tokens of one, is needed.  `state` (rows, heads, dk, dv) float32 holds what sequences go on from, sequence s in row
+    state_row[s] (int32; without it row s); those whose kv_len[s] (int32: all tokens so far, these included) is no more than their tokens here
+    begin with zeros.  Last states go to out["state"], which may be `state` itself, or with want_state to a new tensor, a row for a
+    sequence.  scale defaults to dk^-1/2."""
+    lib = load()
+    a = _linear_attention(q, k, v, log_decay, cu_q, max_q, state, state_row, kv_len, scale, False)
+    y = last = None
+    if out:
+        y, last = out.get("out"), out.get("state")
+    out = dict(out) if out else {}
+    if y is None:
+        y = out["out"] = _new_like(v, stream)
+        a.out_token, a.out_head = a.heads * a.dv, a.dv
+    else:
+        a.out_token, a.out_head = _heads_strides(y, "out", v.shape, v.dtype)
+    if last is not None:
+        _states(last, "out['state']", a.sequences if state_row is None else None if state is None else state.shape[0], a.heads, a.dk, a.dv)
+    elif want_state:
+        if state_row is not None:
+            raise ValueError("want_state: with state_row the last states go to rows of out['state']")
+        last = out["state"] = _new(q, (a.sequences, a.heads, a.dk, a.dv), torch.float32, stream)
+    if last is not None:
+        a.state_out, a.state_rows = last.data_ptr(), last.shape[0]
+    a.out = y.data_ptr()
+    _same_device(q, k, v, log_decay, cu_q, state, state_row, kv_len, y, last, workspace)
+    _here(q, stream)
+    need = lib.ttc_linear_attention_workspace_bytes(a)
+    if need and workspace is None:
+        workspace = _new(q, (need,), torch.uint8, stream)
+    _check(lib.ttc_linear_attention(a, _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream)))
+    return out
+
+
+def ttc_linear_attention_backward(q, k, v, log_decay, grad_out, *, cu_q=None, max_q=None, state=None, state_row=None, kv_len=None, grad_state=None,
+                                  scale=None, out=None, workspace=None, stream=None):
+    """{"gq", "gk", "gv", "glog_decay"} of a loss with the gradient grad_out (tokens, heads, dv) with respect to ttc_linear_attention's out, and
+    grad_state (sequences, heads, dk, dv) with respect to the sequences' last states (None: zeros); with `state` also "gstate" (sequences, heads,
+    dk, dv), with respect to what each began with.  glog_decay is float32, of log_decay's shape; rows that no sequence has are not written."""
+    lib = load()
+    a = _linear_attention(q, k, v, log_decay, cu_q, max_q, state, state_row, kv_len, scale, True)
+    gout_token, gout_head = _heads_strides(grad_out, "grad_out", v.shape, v.dtype)
+    each = (a.sequences, a.heads, a.dk, a.dv)
+    if grad_state is not None:
+        _states(grad_state, "grad_state", *each)
+    shapes = {"gq": (q.shape, q.dtype), "gk": (q.shape, q.dtype), "gv": (v.shape, q.dtype), "glog_decay": (log_decay.shape, torch.float32)}
+    if state is not None:
+        shapes["gstate"] = (each, torch.float32)
+    out = dict(out) if out else {}
+    for name, (shape, dtype) in shapes.items():
+        if out.get(name) is None:
+            out[name] = _new(q, shape, dtype, stream)
+        elif out[name].shape != shape or out[name].dtype is not dtype or not out[name].is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)}")
+    _same_device(q, k, v, log_decay, grad_out, grad_state, cu_q, state, state_row, kv_len, workspace, *(out[name] for name in shapes))
+    _here(q, stream)
+    b = LinearAttentionBackward(a, grad_out.data_ptr(), gout_token, gout_head, _ptr(grad_state), out["gq"].data_ptr(), out["gk"].data_ptr(),
+                                out["gv"].data_ptr(), out["glog_decay"].data_ptr(), _ptr(out["gstate"]) if state is not None else None)
+    need = lib.ttc_linear_attention_backward_workspace_bytes(b)
+    if need and workspace is None:
+        workspace = _new(q, (need,), torch.uint8, stream)
+    _check(lib.ttc_linear_attention_backward(b, _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream)))
+    return out
+
+
+_NORMS = {None: 0, "rms": 1, "layer": 2}
+_GATES = {"identity": 0, "sigmoid": 1, "silu": 2}
+
+
+def _rows_stride(t, name, shape, dtype):
+    """Token stride of a (tokens, features) tensor with contiguous features."""
+    if t.shape != shape or t.dtype is not dtype:
+        raise ValueError(f"{name}: expected a {tuple(shape)} tensor of {dtype}")
+    token, entry = t.stride()
+    if entry != 1 and shape[1] > 1:
+        raise ValueError(f"{name}: the features of a token must be contiguous")
+    return token
+
+
+def _residual_norm(y, residual, gate, activation, post, post_gain, post_offset, groups, post_eps, scale, residual_gain, pre, pre_gain, pre_offset,
+                   pre_eps):
+    if y.dim() != 2:
+        raise ValueError("y: expected (tokens, features)")
+    dtype = _in_dtype(y, gate, residual)
+    if post not in _NORMS or pre not in _NORMS:
+        raise ValueError("post, pre: 'rms', 'layer' or None")
+    if gate is not None and activation not in _GATES:
+        raise ValueError("activation: 'silu', 'sigmoid' or 'identity'")
+    tokens, features = y.shape
+    strides = [0 if t is None else _rows_stride(t, name, y.shape, y.dtype) for name, t in (("y", y), ("gate", gate), ("residual", residual))]
+    vectors = dict(post_gain=post_gain, post_offset=post_offset, residual_gain=residual_gain, pre_gain=pre_gain, pre_offset=pre_offset)
+    for name, t in vectors.items():
+        if t is not None:
+            _vector(t, features, torch.float32, name)
+    if (post is None and (post_gain is not None or post_offset is not None)) or (pre is None and (pre_gain is not None or pre_offset is not None)):
+        raise ValueError("a gain or an offset without its norm")
+    _int32(groups=groups)
+    _same_device(y, gate, residual, *vectors.values())
+    return ResidualNorm(tokens, features, groups, dtype, _NORMS[post], _NORMS[pre], _GATES[activation] if gate is not None else 0, post_eps, pre_eps, scale,
+                        y.data_ptr(), _ptr(gate), _ptr(residual), None, None, *strides, 0, 0, *(_ptr(t) for t in vectors.values())), vectors
+
+
+def ttc_residual_norm(y, *, residual=None, gate=None, activation="silu", post=None, post_gain=None, post_offset=None, groups=1, post_eps=1e-5,
+                      scale=1.0, residual_gain=None, pre=None, pre_gain=None, pre_offset=None, pre_eps=1e-5, out=None, stream=None):
+    """{"r", "h"}: what stands around a block whose result is y (tokens, features; float32 or bfloat16, contiguous features):
+    r = residual + scale * residual_gain * act(gate) * N_post(y), h = N_pre(r), the next block's input.
+
+    post, pre: "rms", "layer" or None (no norm; then no h).  N_post norms each of `groups` equal parts of the features for itself.  activation of
+    the gate: "silu", "sigmoid", "identity".  Gains and offsets are float32 (features).  `out` may carry tensors under the names r and h: r may be
+    residual itself."""
+    n, _ = _residual_norm(y, residual, gate, activation, post, post_gain, post_offset, groups, post_eps, scale, residual_gain, pre, pre_gain, pre_offset,
+                          pre_eps)
+    out = dict(out) if out else {}
+    for name in ("r", "h") if pre is not None else ("r",):
+        if out.get(name) is None:
+            out[name] = _new_like(y, stream) if y.is_contiguous() else _new(y, y.shape, y.dtype, stream)
+    n.r, n.r_token = out["r"].data_ptr(), _rows_stride(out["r"], "r", y.shape, y.dtype)
+    if pre is not None:
+        n.h, n.h_token = out["h"].data_ptr(), _rows_stride(out["h"], "h", y.shape, y.dtype)
+    else:
+        out.setdefault("h", None)
+    _same_device(y, out["r"], out["h"])
+    if y.shape[0] and y.shape[1]:
+        _here(y, stream)
+        _check(load().ttc_residual_norm(n, _stream_ptr(stream)))
+    return out
+
+
+def ttc_residual_norm_backward(y, *, grad_r=None, grad_h=None, residual=None, gate=None, activation="silu", post=None, post_gain=None, post_offset=None,
+                               groups=1, post_eps=1e-5, scale=1.0, residual_gain=None, pre=None, pre_gain=None, pre_offset=None, pre_eps=1e-5, out=None,
+                               workspace=None, stream=None):
+    """{"gy", "ggate", "gresidual", "gpost_gain", "gpost_offset", "gresidual_gain", "gpre_gain", "gpre_offset"}, each where the forward call has
+    what it belongs to, of a loss with the gradients grad_r (None: zeros) and grad_h with respect to ttc_residual_norm's results.  ggate is each
+    token's, also of a gate that is the same for all."""
+    lib = load()
+    n, vectors = _residual_norm(y, residual, gate, activation, post, post_gain, post_offset, groups, post_eps, scale, residual_gain, pre, pre_gain,
+                                pre_offset, pre_eps)
+    if (grad_h is not None) != (pre is not None):
+        raise ValueError("grad_h goes with pre")
+    gr_token, gh_token = (0 if t is None else _rows_stride(t, name, y.shape, y.dtype) for name, t in (("grad_r", grad_r), ("grad_h", grad_h)))
+    rows = {"gy": y, "ggate": gate, "gresidual": residual}
+    wanted = [name for name, t in rows.items() if t is not None] + ["g" + name for name, t in vectors.items() if t is not None]
+    out = dict(out) if out else {}
+    for name in wanted:
+        shape, dtype = (y.shape, y.dtype) if name in rows else (y.shape[1:], torch.float32)
+        if out.get(name) is None:
+            out[name] = _new(y, shape, dtype, stream)
+        elif out[name].shape != shape or out[name].dtype is not dtype or not out[name].is_contiguous():
+            raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)}")
+    _same_device(y, grad_r, grad_h, workspace, *(out[name] for name in wanted))
+    b = ResidualNormBackward(n, _ptr(grad_r), _ptr(grad_h), gr_token, gh_token, *(_ptr(out[name]) if name in wanted else None for name in rows),
+                             *(_ptr(out["g" + name]) if vectors[name] is not None else None for name in NORM_VECTORS))
+    if y.shape[1]:
+        _here(y, stream)
+        need = lib.ttc_residual_norm_backward_workspace_bytes(b)
+        if need and workspace is None:
+            workspace = _new(y, (need,), torch.uint8, stream)
+        _check(lib.ttc_residual_norm_backward(b, _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream)))
     return out

@@ -44,7 +44,12 @@ UNITS = [("ttc_api.hip", None),
          ("ttc_api_attention.hip", None),
          ("k_rope.hip", None),
          ("k_kv.hip", None),
-         ("k_attention.hip", (64, 128, 256))]
+         ("k_place.hip", None),
+         ("k_attention.hip", (64, 128, 256)),
+         ("ttc_api_memory.hip", None),
+         ("k_norm.hip", None),
+         ("k_memory_host.hip", None),
+         ("k_memory.hip", (64, 128, 256))]
 
 # Per (source, state size) compile flags: wavefronts of one 16-wide block each (twice as many per problem) instead of
 # two, where measured faster.  The Riccati and squaring kernels own matrices by columns: at d = 64 one column tile a wavefront

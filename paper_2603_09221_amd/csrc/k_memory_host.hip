@@ -1,0 +1,276 @@
+// Plans and launches of linear attention, and the kernels that do not depend on the heads' size.
+#include "ttc_memory_backward.hpp"
+#include "ttc_memory_launch.hpp"
+
+namespace ttc {
+
+template <> hipError_t launch_memory_chunks<64>(const MemArgs&, bool, bool, bool, uint32_t, hipStream_t);
+template <> hipError_t launch_memory_chunks<128>(const MemArgs&, bool, bool, bool, uint32_t, hipStream_t);
+template <> hipError_t launch_memory_chunks<256>(const MemArgs&, bool, bool, bool, uint32_t, hipStream_t);
+template <> hipError_t launch_memory_step<64>(const MemArgs&, bool, uint32_t, hipStream_t);
+template <> hipError_t launch_memory_step<128>(const MemArgs&, bool, uint32_t, hipStream_t);
+template <> hipError_t launch_memory_step<256>(const MemArgs&, bool, uint32_t, hipStream_t);
+
+namespace {
+
+constexpr int STEP_MOST = 4;  // tokens of a sequence up to which memory_step_kernel takes it
+
+int wide_of(int rows, int cols) { return rows <= 128 && cols > 64; }            // 128 columns a workgroup, else 64
+int slices_of(int rows, int cols) { return wide_of(rows, cols) ? (cols + 127) / 128 : (cols + 63) / 64; }
+
+MemSequences sequences_of(const ttc_linear_attention_t& a, int segment) {
+  MemSequences m = {a.sequences, a.tokens, a.cu_q, a.max_q, segment, a.sequences};
+  if ((int64_t)segment * MEM_CHUNK < a.max_q) m.entries += a.tokens / ((int64_t)segment * MEM_CHUNK);
+  return m;
+}
+
+// Chunks of a segment: all of a sequence where sequences, heads and slices occupy the device, else as many as give it four workgroups a unit
+int segment_of(const ttc_linear_attention_t& a, int slices, int cus) {
+  const int chunks = (int)(((int64_t)a.max_q + MEM_CHUNK - 1) / MEM_CHUNK);
+  const double base = (double)a.sequences * a.heads * slices;
+  if (chunks <= 1 || base >= 2. * cus) return chunks < 1 ? 1 : chunks;
+  const double wanted = 4. * cus / base;
+  const int each = (int)(chunks / wanted);
+  return each < 4 ? (chunks < 4 ? chunks : 4) : each;
+}
+
+MemRows rows_of(const void* p, int64_t token, int64_t head, int group, int d, bool bf16) {
+  const int64_t bytes = bf16 ? 2 : 4;
+  return {p, token, head, group, d, (uint64_t)p % 16 == 0 && token * bytes % 16 == 0 && head * bytes % 16 == 0};
+}
+
+MemArgs forward_args(const ttc_linear_attention_t& a) {
+  const bool bf16 = a.dtype == TTC_BF16;
+  const int group = a.heads / a.heads_qk;
+  MemArgs p = {};
+  p.x = rows_of(a.q, a.q_token, a.q_head, group, a.dk, bf16);
+  p.w = rows_of(a.k, a.k_token, a.k_head, group, a.dk, bf16);
+  p.v = rows_of(a.v, a.v_token, a.v_head, 1, a.dv, bf16);
+  p.out = a.out;
+  p.out_token = a.out_token;
+  p.out_head = a.out_head;
+  p.out_vec = rows_of(a.out, a.out_token, a.out_head, 1, a.dv, bf16).vec;
+  p.heads = a.heads;
+  p.pair_scale = p.in_scale = a.scale;
+  p.up_scale = 1.f;
+  p.log_decay = a.log_decay;
+  p.g_token = a.g_token;
+  p.g_head = a.g_head;
+  p.states = {a.state_in, a.state_out, a.state_rows, a.state_row, a.kv_len};
+  p.s_row = a.dv;
+  p.s_col = 1;
+  p.dk = a.dk;
+  p.dv = a.dv;
+  return p;
+}
+
+hipError_t run_chunks(MemArgs p, bool bf16, bool states, hipStream_t st) {
+  const int rows = states ? p.w.d : p.x.d;
+  const bool wide = wide_of(rows, p.v.d);
+  p.slices = slices_of(rows, p.v.d);
+  const double grid = (double)p.m.entries * p.heads * p.slices;
+  if (grid >= 2147483648.) return hipErrorInvalidValue;
+  const uint32_t n = (uint32_t)grid;
+  return rows <= 64 ? launch_memory_chunks<64>(p, bf16, wide, states, n, st)
+                    : rows <= 128 ? launch_memory_chunks<128>(p, bf16, wide, states, n, st) : launch_memory_chunks<256>(p, bf16, wide, states, n, st);
+}
+
+// What the segments add to their states, and from that what each finds
+hipError_t run_starts(const MemArgs& p, bool bf16, hipStream_t st) {
+  if (const hipError_t e = run_chunks(p, bf16, true, st); e != hipSuccess) return e;
+  const int64_t blocks = (p.dk * p.dv / 4 + 255) / 256;
+  hipLaunchKernelGGL(memory_scan_kernel, dim3((uint32_t)(p.m.sequences * p.heads * blocks)), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+
+uint64_t round16(uint64_t n) { return (n + 15) & ~15ull; }
+
+}  // namespace
+
+uint64_t linear_attention_workspace(const ttc_linear_attention_t& a, int cus) {
+  if (a.max_q <= STEP_MOST) return 0;
+  const MemSequences m = sequences_of(a, segment_of(a, slices_of(a.dk, a.dv), cus));
+  if (m.entries == m.sequences) return 0;
+  return (uint64_t)m.entries * a.heads * a.dk * a.dv * 4 + round16((uint64_t)m.entries * a.heads * 4);
+}
+
+hipError_t launch_linear_attention(const ttc_linear_attention_t& a, int cus, void* workspace, hipStream_t st) {
+  const bool bf16 = a.dtype == TTC_BF16;
+  MemArgs p = forward_args(a);
+  if (a.max_q <= STEP_MOST) {
+    p.m = sequences_of(a, 1);
+    p.m.entries = a.sequences;
+    p.slices = (a.dv + 63) / 64;
+    const uint32_t grid = (uint32_t)(a.sequences * a.heads * p.slices);
+    return a.dk <= 64 ? launch_memory_step<64>(p, bf16, grid, st) : a.dk <= 128 ? launch_memory_step<128>(p, bf16, grid, st) : launch_memory_step<256>(p, bf16, grid, st);
+  }
+  p.m = sequences_of(a, segment_of(a, slices_of(a.dk, a.dv), cus));
+  if (p.m.entries != p.m.sequences) {
+    p.added = static_cast<float*>(workspace);
+    p.faded = p.added + p.m.entries * a.heads * a.dk * a.dv;
+    if (const hipError_t e = run_starts(p, bf16, st); e != hipSuccess) return e;
+    p.starts = p.added;
+  }
+  return run_chunks(p, bf16, false, st);
+}
+
+namespace {
+
+// Places in the workspace of a backward pass, in bytes from its beginning
+struct BackwardPlan {
+  MemSequences m, chunks;
+  int slices;           // of dq's and dk's columns
+  uint64_t added, faded, added_r, faded_r, a, b, pairs, gstate, sums, gq, gk, bytes;
+};
+
+BackwardPlan plan_backward(const ttc_linear_attention_backward_t& b, int cus) {
+  const ttc_linear_attention_t& f = b.forward;
+  BackwardPlan p = {};
+  p.slices = slices_of(f.dv, f.dk);
+  p.m = sequences_of(f, segment_of(f, p.slices, cus));
+  p.chunks = sequences_of(f, 1);
+  uint64_t at = 0;
+  const auto take = [&](uint64_t& place, uint64_t bytes) {
+    place = at;
+    at += round16(bytes);
+  };
+  const uint64_t state = (uint64_t)f.dk * f.dv * 4;
+  if (p.m.entries != p.m.sequences) {
+    take(p.added, p.m.entries * f.heads * state);
+    take(p.faded, p.m.entries * f.heads * 4);
+    take(p.added_r, p.m.entries * f.heads * state);
+    take(p.faded_r, p.m.entries * f.heads * 4);
+  }
+  take(p.a, (uint64_t)p.slices * f.heads * f.tokens * 4);
+  take(p.b, (uint64_t)p.slices * f.heads * f.tokens * 4);
+  take(p.pairs, (uint64_t)f.heads * f.tokens * 4);
+  if (f.state_in && !b.gstate) take(p.gstate, f.sequences * f.heads * state);
+  if (!f.g_token) take(p.sums, (uint64_t)p.m.entries * f.heads * 8);
+  if (f.heads != f.heads_qk) {
+    take(p.gq, (uint64_t)f.tokens * f.heads * f.dk * 4);
+    take(p.gk, (uint64_t)f.tokens * f.heads * f.dk * 4);
+  }
+  p.bytes = at;
+  return p;
+}
+
+}  // namespace
+
+uint64_t linear_attention_backward_workspace(const ttc_linear_attention_backward_t& b, int cus) { return plan_backward(b, cus).bytes; }
+
+hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_t& b, int cus, void* workspace, hipStream_t st) {
+  const ttc_linear_attention_t& f = b.forward;
+  const BackwardPlan plan = plan_backward(b, cus);
+  const bool bf16 = f.dtype == TTC_BF16, segmented = plan.m.entries != f.sequences;
+  const int group = f.heads / f.heads_qk;
+  char* const ws = static_cast<char*>(workspace);
+  const auto place = [&](uint64_t at) { return reinterpret_cast<float*>(ws + at); };
+  float* const gstate = b.gstate ? b.gstate : f.state_in ? place(plan.gstate) : nullptr;
+
+  MemArgs base = forward_args(f);
+  base.m = plan.m;
+  base.states.out = nullptr;
+  const MemRows q = base.x, k = base.w, v = base.v, gout = rows_of(b.gout, b.gout_token, b.gout_head, 1, f.dv, bf16);
+  const MemStates begin = base.states, end = {b.gstate_out, gstate, f.sequences, nullptr, nullptr};
+  MemArgs back = base;
+  back.reverse = 1;
+  back.states = end;
+  back.rule = begin;
+  back.ruled = 1;
+  back.in_scale = 1.f;
+  back.up_scale = f.scale;
+  back.x = k;
+  back.w = q;
+  back.v = gout;
+  hipError_t e;
+  if (!f.sequences) {
+    if (!f.g_token) hipLaunchKernelGGL(memory_decay_sum_kernel, dim3((f.heads + 63) / 64), dim3(64), 0, st, nullptr, 0, f.heads, b.glog_decay);
+    return hipGetLastError();
+  }
+  if (segmented) {
+    base.added = place(plan.added);
+    base.faded = place(plan.faded);
+    if ((e = run_starts(base, bf16, st)) != hipSuccess) return e;
+    base.starts = base.added;
+    back.added = place(plan.added_r);
+    back.faded = place(plan.faded_r);
+    if ((e = run_starts(back, bf16, st)) != hipSuccess) return e;
+    back.starts = back.added;
+  }
+  const auto result = [&](MemArgs& p, void* out, uint64_t parts, int heads, int d) {
+    const bool shared = heads != f.heads;
+    p.out = shared ? ws + parts : out;
+    p.out_float = shared;
+    p.out_token = (int64_t)f.heads * d;
+    p.out_head = d;
+    p.out_vec = rows_of(p.out, p.out_token, d, 1, d, bf16 && !shared).vec;
+  };
+  MemArgs dv = back;
+  result(dv, b.gv, 0, f.heads, f.dv);
+  if ((e = run_chunks(dv, bf16, false, st)) != hipSuccess) return e;
+  MemArgs dk = back;
+  dk.x = v;
+  dk.w = gout;
+  dk.v = q;
+  dk.states.out = nullptr;
+  dk.s_row = 1;
+  dk.s_col = f.dv;
+  dk.dot = k;
+  dk.dots = place(plan.b);
+  result(dk, b.gk, plan.gk, f.heads_qk, f.dk);
+  if ((e = run_chunks(dk, bf16, false, st)) != hipSuccess) return e;
+  MemArgs dq = base;
+  dq.x = gout;
+  dq.w = v;
+  dq.v = k;
+  dq.s_row = 1;
+  dq.s_col = f.dv;
+  dq.dot = q;
+  dq.dots = place(plan.a);
+  result(dq, b.gq, plan.gq, f.heads_qk, f.dk);
+  if ((e = run_chunks(dq, bf16, false, st)) != hipSuccess) return e;
+  if (group > 1) {
+    const dim3 grid((uint32_t)(plan.chunks.entries * f.heads_qk));
+    for (int i = 0; i < 2; ++i) {
+      const float* parts = place(i ? plan.gk : plan.gq);
+      void* out = i ? b.gk : b.gq;
+      if (bf16) hipLaunchKernelGGL((memory_heads_kernel<unsigned short>), grid, dim3(256), 0, st, plan.chunks, parts, static_cast<unsigned short*>(out), f.heads_qk, group, f.dk);
+      else hipLaunchKernelGGL((memory_heads_kernel<float>), grid, dim3(256), 0, st, plan.chunks, parts, static_cast<float*>(out), f.heads_qk, group, f.dk);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  MemDecayArgs d = {};
+  d.m = plan.chunks;
+  d.q = q;
+  d.k = k;
+  d.v = v;
+  d.gout = gout;
+  d.heads = f.heads;
+  d.dk = f.dk;
+  d.dv = f.dv;
+  d.slices = plan.slices;
+  d.scale = f.scale;
+  d.log_decay = f.log_decay;
+  d.g_token = f.g_token;
+  d.g_head = f.g_head;
+  d.pairs = place(plan.pairs);
+  d.a = place(plan.a);
+  d.b = place(plan.b);
+  d.begin = begin;
+  d.gstate = gstate;
+  d.out = f.g_token ? b.glog_decay : nullptr;
+  d.sums = f.g_token ? nullptr : reinterpret_cast<double*>(ws + plan.sums);
+  d.found = base.starts;
+  d.found_r = back.starts;
+  const dim3 grid((uint32_t)(plan.chunks.entries * f.heads));
+  if (bf16) hipLaunchKernelGGL((memory_pairs_kernel<unsigned short>), grid, dim3(256), 0, st, d);
+  else hipLaunchKernelGGL((memory_pairs_kernel<float>), grid, dim3(256), 0, st, d);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  d.m = plan.m;
+  hipLaunchKernelGGL(memory_decay_kernel, dim3((uint32_t)(plan.m.entries * f.heads)), dim3(MEM_SUM_THREADS), 0, st, d);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (!f.g_token) hipLaunchKernelGGL(memory_decay_sum_kernel, dim3((f.heads + 63) / 64), dim3(64), 0, st, d.sums, plan.m.entries, f.heads, b.glog_decay);
+  return hipGetLastError();
+}
+
+}  // namespace ttc

@@ -1,0 +1,104 @@
+// residual_norm_kernel, residual_norm_backward_kernel, norm_parts_kernel (ttc_residual_norm, ttc_residual_norm_backward).
+#include "ttc_memory_launch.hpp"
+#include "ttc_norm.hpp"
+
+namespace ttc {
+
+static bool row16(const void* p, int64_t stride, int32_t dtype) {
+  const int64_t bytes = dtype == TTC_BF16 ? 2 : 4;
+  return (uint64_t)p % 16 == 0 && stride * bytes % 16 == 0;
+}
+
+// The fewest threads that hold a row in eights, two at most
+template <typename F>
+static void norm_shape(int features, F&& f) {
+  if (features <= 512) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
+  else if (features <= 1024) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
+  else if (features <= 2048) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
+  else if (features <= 4096) f(std::integral_constant<int, 512>{}, std::integral_constant<int, 1>{});
+  else if (features <= 8192) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 1>{});
+  else f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
+}
+
+hipError_t launch_residual_norm(const ttc_residual_norm_t& n, hipStream_t st) {
+  NormArgs a = {};
+  a.n = n;
+  a.group = n.features / n.groups;
+  a.vec = row16(n.y, n.y_token, n.dtype) << ROW_Y | row16(n.gate, n.gate_token, n.dtype) << ROW_GATE |
+          row16(n.residual, n.residual_token, n.dtype) << ROW_RESIDUAL | row16(n.r, n.r_token, n.dtype) << ROW_R | row16(n.h, n.h_token, n.dtype) << ROW_H;
+  norm_shape(n.features, [&](auto lanes, auto pieces) {
+    typedef NormShape<decltype(lanes)::value, decltype(pieces)::value> S;
+    const dim3 grid((uint32_t)((n.tokens + S::ROWS - 1) / S::ROWS));
+    if (n.dtype == TTC_BF16) hipLaunchKernelGGL((residual_norm_kernel<unsigned short, lanes(), pieces()>), grid, dim3(S::THREADS), 0, st, a);
+    else hipLaunchKernelGGL((residual_norm_kernel<float, lanes(), pieces()>), grid, dim3(S::THREADS), 0, st, a);
+  });
+  return hipGetLastError();
+}
+
+// Workgroups of the backward pass, and the rows of each of its parts
+static void norm_grid(const ttc_residual_norm_t& n, int cus, int& grid, int& parts) {
+  norm_shape(n.features, [&](auto lanes, auto pieces) {
+    typedef NormShape<decltype(lanes)::value, decltype(pieces)::value> S;
+    const int64_t rows = (n.tokens + S::ROWS - 1) / S::ROWS, most = (int64_t)cus * (1024 / S::THREADS);
+    grid = (int)(rows < most ? rows : most);
+    parts = grid * S::ROWS;
+  });
+}
+
+static void norm_wanted(const ttc_residual_norm_backward_t& b, float* (&out)[5]) {
+  out[0] = b.gpost_gain;
+  out[1] = b.gpost_offset;
+  out[2] = b.gresidual_gain;
+  out[3] = b.gpre_gain;
+  out[4] = b.gpre_offset;
+}
+
+uint64_t norm_backward_workspace(const ttc_residual_norm_backward_t& b, int cus) {
+  int grid, parts, vectors = 0;
+  norm_grid(b.forward, cus, grid, parts);
+  float* out[5];
+  norm_wanted(b, out);
+  for (float* v : out) vectors += v != nullptr;
+  return (uint64_t)vectors * parts * b.forward.features * 4;
+}
+
+hipError_t launch_residual_norm_backward(const ttc_residual_norm_backward_t& b, int cus, void* workspace, hipStream_t st) {
+  const ttc_residual_norm_t& n = b.forward;
+  NormArgs a = {};
+  a.n = n;
+  a.group = n.features / n.groups;
+  a.gr = b.gr; a.gh = b.gh; a.gr_token = b.gr_token; a.gh_token = b.gh_token;
+  a.gy = b.gy; a.ggate = b.ggate; a.gresidual = b.gresidual;
+  const auto rows = [&](const void* in, int64_t stride, const void* result) {  // one bit for what is read and its gradient
+    return row16(in, stride, n.dtype) && row16(result, n.features, n.dtype);
+  };
+  a.vec = rows(n.y, n.y_token, b.gy) << ROW_Y | rows(n.gate, n.gate_token, b.ggate) << ROW_GATE |
+          rows(n.residual, n.residual_token, b.gresidual) << ROW_RESIDUAL | row16(b.gr, b.gr_token, n.dtype) << ROW_R | row16(b.gh, b.gh_token, n.dtype) << ROW_H;
+  int grid, parts;
+  norm_grid(n, cus, grid, parts);
+  NormParts sum = {};
+  float* out[5];
+  norm_wanted(b, out);
+  float* at = static_cast<float*>(workspace);
+  int vectors = 0;
+  for (int v = 0; v < 5; ++v)
+    if (out[v]) {
+      a.part[v] = at;
+      sum.part[vectors] = at;
+      sum.out[vectors++] = out[v];
+      at += (int64_t)parts * n.features;
+    }
+  a.parts = sum.parts = parts;
+  sum.features = n.features;
+  sum.chunks = (n.features + 63) / 64;
+  if (grid) norm_shape(n.features, [&](auto lanes, auto pieces) {
+    typedef NormShape<decltype(lanes)::value, decltype(pieces)::value> S;
+    if (n.dtype == TTC_BF16) hipLaunchKernelGGL((residual_norm_backward_kernel<unsigned short, lanes(), pieces()>), dim3(grid), dim3(S::THREADS), 0, st, a);
+    else hipLaunchKernelGGL((residual_norm_backward_kernel<float, lanes(), pieces()>), dim3(grid), dim3(S::THREADS), 0, st, a);
+  });
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (vectors) hipLaunchKernelGGL(norm_parts_kernel, dim3(vectors * sum.chunks), dim3(256), 0, st, sum);
+  return hipGetLastError();
+}
+
+}  // namespace ttc

@@ -1,4 +1,4 @@
-// Entry points of include/ttc_attention.h: argument checks and the launches.  The kernels live in k_rope.hip, k_kv.hip, k_attention.hip.
+// Entry points of include/ttc_attention.h: argument checks and the launches.  The kernels live in k_rope.hip, k_kv.hip, k_place.hip, k_attention.hip.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -10,11 +10,7 @@
 #include "../../include/ttc_attention.h"
 #include "ttc_serve_launch.hpp"
 
-namespace {
-
-bool aligned(const void* p, uint64_t n) { return (uint64_t)p % n == 0; }
-bool known_dtype(int32_t t) { return t == TTC_F32 || t == TTC_BF16; }
-uint64_t bytes_of(int32_t t) { return t == TTC_BF16 ? 2 : 4; }
+namespace ttc {
 
 // compute units of the current device, asked once per device
 int compute_units() {
@@ -37,6 +33,16 @@ int compute_units() {
   });
   return count[dev];
 }
+
+}  // namespace ttc
+
+namespace {
+
+using ttc::compute_units;
+
+bool aligned(const void* p, uint64_t n) { return (uint64_t)p % n == 0; }
+bool known_dtype(int32_t t) { return t == TTC_F32 || t == TTC_BF16; }
+uint64_t bytes_of(int32_t t) { return t == TTC_BF16 ? 2 : 4; }
 
 // 64 bits that what lies in a workspace has by chance only: a counter from a starting point of the process's own, mixed
 uint64_t next_mark() {
@@ -124,6 +130,21 @@ ttc_status_t ttc_kv_read(const ttc_kv_cache_t* c, const int64_t* slots, int64_t 
   if (!slots || !aligned(slots, 8) || !aligned(k_out, 16) || !aligned(v_out, 16)) return TTC_ERR_INVALID_ARG;
   if (n > (1 << 26) || c->heads > 65535) return TTC_ERR_UNSUPPORTED;  // (fewer than 2^32 threads along the tokens, 2^16 workgroups along the heads)
   return ttc::launch_kv_read(*c, slots, n, out_dtype == TTC_BF16, k_out, v_out, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? TTC_OK : TTC_ERR_DEVICE;
+}
+
+ttc_status_t ttc_kv_place(const ttc_kv_place_t* p, void* hip_stream) {
+  if (!p || p->sequences < 0 || p->tokens < 0 || p->pages < 0 || p->width < 0) return TTC_ERR_INVALID_ARG;
+  if (p->page < 1 || p->page > 65536 || p->sequences >= (1 << 30) || p->tokens >= (1 << 30) || p->pages > 0x7fffffffll) return TTC_ERR_UNSUPPORTED;
+  if (!p->cu_q || !aligned(p->cu_q, 4)) return TTC_ERR_INVALID_ARG;
+  if (p->sequences && (!p->past || !p->new_tokens || !p->kv_len || !aligned(p->past, 4) || !aligned(p->new_tokens, 4) || !aligned(p->kv_len, 4)))
+    return TTC_ERR_INVALID_ARG;
+  if (p->sequences && p->width && (!p->block_table || !aligned(p->block_table, 4) || p->table_stride < 0)) return TTC_ERR_INVALID_ARG;
+  if (p->sequences > 1 && p->table_stride < p->width && p->free_pages) return TTC_ERR_INVALID_ARG;  // rows of the table would share pages
+  if (p->tokens && (!p->positions || !p->slots || !aligned(p->positions, 8) || !aligned(p->slots, 8))) return TTC_ERR_INVALID_ARG;
+  if (!aligned(p->sequence, 4) || !aligned(p->missing, 4)) return TTC_ERR_INVALID_ARG;
+  if (p->free_pages && (!p->free_count || !p->free_count_out || p->free_capacity < 0 || p->free_capacity > 0x7fffffffll || !aligned(p->free_pages, 4) ||
+                        !aligned(p->free_count, 4) || !aligned(p->free_count_out, 4))) return TTC_ERR_INVALID_ARG;
+  return ttc::launch_kv_place(*p, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? TTC_OK : TTC_ERR_DEVICE;
 }
 
 size_t ttc_attention_workspace_bytes(const ttc_attention_t* a) {

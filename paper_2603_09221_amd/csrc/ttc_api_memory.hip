@@ -1,0 +1,133 @@
+// Entry points of include/ttc_memory.h: argument checks and the launches.  The kernels live in k_memory.hip, k_memory_host.hip, k_norm.hip.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "ttc_memory_launch.hpp"
+#include "ttc_serve_launch.hpp"
+
+namespace {
+
+bool aligned(const void* p, uint64_t n) { return (uint64_t)p % n == 0; }
+bool known_dtype(int32_t t) { return t == TTC_F32 || t == TTC_BF16; }
+uint64_t bytes_of(int32_t t) { return t == TTC_BF16 ? 2 : 4; }
+
+// Sizes and numbers, which the workspace depends on
+ttc_status_t check_sizes(const ttc_linear_attention_t& a) {
+  if (a.sequences < 0 || a.tokens < 0 || a.heads < 1 || a.heads_qk < 1 || a.heads % a.heads_qk || !known_dtype(a.dtype) || a.max_q < 0 || !isfinite(a.scale))
+    return TTC_ERR_INVALID_ARG;
+  if (!a.cu_q && a.tokens != a.sequences) return TTC_ERR_INVALID_ARG;
+  if (a.dk < 8 || a.dk > 256 || a.dk % 8 || a.dv < 8 || a.dv > 256 || a.dv % 8) return TTC_ERR_UNSUPPORTED;
+  // workgroups of a launch, and a workspace that can be counted: at most one for every head and 64 tokens, times four slices
+  if (a.tokens > 0x7fffffffll || a.sequences > 0x7fffffffll || ((double)a.tokens / 64 + a.sequences) * a.heads * 64 >= 2147483648.) return TTC_ERR_UNSUPPORTED;
+  return TTC_OK;
+}
+
+ttc_status_t check_pointers(const ttc_linear_attention_t& a) {
+  const uint64_t n = bytes_of(a.dtype);
+  if (a.tokens && (!a.q || !a.k || !a.v || !a.log_decay || !aligned(a.q, n) || !aligned(a.k, n) || !aligned(a.v, n) || !aligned(a.log_decay, 4)))
+    return TTC_ERR_INVALID_ARG;
+  if (!aligned(a.cu_q, 4) || !aligned(a.state_row, 4) || !aligned(a.kv_len, 4) || !aligned(a.state_in, 16) || !aligned(a.state_out, 16) || a.state_rows < 0)
+    return TTC_ERR_INVALID_ARG;
+  return TTC_OK;
+}
+
+ttc_status_t check_norm(const ttc_residual_norm_t& n) {
+  if (n.tokens < 0 || n.features < 1 || n.groups < 1 || n.features % n.groups || !known_dtype(n.dtype)) return TTC_ERR_INVALID_ARG;
+  for (int32_t kind : {n.post, n.pre})
+    if (kind != TTC_NORM_NONE && kind != TTC_NORM_RMS && kind != TTC_NORM_LAYER) return TTC_ERR_INVALID_ARG;
+  if (n.gate && n.act != TTC_GATE_IDENTITY && n.act != TTC_GATE_SIGMOID && n.act != TTC_GATE_SILU) return TTC_ERR_INVALID_ARG;
+  if (!(n.post_eps >= 0.f) || !(n.pre_eps >= 0.f) || !isfinite(n.post_eps) || !isfinite(n.pre_eps) || !isfinite(n.scale)) return TTC_ERR_INVALID_ARG;
+  if (n.features > 16384 || n.tokens > 0x7fffffffll || (n.groups > 1 && n.features / n.groups % 8)) return TTC_ERR_UNSUPPORTED;
+  const uint64_t b = bytes_of(n.dtype);
+  if (n.tokens && (!n.y || !aligned(n.y, b) || !aligned(n.gate, b) || !aligned(n.residual, b))) return TTC_ERR_INVALID_ARG;
+  for (const float* v : {n.post_gain, n.post_offset, n.residual_gain, n.pre_gain, n.pre_offset})
+    if (!aligned(v, 4)) return TTC_ERR_INVALID_ARG;
+  return TTC_OK;
+}
+
+bool rows_apart(int64_t stride, const ttc_residual_norm_t& n) { return n.tokens < 2 || stride >= n.features || -stride >= n.features; }
+
+ttc_status_t check_norm_backward(const ttc_residual_norm_backward_t* b) {
+  if (!b) return TTC_ERR_INVALID_ARG;
+  const ttc_residual_norm_t& n = b->forward;
+  if (const ttc_status_t s = check_norm(n); s != TTC_OK) return s;
+  const uint64_t e = bytes_of(n.dtype);
+  if (!aligned(b->gr, e) || !aligned(b->gh, e) || !aligned(b->gy, e) || !aligned(b->ggate, e) || !aligned(b->gresidual, e)) return TTC_ERR_INVALID_ARG;
+  if (n.tokens && (b->gh != nullptr) != (n.pre != TTC_NORM_NONE)) return TTC_ERR_INVALID_ARG;
+  if ((b->ggate && !n.gate) || (b->gresidual && !n.residual)) return TTC_ERR_INVALID_ARG;
+  const float* given[5] = {n.post ? n.post_gain : nullptr, n.post ? n.post_offset : nullptr, n.residual_gain, n.pre ? n.pre_gain : nullptr,
+                           n.pre ? n.pre_offset : nullptr};
+  const float* wanted[5] = {b->gpost_gain, b->gpost_offset, b->gresidual_gain, b->gpre_gain, b->gpre_offset};
+  for (int i = 0; i < 5; ++i)
+    if (wanted[i] && (!aligned(wanted[i], 4) || (n.tokens && !given[i]))) return TTC_ERR_INVALID_ARG;
+  return TTC_OK;
+}
+
+ttc_status_t check_backward(const ttc_linear_attention_backward_t* b) {
+  if (!b) return TTC_ERR_INVALID_ARG;
+  if (const ttc_status_t s = check_sizes(b->forward); s != TTC_OK) return s;
+  return check_pointers(b->forward);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ttc_linear_attention_workspace_bytes(const ttc_linear_attention_t* a) {
+  return a && check_sizes(*a) == TTC_OK ? ttc::linear_attention_workspace(*a, ttc::compute_units()) : 0;
+}
+
+ttc_status_t ttc_linear_attention(const ttc_linear_attention_t* a, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!a) return TTC_ERR_INVALID_ARG;
+  if (const ttc_status_t s = check_sizes(*a); s != TTC_OK) return s;
+  if (const ttc_status_t s = check_pointers(*a); s != TTC_OK) return s;
+  if (a->tokens && (!a->out || !aligned(a->out, bytes_of(a->dtype)) || a->out == a->q || a->out == a->k || a->out == a->v)) return TTC_ERR_INVALID_ARG;
+  if (!a->sequences || (!a->state_out && (!a->tokens || !a->max_q))) return TTC_OK;
+  const uint64_t need = ttc::linear_attention_workspace(*a, ttc::compute_units());
+  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return TTC_ERR_WORKSPACE;
+  return ttc::launch_linear_attention(*a, ttc::compute_units(), workspace, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? TTC_OK : TTC_ERR_DEVICE;
+}
+
+size_t ttc_linear_attention_backward_workspace_bytes(const ttc_linear_attention_backward_t* b) {
+  return check_backward(b) == TTC_OK ? ttc::linear_attention_backward_workspace(*b, ttc::compute_units()) : 0;
+}
+
+ttc_status_t ttc_linear_attention_backward(const ttc_linear_attention_backward_t* b, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (const ttc_status_t s = check_backward(b); s != TTC_OK) return s;
+  const ttc_linear_attention_t& f = b->forward;
+  const uint64_t n = bytes_of(f.dtype);
+  if (f.tokens && (!b->gout || !b->gq || !b->gk || !b->gv || !aligned(b->gout, n) || !aligned(b->gq, n) || !aligned(b->gk, n) || !aligned(b->gv, n)))
+    return TTC_ERR_INVALID_ARG;
+  if (((f.tokens || !f.g_token) && !b->glog_decay) || !aligned(b->glog_decay, 4) || !aligned(b->gstate_out, 16) || !aligned(b->gstate, 16)) return TTC_ERR_INVALID_ARG;
+  const uint64_t need = ttc::linear_attention_backward_workspace(*b, ttc::compute_units());
+  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return TTC_ERR_WORKSPACE;
+  return ttc::launch_linear_attention_backward(*b, ttc::compute_units(), workspace, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? TTC_OK : TTC_ERR_DEVICE;
+}
+
+ttc_status_t ttc_residual_norm(const ttc_residual_norm_t* n, void* hip_stream) {
+  if (!n) return TTC_ERR_INVALID_ARG;
+  if (const ttc_status_t s = check_norm(*n); s != TTC_OK) return s;
+  if (!n->tokens) return TTC_OK;
+  const uint64_t b = bytes_of(n->dtype);
+  if (!aligned(n->r, b) || !aligned(n->h, b) || (n->h != nullptr) != (n->pre != TTC_NORM_NONE) || (!n->r && !n->h) || n->r == n->h) return TTC_ERR_INVALID_ARG;
+  if ((n->r && !rows_apart(n->r_token, *n)) || (n->h && !rows_apart(n->h_token, *n))) return TTC_ERR_INVALID_ARG;
+  const void* in[3] = {n->y, n->gate, n->residual};
+  const int64_t stride[3] = {n->y_token, n->gate_token, n->residual_token};
+  for (int i = 0; i < 3; ++i)
+    if (in[i] && ((in[i] == n->r && stride[i] != n->r_token) || (in[i] == n->h && stride[i] != n->h_token))) return TTC_ERR_INVALID_ARG;
+  return ttc::launch_residual_norm(*n, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? TTC_OK : TTC_ERR_DEVICE;
+}
+
+size_t ttc_residual_norm_backward_workspace_bytes(const ttc_residual_norm_backward_t* b) {
+  return check_norm_backward(b) == TTC_OK ? ttc::norm_backward_workspace(*b, ttc::compute_units()) : 0;
+}
+
+ttc_status_t ttc_residual_norm_backward(const ttc_residual_norm_backward_t* b, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (const ttc_status_t s = check_norm_backward(b); s != TTC_OK) return s;
+  const uint64_t need = ttc::norm_backward_workspace(*b, ttc::compute_units());
+  if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return TTC_ERR_WORKSPACE;
+  return ttc::launch_residual_norm_backward(*b, ttc::compute_units(), workspace, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? TTC_OK : TTC_ERR_DEVICE;
+}
+
+}  // extern "C"

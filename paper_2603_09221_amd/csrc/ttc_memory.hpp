@@ -1,0 +1,614 @@
+// Linear attention with a decay of each head (ttc_linear_attention, ttc_linear_attention_backward).
+//
+// With G_t = g_1 + .. + g_t within a chunk of 64 tokens and S the state that the chunk finds,
+//     out_i = in_i (x_i S) + sum_{j <= i} exp(G_i - G_j) (x_i . w_j) v_j,     in_i = exp(G_i),
+//     S    <- exp(G_64) S + sum_j w_j (up_j v_j)^T,                           up_j = exp(G_64 - G_j),
+// for queries x, keys w, values v: three products of matrices.  The gradients are the same sums with other rows in these places,
+//     dq: x = dout, w = v, v = k, S transposed;    dk: x = v, w = dout, v = q;    dv: x = k, w = q, v = dout,
+// the last two from the last token to the first (j >= i, in_i = exp(G_64 - G_i), up_j = exp(G_j)) over the state's gradient R.  So one kernel
+// does all four.
+#pragma once
+#include "../../include/ttc_memory.h"
+#include "ttc_serve.hpp"
+
+namespace ttc {
+
+constexpr int MEM_CHUNK = 64;      // tokens of a chunk: a lane each where decays are added up
+constexpr int MEM_WAVES = 4;
+
+// ---- sequences and their segments ---------------------------------------------------------------------------------------------
+
+struct MemSequences {
+  int64_t sequences, tokens;
+  const int32_t* cu_q;
+  int32_t max_q;
+  int32_t segment;     // chunks of a segment
+  int64_t entries;     // segments of all sequences at most; every sequence has one
+};
+
+__device__ __forceinline__ void mem_rows(const MemSequences& m, int64_t s, int64_t& first, int& n) {
+  if (!m.cu_q) {
+    first = s;
+    n = s < m.tokens ? min(1, m.max_q) : 0;
+    return;
+  }
+  first = min((int64_t)max(m.cu_q[s], 0), m.tokens);
+  const int64_t end = min((int64_t)m.cu_q[s + 1], m.tokens);
+  n = (int)max(min(end - first, (int64_t)m.max_q), (int64_t)0);
+}
+__device__ __forceinline__ int mem_segments(const MemSequences& m, int64_t s) {
+  int64_t first;
+  int n;
+  mem_rows(m, s, first, n);
+  const int each = m.segment * MEM_CHUNK;
+  return n > each ? (int)(((int64_t)n + each - 1) / each) : 1;
+}
+
+// Segment number `at` of all: its sequence, and which of that one's segments it is; false if there are fewer.  Each wavefront adds up the
+// sequences for itself, a run of them to a lane.
+__device__ __forceinline__ bool mem_segment(const MemSequences& m, int64_t at, int64_t& seq, int& segment) {
+  if (m.entries == m.sequences) {
+    seq = at;
+    segment = 0;
+    return at < m.sequences;
+  }
+  const int lane = threadIdx.x & 63;
+  const int64_t run = (m.sequences + 63) / 64, first = min(lane * run, m.sequences), last = min(first + run, m.sequences);
+  uint32_t own = 0;
+  for (int64_t s = first; s < last; ++s) own += mem_segments(m, s);
+  uint32_t sum = own;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t x = __shfl_up(sum, o, 64);
+    sum += lane >= o ? x : 0;
+  }
+  if (at >= __builtin_amdgcn_readlane(sum, 63)) return false;
+  const int who = __builtin_ctzll(__builtin_amdgcn_ballot_w64(at < sum));
+  uint32_t before = __builtin_amdgcn_readlane(sum - own, who);
+  int64_t s = who * run;
+  for (;; ++s) {
+    const uint32_t n = __builtin_amdgcn_readfirstlane(mem_segments(m, s));
+    if (at < before + n) break;
+    before += n;
+  }
+  seq = s;
+  segment = (int)(at - before);
+  return true;
+}
+
+// ---- states ---------------------------------------------------------------------------------------------------------------
+
+struct MemStates {
+  const float* in;
+  float* out;
+  int64_t rows;
+  const int32_t* row;
+  const int32_t* kv_len;
+};
+
+// Row of sequence s that it goes on from; -1: it begins with zeros
+__device__ __forceinline__ int64_t mem_begin(const MemStates& t, int64_t s, int n) {
+  if (!t.in || (t.kv_len && t.kv_len[s] <= n)) return -1;
+  const int64_t r = t.row ? t.row[s] : s;
+  return r >= 0 && r < t.rows ? r : -1;
+}
+__device__ __forceinline__ int64_t mem_end(const MemStates& t, int64_t s) {
+  if (!t.out) return -1;
+  const int64_t r = t.row ? t.row[s] : s;
+  return r >= 0 && r < t.rows ? r : -1;
+}
+
+__device__ __forceinline__ float mem_decay(float g) { return g < -200.f ? -200.f : g; }  // (exp(-200) is 0 in float32; NaN stays)
+
+// ---- operands ---------------------------------------------------------------------------------------------------------------
+// A lane's share of an operand of 16 x 32 numbers: eight of row (or column) lane % 16.  float32 takes eight instructions of depth 4, whose
+// k-th numbers are the lanes' k-th; which numbers of the sum these are does not matter as long as both operands agree.
+
+template <typename T> struct MemOperand;
+template <> struct MemOperand<unsigned short> { typedef srv_bf16x8 type; };
+struct mem_float8 { float x[8]; };
+template <> struct MemOperand<float> { typedef mem_float8 type; };
+
+__device__ __forceinline__ srv_floatx4 mem_mma(const srv_bf16x8& a, const srv_bf16x8& b, srv_floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ srv_floatx4 mem_mma(const mem_float8& a, const mem_float8& b, srv_floatx4 c) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.x[i], b.x[i], c, 0, 0, 0);
+  return c;
+}
+
+// numbers side by side at p and at q, four each
+__device__ __forceinline__ srv_bf16x8 mem_operand(const unsigned short* p, const unsigned short* q) {
+  const srv_uintx2 a = *reinterpret_cast<const srv_uintx2*>(p), b = *reinterpret_cast<const srv_uintx2*>(q);
+  return __builtin_bit_cast(srv_bf16x8, srv_uintx4{a[0], a[1], b[0], b[1]});
+}
+__device__ __forceinline__ mem_float8 mem_operand(const float* p, const float* q) {
+  const srv_floatx4 a = *reinterpret_cast<const srv_floatx4*>(p), b = *reinterpret_cast<const srv_floatx4*>(q);
+  return {{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
+}
+// numbers `step` apart
+__device__ __forceinline__ srv_bf16x8 mem_column(const unsigned short* p, int step) {
+  srv_u16x8 x;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = p[i * step];
+  return __builtin_bit_cast(srv_bf16x8, x);
+}
+__device__ __forceinline__ mem_float8 mem_column(const float* p, int step) {
+  mem_float8 x;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x.x[i] = p[i * step];
+  return x;
+}
+__device__ __forceinline__ float mem_entry(const srv_bf16x8& v, int i) { return (float)v[i]; }
+__device__ __forceinline__ float mem_entry(const mem_float8& v, int i) { return v.x[i]; }
+
+// Eight float32 numbers as a sum of PARTS operands, the largest part first.  bfloat16 parts are cut off, not rounded, so that three hold all
+// 24 bits (two hold 16) and none passes the largest number.  (An infinity leaves NaN in the second.)
+template <int PARTS>
+__device__ __forceinline__ void mem_split(const float (&x)[8], srv_bf16x8 (&part)[PARTS]) {
+  float rest[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) rest[i] = x[i];
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k) {
+    srv_uintx4 p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t lo = __float_as_uint(rest[2 * i]), hi = __float_as_uint(rest[2 * i + 1]);
+      p[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302);
+      if (k + 1 < PARTS) {
+        rest[2 * i] -= __uint_as_float(lo & 0xffff0000u);
+        rest[2 * i + 1] -= __uint_as_float(hi & 0xffff0000u);
+      }
+    }
+    part[k] = __builtin_bit_cast(srv_bf16x8, p);
+  }
+}
+template <int PARTS>
+__device__ __forceinline__ void mem_split(const float (&x)[8], mem_float8 (&part)[PARTS]) {
+  static_assert(PARTS == 1);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) part[0].x[i] = x[i];
+}
+
+__device__ __forceinline__ void mem_store4(unsigned short* p, const float (&x)[4]) {
+  typedef unsigned short u16x4 __attribute__((ext_vector_type(4)));
+  *reinterpret_cast<u16x4*>(p) = u16x4{srv_narrow<unsigned short>(x[0]), srv_narrow<unsigned short>(x[1]), srv_narrow<unsigned short>(x[2]),
+                                       srv_narrow<unsigned short>(x[3])};
+}
+__device__ __forceinline__ void mem_store4(float* p, const float (&x)[4]) { *reinterpret_cast<srv_floatx4*>(p) = srv_floatx4{x[0], x[1], x[2], x[3]}; }
+__device__ __forceinline__ void mem_store8(unsigned short* p, const float (&x)[8]) { srv_st8(p, true, x); }
+__device__ __forceinline__ void mem_store8(float* p, const float (&x)[8]) { srv_st8(p, true, x); }
+
+// ---- the kernel of chunks ---------------------------------------------------------------------------------------------------
+
+struct MemRows {
+  const void* p;
+  int64_t token, head;
+  int32_t group;       // heads that share a row
+  int32_t d;           // entries
+  int32_t vec;         // 16-byte alignment
+};
+
+struct MemArgs {
+  MemSequences m;
+  MemRows x, w, v;
+  void* out;
+  int64_t out_token, out_head;
+  int32_t out_vec, out_float;   // alignment; float32 whatever the rows' type
+  int32_t heads, slices;
+  int32_t reverse;
+  float pair_scale, in_scale, up_scale;
+  const float* log_decay;
+  int64_t g_token, g_head;
+  MemStates states;             // of the sequences
+  MemStates rule;               // whose beginning says where the last state is 0 (gstate); in NULL: no rule
+  int32_t ruled;
+  const float* starts;          // of the segments: (entries, heads, dk, dv), or NULL: a sequence is one segment
+  float* added;                 // likewise, what a segment adds to a state that it finds as zeros (mem_state_kernel)
+  float* faded;                 // (entries, heads): and the factor on what it finds
+  int32_t s_row, s_col;         // of a state's numbers, in elements
+  int32_t dk, dv;               // rows and columns of a state as it is stored
+  MemRows dot;                  // rows whose product with what a token reads of the state is wanted (p NULL: not)
+  float* dots;                  // (slices, heads, tokens)
+};
+
+// Decays of a chunk: wavefront 0, a token to a lane, in float64, so that the differences of sums are as exact as the decays themselves.
+struct MemDecays {
+  float hi[MEM_CHUNK], lo[MEM_CHUNK];   // G as a sum of two
+  float in[MEM_CHUNK], up[MEM_CHUNK];
+  float whole;
+};
+
+__device__ __forceinline__ double mem_decay_sums(double g, int lane) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double y = __shfl_up(g, o, 64);
+    g += lane >= o ? y : 0.0;
+  }
+  return g;
+}
+
+__device__ __forceinline__ float mem_between(const MemDecays& d, int late, int early) {
+  return expf((d.hi[late] - d.hi[early]) + (d.lo[late] - d.lo[early]));
+}
+
+template <typename T, int DK, int NT>
+struct MemShape {
+  static constexpr int PAD = 16 / sizeof(T);
+  static constexpr int XS = DK + PAD, VS = 64 * NT + PAD, PS = MEM_CHUNK + PAD;  // rows in LDS
+  static constexpr int COLS = 16 * NT * MEM_WAVES;
+  static constexpr int X = MEM_CHUNK * (XS > PS ? XS : PS);  // the pairs' products take the place of x
+};
+
+// 64 rows, zeros behind the last and behind the last entry
+template <typename T, int D, int STEP>
+__device__ __forceinline__ void mem_fill(T* lds, const MemRows& r, const T* base, int64_t first, int n, int entry, int entries) {
+  constexpr int PIECES = D / 8;
+  for (int i = threadIdx.x; i < MEM_CHUNK * PIECES; i += 64 * MEM_WAVES) {
+    const int t = i / PIECES, e = i % PIECES * 8;
+    float x[8] = {};
+    if (t < n && entry + e < entries) srv_ld8(base + (first + t) * r.token + entry + e, r.vec, x);
+    mem_store8(lds + t * STEP + e, x);
+  }
+}
+
+// A workgroup takes one segment of one head of one sequence, and of the values' columns a slice of 64 * NT; a wavefront owns 16 * NT of them and
+// their state, DK numbers each, which stays in its registers from chunk to chunk: what a lane holds of it as a result is what it has to hold of it as an
+// operand if the sum's order follows.  STATES: only what the segment adds to its state.
+template <typename T, int DK, int NT, bool STATES>
+__global__ void __launch_bounds__(64 * MEM_WAVES) memory_chunk_kernel(const MemArgs a) {
+  typedef MemShape<T, DK, NT> S;
+  typedef typename MemOperand<T>::type op_t;
+  constexpr bool BF16 = sizeof(T) == 2;
+  constexpr int IN = BF16 ? 3 : 1, UP = BF16 ? 3 : 1, KT = DK / 16;
+  __shared__ alignas(16) T xl[STATES ? 8 : S::X], wl[MEM_CHUNK * S::XS], vl[MEM_CHUNK * S::VS];
+  __shared__ MemDecays dl;
+  __shared__ float meet[MEM_WAVES][MEM_CHUNK];
+  T* const pl = xl;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+  const int slice = blockIdx.x % a.slices, head = blockIdx.x / a.slices % a.heads;
+  const int64_t entry = blockIdx.x / a.slices / a.heads;
+  int64_t seq, first;
+  int segment, n;
+  if (!mem_segment(a.m, entry, seq, segment)) return;
+  mem_rows(a.m, seq, first, n);
+  const int segments = mem_segments(a.m, seq), chunks = (n + MEM_CHUNK - 1) / MEM_CHUNK;
+  const int c0 = segment * a.m.segment, c1 = min(c0 + a.m.segment, chunks);
+  if (STATES && segment == (a.reverse ? 0 : segments - 1)) return;  // nobody finds what this one leaves
+  const int col0 = slice * S::COLS + wave * 16 * NT, cols = a.v.d;
+
+  srv_floatx4 s[KT][NT] = {};
+  double grown = 0.0;
+  if (!STATES) {
+    const int64_t row = mem_begin(a.states, seq, n);
+    const float* from = a.starts ? a.starts + (entry * a.heads + head) * a.dk * a.dv : row >= 0 ? a.states.in + (row * a.heads + head) * a.dk * a.dv : nullptr;
+    if (from)
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int k = 0; k < KT; ++k)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int i = 16 * k + 4 * g + r, j = col0 + 16 * t + c;
+            if (i < a.x.d && j < cols) s[k][t][r] = from[(int64_t)i * a.s_row + (int64_t)j * a.s_col];
+          }
+  }
+  const T* xp = static_cast<const T*>(a.x.p) + (STATES ? 0 : head / a.x.group * a.x.head);
+  const T* wp = static_cast<const T*>(a.w.p) + head / a.w.group * a.w.head;
+  const T* vp = static_cast<const T*>(a.v.p) + head / a.v.group * a.v.head;
+
+  for (int turn = c0; turn < c1; ++turn) {
+    const int chunk = a.reverse ? c1 - 1 - (turn - c0) : turn, at = chunk * MEM_CHUNK, rows = min(MEM_CHUNK, n - at);
+    const int64_t t0 = first + at;
+    __syncthreads();
+    if (!STATES) mem_fill<T, DK, S::XS>(xl, a.x, xp, t0, rows, 0, a.x.d);
+    mem_fill<T, DK, S::XS>(wl, a.w, wp, t0, rows, 0, a.w.d);
+    mem_fill<T, 64 * NT, S::VS>(vl, a.v, vp, t0, rows, slice * S::COLS, cols);
+    if (wave == 0) {
+      double sum = lane < rows ? mem_decay(a.log_decay[(t0 + lane) * a.g_token + head * a.g_head]) : 0.f;
+      sum = mem_decay_sums(sum, lane);
+      const double whole = __shfl(sum, 63, 64);
+      const float hi = (float)sum;
+      dl.hi[lane] = hi;
+      dl.lo[lane] = (float)(sum - hi);
+      const float since = expf((float)sum), left = expf((float)(whole - sum));
+      dl.in[lane] = a.in_scale * (a.reverse ? left : since);
+      dl.up[lane] = a.up_scale * (a.reverse ? since : left);
+      if (lane == 0) dl.whole = expf((float)whole);
+      grown += whole;
+    }
+    __syncthreads();
+
+    srv_floatx4 o[4][NT] = {};
+    if constexpr (!STATES) {
+      // what the tokens read of the state
+#pragma unroll
+      for (int k = 0; k < KT; k += 2) {
+        op_t part[NT][IN];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const float x[8] = {s[k][t][0], s[k][t][1], s[k][t][2], s[k][t][3], s[k + 1][t][0], s[k + 1][t][1], s[k + 1][t][2], s[k + 1][t][3]};
+          mem_split<IN>(x, part[t]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const T* row = xl + (16 * i + c) * S::XS + 16 * k + 4 * g;
+          const op_t x = mem_operand(row, row + 16);
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int p = IN - 1; p >= 0; --p) o[i][t] = mem_mma(part[t][p], x, o[i][t]);
+        }
+      }
+      // pairs: wavefront w has the products of rows 16 w .. with all
+      srv_floatx4 z[4] = {};
+#pragma unroll
+      for (int k = 0; k < DK / 32; ++k) {
+        const T* row = xl + (16 * wave + c) * S::XS + 32 * k + 8 * g;
+        const op_t x = mem_operand(row, row + 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const T* key = wl + (16 * j + c) * S::XS + 32 * k + 8 * g;
+          z[j] = mem_mma(mem_operand(key, key + 4), x, z[j]);
+        }
+      }
+      __syncthreads();  // x has been read
+      const int i = 16 * wave + c;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float p[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int e = 16 * j + 4 * g + r;
+          const bool seen = a.reverse ? e >= i : e <= i;
+          p[r] = seen ? a.pair_scale * z[j][r] * (a.reverse ? mem_between(dl, e, i) : mem_between(dl, i, e)) : 0.f;
+        }
+        mem_store4(pl + i * S::PS + 16 * j + 4 * g, p);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) o[i][t] *= dl.in[16 * i + c];
+      if (a.dot.p) {
+        const T* dot = static_cast<const T*>(a.dot.p) + head / a.dot.group * a.dot.head;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float sum = 0.f;
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const int e = col0 + 16 * t + 4 * g;
+            if (16 * i + c < rows && e < cols)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) sum += o[i][t][r] * srv_widen(dot[(t0 + 16 * i + c) * a.dot.token + e + r]);
+          }
+          sum += __shfl_xor(sum, 16, 64);
+          sum += __shfl_xor(sum, 32, 64);
+          if (g == 0) meet[wave][16 * i + c] = sum;
+        }
+      }
+      __syncthreads();
+      if (a.dot.p && wave == 0 && lane < rows)
+        a.dots[((int64_t)slice * a.heads + head) * a.m.tokens + t0 + lane] = (meet[0][lane] + meet[1][lane]) + (meet[2][lane] + meet[3][lane]);
+    }
+    // the values, tokens side by side in a lane
+    op_t v[2][NT];
+    bool bad = false;
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        v[k][t] = mem_column(vl + (32 * k + 8 * g) * S::VS + wave * 16 * NT + 16 * t + c, S::VS);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) bad |= !isfinite(mem_entry(v[k][t], e));
+      }
+    const bool any_bad = __builtin_amdgcn_ballot_w64(bad) != 0;
+    if constexpr (!STATES) {
+      op_t clean[2][NT];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          clean[k][t] = v[k][t];
+          if (any_bad) {  // a weight of 0 times NaN would be NaN
+            float x[8];
+            op_t y[1];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = isfinite(mem_entry(v[k][t], e)) ? mem_entry(v[k][t], e) : 0.f;
+            mem_split<1>(x, y);
+            clean[k][t] = y[0];
+          }
+        }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const T* row = pl + (16 * i + c) * S::PS + 32 * k + 8 * g;
+          const op_t p = mem_operand(row, row + 4);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) o[i][t] = mem_mma(clean[k][t], p, o[i][t]);
+        }
+      if (any_bad)
+        for (int j = 0; j < rows; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const float y = srv_widen(vl[j * S::VS + wave * 16 * NT + 16 * t + 4 * g + r]);
+                const bool seen = a.reverse ? j >= 16 * i + c : j <= 16 * i + c;
+                if (seen && !isfinite(y)) o[i][t][r] += srv_widen(pl[(16 * i + c) * S::PS + j]) * y;
+              }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const int e = col0 + 16 * t + 4 * g;
+          if (16 * i + c >= rows || e >= cols) continue;
+          const int64_t to = (t0 + 16 * i + c) * a.out_token + head * a.out_head + e;
+          const float y[4] = {o[i][t][0], o[i][t][1], o[i][t][2], o[i][t][3]};
+          if (a.out_float) srv_st<float, 4>(static_cast<float*>(a.out) + to, a.out_vec, y);
+          else srv_st<T, 4>(static_cast<T*>(a.out) + to, a.out_vec, y);
+        }
+    }
+    // the state
+    const float whole = dl.whole;
+#pragma unroll
+    for (int k = 0; k < KT; ++k)
+#pragma unroll
+      for (int t = 0; t < NT; ++t) s[k][t] *= whole;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      op_t part[NT][UP];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = mem_entry(v[h][t], e) * dl.up[32 * h + 8 * g + e];
+        mem_split<UP>(x, part[t]);
+      }
+#pragma unroll
+      for (int k = 0; k < KT; ++k) {
+        const op_t w = mem_column(wl + (32 * h + 8 * g) * S::XS + 16 * k + c, S::XS);
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int p = UP - 1; p >= 0; --p) s[k][t] = mem_mma(w, part[t][p], s[k][t]);
+      }
+    }
+  }
+  float* to = nullptr;
+  bool none = false;
+  if (STATES) {
+    to = a.added + (entry * a.heads + head) * a.dk * a.dv;
+    if (threadIdx.x == 0 && slice == 0) a.faded[entry * a.heads + head] = expf((float)grown);
+  } else if (segment == (a.reverse ? 0 : segments - 1)) {
+    const int64_t row = mem_end(a.states, seq);
+    if (row >= 0) to = a.states.out + (row * a.heads + head) * a.dk * a.dv;
+    none = a.ruled && mem_begin(a.rule, seq, n) < 0;
+  }
+  if (to)
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int k = 0; k < KT; ++k)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int i = 16 * k + 4 * g + r, j = col0 + 16 * t + c;
+          if (i < a.w.d && j < cols) to[(int64_t)i * a.s_row + (int64_t)j * a.s_col] = none ? 0.f : s[k][t][r];
+        }
+}
+
+// The segments' states: what each adds becomes what each finds, four numbers of one head's state to a thread.
+static __global__ void __launch_bounds__(256) memory_scan_kernel(const MemArgs a) {
+  const int quads = a.dk * a.dv / 4, blocks = (quads + 255) / 256;
+  const int head = blockIdx.x / blocks % a.heads, e = (blockIdx.x % blocks * 256 + threadIdx.x) * 4;
+  const int64_t seq = blockIdx.x / blocks / a.heads;
+  int64_t entry = 0, first;
+  for (int64_t s = threadIdx.x & 63; s < seq; s += 64) entry += mem_segments(a.m, s);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) entry += __shfl_xor(entry, o, 64);
+  if (e >= a.dk * a.dv) return;
+  int n;
+  mem_rows(a.m, seq, first, n);
+  const int segments = (int)min((int64_t)mem_segments(a.m, seq), a.m.entries - entry);  // (fewer only where cu_q does not ascend)
+  const int64_t row = mem_begin(a.states, seq, n), size = (int64_t)a.heads * a.dk * a.dv;
+  srv_floatx4 now = {};
+  if (row >= 0) now = *reinterpret_cast<const srv_floatx4*>(a.states.in + row * size + (int64_t)head * a.dk * a.dv + e);
+  float* at = a.added + entry * size + (int64_t)head * a.dk * a.dv + e;
+  const float* faded = a.faded + entry * a.heads + head;
+  constexpr int AHEAD = 8;  // loads under way
+  for (int i = 0; i < segments; i += AHEAD) {
+    srv_floatx4 x[AHEAD];
+    float f[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (i + k < segments) {
+        const int seg = a.reverse ? segments - 1 - i - k : i + k;
+        x[k] = *reinterpret_cast<const srv_floatx4*>(at + seg * size);
+        f[k] = faded[(int64_t)seg * a.heads];
+      }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (i + k < segments) {
+        const int seg = a.reverse ? segments - 1 - i - k : i + k;
+        *reinterpret_cast<srv_floatx4*>(at + seg * size) = now;
+        now = now * f[k] + x[k];
+      }
+  }
+}
+
+// ---- few tokens ---------------------------------------------------------------------------------------------------------------
+// One token after the other, for sequences of few: every state is read once and written once, which is what it takes.  A workgroup has 64 columns of
+// a head's state, a thread four of them in every sixteenth row.
+
+constexpr int MEM_STEP_ROWS = 16;
+
+template <typename T, int DK>
+__global__ void __launch_bounds__(256) memory_step_kernel(const MemArgs a) {
+  constexpr int ROWS = DK / MEM_STEP_ROWS;
+  __shared__ alignas(16) float xl[DK], wl[DK], meet[MEM_WAVES][64];
+  const int tid = threadIdx.x, col = tid % 16 * 4, r0 = tid / 16;
+  const int slice = blockIdx.x % a.slices, head = blockIdx.x / a.slices % a.heads, e = slice * 64 + col;
+  const int64_t seq = blockIdx.x / a.slices / a.heads;
+  int64_t first;
+  int n;
+  mem_rows(a.m, seq, first, n);
+  const int64_t from = mem_begin(a.states, seq, n), to = mem_end(a.states, seq);
+  const bool mine = e < a.dv;
+  srv_floatx4 s[ROWS] = {};
+  if (from >= 0 && mine) {
+    const float* p = a.states.in + (from * a.heads + head) * a.dk * a.dv + e;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+      if (r0 + 16 * i < a.dk) s[i] = *reinterpret_cast<const srv_floatx4*>(p + (int64_t)(r0 + 16 * i) * a.dv);
+  }
+  const T* xp = static_cast<const T*>(a.x.p) + head / a.x.group * a.x.head;
+  const T* wp = static_cast<const T*>(a.w.p) + head / a.w.group * a.w.head;
+  const T* vp = static_cast<const T*>(a.v.p) + head * a.v.head + e;
+  for (int t = 0; t < n; ++t) {
+    const int64_t at = first + t;
+    __syncthreads();
+    if (tid < DK) {
+      xl[tid] = tid < a.dk ? srv_widen(xp[at * a.x.token + tid]) : 0.f;
+      wl[tid] = tid < a.dk ? srv_widen(wp[at * a.w.token + tid]) : 0.f;
+    }
+    float v[4] = {};
+    if (mine)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = srv_widen(vp[at * a.v.token + k]);
+    const float fade = expf(mem_decay(a.log_decay[at * a.g_token + head * a.g_head]));
+    __syncthreads();
+    srv_floatx4 o = {};
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      const float w = wl[r0 + 16 * i], x = xl[r0 + 16 * i];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        s[i][k] = s[i][k] * fade + w * v[k];
+        o[k] += x * s[i][k];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      o[k] += __shfl_xor(o[k], 16, 64);
+      o[k] += __shfl_xor(o[k], 32, 64);
+    }
+    if ((tid & 63) < 16) *reinterpret_cast<srv_floatx4*>(&meet[tid >> 6][col]) = o;
+    __syncthreads();
+    if (tid < 64 && slice * 64 + tid < a.dv) {
+      const float y = a.in_scale * ((meet[0][tid] + meet[1][tid]) + (meet[2][tid] + meet[3][tid]));
+      static_cast<T*>(a.out)[at * a.out_token + head * a.out_head + slice * 64 + tid] = srv_narrow<T>(y);
+    }
+  }
+  if (to >= 0 && mine) {
+    float* p = a.states.out + (to * a.heads + head) * a.dk * a.dv + e;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i)
+      if (r0 + 16 * i < a.dk) *reinterpret_cast<srv_floatx4*>(p + (int64_t)(r0 + 16 * i) * a.dv) = s[i];
+  }
+}
+
+}  // namespace ttc

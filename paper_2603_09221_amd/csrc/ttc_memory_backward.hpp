@@ -1,0 +1,201 @@
+// What the gradients of linear attention need beside memory_chunk_kernel's: those of the log decays, and sums over heads that share a query.
+//
+// With <R_t, S_t> the product of a state and of the loss's gradient with respect to it, dl/dg_t = exp(g_t) <R_t, S_{t-1}>: what tokens before t
+// put in, as far as tokens from t on read it.  Pairs of one chunk are added up one by one (no difference of large sums):
+//     dl/dg_t = sum_{j < t <= i} m_ij + I + sum_{s < t} (b_s - a_s),      m_ij = scale exp(G_i - G_j) (q_i . k_j) (dout_i . v_j),
+// the last sum over the earlier tokens of the segment: a_s is q_s times what dq_s has from the state before its chunk, b_s is k_s times what dk_s
+// has from the state's gradient behind its chunk, I = <R, S> where the segment begins.  Sums over tokens are float64; their terms' errors of
+// 2^-24 add up from one such beginning to the next.
+#pragma once
+#include "ttc_memory.hpp"
+
+namespace ttc {
+
+struct MemDecayArgs {
+  MemSequences m;
+  MemRows q, k, v, gout;
+  int32_t heads, dk, dv, slices;
+  float scale;
+  const float* log_decay;
+  int64_t g_token, g_head;
+  float* pairs;                 // (heads, tokens)
+  const float *a, *b;           // (slices, heads, tokens)
+  MemStates begin;              // of the forward call
+  const float* gstate;          // (sequences, heads, dk, dv), where a sequence began with a state
+  const float *found, *found_r; // (entries, heads, dk, dv): the segments' states from before, and their gradients from behind
+  float* out;                   // (tokens, heads), or
+  double* sums;                 // (entries, heads): sums over tokens instead
+};
+
+template <typename T>
+__device__ __forceinline__ typename MemOperand<T>::type mem_global(const T* p, bool vec, bool there);
+template <>
+__device__ __forceinline__ srv_bf16x8 mem_global(const unsigned short* p, bool vec, bool there) { return there ? srv_ld8_bf16(p, vec) : srv_bf16x8{}; }
+template <>
+__device__ __forceinline__ mem_float8 mem_global(const float* p, bool vec, bool there) {
+  mem_float8 x = {};
+  if (there) srv_ld8(p, vec, x.x);
+  return x;
+}
+
+// sum_{j < t <= i} m_ij for the tokens t of one chunk of one head: its steps are column sums below and row sums left of the diagonal.
+template <typename T>
+__global__ void __launch_bounds__(256) memory_pairs_kernel(const MemDecayArgs a) {
+  typedef typename MemOperand<T>::type op_t;
+  __shared__ MemDecays dl;
+  __shared__ float left[MEM_CHUNK], below[MEM_WAVES][MEM_CHUNK];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+  const int head = blockIdx.x % a.heads;
+  int64_t seq, first;
+  int chunk, n;
+  if (!mem_segment(a.m, blockIdx.x / a.heads, seq, chunk)) return;
+  mem_rows(a.m, seq, first, n);
+  const int64_t t0 = first + (int64_t)chunk * MEM_CHUNK;
+  const int rows = min(MEM_CHUNK, n - chunk * MEM_CHUNK);
+  if (rows <= 0) return;
+  if (wave == 0) {
+    const double sum = mem_decay_sums(lane < rows ? mem_decay(a.log_decay[(t0 + lane) * a.g_token + head * a.g_head]) : 0.f, lane);
+    dl.hi[lane] = (float)sum;
+    dl.lo[lane] = (float)(sum - (float)sum);
+  }
+  srv_floatx4 z[2][4] = {};
+  const auto products = [&](const MemRows& late, const MemRows& early, srv_floatx4 (&to)[4]) {
+    const T* x = static_cast<const T*>(late.p) + head / late.group * late.head + t0 * late.token;
+    const T* y = static_cast<const T*>(early.p) + head / early.group * early.head + t0 * early.token;
+    const int i = 16 * wave + c;
+    for (int e = 8 * g; e < ((late.d + 31) & ~31); e += 32) {
+      const op_t b = mem_global(x + i * late.token + e, late.vec, i < rows && e < late.d);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        to[j] = mem_mma(mem_global(y + (16 * j + c) * early.token + e, early.vec, 16 * j + c < rows && e < early.d), b, to[j]);
+    }
+  };
+  products(a.q, a.k, z[0]);
+  products(a.gout, a.v, z[1]);
+  __syncthreads();
+  const int i = 16 * wave + c;
+  float row = 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int e = 16 * j + 4 * g + r;
+      float x = e < i ? a.scale * z[0][j][r] * z[1][j][r] * mem_between(dl, i, e) : 0.f;
+      row += x;
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) x += __shfl_xor(x, o, 64);
+      if (c == 0) below[wave][e] = x;
+    }
+  row += __shfl_xor(row, 16, 64);
+  row += __shfl_xor(row, 32, 64);
+  if (g == 0) left[i] = row;
+  __syncthreads();
+  if (wave == 0) {
+    const double step = (double)((below[0][lane] + below[1][lane]) + (below[2][lane] + below[3][lane])) - left[lane];
+    const double sum = mem_decay_sums(step, lane) - step;
+    if (lane < rows) a.pairs[head * a.m.tokens + t0 + lane] = (float)sum;
+  }
+}
+
+constexpr int MEM_SUM_THREADS = 1024;
+
+// One head of one segment: 1024 tokens at a time
+static __global__ void __launch_bounds__(MEM_SUM_THREADS) memory_decay_kernel(const MemDecayArgs a) {
+  __shared__ double meet[2][MEM_SUM_THREADS / 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, head = blockIdx.x % a.heads;
+  const int64_t entry = blockIdx.x / a.heads, size = (int64_t)a.dk * a.dv;
+  int64_t seq, first;
+  int segment, n;
+  if (!mem_segment(a.m, entry, seq, segment)) {
+    if (a.sums && tid == 0) a.sums[entry * a.heads + head] = 0.0;
+    return;
+  }
+  mem_rows(a.m, seq, first, n);
+  const int t0 = segment * a.m.segment * MEM_CHUNK, t1 = (int)min((int64_t)t0 + (int64_t)a.m.segment * MEM_CHUNK, (int64_t)n);
+  const auto whole = [&](double x) {
+#pragma unroll
+    for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o, 64);
+    __syncthreads();
+    if (lane == 0) meet[0][wave] = x;
+    __syncthreads();
+    x = 0.0;
+    for (int w = 0; w < MEM_SUM_THREADS / 64; ++w) x += meet[0][w];
+    return x;
+  };
+  const float *s = nullptr, *r = nullptr;
+  if (segment) {
+    s = a.found + (entry * a.heads + head) * size;
+    r = a.found_r + ((entry - 1) * a.heads + head) * size;
+  } else if (const int64_t row = mem_begin(a.begin, seq, n); row >= 0) {
+    s = a.begin.in + (row * a.heads + head) * size;
+    r = a.gstate + (seq * a.heads + head) * size;
+  }
+  double now = 0.0;
+  if (s) {
+    for (int64_t e = tid * 4; e < size; e += MEM_SUM_THREADS * 4) {
+      const srv_floatx4 x = *reinterpret_cast<const srv_floatx4*>(s + e), y = *reinterpret_cast<const srv_floatx4*>(r + e);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) now += (double)x[k] * y[k];
+    }
+    now = whole(now);
+  }
+  double total = 0.0;
+  for (int at = t0; at < t1; at += MEM_SUM_THREADS) {
+    const int64_t t = head * a.m.tokens + first + at + tid;
+    const bool real = at + tid < t1;
+    double step = 0.0;
+    if (real)
+      for (int s = 0; s < a.slices; ++s) step += (double)a.b[s * a.heads * a.m.tokens + t] - a.a[s * a.heads * a.m.tokens + t];
+    double sum = mem_decay_sums(step, lane);
+    __syncthreads();
+    if (lane == 63) meet[1][wave] = sum;
+    __syncthreads();
+    double all = 0.0;
+#pragma unroll
+    for (int w = 0; w < MEM_SUM_THREADS / 64; ++w) {
+      const double x = meet[1][w];
+      sum += w < wave ? x : 0.0;
+      all += x;
+    }
+    if (real) {
+      const double grad = a.pairs[t] + now + (sum - step);
+      if (a.out) a.out[(first + at + tid) * a.heads + head] = (float)grad;
+      total += grad;
+    }
+    now += all;
+  }
+  if (a.sums) {
+    total = whole(total);
+    if (tid == 0) a.sums[entry * a.heads + head] = total;
+  }
+}
+
+static __global__ void memory_decay_sum_kernel(const double* sums, int64_t entries, int heads, float* out) {
+  const int h = blockIdx.x * 64 + threadIdx.x;
+  if (h >= heads) return;
+  double x = 0.0;
+  for (int64_t s = 0; s < entries; ++s) x += sums[s * heads + h];
+  out[h] = (float)x;
+}
+
+// The gradients of heads that share a row, in their order: a chunk's tokens of one shared head to a workgroup, four entries at a time to a thread
+template <typename T>
+__global__ void __launch_bounds__(256) memory_heads_kernel(const MemSequences m, const float* parts, T* out, int heads, int group, int d) {
+  const int head = blockIdx.x % heads;
+  int64_t seq, first;
+  int chunk, n;
+  if (!mem_segment(m, blockIdx.x / heads, seq, chunk)) return;
+  mem_rows(m, seq, first, n);
+  const int64_t t0 = first + (int64_t)chunk * MEM_CHUNK;
+  const int quads = min(MEM_CHUNK, n - chunk * MEM_CHUNK) * (d / 4);
+  for (int i = threadIdx.x; i < quads; i += 256) {
+    const int64_t row = (t0 + i / (d / 4)) * heads + head;
+    const int e = i % (d / 4) * 4;
+    srv_floatx4 x = {};
+    for (int h = 0; h < group; ++h) x += *reinterpret_cast<const srv_floatx4*>(parts + (row * group + h) * d + e);
+    const float y[4] = {x[0], x[1], x[2], x[3]};
+    srv_st<T, 4>(out + row * d + e, ((uint64_t)out & 15) == 0, y);
+  }
+}
+
+}  // namespace ttc
