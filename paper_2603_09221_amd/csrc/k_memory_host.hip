@@ -4,9 +4,9 @@
 
 namespace ttc {
 
-template <> hipError_t launch_memory_chunks<64>(const MemArgs&, bool, bool, bool, uint32_t, hipStream_t);
-template <> hipError_t launch_memory_chunks<128>(const MemArgs&, bool, bool, bool, uint32_t, hipStream_t);
-template <> hipError_t launch_memory_chunks<256>(const MemArgs&, bool, bool, bool, uint32_t, hipStream_t);
+template <> hipError_t launch_memory_chunks<64>(const MemArgs&, bool, bool, int, uint32_t, hipStream_t);
+template <> hipError_t launch_memory_chunks<128>(const MemArgs&, bool, bool, int, uint32_t, hipStream_t);
+template <> hipError_t launch_memory_chunks<256>(const MemArgs&, bool, bool, int, uint32_t, hipStream_t);
 template <> hipError_t launch_memory_step<64>(const MemArgs&, bool, uint32_t, hipStream_t);
 template <> hipError_t launch_memory_step<128>(const MemArgs&, bool, uint32_t, hipStream_t);
 template <> hipError_t launch_memory_step<256>(const MemArgs&, bool, uint32_t, hipStream_t);
@@ -24,32 +24,25 @@ MemSequences sequences_of(const ttc_linear_attention_t& a, int segment) {
   return m;
 }
 
-// Chunks of a segment: all of a sequence where sequences, heads and slices occupy the device, else as many as give it four workgroups a unit
+// Chunks of a segment: all of a sequence where sequences, heads and slices occupy the device, else as many as give it two workgroups a unit
 int segment_of(const ttc_linear_attention_t& a, int slices, int cus) {
   const int chunks = (int)(((int64_t)a.max_q + MEM_CHUNK - 1) / MEM_CHUNK);
   const double base = (double)a.sequences * a.heads * slices;
   if (chunks <= 1 || base >= 2. * cus) return chunks < 1 ? 1 : chunks;
-  const double wanted = 4. * cus / base;
-  const int each = (int)(chunks / wanted);
+  const double wanted = 2. * cus / base;
+  const int each = (int)ceil(chunks / wanted);
   return each < 4 ? (chunks < 4 ? chunks : 4) : each;
 }
 
-MemRows rows_of(const void* p, int64_t token, int64_t head, int group, int d, bool bf16) {
-  const int64_t bytes = bf16 ? 2 : 4;
-  return {p, token, head, group, d, (uint64_t)p % 16 == 0 && token * bytes % 16 == 0 && head * bytes % 16 == 0};
-}
-
 MemArgs forward_args(const ttc_linear_attention_t& a) {
-  const bool bf16 = a.dtype == TTC_BF16;
   const int group = a.heads / a.heads_qk;
   MemArgs p = {};
-  p.x = rows_of(a.q, a.q_token, a.q_head, group, a.dk, bf16);
-  p.w = rows_of(a.k, a.k_token, a.k_head, group, a.dk, bf16);
-  p.v = rows_of(a.v, a.v_token, a.v_head, 1, a.dv, bf16);
+  p.x = {a.q, a.q_token, a.q_head, group, a.dk};
+  p.w = {a.k, a.k_token, a.k_head, group, a.dk};
+  p.v = {a.v, a.v_token, a.v_head, 1, a.dv};
   p.out = a.out;
   p.out_token = a.out_token;
   p.out_head = a.out_head;
-  p.out_vec = rows_of(a.out, a.out_token, a.out_head, 1, a.dv, bf16).vec;
   p.heads = a.heads;
   p.pair_scale = p.in_scale = a.scale;
   p.up_scale = 1.f;
@@ -64,20 +57,18 @@ MemArgs forward_args(const ttc_linear_attention_t& a) {
   return p;
 }
 
-hipError_t run_chunks(MemArgs p, bool bf16, bool states, hipStream_t st) {
-  const int rows = states ? p.w.d : p.x.d;
+hipError_t run_chunks(MemArgs p, bool bf16, int what, hipStream_t st) {
+  const int rows = p.w.d;
   const bool wide = wide_of(rows, p.v.d);
   p.slices = slices_of(rows, p.v.d);
-  const double grid = (double)p.m.entries * p.heads * p.slices;
-  if (grid >= 2147483648.) return hipErrorInvalidValue;
-  const uint32_t n = (uint32_t)grid;
-  return rows <= 64 ? launch_memory_chunks<64>(p, bf16, wide, states, n, st)
-                    : rows <= 128 ? launch_memory_chunks<128>(p, bf16, wide, states, n, st) : launch_memory_chunks<256>(p, bf16, wide, states, n, st);
+  const uint32_t grid = (uint32_t)((p.m.entries * p.heads * p.slices + 7) / 8 * 8);  // (the kernel deals them out to eight XCDs)
+  return rows <= 64 ? launch_memory_chunks<64>(p, bf16, wide, what, grid, st)
+                    : rows <= 128 ? launch_memory_chunks<128>(p, bf16, wide, what, grid, st) : launch_memory_chunks<256>(p, bf16, wide, what, grid, st);
 }
 
 // What the segments add to their states, and from that what each finds
 hipError_t run_starts(const MemArgs& p, bool bf16, hipStream_t st) {
-  if (const hipError_t e = run_chunks(p, bf16, true, st); e != hipSuccess) return e;
+  if (const hipError_t e = run_chunks(p, bf16, MEM_STATES, st); e != hipSuccess) return e;
   const int64_t blocks = (p.dk * p.dv / 4 + 255) / 256;
   hipLaunchKernelGGL(memory_scan_kernel, dim3((uint32_t)(p.m.sequences * p.heads * blocks)), dim3(256), 0, st, p);
   return hipGetLastError();
@@ -111,7 +102,7 @@ hipError_t launch_linear_attention(const ttc_linear_attention_t& a, int cus, voi
     if (const hipError_t e = run_starts(p, bf16, st); e != hipSuccess) return e;
     p.starts = p.added;
   }
-  return run_chunks(p, bf16, false, st);
+  return run_chunks(p, bf16, MEM_OUT, st);
 }
 
 namespace {
@@ -170,7 +161,7 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
   MemArgs base = forward_args(f);
   base.m = plan.m;
   base.states.out = nullptr;
-  const MemRows q = base.x, k = base.w, v = base.v, gout = rows_of(b.gout, b.gout_token, b.gout_head, 1, f.dv, bf16);
+  const MemRows q = base.x, k = base.w, v = base.v, gout = {b.gout, b.gout_token, b.gout_head, 1, f.dv};
   const MemStates begin = base.states, end = {b.gstate_out, gstate, f.sequences, nullptr, nullptr};
   MemArgs back = base;
   back.reverse = 1;
@@ -203,11 +194,10 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
     p.out_float = shared;
     p.out_token = (int64_t)f.heads * d;
     p.out_head = d;
-    p.out_vec = rows_of(p.out, p.out_token, d, 1, d, bf16 && !shared).vec;
   };
   MemArgs dv = back;
   result(dv, b.gv, 0, f.heads, f.dv);
-  if ((e = run_chunks(dv, bf16, false, st)) != hipSuccess) return e;
+  if ((e = run_chunks(dv, bf16, MEM_OUT, st)) != hipSuccess) return e;
   MemArgs dk = back;
   dk.x = v;
   dk.w = gout;
@@ -218,7 +208,7 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
   dk.dot = k;
   dk.dots = place(plan.b);
   result(dk, b.gk, plan.gk, f.heads_qk, f.dk);
-  if ((e = run_chunks(dk, bf16, false, st)) != hipSuccess) return e;
+  if ((e = run_chunks(dk, bf16, MEM_OUT_DOTS, st)) != hipSuccess) return e;
   MemArgs dq = base;
   dq.x = gout;
   dq.w = v;
@@ -228,7 +218,7 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
   dq.dot = q;
   dq.dots = place(plan.a);
   result(dq, b.gq, plan.gq, f.heads_qk, f.dk);
-  if ((e = run_chunks(dq, bf16, false, st)) != hipSuccess) return e;
+  if ((e = run_chunks(dq, bf16, MEM_OUT_DOTS, st)) != hipSuccess) return e;
   if (group > 1) {
     const dim3 grid((uint32_t)(plan.chunks.entries * f.heads_qk));
     for (int i = 0; i < 2; ++i) {

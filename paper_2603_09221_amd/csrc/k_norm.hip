@@ -4,23 +4,25 @@
 
 namespace ttc {
 
+constexpr int NORM_THREADS = 2048;  // of a compute unit, forward
+
 static bool row16(const void* p, int64_t stride, int32_t dtype) {
   const int64_t bytes = dtype == TTC_BF16 ? 2 : 4;
   return (uint64_t)p % 16 == 0 && stride * bytes % 16 == 0;
 }
 
-// The fewest threads that hold a row in eights, two at most
+// The fewest threads that hold a row in eights: more eights to a thread take registers that the wavefronts in flight lack
 template <typename F>
 static void norm_shape(int features, F&& f) {
   if (features <= 512) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
-  else if (features <= 1024) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
+  else if (features <= 1024) f(std::integral_constant<int, 128>{}, std::integral_constant<int, 1>{});
   else if (features <= 2048) f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
   else if (features <= 4096) f(std::integral_constant<int, 512>{}, std::integral_constant<int, 1>{});
   else if (features <= 8192) f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 1>{});
   else f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
 }
 
-hipError_t launch_residual_norm(const ttc_residual_norm_t& n, hipStream_t st) {
+hipError_t launch_residual_norm(const ttc_residual_norm_t& n, int cus, hipStream_t st) {
   NormArgs a = {};
   a.n = n;
   a.group = n.features / n.groups;
@@ -28,21 +30,23 @@ hipError_t launch_residual_norm(const ttc_residual_norm_t& n, hipStream_t st) {
           row16(n.residual, n.residual_token, n.dtype) << ROW_RESIDUAL | row16(n.r, n.r_token, n.dtype) << ROW_R | row16(n.h, n.h_token, n.dtype) << ROW_H;
   norm_shape(n.features, [&](auto lanes, auto pieces) {
     typedef NormShape<decltype(lanes)::value, decltype(pieces)::value> S;
-    const dim3 grid((uint32_t)((n.tokens + S::ROWS - 1) / S::ROWS));
+    const int64_t rows = (n.tokens + S::ROWS - 1) / S::ROWS, most = (int64_t)cus * (NORM_THREADS / S::THREADS);
+    const dim3 grid((uint32_t)(rows < most ? rows : most));
     if (n.dtype == TTC_BF16) hipLaunchKernelGGL((residual_norm_kernel<unsigned short, lanes(), pieces()>), grid, dim3(S::THREADS), 0, st, a);
     else hipLaunchKernelGGL((residual_norm_kernel<float, lanes(), pieces()>), grid, dim3(S::THREADS), 0, st, a);
   });
   return hipGetLastError();
 }
 
-// Workgroups of the backward pass, and the rows of each of its parts
-static void norm_grid(const ttc_residual_norm_t& n, int cus, int& grid, int& parts) {
+// Workgroups of the backward pass, each of which leaves a part of every sum
+static int norm_grid(const ttc_residual_norm_t& n, int cus) {
+  int grid = 0;
   norm_shape(n.features, [&](auto lanes, auto pieces) {
     typedef NormShape<decltype(lanes)::value, decltype(pieces)::value> S;
     const int64_t rows = (n.tokens + S::ROWS - 1) / S::ROWS, most = (int64_t)cus * (1024 / S::THREADS);
     grid = (int)(rows < most ? rows : most);
-    parts = grid * S::ROWS;
   });
+  return grid;
 }
 
 static void norm_wanted(const ttc_residual_norm_backward_t& b, float* (&out)[5]) {
@@ -54,12 +58,11 @@ static void norm_wanted(const ttc_residual_norm_backward_t& b, float* (&out)[5])
 }
 
 uint64_t norm_backward_workspace(const ttc_residual_norm_backward_t& b, int cus) {
-  int grid, parts, vectors = 0;
-  norm_grid(b.forward, cus, grid, parts);
+  int vectors = 0;
   float* out[5];
   norm_wanted(b, out);
   for (float* v : out) vectors += v != nullptr;
-  return (uint64_t)vectors * parts * b.forward.features * 4;
+  return (uint64_t)vectors * norm_grid(b.forward, cus) * b.forward.features * 4;
 }
 
 hipError_t launch_residual_norm_backward(const ttc_residual_norm_backward_t& b, int cus, void* workspace, hipStream_t st) {
@@ -74,8 +77,7 @@ hipError_t launch_residual_norm_backward(const ttc_residual_norm_backward_t& b, 
   };
   a.vec = rows(n.y, n.y_token, b.gy) << ROW_Y | rows(n.gate, n.gate_token, b.ggate) << ROW_GATE |
           rows(n.residual, n.residual_token, b.gresidual) << ROW_RESIDUAL | row16(b.gr, b.gr_token, n.dtype) << ROW_R | row16(b.gh, b.gh_token, n.dtype) << ROW_H;
-  int grid, parts;
-  norm_grid(n, cus, grid, parts);
+  const int grid = norm_grid(n, cus);
   NormParts sum = {};
   float* out[5];
   norm_wanted(b, out);
@@ -86,9 +88,9 @@ hipError_t launch_residual_norm_backward(const ttc_residual_norm_backward_t& b, 
       a.part[v] = at;
       sum.part[vectors] = at;
       sum.out[vectors++] = out[v];
-      at += (int64_t)parts * n.features;
+      at += (int64_t)grid * n.features;
     }
-  a.parts = sum.parts = parts;
+  sum.parts = grid;
   sum.features = n.features;
   sum.chunks = (n.features + 63) / 64;
   if (grid) norm_shape(n.features, [&](auto lanes, auto pieces) {
@@ -97,7 +99,7 @@ hipError_t launch_residual_norm_backward(const ttc_residual_norm_backward_t& b, 
     else hipLaunchKernelGGL((residual_norm_backward_kernel<float, lanes(), pieces()>), dim3(grid), dim3(S::THREADS), 0, st, a);
   });
   if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  if (vectors) hipLaunchKernelGGL(norm_parts_kernel, dim3(vectors * sum.chunks), dim3(256), 0, st, sum);
+  if (vectors) hipLaunchKernelGGL(norm_parts_kernel, dim3(vectors * sum.chunks), dim3(64 * NORM_PARTS_WAVES), 0, st, sum);
   return hipGetLastError();
 }
 

@@ -116,7 +116,7 @@ ttc_status_t ttc_residual_norm(const ttc_residual_norm_t* n, void* hip_stream) {
   const int64_t stride[3] = {n->y_token, n->gate_token, n->residual_token};
   for (int i = 0; i < 3; ++i)
     if (in[i] && ((in[i] == n->r && stride[i] != n->r_token) || (in[i] == n->h && stride[i] != n->h_token))) return TTC_ERR_INVALID_ARG;
-  return ttc::launch_residual_norm(*n, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? TTC_OK : TTC_ERR_DEVICE;
+  return ttc::launch_residual_norm(*n, ttc::compute_units(), static_cast<hipStream_t>(hip_stream)) == hipSuccess ? TTC_OK : TTC_ERR_DEVICE;
 }
 
 size_t ttc_residual_norm_backward_workspace_bytes(const ttc_residual_norm_backward_t* b) {

@@ -127,17 +127,19 @@ __device__ __forceinline__ mem_float8 mem_operand(const float* p, const float* q
   const srv_floatx4 a = *reinterpret_cast<const srv_floatx4*>(p), b = *reinterpret_cast<const srv_floatx4*>(q);
   return {{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
 }
-// numbers `step` apart
-__device__ __forceinline__ srv_bf16x8 mem_column(const unsigned short* p, int step) {
-  srv_u16x8 x;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = p[i * step];
-  return __builtin_bit_cast(srv_bf16x8, x);
+// Column c of the eight rows from `p` on, `step` numbers apart; p: column 0 of 16 in LDS.  Of bfloat16 sixteen lanes read four rows of sixteen
+// numbers, four to a lane, and get a column's four each.
+__device__ __forceinline__ srv_bf16x8 mem_column(const unsigned short* p, int step, int c) {
+  typedef __bf16 four_t __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) four_t* lds_t;
+  const unsigned short* q = p + (c >> 2) * step + (c & 3) * 4;
+  const four_t a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_t)q), b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_t)(q + 4 * step));
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
-__device__ __forceinline__ mem_float8 mem_column(const float* p, int step) {
+__device__ __forceinline__ mem_float8 mem_column(const float* p, int step, int c) {
   mem_float8 x;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x.x[i] = p[i * step];
+  for (int i = 0; i < 8; ++i) x.x[i] = p[i * step + c];
   return x;
 }
 __device__ __forceinline__ float mem_entry(const srv_bf16x8& v, int i) { return (float)v[i]; }
@@ -178,8 +180,30 @@ __device__ __forceinline__ void mem_store4(unsigned short* p, const float (&x)[4
                                        srv_narrow<unsigned short>(x[3])};
 }
 __device__ __forceinline__ void mem_store4(float* p, const float (&x)[4]) { *reinterpret_cast<srv_floatx4*>(p) = srv_floatx4{x[0], x[1], x[2], x[3]}; }
-__device__ __forceinline__ void mem_store8(unsigned short* p, const float (&x)[8]) { srv_st8(p, true, x); }
-__device__ __forceinline__ void mem_store8(float* p, const float (&x)[8]) { srv_st8(p, true, x); }
+
+// Eight numbers of a row, in 16-byte accesses whatever the alignment: device memory takes them at that of a number
+typedef unsigned short mem_u16x8 __attribute__((ext_vector_type(8), aligned(2)));
+typedef float mem_floatx4 __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T> struct MemEight;
+template <> struct MemEight<unsigned short> { srv_u16x8 x; };
+template <> struct MemEight<float> { srv_floatx4 x[2]; };
+__device__ __forceinline__ void mem_fetch(const unsigned short* p, MemEight<unsigned short>& to) { to.x = *reinterpret_cast<const mem_u16x8*>(p); }
+__device__ __forceinline__ void mem_fetch(const float* p, MemEight<float>& to) {
+  to.x[0] = *reinterpret_cast<const mem_floatx4*>(p);
+  to.x[1] = *reinterpret_cast<const mem_floatx4*>(p + 4);
+}
+__device__ __forceinline__ void mem_put(unsigned short* p, const MemEight<unsigned short>& x) { *reinterpret_cast<srv_u16x8*>(p) = x.x; }
+__device__ __forceinline__ void mem_put(float* p, const MemEight<float>& x) {
+  *reinterpret_cast<srv_floatx4*>(p) = x.x[0];
+  *reinterpret_cast<srv_floatx4*>(p + 4) = x.x[1];
+}
+// four numbers to a row of any alignment
+__device__ __forceinline__ void mem_out4(unsigned short* p, const srv_floatx4& x) {
+  typedef unsigned short u16x4 __attribute__((ext_vector_type(4), aligned(2)));
+  *reinterpret_cast<u16x4*>(p) = u16x4{srv_narrow<unsigned short>(x[0]), srv_narrow<unsigned short>(x[1]), srv_narrow<unsigned short>(x[2]),
+                                       srv_narrow<unsigned short>(x[3])};
+}
+__device__ __forceinline__ void mem_out4(float* p, const srv_floatx4& x) { *reinterpret_cast<mem_floatx4*>(p) = x; }
 
 // ---- the kernel of chunks ---------------------------------------------------------------------------------------------------
 
@@ -188,7 +212,6 @@ struct MemRows {
   int64_t token, head;
   int32_t group;       // heads that share a row
   int32_t d;           // entries
-  int32_t vec;         // 16-byte alignment
 };
 
 struct MemArgs {
@@ -196,7 +219,7 @@ struct MemArgs {
   MemRows x, w, v;
   void* out;
   int64_t out_token, out_head;
-  int32_t out_vec, out_float;   // alignment; float32 whatever the rows' type
+  int32_t out_float;            // float32 whatever the rows' type (with dots alone)
   int32_t heads, slices;
   int32_t reverse;
   float pair_scale, in_scale, up_scale;
@@ -214,24 +237,48 @@ struct MemArgs {
   float* dots;                  // (slices, heads, tokens)
 };
 
-// Decays of a chunk: wavefront 0, a token to a lane, in float64, so that the differences of sums are as exact as the decays themselves.
+// Decays of a chunk, a token to a lane, added up in float64, so that the differences of sums are as exact as the decays themselves; powers of two
 struct MemDecays {
-  float hi[MEM_CHUNK], lo[MEM_CHUNK];   // G as a sum of two
+  float hi[MEM_CHUNK], lo[MEM_CHUNK];   // G / ln 2 as a sum of two
   float in[MEM_CHUNK], up[MEM_CHUNK];
   float whole;
 };
 
-__device__ __forceinline__ double mem_decay_sums(double g, int lane) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double y = __shfl_up(g, o, 64);
-    g += lane >= o ? y : 0.0;
-  }
-  return g;
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ double mem_dpp(double x) {  // the number of another lane, 0 where there is none
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xf, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xf, true);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+// Inclusive sums over a wavefront's lanes
+__device__ __forceinline__ double mem_sums(double x) {
+  x += mem_dpp<0x111>(x);       // within sixteen lanes
+  x += mem_dpp<0x112>(x);
+  x += mem_dpp<0x114>(x);
+  x += mem_dpp<0x118>(x);
+  x += mem_dpp<0x142, 0xa>(x);  // what lane 15 has to the next sixteen, what lane 31 has to the upper half
+  x += mem_dpp<0x143, 0xc>(x);
+  return x;
 }
 
-__device__ __forceinline__ float mem_between(const MemDecays& d, int late, int early) {
-  return expf((d.hi[late] - d.hi[early]) + (d.lo[late] - d.lo[early]));
+constexpr double MEM_LOG2E = 1.4426950408889634;
+
+// Sums of a chunk's decays in powers of two; returns the whole
+__device__ __forceinline__ double mem_decays(float g, int lane, bool reverse, float in_scale, float up_scale, MemDecays& to) {
+  const double sum = mem_sums((double)mem_decay(g) * MEM_LOG2E), whole = __shfl(sum, 63, 64);
+  const float hi = (float)sum;
+  to.hi[lane] = hi;
+  to.lo[lane] = (float)(sum - hi);
+  const float since = __builtin_amdgcn_exp2f(hi), left = __builtin_amdgcn_exp2f((float)(whole - sum));
+  to.in[lane] = in_scale * (reverse ? left : since);
+  to.up[lane] = up_scale * (reverse ? since : left);
+  if (lane == 63) to.whole = since;
+  return whole;
+}
+// sign: -1 where the first is the earlier one
+__device__ __forceinline__ float mem_between(float a_hi, float a_lo, float b_hi, float b_lo, float sign) {
+  return __builtin_amdgcn_exp2f(sign * ((a_hi - b_hi) + (a_lo - b_lo)));
 }
 
 template <typename T, int DK, int NT>
@@ -239,48 +286,105 @@ struct MemShape {
   static constexpr int PAD = 16 / sizeof(T);
   static constexpr int XS = DK + PAD, VS = 64 * NT + PAD, PS = MEM_CHUNK + PAD;  // rows in LDS
   static constexpr int COLS = 16 * NT * MEM_WAVES;
-  static constexpr int X = MEM_CHUNK * (XS > PS ? XS : PS);  // the pairs' products take the place of x
+  // the pairs' products have a place of their own unless LDS is too small for it: then that of x, for one more barrier
+  static constexpr bool OWN = 2 * MEM_CHUNK * XS + MEM_CHUNK * VS + MEM_CHUNK * PS <= 38 * 1024;
+  static constexpr int XP = DK / 32, VP = 2 * NT;  // pieces of eight that a thread brings
+  // workgroups of a compute unit that LDS and registers leave room for
+  static constexpr int RESIDENT = sizeof(T) == 2 && DK <= 128 ? 2 : 1;
 };
 
-// 64 rows, zeros behind the last and behind the last entry
-template <typename T, int D, int STEP>
-__device__ __forceinline__ void mem_fill(T* lds, const MemRows& r, const T* base, int64_t first, int n, int entry, int entries) {
-  constexpr int PIECES = D / 8;
-  for (int i = threadIdx.x; i < MEM_CHUNK * PIECES; i += 64 * MEM_WAVES) {
-    const int t = i / PIECES, e = i % PIECES * 8;
-    float x[8] = {};
-    if (t < n && entry + e < entries) srv_ld8(base + (first + t) * r.token + entry + e, r.vec, x);
-    mem_store8(lds + t * STEP + e, x);
+// 64 rows on their way to LDS: zeros behind the last row and behind the last entry
+template <typename T, int D, int STEP, int PIECES>
+struct MemStage {
+  static constexpr int ROW = D / 8, TURN = 64 * MEM_WAVES / ROW;  // pieces of a row, rows of one turn of the workgroup
+  static_assert(PIECES * TURN == MEM_CHUNK);
+  MemEight<T> piece[PIECES];
+  const T* at;         // of the thread's first piece in the chunk that comes next
+  int64_t token;
+  __device__ __forceinline__ void begin(const MemRows& r, const T* base, int64_t first, int entry) {
+    token = r.token;
+    at = base + (first + (int)(threadIdx.x / ROW)) * token + entry + threadIdx.x % ROW * 8;
   }
-}
+  // `whole`: all rows and entries are there
+  __device__ __forceinline__ void fetch(int rows, int entries, bool whole) {
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) mem_fetch(at + i * TURN * token, piece[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) {
+        piece[i] = {};
+        if ((int)(threadIdx.x % ROW) * 8 < entries && (int)(threadIdx.x / ROW) + i * TURN < rows) mem_fetch(at + i * TURN * token, piece[i]);
+      }
+    }
+  }
+  __device__ __forceinline__ void put(T* lds) const {
+    T* p = lds + threadIdx.x / ROW * STEP + threadIdx.x % ROW * 8;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) mem_put(p + i * TURN * STEP, piece[i]);
+  }
+};
+
+enum MemWhat { MEM_STATES, MEM_OUT, MEM_OUT_DOTS };  // what a segment adds to its state; results; results and their products with other rows
 
 // A workgroup takes one segment of one head of one sequence, and of the values' columns a slice of 64 * NT; a wavefront owns 16 * NT of them and
 // their state, DK numbers each, which stays in its registers from chunk to chunk: what a lane holds of it as a result is what it has to hold of it as an
-// operand if the sum's order follows.  STATES: only what the segment adds to its state.
-template <typename T, int DK, int NT, bool STATES>
-__global__ void __launch_bounds__(64 * MEM_WAVES) memory_chunk_kernel(const MemArgs a) {
+// operand if the sum's order follows.  The next chunk's rows and decays are on their way while one is worked on.
+// bfloat16 rows: the state is met in two parts of 8 bits (three where float32 results depend on it), what is added to it in three, so that states are as
+// exact as float32 sums; pairs' products, in one, which the header's documentation states.
+template <typename T, int DK, int NT, int WHAT>
+__global__ void __launch_bounds__(64 * MEM_WAVES, (MemShape<T, DK, NT>::RESIDENT)) memory_chunk_kernel(const MemArgs a) {
   typedef MemShape<T, DK, NT> S;
   typedef typename MemOperand<T>::type op_t;
-  constexpr bool BF16 = sizeof(T) == 2;
-  constexpr int IN = BF16 ? 3 : 1, UP = BF16 ? 3 : 1, KT = DK / 16;
-  __shared__ alignas(16) T xl[STATES ? 8 : S::X], wl[MEM_CHUNK * S::XS], vl[MEM_CHUNK * S::VS];
-  __shared__ MemDecays dl;
-  __shared__ float meet[MEM_WAVES][MEM_CHUNK];
-  T* const pl = xl;
+  constexpr bool BF16 = sizeof(T) == 2, STATES = WHAT == MEM_STATES, DOTS = WHAT == MEM_OUT_DOTS;
+  constexpr int IN = BF16 ? (DOTS ? 3 : 2) : 1, UP = BF16 ? 3 : 1, KT = DK / 16;
+  __shared__ alignas(16) T xl[STATES ? 8 : MEM_CHUNK * (S::OWN || S::XS > S::PS ? S::XS : S::PS)], wl[MEM_CHUNK * S::XS], vl[MEM_CHUNK * S::VS];
+  __shared__ alignas(16) T own[STATES || !S::OWN ? 8 : MEM_CHUNK * S::PS];
+  __shared__ alignas(16) MemDecays decays[2];
+  __shared__ alignas(16) float meet[MEM_WAVES][MEM_CHUNK];
+  T* const pl = S::OWN ? own : xl;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  const int slice = blockIdx.x % a.slices, head = blockIdx.x / a.slices % a.heads;
-  const int64_t entry = blockIdx.x / a.slices / a.heads;
+  // Workgroups of an XCD, every eighth, take neighbouring heads, which may share rows that they then find in its cache, with all their segments:
+  // places without a segment are as many for every XCD (with segments slowest the last XCD had most of them, and the others 68 for 64 places).
+  const uint32_t each = gridDim.x / 8, work = blockIdx.x % 8 * each + blockIdx.x / 8;
+  const int slice = work % a.slices;
+  const int64_t entry = work / a.slices % a.m.entries;
+  const int head = work / a.slices / a.m.entries;
   int64_t seq, first;
   int segment, n;
-  if (!mem_segment(a.m, entry, seq, segment)) return;
+  if (head >= a.heads || !mem_segment(a.m, entry, seq, segment)) return;
   mem_rows(a.m, seq, first, n);
   const int segments = mem_segments(a.m, seq), chunks = (n + MEM_CHUNK - 1) / MEM_CHUNK;
   const int c0 = segment * a.m.segment, c1 = min(c0 + a.m.segment, chunks);
-  if (STATES && segment == (a.reverse ? 0 : segments - 1)) return;  // nobody finds what this one leaves
+  const bool reverse = a.reverse;
+  const float sign = reverse ? -1.f : 1.f;
+  if (STATES && segment == (reverse ? 0 : segments - 1)) return;  // nobody finds what this one leaves
   const int col0 = slice * S::COLS + wave * 16 * NT, cols = a.v.d;
 
+  MemStage<T, DK, S::XS, S::XP> x_rows, w_rows;
+  MemStage<T, 64 * NT, S::VS, S::VP> v_rows;
+  float g_next = 0.f;
+  const int64_t way = reverse ? -MEM_CHUNK : MEM_CHUNK;
+  const int64_t t_first = first + (int64_t)(reverse ? c1 - 1 : c0) * MEM_CHUNK;
+  if (!STATES) x_rows.begin(a.x, static_cast<const T*>(a.x.p) + head / a.x.group * a.x.head, t_first, 0);
+  w_rows.begin(a.w, static_cast<const T*>(a.w.p) + head / a.w.group * a.w.head, t_first, 0);
+  v_rows.begin(a.v, static_cast<const T*>(a.v.p) + head / a.v.group * a.v.head, t_first, slice * S::COLS);
+  const float* g_at = a.log_decay + (t_first + lane) * a.g_token + head * a.g_head;
+  const auto fetch = [&](int chunk) {
+    const int rows = min(MEM_CHUNK, n - chunk * MEM_CHUNK);
+    const bool whole = rows == MEM_CHUNK && a.w.d == DK && (slice + 1) * S::COLS <= cols;
+    if (!STATES) x_rows.fetch(rows, a.w.d, whole);
+    w_rows.fetch(rows, a.w.d, whole);
+    v_rows.fetch(rows, cols - slice * S::COLS, whole);
+    g_next = lane < rows ? *g_at : 0.f;
+    if (!STATES) x_rows.at += way * x_rows.token;
+    w_rows.at += way * w_rows.token;
+    v_rows.at += way * v_rows.token;
+    g_at += way * a.g_token;
+  };
+
+  if (c0 < c1) fetch(reverse ? c1 - 1 : c0);
   srv_floatx4 s[KT][NT] = {};
-  double grown = 0.0;
   if (!STATES) {
     const int64_t row = mem_begin(a.states, seq, n);
     const float* from = a.starts ? a.starts + (entry * a.heads + head) * a.dk * a.dv : row >= 0 ? a.states.in + (row * a.heads + head) * a.dk * a.dv : nullptr;
@@ -295,30 +399,19 @@ __global__ void __launch_bounds__(64 * MEM_WAVES) memory_chunk_kernel(const MemA
             if (i < a.x.d && j < cols) s[k][t][r] = from[(int64_t)i * a.s_row + (int64_t)j * a.s_col];
           }
   }
-  const T* xp = static_cast<const T*>(a.x.p) + (STATES ? 0 : head / a.x.group * a.x.head);
-  const T* wp = static_cast<const T*>(a.w.p) + head / a.w.group * a.w.head;
-  const T* vp = static_cast<const T*>(a.v.p) + head / a.v.group * a.v.head;
+  double grown = 0.0;
+  if (c0 < c1 && wave == 0) grown = mem_decays(g_next, lane, reverse, a.in_scale, a.up_scale, decays[0]);
 
-  for (int turn = c0; turn < c1; ++turn) {
-    const int chunk = a.reverse ? c1 - 1 - (turn - c0) : turn, at = chunk * MEM_CHUNK, rows = min(MEM_CHUNK, n - at);
+  for (int turn = 0; turn < c1 - c0; ++turn) {
+    const int chunk = reverse ? c1 - 1 - turn : c0 + turn, at = chunk * MEM_CHUNK, rows = min(MEM_CHUNK, n - at);
     const int64_t t0 = first + at;
-    __syncthreads();
-    if (!STATES) mem_fill<T, DK, S::XS>(xl, a.x, xp, t0, rows, 0, a.x.d);
-    mem_fill<T, DK, S::XS>(wl, a.w, wp, t0, rows, 0, a.w.d);
-    mem_fill<T, 64 * NT, S::VS>(vl, a.v, vp, t0, rows, slice * S::COLS, cols);
-    if (wave == 0) {
-      double sum = lane < rows ? mem_decay(a.log_decay[(t0 + lane) * a.g_token + head * a.g_head]) : 0.f;
-      sum = mem_decay_sums(sum, lane);
-      const double whole = __shfl(sum, 63, 64);
-      const float hi = (float)sum;
-      dl.hi[lane] = hi;
-      dl.lo[lane] = (float)(sum - hi);
-      const float since = expf((float)sum), left = expf((float)(whole - sum));
-      dl.in[lane] = a.in_scale * (a.reverse ? left : since);
-      dl.up[lane] = a.up_scale * (a.reverse ? since : left);
-      if (lane == 0) dl.whole = expf((float)whole);
-      grown += whole;
-    }
+    const MemDecays& dl = decays[turn & 1];
+    if (turn) __syncthreads();  // the last chunk has been read
+    if (!STATES) x_rows.put(xl);
+    w_rows.put(wl);
+    v_rows.put(vl);
+    const bool more = turn + 1 < c1 - c0;
+    if (more) fetch(reverse ? chunk - 1 : chunk + 1);
     __syncthreads();
 
     srv_floatx4 o[4][NT] = {};
@@ -342,28 +435,33 @@ __global__ void __launch_bounds__(64 * MEM_WAVES) memory_chunk_kernel(const MemA
             for (int p = IN - 1; p >= 0; --p) o[i][t] = mem_mma(part[t][p], x, o[i][t]);
         }
       }
-      // pairs: wavefront w has the products of rows 16 w .. with all
+      // pairs: wavefront w has the products of rows 16 w .. with all that these see
       srv_floatx4 z[4] = {};
 #pragma unroll
       for (int k = 0; k < DK / 32; ++k) {
         const T* row = xl + (16 * wave + c) * S::XS + 32 * k + 8 * g;
         const op_t x = mem_operand(row, row + 4);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const T* key = wl + (16 * j + c) * S::XS + 32 * k + 8 * g;
-          z[j] = mem_mma(mem_operand(key, key + 4), x, z[j]);
-        }
+        for (int j = 0; j < 4; ++j)
+          if (reverse ? j >= wave : j <= wave) {
+            const T* key = wl + (16 * j + c) * S::XS + 32 * k + 8 * g;
+            z[j] = mem_mma(mem_operand(key, key + 4), x, z[j]);
+          }
       }
-      __syncthreads();  // x has been read
+      if constexpr (!S::OWN) __syncthreads();  // x has been read
       const int i = 16 * wave + c;
+      const float own_hi = dl.hi[i], own_lo = dl.lo[i];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        float p[4];
+        float p[4] = {};
+        if (reverse ? j >= wave : j <= wave) {
+          const srv_floatx4 hi = *reinterpret_cast<const srv_floatx4*>(&dl.hi[16 * j + 4 * g]), lo = *reinterpret_cast<const srv_floatx4*>(&dl.lo[16 * j + 4 * g]);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int e = 16 * j + 4 * g + r;
-          const bool seen = a.reverse ? e >= i : e <= i;
-          p[r] = seen ? a.pair_scale * z[j][r] * (a.reverse ? mem_between(dl, e, i) : mem_between(dl, i, e)) : 0.f;
+          for (int r = 0; r < 4; ++r) {
+            const int e = 16 * j + 4 * g + r;
+            const bool seen = reverse ? e >= i : e <= i;
+            p[r] = seen ? a.pair_scale * z[j][r] * mem_between(own_hi, own_lo, hi[r], lo[r], sign) : 0.f;
+          }
         }
         mem_store4(pl + i * S::PS + 16 * j + 4 * g, p);
       }
@@ -371,7 +469,7 @@ __global__ void __launch_bounds__(64 * MEM_WAVES) memory_chunk_kernel(const MemA
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int t = 0; t < NT; ++t) o[i][t] *= dl.in[16 * i + c];
-      if (a.dot.p) {
+      if constexpr (DOTS) {
         const T* dot = static_cast<const T*>(a.dot.p) + head / a.dot.group * a.dot.head;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -388,30 +486,36 @@ __global__ void __launch_bounds__(64 * MEM_WAVES) memory_chunk_kernel(const MemA
           if (g == 0) meet[wave][16 * i + c] = sum;
         }
       }
-      __syncthreads();
-      if (a.dot.p && wave == 0 && lane < rows)
-        a.dots[((int64_t)slice * a.heads + head) * a.m.tokens + t0 + lane] = (meet[0][lane] + meet[1][lane]) + (meet[2][lane] + meet[3][lane]);
     }
     // the values, tokens side by side in a lane
     op_t v[2][NT];
-    bool bad = false;
+    float finite = 0.f;
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        v[k][t] = mem_column(vl + (32 * k + 8 * g) * S::VS + wave * 16 * NT + 16 * t + c, S::VS);
+        v[k][t] = mem_column(vl + (32 * k + 8 * g) * S::VS + wave * 16 * NT + 16 * t, S::VS, c);
+        if constexpr (!STATES)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) bad |= !isfinite(mem_entry(v[k][t], e));
+          for (int e = 0; e < 8; ++e) finite = fmaf(mem_entry(v[k][t], e), 0.f, finite);  // NaN once one is not
       }
-    const bool any_bad = __builtin_amdgcn_ballot_w64(bad) != 0;
+    if (more && wave == ((turn + 1) & 3)) {
+      const double whole = mem_decays(g_next, lane, reverse, a.in_scale, a.up_scale, decays[(turn + 1) & 1]);
+      grown += whole;
+    }
     if constexpr (!STATES) {
+      __syncthreads();
+      if constexpr (DOTS)
+        if (wave == 0 && lane < rows)
+          a.dots[((int64_t)slice * a.heads + head) * a.m.tokens + t0 + lane] = (meet[0][lane] + meet[1][lane]) + (meet[2][lane] + meet[3][lane]);
+      const bool bad = __builtin_amdgcn_ballot_w64(finite != 0.f) != 0;
       op_t clean[2][NT];
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           clean[k][t] = v[k][t];
-          if (any_bad) {  // a weight of 0 times NaN would be NaN
+          if (bad) {  // a weight of 0 times NaN would be NaN
             float x[8];
             op_t y[1];
 #pragma unroll
@@ -423,13 +527,14 @@ __global__ void __launch_bounds__(64 * MEM_WAVES) memory_chunk_kernel(const MemA
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const T* row = pl + (16 * i + c) * S::PS + 32 * k + 8 * g;
-          const op_t p = mem_operand(row, row + 4);
+        for (int k = 0; k < 2; ++k)
+          if (reverse ? 2 * k + 1 >= i : 2 * k <= i) {
+            const T* row = pl + (16 * i + c) * S::PS + 32 * k + 8 * g;
+            const op_t p = mem_operand(row, row + 4);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) o[i][t] = mem_mma(clean[k][t], p, o[i][t]);
-        }
-      if (any_bad)
+            for (int t = 0; t < NT; ++t) o[i][t] = mem_mma(clean[k][t], p, o[i][t]);
+          }
+      if (bad)
         for (int j = 0; j < rows; ++j)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -438,7 +543,7 @@ __global__ void __launch_bounds__(64 * MEM_WAVES) memory_chunk_kernel(const MemA
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
                 const float y = srv_widen(vl[j * S::VS + wave * 16 * NT + 16 * t + 4 * g + r]);
-                const bool seen = a.reverse ? j >= 16 * i + c : j <= 16 * i + c;
+                const bool seen = reverse ? j >= 16 * i + c : j <= 16 * i + c;
                 if (seen && !isfinite(y)) o[i][t][r] += srv_widen(pl[(16 * i + c) * S::PS + j]) * y;
               }
 #pragma unroll
@@ -448,9 +553,8 @@ __global__ void __launch_bounds__(64 * MEM_WAVES) memory_chunk_kernel(const MemA
           const int e = col0 + 16 * t + 4 * g;
           if (16 * i + c >= rows || e >= cols) continue;
           const int64_t to = (t0 + 16 * i + c) * a.out_token + head * a.out_head + e;
-          const float y[4] = {o[i][t][0], o[i][t][1], o[i][t][2], o[i][t][3]};
-          if (a.out_float) srv_st<float, 4>(static_cast<float*>(a.out) + to, a.out_vec, y);
-          else srv_st<T, 4>(static_cast<T*>(a.out) + to, a.out_vec, y);
+          if (DOTS && a.out_float) mem_out4(static_cast<float*>(a.out) + to, o[i][t]);
+          else mem_out4(static_cast<T*>(a.out) + to, o[i][t]);
         }
     }
     // the state
@@ -461,21 +565,22 @@ __global__ void __launch_bounds__(64 * MEM_WAVES) memory_chunk_kernel(const MemA
       for (int t = 0; t < NT; ++t) s[k][t] *= whole;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      op_t part[NT][UP];
+      const srv_floatx4 u0 = *reinterpret_cast<const srv_floatx4*>(&dl.up[32 * h + 8 * g]), u1 = *reinterpret_cast<const srv_floatx4*>(&dl.up[32 * h + 8 * g + 4]);
+      op_t up[NT][UP];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = mem_entry(v[h][t], e) * dl.up[32 * h + 8 * g + e];
-        mem_split<UP>(x, part[t]);
+        for (int e = 0; e < 8; ++e) x[e] = mem_entry(v[h][t], e) * (e < 4 ? u0[e & 3] : u1[e & 3]);
+        mem_split<UP>(x, up[t]);
       }
 #pragma unroll
       for (int k = 0; k < KT; ++k) {
-        const op_t w = mem_column(wl + (32 * h + 8 * g) * S::XS + 16 * k + c, S::XS);
+        const op_t w = mem_column(wl + (32 * h + 8 * g) * S::XS + 16 * k, S::XS, c);
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-          for (int p = UP - 1; p >= 0; --p) s[k][t] = mem_mma(w, part[t][p], s[k][t]);
+          for (int p = UP - 1; p >= 0; --p) s[k][t] = mem_mma(w, up[t][p], s[k][t]);
       }
     }
   }
@@ -483,8 +588,12 @@ __global__ void __launch_bounds__(64 * MEM_WAVES) memory_chunk_kernel(const MemA
   bool none = false;
   if (STATES) {
     to = a.added + (entry * a.heads + head) * a.dk * a.dv;
-    if (threadIdx.x == 0 && slice == 0) a.faded[entry * a.heads + head] = expf((float)grown);
-  } else if (segment == (a.reverse ? 0 : segments - 1)) {
+    // each wavefront has the sums of every fourth chunk
+    double* const all = reinterpret_cast<double*>(&meet[0][0]);
+    if (lane == 0) all[wave] = grown;
+    __syncthreads();
+    if (threadIdx.x == 0 && slice == 0) a.faded[entry * a.heads + head] = exp2f((float)((all[0] + all[1]) + (all[2] + all[3])));
+  } else if (segment == (reverse ? 0 : segments - 1)) {
     const int64_t row = mem_end(a.states, seq);
     if (row >= 0) to = a.states.out + (row * a.heads + head) * a.dk * a.dv;
     none = a.ruled && mem_begin(a.rule, seq, n) < 0;

@@ -27,15 +27,16 @@ struct MemDecayArgs {
   double* sums;                 // (entries, heads): sums over tokens instead
 };
 
-template <typename T>
-__device__ __forceinline__ typename MemOperand<T>::type mem_global(const T* p, bool vec, bool there);
-template <>
-__device__ __forceinline__ srv_bf16x8 mem_global(const unsigned short* p, bool vec, bool there) { return there ? srv_ld8_bf16(p, vec) : srv_bf16x8{}; }
-template <>
-__device__ __forceinline__ mem_float8 mem_global(const float* p, bool vec, bool there) {
-  mem_float8 x = {};
-  if (there) srv_ld8(p, vec, x.x);
-  return x;
+// eight numbers of a row in memory, or zeros
+__device__ __forceinline__ srv_bf16x8 mem_global(const unsigned short* p, bool there) {
+  MemEight<unsigned short> x = {};
+  if (there) mem_fetch(p, x);
+  return __builtin_bit_cast(srv_bf16x8, x.x);
+}
+__device__ __forceinline__ mem_float8 mem_global(const float* p, bool there) {
+  MemEight<float> x = {};
+  if (there) mem_fetch(p, x);
+  return {{x.x[0][0], x.x[0][1], x.x[0][2], x.x[0][3], x.x[1][0], x.x[1][1], x.x[1][2], x.x[1][3]}};
 }
 
 // sum_{j < t <= i} m_ij for the tokens t of one chunk of one head: its steps are column sums below and row sums left of the diagonal.
@@ -54,9 +55,7 @@ __global__ void __launch_bounds__(256) memory_pairs_kernel(const MemDecayArgs a)
   const int rows = min(MEM_CHUNK, n - chunk * MEM_CHUNK);
   if (rows <= 0) return;
   if (wave == 0) {
-    const double sum = mem_decay_sums(lane < rows ? mem_decay(a.log_decay[(t0 + lane) * a.g_token + head * a.g_head]) : 0.f, lane);
-    dl.hi[lane] = (float)sum;
-    dl.lo[lane] = (float)(sum - (float)sum);
+    mem_decays(lane < rows ? a.log_decay[(t0 + lane) * a.g_token + head * a.g_head] : 0.f, lane, false, 1.f, 1.f, dl);
   }
   srv_floatx4 z[2][4] = {};
   const auto products = [&](const MemRows& late, const MemRows& early, srv_floatx4 (&to)[4]) {
@@ -64,23 +63,24 @@ __global__ void __launch_bounds__(256) memory_pairs_kernel(const MemDecayArgs a)
     const T* y = static_cast<const T*>(early.p) + head / early.group * early.head + t0 * early.token;
     const int i = 16 * wave + c;
     for (int e = 8 * g; e < ((late.d + 31) & ~31); e += 32) {
-      const op_t b = mem_global(x + i * late.token + e, late.vec, i < rows && e < late.d);
+      const op_t b = mem_global(x + i * late.token + e, i < rows && e < late.d);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        to[j] = mem_mma(mem_global(y + (16 * j + c) * early.token + e, early.vec, 16 * j + c < rows && e < early.d), b, to[j]);
+        to[j] = mem_mma(mem_global(y + (16 * j + c) * early.token + e, 16 * j + c < rows && e < early.d), b, to[j]);
     }
   };
   products(a.q, a.k, z[0]);
   products(a.gout, a.v, z[1]);
   __syncthreads();
   const int i = 16 * wave + c;
+  const float own_hi = dl.hi[i], own_lo = dl.lo[i];
   float row = 0.f;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int e = 16 * j + 4 * g + r;
-      float x = e < i ? a.scale * z[0][j][r] * z[1][j][r] * mem_between(dl, i, e) : 0.f;
+      float x = e < i ? a.scale * z[0][j][r] * z[1][j][r] * mem_between(own_hi, own_lo, dl.hi[e], dl.lo[e], 1.f) : 0.f;
       row += x;
 #pragma unroll
       for (int o = 1; o < 16; o <<= 1) x += __shfl_xor(x, o, 64);
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(256) memory_pairs_kernel(const MemDecayArgs a)
   __syncthreads();
   if (wave == 0) {
     const double step = (double)((below[0][lane] + below[1][lane]) + (below[2][lane] + below[3][lane])) - left[lane];
-    const double sum = mem_decay_sums(step, lane) - step;
+    const double sum = mem_sums(step) - step;
     if (lane < rows) a.pairs[head * a.m.tokens + t0 + lane] = (float)sum;
   }
 }
@@ -146,7 +146,7 @@ static __global__ void __launch_bounds__(MEM_SUM_THREADS) memory_decay_kernel(co
     double step = 0.0;
     if (real)
       for (int s = 0; s < a.slices; ++s) step += (double)a.b[s * a.heads * a.m.tokens + t] - a.a[s * a.heads * a.m.tokens + t];
-    double sum = mem_decay_sums(step, lane);
+    double sum = mem_sums(step);
     __syncthreads();
     if (lane == 63) meet[1][wave] = sum;
     __syncthreads();
@@ -193,8 +193,7 @@ __global__ void __launch_bounds__(256) memory_heads_kernel(const MemSequences m,
     const int e = i % (d / 4) * 4;
     srv_floatx4 x = {};
     for (int h = 0; h < group; ++h) x += *reinterpret_cast<const srv_floatx4*>(parts + (row * group + h) * d + e);
-    const float y[4] = {x[0], x[1], x[2], x[3]};
-    srv_st<T, 4>(out + row * d + e, ((uint64_t)out & 15) == 0, y);
+    mem_out4(out + row * d + e, x);
   }
 }
 

@@ -11,13 +11,13 @@ hipError_t launch_linear_attention(const ttc_linear_attention_t& a, int cus, voi
 uint64_t linear_attention_backward_workspace(const ttc_linear_attention_backward_t& b, int cus);
 hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_t& b, int cus, void* workspace, hipStream_t st);
 
-hipError_t launch_residual_norm(const ttc_residual_norm_t& n, hipStream_t st);
+hipError_t launch_residual_norm(const ttc_residual_norm_t& n, int cus, hipStream_t st);
 uint64_t norm_backward_workspace(const ttc_residual_norm_backward_t& b, int cus);
 hipError_t launch_residual_norm_backward(const ttc_residual_norm_backward_t& b, int cus, void* workspace, hipStream_t st);
 
-// rows of x and w of up to D entries; what is added to states alone, or everything
+// rows of x and w of up to D entries; what: a MemWhat
 struct MemArgs;
-template <int D> hipError_t launch_memory_chunks(const MemArgs& a, bool bf16, bool wide, bool states, uint32_t grid, hipStream_t st);
+template <int D> hipError_t launch_memory_chunks(const MemArgs& a, bool bf16, bool wide, int what, uint32_t grid, hipStream_t st);
 template <int D> hipError_t launch_memory_step(const MemArgs& a, bool bf16, uint32_t grid, hipStream_t st);
 
 }  // namespace ttc

@@ -1,6 +1,7 @@
 // The norms, the gate and the residual scale around a block (ttc_residual_norm, ttc_residual_norm_backward).  Every row is read once and
 // written once: the memory's rate bounds both.  A row is spread over LANES threads of a workgroup, eight features side by side to a thread and
-// PIECES such eights, and stays in registers between the sums that its norms need.
+// PIECES such eights, and stays in registers between the sums that its norms need.  Workgroups walk the rows: what belongs to the features (gains,
+// offsets, sums over tokens) stays in registers, and the next row is under way while one is worked on.
 #pragma once
 #include "../../include/ttc_memory.h"
 #include "ttc_serve.hpp"
@@ -12,8 +13,7 @@ struct NormArgs {
   const void *gr, *gh;
   int64_t gr_token, gh_token;
   void *gy, *ggate, *gresidual;
-  float* part[5];     // sums of one row of workgroups' threads each: post_gain, post_offset, residual_gain, pre_gain, pre_offset
-  int32_t parts;      // rows of a part
+  float* part[5];     // sums over a workgroup's rows: post_gain, post_offset, residual_gain, pre_gain, pre_offset
   int32_t group;      // features of a group
   uint8_t vec;        // rows of 16-byte alignment: bits by NormRow
 };
@@ -22,72 +22,142 @@ enum NormRow { ROW_Y, ROW_GATE, ROW_RESIDUAL, ROW_R, ROW_H };  // gr as r, gh as
 template <int LANES, int PIECES>
 struct NormShape {
   static constexpr int THREADS = LANES < 256 ? 256 : LANES;
-  static constexpr int ROWS = THREADS / LANES;  // of a workgroup
-  static constexpr int WAVES = LANES / 64;      // of a row
+  static constexpr int ROWS = THREADS / LANES;  // of a workgroup at once
 };
 
-// Sum over the LANES threads of a row, the same in all of them
-template <int LANES>
-__device__ __forceinline__ float norm_sum(float x, float* lds) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o, 64);
-  if constexpr (LANES > 64) {
-    __syncthreads();  // the last sum's readers are done
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = 0.f;
-#pragma unroll
-    for (int w = 0; w < LANES / 64; ++w) x += lds[w];
-  }
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ float norm_dpp(float x) {  // the number of another lane, 0 where there is none
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, ROWS, 0xf, true));
+}
+
+// Sum over a wavefront
+__device__ __forceinline__ float norm_wave_sum(float x) {
+  x += norm_dpp<0x111>(x);       // one to the right within 16 lanes, then two, four, eight
+  x += norm_dpp<0x112>(x);
+  x += norm_dpp<0x114>(x);
+  x += norm_dpp<0x118>(x);
+  x += norm_dpp<0x142, 0xa>(x);  // lane 15 to the next 16, lane 31 to the upper half
+  x += norm_dpp<0x143, 0xc>(x);
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+// Sums over aligned sets of `lanes` lanes, a power of two
+__device__ __forceinline__ float norm_lanes_sum(float x, int lanes) {
+  if (lanes >= 2) x += norm_dpp<0xb1>(x);    // neighbours
+  if (lanes >= 4) x += norm_dpp<0x4e>(x);    // pairs of them
+  if (lanes >= 8) x += norm_dpp<0x141>(x);   // eight mirrored
+  if (lanes >= 16) x += norm_dpp<0x140>(x);  // sixteen mirrored
+  if (lanes >= 32) x += __shfl_xor(x, 16, 64);
+  if (lanes >= 64) x += __shfl_xor(x, 32, 64);
   return x;
 }
 
-// Sums over each group of the features that a thread's pieces belong to, in place.  Groups of 8, 16, .. 512 features lie within a wavefront;
-// others meet in LDS.
 template <int LANES, int PIECES>
-__device__ __forceinline__ void norm_group_sums(float (&x)[PIECES], const NormArgs& a, float* lds, float* pieces) {
-  if (a.n.groups == 1) {
-    float whole = 0.f;
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) whole += x[i];
-    whole = norm_sum<LANES>(whole, lds);
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) x[i] = whole;
-    return;
-  }
-  const int eights = a.group / 8;
-  if (eights <= 64 && (eights & (eights - 1)) == 0) {
-    for (int o = 1; o < eights; o <<= 1)
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) x[i] += __shfl_xor(x[i], o, 64);
-    return;
-  }
-  const int at = threadIdx.x % LANES, row = threadIdx.x / LANES;
-  float* mine = pieces + row * (LANES * PIECES);
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < PIECES; ++i) mine[i * LANES + at] = x[i];
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < PIECES; ++i) {
-    const int e = i * LANES + at, first = e / eights * eights;
-    float sum = 0.f;
-    if (e * 8 < a.n.features)
-      for (int k = 0; k < eights; ++k) sum += mine[first + k];
-    x[i] = sum;
-  }
-}
+struct NormSums {
+  typedef NormShape<LANES, PIECES> S;
+  float (*meet)[16][2];  // two, in turn: a sum's writers need not wait for the readers of the last
+  float* pieces;         // THREADS * PIECES
+  int turn = 0;
 
-// eight features from `e` on; those behind the last are 0
-template <typename T>
-__device__ __forceinline__ void norm_load(const T* row, int e, int features, bool vec, float (&x)[8]) {
-  if (e + 8 <= features) {
-    srv_ld8(row + e, vec, x);
+  // N sums over the LANES threads of a row, the same in all of them
+  template <int N>
+  __device__ __forceinline__ void row(float (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = norm_wave_sum(x[i]);
+    if constexpr (LANES > 64) {
+      if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) meet[turn][threadIdx.x >> 6][i] = x[i];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        x[i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < LANES / 64; ++w) x[i] += meet[turn][threadIdx.x / LANES * (LANES / 64) + w][i];
+      }
+      turn ^= 1;
+    }
+  }
+
+  // Sums over the group that each of a thread's pieces belongs to, in place.  Groups of 8, 16, .. 512 features lie within a wavefront; others
+  // meet in LDS.
+  __device__ __forceinline__ void group(float (&x)[PIECES], const NormArgs& a) {
+    const int eights = a.group / 8;
+    if (eights <= 64 && (eights & (eights - 1)) == 0) {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) x[i] = norm_lanes_sum(x[i], eights);
+      return;
+    }
+    const int at = threadIdx.x % LANES;
+    float* mine = pieces + threadIdx.x / LANES * (LANES * PIECES);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) mine[i * LANES + at] = x[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int e = i * LANES + at, first = e / eights * eights;
+      float sum = 0.f;
+      if (e * 8 < a.n.features)
+        for (int k = 0; k < eights; ++k) sum += mine[first + k];
+      x[i] = sum;
+    }
+  }
+
+  // Sums of two numbers of every piece (the second only if `both`) over a row or over each group
+  __device__ __forceinline__ void pair(float (&x)[PIECES], float (&y)[PIECES], bool both, const NormArgs& a, bool grouped) {
+    if (grouped && a.n.groups > 1) {
+      group(x, a);
+      if (both) group(y, a);
+      return;
+    }
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      s[0] += x[i];
+      s[1] += y[i];
+    }
+    if (both) {
+      row(s);
+    } else {
+      float t[1] = {s[0]};
+      row(t);
+      s[0] = t[0];
+    }
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      x[i] = s[0];
+      y[i] = s[1];
+    }
+  }
+};
+
+// ---- rows ---------------------------------------------------------------------------------------------------------------
+
+// eight features as they lie in memory
+template <typename T> struct NormEight;
+template <> struct NormEight<unsigned short> { srv_u16x8 x; };
+template <> struct NormEight<float> { srv_floatx4 x[2]; };
+
+__device__ __forceinline__ void norm_fetch(const unsigned short* p, int e, int features, bool vec, NormEight<unsigned short>& to) {
+  if (vec && e + 8 <= features) {
+    to.x = __builtin_nontemporal_load(reinterpret_cast<const srv_u16x8*>(p + e));
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = e + k < features ? srv_widen(row[e + k]) : 0.f;
+    for (int k = 0; k < 8; ++k) to.x[k] = e + k < features ? p[e + k] : 0;
   }
 }
+__device__ __forceinline__ void norm_fetch(const float* p, int e, int features, bool vec, NormEight<float>& to) {
+  if (vec && e + 8 <= features) {
+    to.x[0] = __builtin_nontemporal_load(reinterpret_cast<const srv_floatx4*>(p + e));
+    to.x[1] = __builtin_nontemporal_load(reinterpret_cast<const srv_floatx4*>(p + e + 4));
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) to.x[k / 4][k % 4] = e + k < features ? p[e + k] : 0.f;
+  }
+}
+__device__ __forceinline__ float norm_entry(const NormEight<unsigned short>& v, int k) { return srv_widen(v.x[k]); }
+__device__ __forceinline__ float norm_entry(const NormEight<float>& v, int k) { return v.x[k / 4][k % 4]; }
+
 template <typename T>
 __device__ __forceinline__ void norm_store(T* row, int e, int features, bool vec, const float (&x)[8]) {
   if (e + 8 <= features) {
@@ -100,58 +170,46 @@ __device__ __forceinline__ void norm_store(T* row, int e, int features, bool vec
 }
 // of a vector of float32 numbers that every row reads, or `none` where there is no vector
 __device__ __forceinline__ void norm_vector(const float* v, float none, int e, int features, float (&x)[8]) {
-  if (!v) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = none;
+  if (v && e + 8 <= features) {
+    srv_ld8(v + e, (uint64_t)v % 16 == 0, x);
   } else {
-    norm_load(v, e, features, (uint64_t)v % 16 == 0, x);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = v && e + k < features ? v[e + k] : none;
   }
 }
 
-// x -> (x - mean) / sqrt(mean square + eps) by groups; inverse: the factor.  The mean goes first, so that the squares are those of differences.
+// x -> (x - mean) / sqrt(mean square + eps); inverse: the factor.  The mean goes first, so that the squares are those of differences.
 template <int LANES, int PIECES>
-__device__ __forceinline__ void norm_unit(float (&x)[PIECES][8], int kind, float eps, const NormArgs& a, bool grouped, float (&inverse)[PIECES], float* lds,
-                                          float* pieces) {
+__device__ __forceinline__ void norm_unit(float (&x)[PIECES][8], int kind, float eps, const NormArgs& a, bool grouped, float (&inverse)[PIECES],
+                                          NormSums<LANES, PIECES>& sums) {
   const int at = threadIdx.x % LANES;
-  const float n = (float)(grouped ? a.group : a.n.features);
-  const auto sums = [&](float (&s)[PIECES]) {
-    if (grouped) {
-      norm_group_sums<LANES, PIECES>(s, a, lds, pieces);
-    } else {
-      float whole = 0.f;
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) whole += s[i];
-      whole = norm_sum<LANES>(whole, lds);
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) s[i] = whole;
-    }
-  };
+  const float share = 1.f / (float)(grouped ? a.group : a.n.features);
+  float s[PIECES], none[PIECES] = {};
   if (kind == TTC_NORM_LAYER) {
-    float s[PIECES];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       s[i] = 0.f;
 #pragma unroll
       for (int k = 0; k < 8; ++k) s[i] += x[i][k];
     }
-    sums(s);
+    sums.pair(s, none, false, a, grouped);
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const int e = (i * LANES + at) * 8;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[i][k] = e + k < a.n.features ? x[i][k] - s[i] / n : 0.f;
+      for (int k = 0; k < 8; ++k) x[i][k] = e + k < a.n.features ? x[i][k] - s[i] * share : 0.f;
     }
   }
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
-    inverse[i] = 0.f;
+    s[i] = 0.f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) inverse[i] += x[i][k] * x[i][k];
+    for (int k = 0; k < 8; ++k) s[i] += x[i][k] * x[i][k];
   }
-  sums(inverse);
+  sums.pair(s, none, false, a, grouped);
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
-    inverse[i] = 1.f / sqrtf(inverse[i] / n + eps);
+    inverse[i] = rsqrtf(s[i] * share + eps);
 #pragma unroll
     for (int k = 0; k < 8; ++k) x[i][k] *= inverse[i];
   }
@@ -160,8 +218,8 @@ __device__ __forceinline__ void norm_unit(float (&x)[PIECES][8], int kind, float
 // A gradient with respect to unit entries becomes one with respect to the entries: inverse * (g - mean g [layer norm] - unit * mean (g * unit))
 template <int LANES, int PIECES>
 __device__ __forceinline__ void norm_unit_backward(float (&g)[PIECES][8], const float (&unit)[PIECES][8], const float (&inverse)[PIECES], int kind,
-                                                   const NormArgs& a, bool grouped, float* lds, float* pieces) {
-  const float n = (float)(grouped ? a.group : a.n.features);
+                                                   const NormArgs& a, bool grouped, NormSums<LANES, PIECES>& sums) {
+  const float share = 1.f / (float)(grouped ? a.group : a.n.features);
   float along[PIECES], mean[PIECES];
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
@@ -172,202 +230,250 @@ __device__ __forceinline__ void norm_unit_backward(float (&g)[PIECES][8], const 
       mean[i] += g[i][k];
     }
   }
-  const auto sums = [&](float (&s)[PIECES]) {
-    if (grouped) {
-      norm_group_sums<LANES, PIECES>(s, a, lds, pieces);
-    } else {
-      float whole = 0.f;
+  const bool layer = kind == TTC_NORM_LAYER;
+  sums.pair(along, mean, layer, a, grouped);
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) whole += s[i];
-      whole = norm_sum<LANES>(whole, lds);
+  for (int i = 0; i < PIECES; ++i) {
+    const float l = along[i] * share;
+    if (layer) {
+      const int e = (i * LANES + threadIdx.x % LANES) * 8;
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) s[i] = whole;
+      for (int k = 0; k < 8; ++k) g[i][k] -= e + k < a.n.features ? mean[i] * share : 0.f;
     }
-  };
-  sums(along);
-  if (kind == TTC_NORM_LAYER) sums(mean);
 #pragma unroll
-  for (int i = 0; i < PIECES; ++i)
-#pragma unroll
-    for (int k = 0; k < 8; ++k) g[i][k] = inverse[i] * (g[i][k] - (kind == TTC_NORM_LAYER ? mean[i] / n : 0.f) - unit[i][k] * (along[i] / n));
+    for (int k = 0; k < 8; ++k) g[i][k] = inverse[i] * (g[i][k] - unit[i][k] * l);
+  }
 }
 
-// act(x) and its derivative, from exp(-|x|), which never overflows; c = 1 - s comes without a cancellation.  Where a factor is 0 so is the
-// product, of an infinite x too.
+// act(x) and its derivative, from exp(-|x|), which never overflows; c = 1 - s comes without a cancellation.  Beyond 200 all is 0 or 1 in
+// float32, and infinities there would meet zeros; NaN stays.  The exponential is (1 + |x|) 2^-24 of itself off, the reciprocal a step.
 __device__ __forceinline__ void norm_act(int act, float x, float& y, float& slope) {
   if (act == TTC_GATE_IDENTITY) {
     y = x;
     slope = 1.f;
     return;
   }
-  const float e = expf(-fabsf(x)), d = 1.f / (1.f + e), s = x < 0.f ? e * d : d, c = x < 0.f ? d : e * d;
+  const float low = x < -200.f ? -200.f : x, near = low > 200.f ? 200.f : low;
+  const float e = __builtin_amdgcn_exp2f(fabsf(near) * -1.44269504088896340736f), d = __builtin_amdgcn_rcpf(1.f + e), f = e * d;
+  const float s = x < 0.f ? f : d, c = x < 0.f ? d : f;
   if (act == TTC_GATE_SIGMOID) {
     y = s;
     slope = s * c;
   } else {
-    y = s == 0.f ? 0.f : x * s;
-    slope = s == 0.f || c == 0.f ? s : s + x * s * c;
+    y = low * s;
+    slope = s + near * s * c;
   }
 }
 
 template <typename T, int LANES, int PIECES>
 __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_norm_kernel(const NormArgs a) {
   typedef NormShape<LANES, PIECES> S;
-  __shared__ float lds[16];
+  __shared__ float meet[2][16][2];
   __shared__ float pieces[S::THREADS * PIECES];
+  NormSums<LANES, PIECES> sums = {meet, pieces};
   const int at = threadIdx.x % LANES, c = a.n.features;
-  const int64_t token = (int64_t)blockIdx.x * S::ROWS + threadIdx.x / LANES;
-  const bool real = token < a.n.tokens;
-  const int64_t t = real ? token : 0;  // (a wavefront behind the last row works on the first for nothing)
-  const T* y = static_cast<const T*>(a.n.y) + t * a.n.y_token;
-  const T* gate = a.n.gate ? static_cast<const T*>(a.n.gate) + t * a.n.gate_token : nullptr;
-  const T* residual = a.n.residual ? static_cast<const T*>(a.n.residual) + t * a.n.residual_token : nullptr;
-  float x[PIECES][8], g[PIECES][8], r[PIECES][8], inverse[PIECES];
+  const int64_t step = (int64_t)gridDim.x * S::ROWS;
+  float post_gain[PIECES][8], post_offset[PIECES][8], by[PIECES][8], pre_gain[PIECES][8], pre_offset[PIECES][8];
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
     const int e = (i * LANES + at) * 8;
-    norm_load(y, e, c, a.vec >> ROW_Y & 1, x[i]);
-    if (gate) norm_load(gate, e, c, a.vec >> ROW_GATE & 1, g[i]);
-    if (residual) norm_load(residual, e, c, a.vec >> ROW_RESIDUAL & 1, r[i]);
+    norm_vector(a.n.post ? a.n.post_gain : nullptr, 1.f, e, c, post_gain[i]);
+    norm_vector(a.n.post ? a.n.post_offset : nullptr, 0.f, e, c, post_offset[i]);
+    norm_vector(a.n.residual_gain, 1.f, e, c, by[i]);
+    norm_vector(a.n.pre_gain, 1.f, e, c, pre_gain[i]);
+    norm_vector(a.n.pre_offset, 0.f, e, c, pre_offset[i]);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) by[i][k] *= a.n.scale;
   }
-  if (a.n.post) norm_unit<LANES, PIECES>(x, a.n.post, a.n.post_eps, a, true, inverse, lds, pieces);
+  NormEight<T> y[PIECES], gate[PIECES], residual[PIECES];
+  const auto fetch = [&](int64_t t) {  // (behind the last row: the last once more, for nothing)
+    t = t < a.n.tokens ? t : a.n.tokens - 1;
 #pragma unroll
-  for (int i = 0; i < PIECES; ++i) {
-    const int e = (i * LANES + at) * 8;
-    float gain[8], offset[8], by[8];
-    norm_vector(a.n.post ? a.n.post_gain : nullptr, 1.f, e, c, gain);
-    norm_vector(a.n.post ? a.n.post_offset : nullptr, 0.f, e, c, offset);
-    norm_vector(a.n.residual_gain, 1.f, e, c, by);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      float z = x[i][k] * gain[k] + offset[k], act, slope;
-      if (gate) {
-        norm_act(a.n.act, g[i][k], act, slope);
-        z *= act;
-      }
-      z *= a.n.scale * by[k];
-      x[i][k] = e + k < c ? (residual ? r[i][k] + z : z) : 0.f;
+    for (int i = 0; i < PIECES; ++i) {
+      const int e = (i * LANES + at) * 8;
+      norm_fetch(static_cast<const T*>(a.n.y) + t * a.n.y_token, e, c, a.vec >> ROW_Y & 1, y[i]);
+      if (a.n.gate) norm_fetch(static_cast<const T*>(a.n.gate) + t * a.n.gate_token, e, c, a.vec >> ROW_GATE & 1, gate[i]);
+      if (a.n.residual) norm_fetch(static_cast<const T*>(a.n.residual) + t * a.n.residual_token, e, c, a.vec >> ROW_RESIDUAL & 1, residual[i]);
     }
-    if (real && a.n.r) norm_store(static_cast<T*>(a.n.r) + t * a.n.r_token, e, c, a.vec >> ROW_R & 1, x[i]);
-  }
-  if (!a.n.pre) return;
-  norm_unit<LANES, PIECES>(x, a.n.pre, a.n.pre_eps, a, false, inverse, lds, pieces);
-  if (!real) return;
+  };
+  int64_t first = (int64_t)blockIdx.x * S::ROWS;
+  fetch(first + threadIdx.x / LANES);
+  for (; first < a.n.tokens; first += step) {
+    const int64_t t = first + threadIdx.x / LANES;
+    const bool real = t < a.n.tokens;
+    float x[PIECES][8], g[PIECES][8], r[PIECES][8], inverse[PIECES];
 #pragma unroll
-  for (int i = 0; i < PIECES; ++i) {
-    const int e = (i * LANES + at) * 8;
-    float gain[8], offset[8];
-    norm_vector(a.n.pre_gain, 1.f, e, c, gain);
-    norm_vector(a.n.pre_offset, 0.f, e, c, offset);
+    for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[i][k] = x[i][k] * gain[k] + offset[k];
-    norm_store(static_cast<T*>(a.n.h) + t * a.n.h_token, e, c, a.vec >> ROW_H & 1, x[i]);
+      for (int k = 0; k < 8; ++k) {
+        x[i][k] = norm_entry(y[i], k);
+        if (a.n.gate) g[i][k] = norm_entry(gate[i], k);
+        r[i][k] = a.n.residual ? norm_entry(residual[i], k) : 0.f;
+      }
+    if (first + step < a.n.tokens) fetch(t + step);
+    if (a.n.post) norm_unit<LANES, PIECES>(x, a.n.post, a.n.post_eps, a, true, inverse, sums);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int e = (i * LANES + at) * 8;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        float z = x[i][k] * post_gain[i][k] + post_offset[i][k], act, slope;
+        if (a.n.gate) {
+          norm_act(a.n.act, g[i][k], act, slope);
+          z *= act;
+        }
+        x[i][k] = r[i][k] + by[i][k] * z;  // (0 behind the last feature: so are all its terms)
+      }
+      if (real && a.n.r) norm_store(static_cast<T*>(a.n.r) + t * a.n.r_token, e, c, a.vec >> ROW_R & 1, x[i]);
+    }
+    if (!a.n.pre) continue;
+    norm_unit<LANES, PIECES>(x, a.n.pre, a.n.pre_eps, a, false, inverse, sums);
+    if (!real) continue;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[i][k] = x[i][k] * pre_gain[i][k] + pre_offset[i][k];
+      norm_store(static_cast<T*>(a.n.h) + t * a.n.h_token, (i * LANES + at) * 8, c, a.vec >> ROW_H & 1, x[i]);
+    }
   }
 }
 
-// Workgroups walk the rows with the sums over tokens in registers and leave one part of each sum for norm_parts_kernel: which rows make a
-// part depends on the sizes alone.
+// The sums over tokens stay in registers; a workgroup leaves one part of each for norm_parts_kernel, and which rows make a part depends on the
+// sizes alone.
 template <typename T, int LANES, int PIECES>
 __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_norm_backward_kernel(const NormArgs a) {
   typedef NormShape<LANES, PIECES> S;
-  __shared__ float lds[16];
-  __shared__ float pieces[S::THREADS * PIECES];
+  constexpr int WIDTH = LANES * PIECES * 8;
+  __shared__ float meet[2][16][2];
+  __shared__ float pieces[S::ROWS > 1 ? S::ROWS * WIDTH : S::THREADS * PIECES];
+  NormSums<LANES, PIECES> sums = {meet, pieces};
   const int at = threadIdx.x % LANES, c = a.n.features, post = a.n.post, pre = a.n.pre;
-  float sums[5][PIECES][8] = {};
-  for (int64_t first = (int64_t)blockIdx.x * S::ROWS; first < a.n.tokens; first += (int64_t)gridDim.x * S::ROWS) {
-    const int64_t token = first + threadIdx.x / LANES;
-    const bool real = token < a.n.tokens;
-    const int64_t t = real ? token : first;
-    float x[PIECES][8], act[PIECES][8], slope[PIECES][8], total[PIECES][8], gh[PIECES][8], r[PIECES][8], inverse[PIECES];
+  const int64_t step = (int64_t)gridDim.x * S::ROWS;
+  float total_of[5][PIECES][8] = {};
+  float post_gain[PIECES][8], post_offset[PIECES][8], by[PIECES][8], pre_gain[PIECES][8];
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) {
+    const int e = (i * LANES + at) * 8;
+    norm_vector(post ? a.n.post_gain : nullptr, 1.f, e, c, post_gain[i]);
+    norm_vector(post ? a.n.post_offset : nullptr, 0.f, e, c, post_offset[i]);
+    norm_vector(a.n.residual_gain, 1.f, e, c, by[i]);
+    norm_vector(a.n.pre_gain, 1.f, e, c, pre_gain[i]);
+  }
+  NormEight<T> y[PIECES], gate[PIECES], residual[PIECES], gr[PIECES], gh[PIECES];
+  const auto fetch = [&](int64_t t) {  // (behind the last row: the last once more, for nothing)
+    t = t < a.n.tokens ? t : a.n.tokens - 1;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const int e = (i * LANES + at) * 8;
-      norm_load(static_cast<const T*>(a.n.y) + t * a.n.y_token, e, c, a.vec >> ROW_Y & 1, x[i]);
-      if (a.n.gate) norm_load(static_cast<const T*>(a.n.gate) + t * a.n.gate_token, e, c, a.vec >> ROW_GATE & 1, act[i]);
-      if (a.gr) norm_load(static_cast<const T*>(a.gr) + t * a.gr_token, e, c, a.vec >> ROW_R & 1, total[i]);
+      norm_fetch(static_cast<const T*>(a.n.y) + t * a.n.y_token, e, c, a.vec >> ROW_Y & 1, y[i]);
+      if (a.n.gate) norm_fetch(static_cast<const T*>(a.n.gate) + t * a.n.gate_token, e, c, a.vec >> ROW_GATE & 1, gate[i]);
+      if (a.gr) norm_fetch(static_cast<const T*>(a.gr) + t * a.gr_token, e, c, a.vec >> ROW_R & 1, gr[i]);
       if (pre) {
-        norm_load(static_cast<const T*>(a.gh) + t * a.gh_token, e, c, a.vec >> ROW_H & 1, gh[i]);
-        if (a.n.residual) norm_load(static_cast<const T*>(a.n.residual) + t * a.n.residual_token, e, c, a.vec >> ROW_RESIDUAL & 1, r[i]);
+        norm_fetch(static_cast<const T*>(a.gh) + t * a.gh_token, e, c, a.vec >> ROW_H & 1, gh[i]);
+        if (a.n.residual) norm_fetch(static_cast<const T*>(a.n.residual) + t * a.n.residual_token, e, c, a.vec >> ROW_RESIDUAL & 1, residual[i]);
       }
     }
-    if (post) norm_unit<LANES, PIECES>(x, post, a.n.post_eps, a, true, inverse, lds, pieces);
-    float z[PIECES][8], gain[PIECES][8];
+  };
+  int64_t first = (int64_t)blockIdx.x * S::ROWS;
+  fetch(first + threadIdx.x / LANES);
+  for (; first < a.n.tokens; first += step) {
+    const int64_t t = first + threadIdx.x / LANES;
+    const bool real = t < a.n.tokens;
+    float x[PIECES][8], act[PIECES][8], slope[PIECES][8], total[PIECES][8], g[PIECES][8], r[PIECES][8], inverse[PIECES];
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int e = (i * LANES + at) * 8;
-      float offset[8], by[8];
-      norm_vector(post ? a.n.post_gain : nullptr, 1.f, e, c, gain[i]);
-      norm_vector(post ? a.n.post_offset : nullptr, 0.f, e, c, offset);
-      norm_vector(a.n.residual_gain, 1.f, e, c, by);
+    for (int i = 0; i < PIECES; ++i)
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        z[i][k] = x[i][k] * gain[i][k] + offset[k];
-        if (a.n.gate) norm_act(a.n.act, act[i][k], act[i][k], slope[i][k]);
-        else act[i][k] = 1.f;
-        if (!a.gr) total[i][k] = 0.f;
-        by[k] *= a.n.scale;
-        if (pre) r[i][k] = e + k < c ? (a.n.residual ? r[i][k] : 0.f) + by[k] * act[i][k] * z[i][k] : 0.f;
-      }
-    }
-    if (pre) {
-      float unit_inverse[PIECES];
-      norm_unit<LANES, PIECES>(r, pre, a.n.pre_eps, a, false, unit_inverse, lds, pieces);
-#pragma unroll
-      for (int i = 0; i < PIECES; ++i) {
-        const int e = (i * LANES + at) * 8;
-        float pre_gain[8];
-        norm_vector(a.n.pre_gain, 1.f, e, c, pre_gain);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          if (real) {
-            sums[3][i][k] += gh[i][k] * r[i][k];
-            sums[4][i][k] += gh[i][k];
-          }
-          gh[i][k] *= pre_gain[k];
+        x[i][k] = norm_entry(y[i], k);
+        act[i][k] = a.n.gate ? norm_entry(gate[i], k) : 1.f;
+        total[i][k] = a.gr && real ? norm_entry(gr[i], k) : 0.f;
+        if (pre) {
+          g[i][k] = real ? norm_entry(gh[i], k) : 0.f;
+          r[i][k] = a.n.residual ? norm_entry(residual[i], k) : 0.f;
         }
       }
-      norm_unit_backward<LANES, PIECES>(gh, r, unit_inverse, pre, a, false, lds, pieces);
+    if (first + step < a.n.tokens) fetch(t + step);
+    if (post) norm_unit<LANES, PIECES>(x, post, a.n.post_eps, a, true, inverse, sums);
+    if (a.n.gate)
 #pragma unroll
       for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) total[i][k] += gh[i][k];
+        for (int k = 0; k < 8; ++k) norm_act(a.n.act, act[i][k], act[i][k], slope[i][k]);
+    if (pre) {
+      float unit_inverse[PIECES];
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float z = x[i][k] * post_gain[i][k] + post_offset[i][k];
+          r[i][k] += a.n.scale * by[i][k] * (act[i][k] * z);
+        }
+      }
+      norm_unit<LANES, PIECES>(r, pre, a.n.pre_eps, a, false, unit_inverse, sums);
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          total_of[3][i][k] += g[i][k] * r[i][k];
+          if (a.part[4]) total_of[4][i][k] += g[i][k];
+          g[i][k] *= pre_gain[i][k];
+        }
+      norm_unit_backward<LANES, PIECES>(g, r, unit_inverse, pre, a, false, sums);
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) total[i][k] += g[i][k];
     }
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const int e = (i * LANES + at) * 8;
       if (real && a.gresidual) norm_store(static_cast<T*>(a.gresidual) + t * c, e, c, a.vec >> ROW_RESIDUAL & 1, total[i]);
-      float by[8], ggate[8];
-      norm_vector(a.n.residual_gain, 1.f, e, c, by);
+      float ggate[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const float d = e + k < c ? total[i][k] * a.n.scale : 0.f;
-        if (real) sums[2][i][k] += d * act[i][k] * z[i][k];
-        if (a.n.gate) ggate[k] = d * by[k] * z[i][k] * slope[i][k];
-        const float gz = d * by[k] * act[i][k];
-        if (real) {
-          sums[0][i][k] += gz * x[i][k];
-          sums[1][i][k] += gz;
-        }
-        total[i][k] = gz * gain[i][k];
+        const float z = x[i][k] * post_gain[i][k] + post_offset[i][k];
+        const float d = total[i][k] * a.n.scale;
+        total_of[2][i][k] += d * act[i][k] * z;
+        if (a.n.gate) ggate[k] = d * by[i][k] * z * slope[i][k];
+        const float gz = d * by[i][k] * act[i][k];
+        total_of[0][i][k] += gz * x[i][k];
+        if (a.part[1]) total_of[1][i][k] += gz;
+        total[i][k] = gz * post_gain[i][k];
       }
       if (real && a.ggate) norm_store(static_cast<T*>(a.ggate) + t * c, e, c, a.vec >> ROW_GATE & 1, ggate);
     }
-    if (post) norm_unit_backward<LANES, PIECES>(total, x, inverse, post, a, true, lds, pieces);
+    if (post) norm_unit_backward<LANES, PIECES>(total, x, inverse, post, a, true, sums);
     if (real && a.gy)
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) norm_store(static_cast<T*>(a.gy) + t * c, (i * LANES + at) * 8, c, a.vec >> ROW_Y & 1, total[i]);
   }
-  const int64_t part = (int64_t)blockIdx.x * S::ROWS + threadIdx.x / LANES;
 #pragma unroll
   for (int v = 0; v < 5; ++v)
-    if (a.part[v])
+    if (a.part[v]) {
+      if constexpr (S::ROWS > 1) {
+        float* mine = pieces + threadIdx.x / LANES * WIDTH;
+        __syncthreads();
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) {
-        const int e = (i * LANES + at) * 8;
+        for (int i = 0; i < PIECES; ++i)
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if (e + k < c) a.part[v][part * c + e + k] = sums[v][i][k];
+          for (int k = 0; k < 8; ++k) mine[(i * LANES + at) * 8 + k] = total_of[v][i][k];
+        __syncthreads();
+        for (int e = threadIdx.x; e < c; e += S::THREADS) {
+          float sum = 0.f;
+#pragma unroll
+          for (int w = 0; w < S::ROWS; ++w) sum += pieces[w * WIDTH + e];
+          a.part[v][(int64_t)blockIdx.x * c + e] = sum;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+          const int e = (i * LANES + at) * 8;
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (e + k < c) a.part[v][(int64_t)blockIdx.x * c + e + k] = total_of[v][i][k];
+        }
       }
+    }
 }
 
 struct NormParts {
@@ -376,16 +482,24 @@ struct NormParts {
   int32_t parts, features, chunks;  // chunks: workgroups to a vector
 };
 
-// 64 features of one vector: four wavefronts a quarter of the parts each, added up in float64 (a feature may have 4096 parts)
-static __global__ void __launch_bounds__(256) norm_parts_kernel(const NormParts a) {
-  __shared__ double meet[4][64];
-  const int v = blockIdx.x / a.chunks, e = blockIdx.x % a.chunks * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
+constexpr int NORM_PARTS_WAVES = 16;
+
+// 64 features of one vector, sixteen wavefronts a share of the parts each, added up in float64
+static __global__ void __launch_bounds__(64 * NORM_PARTS_WAVES) norm_parts_kernel(const NormParts a) {
+  __shared__ double meet[NORM_PARTS_WAVES][64];
+  const int v = blockIdx.x / a.chunks, lane = threadIdx.x & 63, e = blockIdx.x % a.chunks * 64 + lane, wave = threadIdx.x >> 6;
+  const float* from = a.part[v] + e;
   double sum = 0.0;
   if (e < a.features)
-    for (int p = wave; p < a.parts; p += 4) sum += a.part[v][(int64_t)p * a.features + e];
-  meet[wave][threadIdx.x & 63] = sum;
+#pragma unroll 8
+    for (int p = wave; p < a.parts; p += NORM_PARTS_WAVES) sum += from[(int64_t)p * a.features];
+  meet[wave][lane] = sum;
   __syncthreads();
-  if (wave == 0 && e < a.features) a.out[v][e] = (float)((meet[0][threadIdx.x] + meet[1][threadIdx.x]) + (meet[2][threadIdx.x] + meet[3][threadIdx.x]));
+  if (wave == 0 && e < a.features) {
+#pragma unroll
+    for (int w = 1; w < NORM_PARTS_WAVES; ++w) sum += meet[w][lane];
+    a.out[v][e] = (float)sum;
+  }
 }
 
 }  // namespace ttc
