@@ -4,26 +4,28 @@
 
 namespace ttc {
 
-template <typename T, int NT>
+template <typename T, int WAVES>
 static void chunks(const MemArgs& a, int what, uint32_t grid, hipStream_t st) {
   switch (what) {
-    case MEM_STATES: hipLaunchKernelGGL((memory_chunk_kernel<T, TTC_D, NT, MEM_STATES>), dim3(grid), dim3(64 * MEM_WAVES), 0, st, a); break;
-    case MEM_OUT: hipLaunchKernelGGL((memory_chunk_kernel<T, TTC_D, NT, MEM_OUT>), dim3(grid), dim3(64 * MEM_WAVES), 0, st, a); break;
-    case MEM_OUT_DOTS: hipLaunchKernelGGL((memory_chunk_kernel<T, TTC_D, NT, MEM_OUT_DOTS>), dim3(grid), dim3(64 * MEM_WAVES), 0, st, a); break;
+    case MEM_STATES: hipLaunchKernelGGL((memory_chunk_kernel<T, TTC_D, WAVES, MEM_STATES>), dim3(grid), dim3(64 * WAVES), 0, st, a); break;
+    case MEM_OUT: hipLaunchKernelGGL((memory_chunk_kernel<T, TTC_D, WAVES, MEM_OUT>), dim3(grid), dim3(64 * WAVES), 0, st, a); break;
+    case MEM_OUT_DOTS: hipLaunchKernelGGL((memory_chunk_kernel<T, TTC_D, WAVES, MEM_OUT_DOTS>), dim3(grid), dim3(64 * WAVES), 0, st, a); break;
   }
 }
 
 template <>
-hipError_t launch_memory_chunks<TTC_D>(const MemArgs& a, bool bf16, bool wide, int what, uint32_t grid, hipStream_t st) {
+hipError_t launch_memory_chunks<TTC_D>(const MemArgs& a, bool bf16, int columns, int what, uint32_t grid, hipStream_t st) {
+  if (columns == 128) {
+    if (bf16) chunks<unsigned short, 8>(a, what, grid, st);
 #if TTC_D <= 128
-  if (wide) {
-    if (bf16) chunks<unsigned short, 2>(a, what, grid, st);
-    else chunks<float, 2>(a, what, grid, st);
-    return hipGetLastError();
-  }
+    else chunks<float, 8>(a, what, grid, st);
+#else
+    else return hipErrorInvalidValue;  // (not in LDS)
 #endif
-  if (bf16) chunks<unsigned short, 1>(a, what, grid, st);
-  else chunks<float, 1>(a, what, grid, st);
+  } else {
+    if (bf16) chunks<unsigned short, 4>(a, what, grid, st);
+    else chunks<float, 4>(a, what, grid, st);
+  }
   return hipGetLastError();
 }
 

@@ -4,9 +4,9 @@
 
 namespace ttc {
 
-template <> hipError_t launch_memory_chunks<64>(const MemArgs&, bool, bool, int, uint32_t, hipStream_t);
-template <> hipError_t launch_memory_chunks<128>(const MemArgs&, bool, bool, int, uint32_t, hipStream_t);
-template <> hipError_t launch_memory_chunks<256>(const MemArgs&, bool, bool, int, uint32_t, hipStream_t);
+template <> hipError_t launch_memory_chunks<64>(const MemArgs&, bool, int, int, uint32_t, hipStream_t);
+template <> hipError_t launch_memory_chunks<128>(const MemArgs&, bool, int, int, uint32_t, hipStream_t);
+template <> hipError_t launch_memory_chunks<256>(const MemArgs&, bool, int, int, uint32_t, hipStream_t);
 template <> hipError_t launch_memory_step<64>(const MemArgs&, bool, uint32_t, hipStream_t);
 template <> hipError_t launch_memory_step<128>(const MemArgs&, bool, uint32_t, hipStream_t);
 template <> hipError_t launch_memory_step<256>(const MemArgs&, bool, uint32_t, hipStream_t);
@@ -15,8 +15,9 @@ namespace {
 
 constexpr int STEP_MOST = 4;  // tokens of a sequence up to which memory_step_kernel takes it
 
-int wide_of(int rows, int cols) { return rows <= 128 && cols > 64; }            // 128 columns a workgroup, else 64
-int slices_of(int rows, int cols) { return wide_of(rows, cols) ? (cols + 127) / 128 : (cols + 63) / 64; }
+// Columns of a workgroup, and workgroups to the columns of a state.  float32 rows of more than 128 entries leave LDS room for 64.
+int columns_of(int rows, int cols, bool bf16) { return cols > 64 && (bf16 || rows <= 128) ? 128 : 64; }
+int slices_of(int rows, int cols, bool bf16) { return (cols + columns_of(rows, cols, bf16) - 1) / columns_of(rows, cols, bf16); }
 
 MemSequences sequences_of(const ttc_linear_attention_t& a, int segment) {
   MemSequences m = {a.sequences, a.tokens, a.cu_q, a.max_q, segment, a.sequences};
@@ -26,7 +27,8 @@ MemSequences sequences_of(const ttc_linear_attention_t& a, int segment) {
 
 // Chunks of a segment: all of a sequence where sequences, heads and slices occupy the device, else as many as give it two workgroups a unit
 int segment_of(const ttc_linear_attention_t& a, int slices, int cus) {
-  const int chunks = (int)(((int64_t)a.max_q + MEM_CHUNK - 1) / MEM_CHUNK);
+  const int64_t longest = a.max_q < a.tokens ? a.max_q : a.tokens;
+  const int chunks = (int)((longest + MEM_CHUNK - 1) / MEM_CHUNK);
   const double base = (double)a.sequences * a.heads * slices;
   if (chunks <= 1 || base >= 2. * cus) return chunks < 1 ? 1 : chunks;
   const double wanted = 2. * cus / base;
@@ -59,11 +61,11 @@ MemArgs forward_args(const ttc_linear_attention_t& a) {
 
 hipError_t run_chunks(MemArgs p, bool bf16, int what, hipStream_t st) {
   const int rows = p.w.d;
-  const bool wide = wide_of(rows, p.v.d);
-  p.slices = slices_of(rows, p.v.d);
+  const int columns = columns_of(rows, p.v.d, bf16);
+  p.slices = slices_of(rows, p.v.d, bf16);
   const uint32_t grid = (uint32_t)((p.m.entries * p.heads * p.slices + 7) / 8 * 8);  // (the kernel deals them out to eight XCDs)
-  return rows <= 64 ? launch_memory_chunks<64>(p, bf16, wide, what, grid, st)
-                    : rows <= 128 ? launch_memory_chunks<128>(p, bf16, wide, what, grid, st) : launch_memory_chunks<256>(p, bf16, wide, what, grid, st);
+  return rows <= 64 ? launch_memory_chunks<64>(p, bf16, columns, what, grid, st)
+                    : rows <= 128 ? launch_memory_chunks<128>(p, bf16, columns, what, grid, st) : launch_memory_chunks<256>(p, bf16, columns, what, grid, st);
 }
 
 // What the segments add to their states, and from that what each finds
@@ -80,7 +82,7 @@ uint64_t round16(uint64_t n) { return (n + 15) & ~15ull; }
 
 uint64_t linear_attention_workspace(const ttc_linear_attention_t& a, int cus) {
   if (a.max_q <= STEP_MOST) return 0;
-  const MemSequences m = sequences_of(a, segment_of(a, slices_of(a.dk, a.dv), cus));
+  const MemSequences m = sequences_of(a, segment_of(a, slices_of(a.dk, a.dv, a.dtype == TTC_BF16), cus));
   if (m.entries == m.sequences) return 0;
   return (uint64_t)m.entries * a.heads * a.dk * a.dv * 4 + round16((uint64_t)m.entries * a.heads * 4);
 }
@@ -95,7 +97,7 @@ hipError_t launch_linear_attention(const ttc_linear_attention_t& a, int cus, voi
     const uint32_t grid = (uint32_t)(a.sequences * a.heads * p.slices);
     return a.dk <= 64 ? launch_memory_step<64>(p, bf16, grid, st) : a.dk <= 128 ? launch_memory_step<128>(p, bf16, grid, st) : launch_memory_step<256>(p, bf16, grid, st);
   }
-  p.m = sequences_of(a, segment_of(a, slices_of(a.dk, a.dv), cus));
+  p.m = sequences_of(a, segment_of(a, slices_of(a.dk, a.dv, a.dtype == TTC_BF16), cus));
   if (p.m.entries != p.m.sequences) {
     p.added = static_cast<float*>(workspace);
     p.faded = p.added + p.m.entries * a.heads * a.dk * a.dv;
@@ -117,7 +119,7 @@ struct BackwardPlan {
 BackwardPlan plan_backward(const ttc_linear_attention_backward_t& b, int cus) {
   const ttc_linear_attention_t& f = b.forward;
   BackwardPlan p = {};
-  p.slices = slices_of(f.dv, f.dk);
+  p.slices = slices_of(f.dv, f.dk, f.dtype == TTC_BF16);
   p.m = sequences_of(f, segment_of(f, p.slices, cus));
   p.chunks = sequences_of(f, 1);
   uint64_t at = 0;

@@ -20,6 +20,9 @@ ttc_status_t check_sizes(const ttc_linear_attention_t& a) {
   if (a.dk < 8 || a.dk > 256 || a.dk % 8 || a.dv < 8 || a.dv > 256 || a.dv % 8) return TTC_ERR_UNSUPPORTED;
   // workgroups of a launch, and a workspace that can be counted: at most one for every head and 64 tokens, times four slices
   if (a.tokens > 0x7fffffffll || a.sequences > 0x7fffffffll || ((double)a.tokens / 64 + a.sequences) * a.heads * 64 >= 2147483648.) return TTC_ERR_UNSUPPORTED;
+  // 64 rows of a chunk lie within 2^31 bytes
+  for (int64_t step : {a.q_token, a.k_token, a.v_token, a.out_token})
+    if (a.tokens > 1 && (step < 0 || step >= (1 << 23))) return TTC_ERR_UNSUPPORTED;
   return TTC_OK;
 }
 
@@ -100,6 +103,7 @@ ttc_status_t ttc_linear_attention_backward(const ttc_linear_attention_backward_t
   if (f.tokens && (!b->gout || !b->gq || !b->gk || !b->gv || !aligned(b->gout, n) || !aligned(b->gq, n) || !aligned(b->gk, n) || !aligned(b->gv, n)))
     return TTC_ERR_INVALID_ARG;
   if (((f.tokens || !f.g_token) && !b->glog_decay) || !aligned(b->glog_decay, 4) || !aligned(b->gstate_out, 16) || !aligned(b->gstate, 16)) return TTC_ERR_INVALID_ARG;
+  if (f.tokens > 1 && (b->gout_token < 0 || b->gout_token >= (1 << 23))) return TTC_ERR_UNSUPPORTED;
   const uint64_t need = ttc::linear_attention_backward_workspace(*b, ttc::compute_units());
   if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return TTC_ERR_WORKSPACE;
   return ttc::launch_linear_attention_backward(*b, ttc::compute_units(), workspace, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? TTC_OK : TTC_ERR_DEVICE;

@@ -14,7 +14,6 @@
 namespace ttc {
 
 constexpr int MEM_CHUNK = 64;      // tokens of a chunk: a lane each where decays are added up
-constexpr int MEM_WAVES = 4;
 
 // ---- sequences and their segments ---------------------------------------------------------------------------------------------
 
@@ -26,6 +25,7 @@ struct MemSequences {
   int64_t entries;     // segments of all sequences at most; every sequence has one
 };
 
+// The rows of sequence s: numbers for all lanes if s is one
 __device__ __forceinline__ void mem_rows(const MemSequences& m, int64_t s, int64_t& first, int& n) {
   if (!m.cu_q) {
     first = s;
@@ -40,8 +40,8 @@ __device__ __forceinline__ int mem_segments(const MemSequences& m, int64_t s) {
   int64_t first;
   int n;
   mem_rows(m, s, first, n);
-  const int each = m.segment * MEM_CHUNK;
-  return n > each ? (int)(((int64_t)n + each - 1) / each) : 1;
+  const int chunks = (int)(((int64_t)n + MEM_CHUNK - 1) / MEM_CHUNK);
+  return max(1, (chunks + m.segment - 1) / m.segment);
 }
 
 // Segment number `at` of all: its sequence, and which of that one's segments it is; false if there are fewer.  Each wavefront adds up the
@@ -281,69 +281,115 @@ __device__ __forceinline__ float mem_between(float a_hi, float a_lo, float b_hi,
   return __builtin_amdgcn_exp2f(sign * ((a_hi - b_hi) + (a_lo - b_lo)));
 }
 
-template <typename T, int DK, int NT>
+template <typename T, int DK, int WAVES>
 struct MemShape {
   static constexpr int PAD = 16 / sizeof(T);
-  static constexpr int XS = DK + PAD, VS = 64 * NT + PAD, PS = MEM_CHUNK + PAD;  // rows in LDS
-  static constexpr int COLS = 16 * NT * MEM_WAVES;
+  static constexpr int COLS = 16 * WAVES;
+  static constexpr int XS = DK + PAD, VS = COLS + PAD, PS = MEM_CHUNK + PAD;  // rows in LDS
   // the pairs' products have a place of their own unless LDS is too small for it: then that of x, for one more barrier
-  static constexpr bool OWN = 2 * MEM_CHUNK * XS + MEM_CHUNK * VS + MEM_CHUNK * PS <= 38 * 1024;
-  static constexpr int XP = DK / 32, VP = 2 * NT;  // pieces of eight that a thread brings
-  // workgroups of a compute unit that LDS and registers leave room for
-  static constexpr int RESIDENT = sizeof(T) == 2 && DK <= 128 ? 2 : 1;
+  static constexpr bool OWN = (2 * MEM_CHUNK * XS + MEM_CHUNK * VS + MEM_CHUNK * PS) * sizeof(T) <= 150 * 1024;
+  static constexpr int XP = DK / 8 / WAVES, VP = 2;  // pieces of eight that a thread brings
+  // wavefronts of a SIMD that registers are kept for: two workgroups on a compute unit, where LDS has room for them; two at least, for with all 512
+  // registers of one the compiler puts sums into accumulation registers and reads some of them too early behind a branch (the build looks for that)
+  static constexpr int RESIDENT = sizeof(T) == 2 && DK <= 128 ? WAVES / 2 : 2;
+  static constexpr bool AHEAD = sizeof(T) == 2 || DK * 8 <= 128 * WAVES;  // registers for the next chunk's rows
 };
 
-// 64 rows on their way to LDS: zeros behind the last row and behind the last entry
-template <typename T, int D, int STEP, int PIECES>
+// 64 rows on their way to LDS: zeros behind the last row and behind the last entry.  Those places are read from the last row and entry that
+// are there, so that no load waits for a branch.
+template <typename T, int D, int STEP, int PIECES, int THREADS>
 struct MemStage {
-  static constexpr int ROW = D / 8, TURN = 64 * MEM_WAVES / ROW;  // pieces of a row, rows of one turn of the workgroup
+  static constexpr int ROW = D / 8, TURN = THREADS / ROW;  // pieces of a row, rows of one turn of the workgroup
   static_assert(PIECES * TURN == MEM_CHUNK);
   MemEight<T> piece[PIECES];
-  const T* at;         // of the thread's first piece in the chunk that comes next
+  const T* at;         // of the chunk that comes next; the same for all threads
   int64_t token;
-  __device__ __forceinline__ void begin(const MemRows& r, const T* base, int64_t first, int entry) {
+  uint32_t mine;       // of the thread's first piece from there on (64 rows are less than 2^31 bytes)
+  __device__ __forceinline__ void begin(const MemRows& r, const T* base, int64_t first, int entry, int entries) {
+    const int e = threadIdx.x % ROW * 8;
     token = r.token;
-    at = base + (first + (int)(threadIdx.x / ROW)) * token + entry + threadIdx.x % ROW * 8;
+    at = base + first * token + entry;
+    mine = threadIdx.x / ROW * (uint32_t)token + (e < entries ? e : 0);
   }
-  // `whole`: all rows and entries are there
-  __device__ __forceinline__ void fetch(int rows, int entries, bool whole) {
+  __device__ __forceinline__ void fetch(int rows) {
+    if (rows == MEM_CHUNK) {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) mem_fetch(at + i * TURN * token + mine, piece[i]);
+    } else {
+      const uint32_t row = threadIdx.x / ROW;
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) mem_fetch(at + mine + (int64_t)((int)min(row + i * TURN, (uint32_t)rows - 1) - (int)row) * token, piece[i]);
+    }
+  }
+  __device__ __forceinline__ void put(T* lds, int rows, int entries, bool whole) const {
+    T* p = lds + threadIdx.x / ROW * STEP + threadIdx.x % ROW * 8;
     if (whole) {
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) mem_fetch(at + i * TURN * token, piece[i]);
+      for (int i = 0; i < PIECES; ++i) mem_put(p + i * TURN * STEP, piece[i]);
     } else {
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
-        piece[i] = {};
-        if ((int)(threadIdx.x % ROW) * 8 < entries && (int)(threadIdx.x / ROW) + i * TURN < rows) mem_fetch(at + i * TURN * token, piece[i]);
+        const bool there = (int)(threadIdx.x % ROW) * 8 < entries && (int)(threadIdx.x / ROW) + i * TURN < rows;
+        mem_put(p + i * TURN * STEP, there ? piece[i] : MemEight<T>{});
       }
     }
   }
-  __device__ __forceinline__ void put(T* lds) const {
-    T* p = lds + threadIdx.x / ROW * STEP + threadIdx.x % ROW * 8;
+};
+
+// A wavefront's numbers of a state in memory: rows 16 k + 4 g + r of column c, `row` numbers apart
+template <int KT>
+struct MemPlace {
+  uint32_t at;          // of the lane's first number
+  int rows;             // of the state from the lane's first on; 0: it has no such column
+  int row;
+  __device__ __forceinline__ void load(const float* p, bool whole, srv_floatx4 (&s)[KT]) const {
+    p += at;
+    if (whole && row == 1) {
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) mem_put(p + i * TURN * STEP, piece[i]);
+      for (int k = 0; k < KT; ++k) s[k] = *reinterpret_cast<const srv_floatx4*>(p + 16 * k);
+    } else if (whole) {
+#pragma unroll
+      for (int k = 0; k < KT; ++k)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[k][r] = p[(16 * k + r) * row];
+    } else {
+#pragma unroll
+      for (int k = 0; k < KT; ++k)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[k][r] = 16 * k + r < rows ? p[(16 * k + r) * row] : 0.f;
+    }
+  }
+  __device__ __forceinline__ void store(float* p, bool whole, const srv_floatx4 (&s)[KT], bool none) const {
+    p += at;
+#pragma unroll
+    for (int k = 0; k < KT; ++k)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (whole || 16 * k + r < rows) p[(16 * k + r) * row] = none ? 0.f : s[k][r];
   }
 };
 
 enum MemWhat { MEM_STATES, MEM_OUT, MEM_OUT_DOTS };  // what a segment adds to its state; results; results and their products with other rows
 
-// A workgroup takes one segment of one head of one sequence, and of the values' columns a slice of 64 * NT; a wavefront owns 16 * NT of them and
-// their state, DK numbers each, which stays in its registers from chunk to chunk: what a lane holds of it as a result is what it has to hold of it as an
-// operand if the sum's order follows.  The next chunk's rows and decays are on their way while one is worked on.
+// A workgroup takes one segment of one head of one sequence, and of the values' columns a slice of 16 * WAVES; a wavefront owns 16 of them and their
+// state, DK numbers each, which stays in its registers from chunk to chunk: what a lane holds of it as a result is what it has to hold of it as an operand
+// if the sum's order follows.  The next chunk's rows and decays are on their way while one is worked on.
 // bfloat16 rows: the state is met in two parts of 8 bits (three where float32 results depend on it), what is added to it in three, so that states are as
 // exact as float32 sums; pairs' products, in one, which the header's documentation states.
-template <typename T, int DK, int NT, int WHAT>
-__global__ void __launch_bounds__(64 * MEM_WAVES, (MemShape<T, DK, NT>::RESIDENT)) memory_chunk_kernel(const MemArgs a) {
-  typedef MemShape<T, DK, NT> S;
+template <typename T, int DK, int WAVES, int WHAT>
+__global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)) memory_chunk_kernel(const MemArgs a) {
+  typedef MemShape<T, DK, WAVES> S;
   typedef typename MemOperand<T>::type op_t;
   constexpr bool BF16 = sizeof(T) == 2, STATES = WHAT == MEM_STATES, DOTS = WHAT == MEM_OUT_DOTS;
   constexpr int IN = BF16 ? (DOTS ? 3 : 2) : 1, UP = BF16 ? 3 : 1, KT = DK / 16;
+  constexpr int HALVES = WAVES / 4;  // wavefronts that share sixteen rows of pairs
   __shared__ alignas(16) T xl[STATES ? 8 : MEM_CHUNK * (S::OWN || S::XS > S::PS ? S::XS : S::PS)], wl[MEM_CHUNK * S::XS], vl[MEM_CHUNK * S::VS];
   __shared__ alignas(16) T own[STATES || !S::OWN ? 8 : MEM_CHUNK * S::PS];
   __shared__ alignas(16) MemDecays decays[2];
-  __shared__ alignas(16) float meet[MEM_WAVES][MEM_CHUNK];
+  __shared__ alignas(16) float meet[WAVES][MEM_CHUNK];
   T* const pl = S::OWN ? own : xl;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int c = lane & 15, g = lane >> 4;
   // Workgroups of an XCD, every eighth, take neighbouring heads, which may share rows that they then find in its cache, with all their segments:
   // places without a segment are as many for every XCD (with segments slowest the last XCD had most of them, and the others 68 for 64 places).
   const uint32_t each = gridDim.x / 8, work = blockIdx.x % 8 * each + blockIdx.x / 8;
@@ -354,133 +400,145 @@ __global__ void __launch_bounds__(64 * MEM_WAVES, (MemShape<T, DK, NT>::RESIDENT
   int segment, n;
   if (head >= a.heads || !mem_segment(a.m, entry, seq, segment)) return;
   mem_rows(a.m, seq, first, n);
-  const int segments = mem_segments(a.m, seq), chunks = (n + MEM_CHUNK - 1) / MEM_CHUNK;
+  first = __builtin_amdgcn_readfirstlane((int)first);  // (tokens are below 2^31)
+  n = __builtin_amdgcn_readfirstlane(n);
+  segment = __builtin_amdgcn_readfirstlane(segment);
+  const int chunks = (int)(((int64_t)n + MEM_CHUNK - 1) / MEM_CHUNK), segments = max(1, (chunks + a.m.segment - 1) / a.m.segment);
   const int c0 = segment * a.m.segment, c1 = min(c0 + a.m.segment, chunks);
   const bool reverse = a.reverse;
   const float sign = reverse ? -1.f : 1.f;
   if (STATES && segment == (reverse ? 0 : segments - 1)) return;  // nobody finds what this one leaves
-  const int col0 = slice * S::COLS + wave * 16 * NT, cols = a.v.d;
+  const int col0 = slice * S::COLS + wave * 16, cols = a.v.d;
 
-  MemStage<T, DK, S::XS, S::XP> x_rows, w_rows;
-  MemStage<T, 64 * NT, S::VS, S::VP> v_rows;
+  MemStage<T, DK, S::XS, S::XP, 64 * WAVES> x_rows, w_rows;
+  MemStage<T, S::COLS, S::VS, S::VP, 64 * WAVES> v_rows;
   float g_next = 0.f;
   const int64_t way = reverse ? -MEM_CHUNK : MEM_CHUNK;
   const int64_t t_first = first + (int64_t)(reverse ? c1 - 1 : c0) * MEM_CHUNK;
-  if (!STATES) x_rows.begin(a.x, static_cast<const T*>(a.x.p) + head / a.x.group * a.x.head, t_first, 0);
-  w_rows.begin(a.w, static_cast<const T*>(a.w.p) + head / a.w.group * a.w.head, t_first, 0);
-  v_rows.begin(a.v, static_cast<const T*>(a.v.p) + head / a.v.group * a.v.head, t_first, slice * S::COLS);
-  const float* g_at = a.log_decay + (t_first + lane) * a.g_token + head * a.g_head;
-  const auto fetch = [&](int chunk) {
-    const int rows = min(MEM_CHUNK, n - chunk * MEM_CHUNK);
-    const bool whole = rows == MEM_CHUNK && a.w.d == DK && (slice + 1) * S::COLS <= cols;
-    if (!STATES) x_rows.fetch(rows, a.w.d, whole);
-    w_rows.fetch(rows, a.w.d, whole);
-    v_rows.fetch(rows, cols - slice * S::COLS, whole);
-    g_next = lane < rows ? *g_at : 0.f;
+  if (!STATES) x_rows.begin(a.x, static_cast<const T*>(a.x.p) + head / a.x.group * a.x.head, t_first, 0, a.x.d);
+  w_rows.begin(a.w, static_cast<const T*>(a.w.p) + head / a.w.group * a.w.head, t_first, 0, a.w.d);
+  v_rows.begin(a.v, static_cast<const T*>(a.v.p) + head / a.v.group * a.v.head, t_first, slice * S::COLS, cols - slice * S::COLS);
+  const float* g_at = a.log_decay + t_first * a.g_token + head * a.g_head;
+  const auto fetch = [&](int rows) {
+    if (!STATES) x_rows.fetch(rows);
+    w_rows.fetch(rows);
+    v_rows.fetch(rows);
     if (!STATES) x_rows.at += way * x_rows.token;
     w_rows.at += way * w_rows.token;
     v_rows.at += way * v_rows.token;
+  };
+  const auto fetch_decays = [&](int rows) {
+    g_next = g_at[min(lane, rows - 1) * a.g_token];
     g_at += way * a.g_token;
   };
+  const auto rows_of = [&](int chunk) { return min(MEM_CHUNK, n - chunk * MEM_CHUNK); };
+  const auto decays_of = [&](int chunk, MemDecays& to) {
+    return mem_decays(lane < rows_of(chunk) ? g_next : 0.f, lane, reverse, a.in_scale, a.up_scale, to);
+  };
+  const bool whole_state = a.w.d == DK && (slice + 1) * S::COLS <= cols;
 
-  if (c0 < c1) fetch(reverse ? c1 - 1 : c0);
-  srv_floatx4 s[KT][NT] = {};
+  const int begin = reverse ? c1 - 1 : c0;
+  if (c0 < c1) {
+    fetch_decays(rows_of(begin));
+    if (S::AHEAD) fetch(rows_of(begin));
+  }
+  srv_floatx4 s[KT] = {};
+  const MemPlace<KT> place = {(uint32_t)(4 * g * a.s_row + (col0 + c) * a.s_col), col0 + c < cols ? a.w.d - 4 * g : 0, a.s_row};
   if (!STATES) {
     const int64_t row = mem_begin(a.states, seq, n);
     const float* from = a.starts ? a.starts + (entry * a.heads + head) * a.dk * a.dv : row >= 0 ? a.states.in + (row * a.heads + head) * a.dk * a.dv : nullptr;
-    if (from)
+    if (from) place.load(from, whole_state, s);
+    // a use here: left to the loop, every turn would wait for the loads in flight, the next chunk's
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int k = 0; k < KT; ++k)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int i = 16 * k + 4 * g + r, j = col0 + 16 * t + c;
-            if (i < a.x.d && j < cols) s[k][t][r] = from[(int64_t)i * a.s_row + (int64_t)j * a.s_col];
-          }
+    for (int k = 0; k < KT; ++k) asm volatile("" : "+v"(s[k]));
   }
   double grown = 0.0;
-  if (c0 < c1 && wave == 0) grown = mem_decays(g_next, lane, reverse, a.in_scale, a.up_scale, decays[0]);
+  if (c0 < c1 && wave == 0) {
+    const double sum = decays_of(begin, decays[0]);
+    if (STATES) grown = sum;
+  }
 
   for (int turn = 0; turn < c1 - c0; ++turn) {
-    const int chunk = reverse ? c1 - 1 - turn : c0 + turn, at = chunk * MEM_CHUNK, rows = min(MEM_CHUNK, n - at);
-    const int64_t t0 = first + at;
+    const int chunk = reverse ? c1 - 1 - turn : c0 + turn, after = reverse ? chunk - 1 : chunk + 1, rows = rows_of(chunk);
+    const int64_t t0 = first + (int64_t)chunk * MEM_CHUNK;
+    const bool whole = whole_state && rows == MEM_CHUNK;
+    asm volatile("" : "+v"(c), "+v"(g));  // places and masks are found anew: kept over the loop they would take registers that spill
     const MemDecays& dl = decays[turn & 1];
+    if (!S::AHEAD) fetch(rows);
     if (turn) __syncthreads();  // the last chunk has been read
-    if (!STATES) x_rows.put(xl);
-    w_rows.put(wl);
-    v_rows.put(vl);
+    if (!STATES) x_rows.put(xl, rows, a.x.d, whole);
+    w_rows.put(wl, rows, a.w.d, whole);
+    v_rows.put(vl, rows, cols - slice * S::COLS, whole);
     const bool more = turn + 1 < c1 - c0;
-    if (more) fetch(reverse ? chunk - 1 : chunk + 1);
+    if (more) {
+      fetch_decays(rows_of(after));  // first: they are used before the rows are
+      if (S::AHEAD) fetch(rows_of(after));
+    }
     __syncthreads();
 
-    srv_floatx4 o[4][NT] = {};
+    srv_floatx4 o[4] = {};
     if constexpr (!STATES) {
       // what the tokens read of the state
 #pragma unroll
       for (int k = 0; k < KT; k += 2) {
-        op_t part[NT][IN];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const float x[8] = {s[k][t][0], s[k][t][1], s[k][t][2], s[k][t][3], s[k + 1][t][0], s[k + 1][t][1], s[k + 1][t][2], s[k + 1][t][3]};
-          mem_split<IN>(x, part[t]);
-        }
+        op_t part[IN];
+        const float x[8] = {s[k][0], s[k][1], s[k][2], s[k][3], s[k + 1][0], s[k + 1][1], s[k + 1][2], s[k + 1][3]};
+        mem_split<IN>(x, part);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const T* row = xl + (16 * i + c) * S::XS + 16 * k + 4 * g;
-          const op_t x = mem_operand(row, row + 16);
+          const op_t y = mem_operand(row, row + 16);
 #pragma unroll
-          for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int p = IN - 1; p >= 0; --p) o[i][t] = mem_mma(part[t][p], x, o[i][t]);
+          for (int p = IN - 1; p >= 0; --p) o[i] = mem_mma(part[p], y, o[i]);
         }
+        if constexpr (S::RESIDENT == 4) __builtin_amdgcn_sched_barrier(0);  // reads that go ahead take registers: spilled ones cost more
       }
-      // pairs: wavefront w has the products of rows 16 w .. with all that these see
-      srv_floatx4 z[4] = {};
+      // pairs: a wavefront has the products of sixteen rows with those, or with every other sixteen of those, that they see
+      const int own_rows = wave & 3, j0 = HALVES == 1 ? 0 : wave >> 2;
+      srv_floatx4 z[4 / HALVES] = {};
 #pragma unroll
       for (int k = 0; k < DK / 32; ++k) {
-        const T* row = xl + (16 * wave + c) * S::XS + 32 * k + 8 * g;
+        const T* row = xl + (16 * own_rows + c) * S::XS + 32 * k + 8 * g;
         const op_t x = mem_operand(row, row + 4);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (reverse ? j >= wave : j <= wave) {
+        for (int u = 0; u < 4 / HALVES; ++u) {
+          const int j = j0 + HALVES * u;
+          if (reverse ? j >= own_rows : j <= own_rows) {
             const T* key = wl + (16 * j + c) * S::XS + 32 * k + 8 * g;
-            z[j] = mem_mma(mem_operand(key, key + 4), x, z[j]);
+            z[u] = mem_mma(mem_operand(key, key + 4), x, z[u]);
           }
+        }
+        if constexpr (S::RESIDENT == 4) __builtin_amdgcn_sched_barrier(0);
       }
       if constexpr (!S::OWN) __syncthreads();  // x has been read
-      const int i = 16 * wave + c;
+      const int i = 16 * own_rows + c;
       const float own_hi = dl.hi[i], own_lo = dl.lo[i];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int u = 0; u < 4 / HALVES; ++u) {
+        const int j = j0 + HALVES * u;
         float p[4] = {};
-        if (reverse ? j >= wave : j <= wave) {
+        if (reverse ? j >= own_rows : j <= own_rows) {
           const srv_floatx4 hi = *reinterpret_cast<const srv_floatx4*>(&dl.hi[16 * j + 4 * g]), lo = *reinterpret_cast<const srv_floatx4*>(&dl.lo[16 * j + 4 * g]);
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int e = 16 * j + 4 * g + r;
             const bool seen = reverse ? e >= i : e <= i;
-            p[r] = seen ? a.pair_scale * z[j][r] * mem_between(own_hi, own_lo, hi[r], lo[r], sign) : 0.f;
+            p[r] = seen ? a.pair_scale * z[u][r] * mem_between(own_hi, own_lo, hi[r], lo[r], sign) : 0.f;
           }
         }
         mem_store4(pl + i * S::PS + 16 * j + 4 * g, p);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) o[i][t] *= dl.in[16 * i + c];
+      for (int i = 0; i < 4; ++i) o[i] *= dl.in[16 * i + c];
       if constexpr (DOTS) {
-        const T* dot = static_cast<const T*>(a.dot.p) + head / a.dot.group * a.dot.head;
+        const T* dot = static_cast<const T*>(a.dot.p) + head / a.dot.group * a.dot.head + t0 * a.dot.token + col0;
+        const uint32_t mine = c * (uint32_t)a.dot.token + 4 * g;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float sum = 0.f;
+          if (whole || (16 * i + c < rows && col0 + 4 * g < cols))
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            const int e = col0 + 16 * t + 4 * g;
-            if (16 * i + c < rows && e < cols)
-#pragma unroll
-              for (int r = 0; r < 4; ++r) sum += o[i][t][r] * srv_widen(dot[(t0 + 16 * i + c) * a.dot.token + e + r]);
-          }
+            for (int r = 0; r < 4; ++r) sum += o[i][r] * srv_widen(dot[16 * i * a.dot.token + mine + r]);
           sum += __shfl_xor(sum, 16, 64);
           sum += __shfl_xor(sum, 32, 64);
           if (g == 0) meet[wave][16 * i + c] = sum;
@@ -488,99 +546,87 @@ __global__ void __launch_bounds__(64 * MEM_WAVES, (MemShape<T, DK, NT>::RESIDENT
       }
     }
     // the values, tokens side by side in a lane
-    op_t v[2][NT];
+    op_t v[2];
     float finite = 0.f;
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int k = 0; k < 2; ++k) {
+      v[k] = mem_column(vl + (32 * k + 8 * g) * S::VS + wave * 16, S::VS, c);
+      if constexpr (!STATES)
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        v[k][t] = mem_column(vl + (32 * k + 8 * g) * S::VS + wave * 16 * NT + 16 * t, S::VS, c);
-        if constexpr (!STATES)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) finite = fmaf(mem_entry(v[k][t], e), 0.f, finite);  // NaN once one is not
-      }
-    if (more && wave == ((turn + 1) & 3)) {
-      const double whole = mem_decays(g_next, lane, reverse, a.in_scale, a.up_scale, decays[(turn + 1) & 1]);
-      grown += whole;
+        for (int e = 0; e < 8; ++e) finite = fmaf(mem_entry(v[k], e), 0.f, finite);  // NaN once one is not
+    }
+    if (more && wave == ((turn + 1) & (WAVES - 1))) {
+      const double sum = decays_of(after, decays[(turn + 1) & 1]);
+      if (STATES) grown += sum;
     }
     if constexpr (!STATES) {
       __syncthreads();
       if constexpr (DOTS)
-        if (wave == 0 && lane < rows)
-          a.dots[((int64_t)slice * a.heads + head) * a.m.tokens + t0 + lane] = (meet[0][lane] + meet[1][lane]) + (meet[2][lane] + meet[3][lane]);
-      const bool bad = __builtin_amdgcn_ballot_w64(finite != 0.f) != 0;
-      op_t clean[2][NT];
+        if (wave == 0 && lane < rows) {
+          float sum = 0.f;
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          clean[k][t] = v[k][t];
-          if (bad) {  // a weight of 0 times NaN would be NaN
-            float x[8];
-            op_t y[1];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = isfinite(mem_entry(v[k][t], e)) ? mem_entry(v[k][t], e) : 0.f;
-            mem_split<1>(x, y);
-            clean[k][t] = y[0];
-          }
+          for (int w = 0; w < WAVES; ++w) sum += meet[w][lane];
+          a.dots[((int64_t)slice * a.heads + head) * a.m.tokens + t0 + lane] = sum;
         }
+      const bool bad = __builtin_amdgcn_ballot_w64(finite != 0.f) != 0;
+      op_t clean[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        clean[k] = v[k];
+        if (bad) {  // a weight of 0 times NaN would be NaN
+          float x[8];
+          op_t y[1];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = isfinite(mem_entry(v[k], e)) ? mem_entry(v[k], e) : 0.f;
+          mem_split<1>(x, y);
+          clean[k] = y[0];
+        }
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int k = 0; k < 2; ++k)
           if (reverse ? 2 * k + 1 >= i : 2 * k <= i) {
             const T* row = pl + (16 * i + c) * S::PS + 32 * k + 8 * g;
-            const op_t p = mem_operand(row, row + 4);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) o[i][t] = mem_mma(clean[k][t], p, o[i][t]);
+            o[i] = mem_mma(clean[k], mem_operand(row, row + 4), o[i]);
           }
       if (bad)
         for (int j = 0; j < rows; ++j)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int r = 0; r < 4; ++r) {
+              const float y = srv_widen(vl[j * S::VS + wave * 16 + 4 * g + r]);
+              const bool seen = reverse ? j >= 16 * i + c : j <= 16 * i + c;
+              if (seen && !isfinite(y)) o[i][r] += srv_widen(pl[(16 * i + c) * S::PS + j]) * y;
+            }
+      const int64_t out_at = t0 * a.out_token + head * a.out_head + col0;
+      const uint32_t mine = c * (uint32_t)a.out_token + 4 * g;
 #pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                const float y = srv_widen(vl[j * S::VS + wave * 16 * NT + 16 * t + 4 * g + r]);
-                const bool seen = reverse ? j >= 16 * i + c : j <= 16 * i + c;
-                if (seen && !isfinite(y)) o[i][t][r] += srv_widen(pl[(16 * i + c) * S::PS + j]) * y;
-              }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const int e = col0 + 16 * t + 4 * g;
-          if (16 * i + c >= rows || e >= cols) continue;
-          const int64_t to = (t0 + 16 * i + c) * a.out_token + head * a.out_head + e;
-          if (DOTS && a.out_float) mem_out4(static_cast<float*>(a.out) + to, o[i][t]);
-          else mem_out4(static_cast<T*>(a.out) + to, o[i][t]);
-        }
+      for (int i = 0; i < 4; ++i) {
+        if (!whole && (16 * i + c >= rows || col0 + 4 * g >= cols)) continue;
+        const int64_t to = out_at + 16 * i * a.out_token;
+        if (DOTS && a.out_float) mem_out4(static_cast<float*>(a.out) + to + mine, o[i]);
+        else mem_out4(static_cast<T*>(a.out) + to + mine, o[i]);
+      }
     }
     // the state
-    const float whole = dl.whole;
+    const float fade = dl.whole;
 #pragma unroll
-    for (int k = 0; k < KT; ++k)
-#pragma unroll
-      for (int t = 0; t < NT; ++t) s[k][t] *= whole;
+    for (int k = 0; k < KT; ++k) s[k] *= fade;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const srv_floatx4 u0 = *reinterpret_cast<const srv_floatx4*>(&dl.up[32 * h + 8 * g]), u1 = *reinterpret_cast<const srv_floatx4*>(&dl.up[32 * h + 8 * g + 4]);
-      op_t up[NT][UP];
+      op_t up[UP];
+      float x[8];
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = mem_entry(v[h][t], e) * (e < 4 ? u0[e & 3] : u1[e & 3]);
-        mem_split<UP>(x, up[t]);
-      }
+      for (int e = 0; e < 8; ++e) x[e] = mem_entry(v[h], e) * (e < 4 ? u0[e & 3] : u1[e & 3]);
+      mem_split<UP>(x, up);
 #pragma unroll
       for (int k = 0; k < KT; ++k) {
         const op_t w = mem_column(wl + (32 * h + 8 * g) * S::XS + 16 * k, S::XS, c);
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int p = UP - 1; p >= 0; --p) s[k][t] = mem_mma(w, up[t][p], s[k][t]);
+        for (int p = UP - 1; p >= 0; --p) s[k] = mem_mma(w, up[p], s[k]);
       }
     }
   }
@@ -588,26 +634,24 @@ __global__ void __launch_bounds__(64 * MEM_WAVES, (MemShape<T, DK, NT>::RESIDENT
   bool none = false;
   if (STATES) {
     to = a.added + (entry * a.heads + head) * a.dk * a.dv;
-    // each wavefront has the sums of every fourth chunk
+    // the wavefronts have the chunks' sums in turn
     double* const all = reinterpret_cast<double*>(&meet[0][0]);
     if (lane == 0) all[wave] = grown;
     __syncthreads();
-    if (threadIdx.x == 0 && slice == 0) a.faded[entry * a.heads + head] = exp2f((float)((all[0] + all[1]) + (all[2] + all[3])));
+    if (threadIdx.x == 0 && slice == 0) {
+      double sum = 0.0;
+      for (int w = 0; w < WAVES; ++w) sum += all[w];
+      a.faded[entry * a.heads + head] = exp2f((float)sum);
+    }
   } else if (segment == (reverse ? 0 : segments - 1)) {
     const int64_t row = mem_end(a.states, seq);
     if (row >= 0) to = a.states.out + (row * a.heads + head) * a.dk * a.dv;
     none = a.ruled && mem_begin(a.rule, seq, n) < 0;
   }
-  if (to)
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int k = 0; k < KT; ++k)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int i = 16 * k + 4 * g + r, j = col0 + 16 * t + c;
-          if (i < a.w.d && j < cols) to[(int64_t)i * a.s_row + (int64_t)j * a.s_col] = none ? 0.f : s[k][t][r];
-        }
+  if (to) {
+    if (whole_state) place.store(to, true, s, none);
+    else place.store(to, false, s, none);
+  }
 }
 
 // The segments' states: what each adds becomes what each finds, four numbers of one head's state to a thread.
@@ -658,7 +702,7 @@ constexpr int MEM_STEP_ROWS = 16;
 template <typename T, int DK>
 __global__ void __launch_bounds__(256) memory_step_kernel(const MemArgs a) {
   constexpr int ROWS = DK / MEM_STEP_ROWS;
-  __shared__ alignas(16) float xl[DK], wl[DK], meet[MEM_WAVES][64];
+  __shared__ alignas(16) float xl[DK], wl[DK], meet[4][64];
   const int tid = threadIdx.x, col = tid % 16 * 4, r0 = tid / 16;
   const int slice = blockIdx.x % a.slices, head = blockIdx.x / a.slices % a.heads, e = slice * 64 + col;
   const int64_t seq = blockIdx.x / a.slices / a.heads;

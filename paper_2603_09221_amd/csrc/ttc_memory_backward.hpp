@@ -44,7 +44,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) memory_pairs_kernel(const MemDecayArgs a) {
   typedef typename MemOperand<T>::type op_t;
   __shared__ MemDecays dl;
-  __shared__ float left[MEM_CHUNK], below[MEM_WAVES][MEM_CHUNK];
+  __shared__ float left[MEM_CHUNK], below[4][MEM_CHUNK];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
   const int head = blockIdx.x % a.heads;
   int64_t seq, first;

@@ -15,9 +15,9 @@ hipError_t launch_residual_norm(const ttc_residual_norm_t& n, int cus, hipStream
 uint64_t norm_backward_workspace(const ttc_residual_norm_backward_t& b, int cus);
 hipError_t launch_residual_norm_backward(const ttc_residual_norm_backward_t& b, int cus, void* workspace, hipStream_t st);
 
-// rows of x and w of up to D entries; what: a MemWhat
+// rows of x and w of up to D entries; columns of a workgroup (64 or 128); what: a MemWhat
 struct MemArgs;
-template <int D> hipError_t launch_memory_chunks(const MemArgs& a, bool bf16, bool wide, int what, uint32_t grid, hipStream_t st);
+template <int D> hipError_t launch_memory_chunks(const MemArgs& a, bool bf16, int columns, int what, uint32_t grid, hipStream_t st);
 template <int D> hipError_t launch_memory_step(const MemArgs& a, bool bf16, uint32_t grid, hipStream_t st);
 
 }  // namespace ttc
