@@ -19,10 +19,21 @@ constexpr int STEP_MOST = 4;  // tokens of a sequence up to which memory_step_ke
 int columns_of(int rows, int cols, bool bf16) { return cols > 64 && (bf16 || rows <= 128) ? 128 : 64; }
 int slices_of(int rows, int cols, bool bf16) { return (cols + columns_of(rows, cols, bf16) - 1) / columns_of(rows, cols, bf16); }
 
+// Blocks of heads: one where there are segments for the XCDs to take in turn, else the fewest that make enough
+int blocks_of(int64_t entries, int heads) {
+  int n = 1;
+  while (n < heads && (entries * n < 16 || heads % n)) ++n;
+  return n;
+}
 MemSequences sequences_of(const ttc_linear_attention_t& a, int segment) {
-  MemSequences m = {a.sequences, a.tokens, a.cu_q, a.max_q, segment, a.sequences};
+  MemSequences m = {a.sequences, a.tokens, a.cu_q, a.max_q, segment, a.sequences, 1};
   if ((int64_t)segment * MEM_CHUNK < a.max_q) m.entries += a.tokens / ((int64_t)segment * MEM_CHUNK);
+  m.blocks = blocks_of(m.entries, a.heads);
   return m;
+}
+// Workgroups of mem_deal
+uint32_t dealt(const MemSequences& m, int heads, int per_head) {
+  return (uint32_t)((m.entries * m.blocks + 7) / 8 * 8 * (heads / m.blocks) * per_head);
 }
 
 // Chunks of a segment: all of a sequence where sequences, heads and slices occupy the device, else as many as give it two workgroups a unit
@@ -63,14 +74,14 @@ hipError_t run_chunks(MemArgs p, bool bf16, int what, hipStream_t st) {
   const int rows = p.w.d;
   const int columns = columns_of(rows, p.v.d, bf16);
   p.slices = slices_of(rows, p.v.d, bf16);
-  const uint32_t grid = (uint32_t)((p.m.entries * p.heads * p.slices + 7) / 8 * 8);  // (the kernel deals them out to eight XCDs)
+  const uint32_t grid = dealt(p.m, p.heads, p.slices);
   return rows <= 64 ? launch_memory_chunks<64>(p, bf16, columns, what, grid, st)
                     : rows <= 128 ? launch_memory_chunks<128>(p, bf16, columns, what, grid, st) : launch_memory_chunks<256>(p, bf16, columns, what, grid, st);
 }
 
 // What the segments add to their states, and from that what each finds
-hipError_t run_starts(const MemArgs& p, bool bf16, hipStream_t st) {
-  if (const hipError_t e = run_chunks(p, bf16, MEM_STATES, st); e != hipSuccess) return e;
+hipError_t run_starts(const MemArgs& p, bool bf16, int what, hipStream_t st) {
+  if (const hipError_t e = run_chunks(p, bf16, what, st); e != hipSuccess) return e;
   const int64_t blocks = (p.dk * p.dv / 4 + 255) / 256;
   hipLaunchKernelGGL(memory_scan_kernel, dim3((uint32_t)(p.m.sequences * p.heads * blocks)), dim3(256), 0, st, p);
   return hipGetLastError();
@@ -101,7 +112,7 @@ hipError_t launch_linear_attention(const ttc_linear_attention_t& a, int cus, voi
   if (p.m.entries != p.m.sequences) {
     p.added = static_cast<float*>(workspace);
     p.faded = p.added + p.m.entries * a.heads * a.dk * a.dv;
-    if (const hipError_t e = run_starts(p, bf16, st); e != hipSuccess) return e;
+    if (const hipError_t e = run_starts(p, bf16, MEM_STATES, st); e != hipSuccess) return e;
     p.starts = p.added;
   }
   return run_chunks(p, bf16, MEM_OUT, st);
@@ -183,11 +194,11 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
   if (segmented) {
     base.added = place(plan.added);
     base.faded = place(plan.faded);
-    if ((e = run_starts(base, bf16, st)) != hipSuccess) return e;
+    if ((e = run_starts(base, bf16, MEM_STATES_DOTS, st)) != hipSuccess) return e;
     base.starts = base.added;
     back.added = place(plan.added_r);
     back.faded = place(plan.faded_r);
-    if ((e = run_starts(back, bf16, st)) != hipSuccess) return e;
+    if ((e = run_starts(back, bf16, MEM_STATES_DOTS, st)) != hipSuccess) return e;
     back.starts = back.added;
   }
   const auto result = [&](MemArgs& p, void* out, uint64_t parts, int heads, int d) {
@@ -222,12 +233,14 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
   result(dq, b.gq, plan.gq, f.heads_qk, f.dk);
   if ((e = run_chunks(dq, bf16, MEM_OUT_DOTS, st)) != hipSuccess) return e;
   if (group > 1) {
-    const dim3 grid((uint32_t)(plan.chunks.entries * f.heads_qk));
+    MemSequences m = plan.chunks;
+    m.blocks = blocks_of(m.entries, f.heads_qk);
+    const dim3 grid(dealt(m, f.heads_qk, 1));
     for (int i = 0; i < 2; ++i) {
       const float* parts = place(i ? plan.gk : plan.gq);
       void* out = i ? b.gk : b.gq;
-      if (bf16) hipLaunchKernelGGL((memory_heads_kernel<unsigned short>), grid, dim3(256), 0, st, plan.chunks, parts, static_cast<unsigned short*>(out), f.heads_qk, group, f.dk);
-      else hipLaunchKernelGGL((memory_heads_kernel<float>), grid, dim3(256), 0, st, plan.chunks, parts, static_cast<float*>(out), f.heads_qk, group, f.dk);
+      if (bf16) hipLaunchKernelGGL((memory_heads_kernel<unsigned short>), grid, dim3(256), 0, st, m, parts, static_cast<unsigned short*>(out), f.heads_qk, group, f.dk);
+      else hipLaunchKernelGGL((memory_heads_kernel<float>), grid, dim3(256), 0, st, m, parts, static_cast<float*>(out), f.heads_qk, group, f.dk);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
@@ -254,7 +267,7 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
   d.sums = f.g_token ? nullptr : reinterpret_cast<double*>(ws + plan.sums);
   d.found = base.starts;
   d.found_r = back.starts;
-  const dim3 grid((uint32_t)(plan.chunks.entries * f.heads));
+  const dim3 grid(dealt(d.m, f.heads, 1));
   if (bf16) hipLaunchKernelGGL((memory_pairs_kernel<unsigned short>), grid, dim3(256), 0, st, d);
   else hipLaunchKernelGGL((memory_pairs_kernel<float>), grid, dim3(256), 0, st, d);
   if ((e = hipGetLastError()) != hipSuccess) return e;

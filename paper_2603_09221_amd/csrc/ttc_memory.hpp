@@ -23,7 +23,17 @@ struct MemSequences {
   int32_t max_q;
   int32_t segment;     // chunks of a segment
   int64_t entries;     // segments of all sequences at most; every sequence has one
+  int32_t blocks;      // of heads: what the XCDs take in turn is a segment of one block's heads (mem_deal)
 };
+
+// Workgroup b's segment and head, of `per_head` workgroups for each.  Every eighth workgroup lies on one XCD.  An XCD takes whole segments, of all heads
+// or of a block of them: rows that heads share are in its cache.  Places without a segment come last.
+__device__ __forceinline__ void mem_deal(const MemSequences& m, int heads, uint32_t per_head, int64_t& entry, int& head, int& rest) {
+  const uint32_t inner = heads / m.blocks * per_head, turn = blockIdx.x / 8, item = turn / inner * 8 + blockIdx.x % 8, in = turn % inner;
+  entry = item / m.blocks;
+  head = item % m.blocks * (heads / m.blocks) + in / per_head;
+  rest = in % per_head;
+}
 
 // The rows of sequence s: numbers for all lanes if s is one
 __device__ __forceinline__ void mem_rows(const MemSequences& m, int64_t s, int64_t& first, int& n) {
@@ -145,8 +155,21 @@ __device__ __forceinline__ mem_float8 mem_column(const float* p, int step, int c
 __device__ __forceinline__ float mem_entry(const srv_bf16x8& v, int i) { return (float)v[i]; }
 __device__ __forceinline__ float mem_entry(const mem_float8& v, int i) { return v.x[i]; }
 
-// Eight float32 numbers as a sum of PARTS operands, the largest part first.  bfloat16 parts are cut off, not rounded, so that three hold all
-// 24 bits (two hold 16) and none passes the largest number.  (An infinity leaves NaN in the second.)
+// `so_far`, 0, or NaN if one of the numbers is not finite
+__device__ __forceinline__ float mem_finite(const srv_bf16x8& v, float so_far) {
+  const srv_bf16x2 none = {};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) so_far = __builtin_amdgcn_fdot2_f32_bf16(srv_bf16x2{v[2 * i], v[2 * i + 1]}, none, so_far, false);
+  return so_far;
+}
+__device__ __forceinline__ float mem_finite(const mem_float8& v, float so_far) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) so_far = fmaf(v.x[i], 0.f, so_far);
+  return so_far;
+}
+
+// Eight float32 numbers as a sum of PARTS operands, the largest part first.  One or two parts are rounded to nearest: 8 or 17 significant bits, 2^-9 or 2^-18
+// of a number at most; three are cut off and hold all 24.  (An infinity leaves NaN in the second, as does a number beyond the largest bfloat16.)
 template <int PARTS>
 __device__ __forceinline__ void mem_split(const float (&x)[8], srv_bf16x8 (&part)[PARTS]) {
   float rest[8];
@@ -154,17 +177,23 @@ __device__ __forceinline__ void mem_split(const float (&x)[8], srv_bf16x8 (&part
   for (int i = 0; i < 8; ++i) rest[i] = x[i];
 #pragma unroll
   for (int k = 0; k < PARTS; ++k) {
-    srv_uintx4 p;
+    if constexpr (PARTS == 3) {
+      srv_uintx4 p;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t lo = __float_as_uint(rest[2 * i]), hi = __float_as_uint(rest[2 * i + 1]);
-      p[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302);
-      if (k + 1 < PARTS) {
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = __float_as_uint(rest[2 * i]), hi = __float_as_uint(rest[2 * i + 1]);
+        p[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302);
         rest[2 * i] -= __uint_as_float(lo & 0xffff0000u);
         rest[2 * i + 1] -= __uint_as_float(hi & 0xffff0000u);
       }
+      part[k] = __builtin_bit_cast(srv_bf16x8, p);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) part[k][i] = static_cast<__bf16>(rest[i]);
+      if (k + 1 < PARTS)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rest[i] -= (float)part[k][i];
     }
-    part[k] = __builtin_bit_cast(srv_bf16x8, p);
   }
 }
 template <int PARTS>
@@ -204,6 +233,8 @@ __device__ __forceinline__ void mem_out4(unsigned short* p, const srv_floatx4& x
                                        srv_narrow<unsigned short>(x[3])};
 }
 __device__ __forceinline__ void mem_out4(float* p, const srv_floatx4& x) { *reinterpret_cast<mem_floatx4*>(p) = x; }
+// and from one
+template <typename T> struct MemFour { typedef T type __attribute__((ext_vector_type(4), aligned(sizeof(T)))); };
 
 // ---- the kernel of chunks ---------------------------------------------------------------------------------------------------
 
@@ -241,6 +272,8 @@ struct MemArgs {
 struct MemDecays {
   float hi[MEM_CHUNK], lo[MEM_CHUNK];   // G / ln 2 as a sum of two
   float in[MEM_CHUNK], up[MEM_CHUNK];
+  float since[MEM_CHUNK], left[MEM_CHUNK];  // factors from the beginning, and to the end, of a token's sixteen (the other way round from the last token on)
+  float border[4][2];                   // G / ln 2 where a sixteen begins and ends
   float whole;
 };
 
@@ -274,6 +307,14 @@ __device__ __forceinline__ double mem_decays(float g, int lane, bool reverse, fl
   to.in[lane] = in_scale * (reverse ? left : since);
   to.up[lane] = up_scale * (reverse ? since : left);
   if (lane == 63) to.whole = since;
+  const double end = __shfl(sum, lane | 15, 64), ends = __shfl(sum, (lane & 48) - 1, 64), begin = lane < 16 ? 0.0 : ends;  // (all lanes take part)
+  const float after = __builtin_amdgcn_exp2f((float)(sum - begin)), ahead = __builtin_amdgcn_exp2f((float)(end - sum));
+  to.since[lane] = reverse ? ahead : after;
+  to.left[lane] = reverse ? after : ahead;
+  if ((lane & 15) == 0) {
+    to.border[lane >> 4][0] = (float)begin;
+    to.border[lane >> 4][1] = (float)end;
+  }
   return whole;
 }
 // sign: -1 where the first is the earlier one
@@ -302,23 +343,17 @@ struct MemStage {
   static constexpr int ROW = D / 8, TURN = THREADS / ROW;  // pieces of a row, rows of one turn of the workgroup
   static_assert(PIECES * TURN == MEM_CHUNK);
   MemEight<T> piece[PIECES];
-  const T* at;         // of the chunk that comes next; the same for all threads
-  int64_t token;
-  uint32_t mine;       // of the thread's first piece from there on (64 rows are less than 2^31 bytes)
-  __device__ __forceinline__ void begin(const MemRows& r, const T* base, int64_t first, int entry, int entries) {
-    const int e = threadIdx.x % ROW * 8;
-    token = r.token;
-    at = base + first * token + entry;
-    mine = threadIdx.x / ROW * (uint32_t)token + (e < entries ? e : 0);
-  }
-  __device__ __forceinline__ void fetch(int rows) {
+  // 64 rows are less than 2^31 bytes.  Places are found anew every time: kept over the loop, with their upper halves, they would take registers that spill.
+  __device__ __forceinline__ void fetch(const T* at, int64_t token, int rows, int entries) {
+    uint32_t thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    const uint32_t row = thread / ROW, e = thread % ROW * 8, mine = e < (uint32_t)entries ? e : 0;
     if (rows == MEM_CHUNK) {
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) mem_fetch(at + i * TURN * token + mine, piece[i]);
+      for (int i = 0; i < PIECES; ++i) mem_fetch(at + i * TURN * token + (row * (uint32_t)token + mine), piece[i]);
     } else {
-      const uint32_t row = threadIdx.x / ROW;
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) mem_fetch(at + mine + (int64_t)((int)min(row + i * TURN, (uint32_t)rows - 1) - (int)row) * token, piece[i]);
+      for (int i = 0; i < PIECES; ++i) mem_fetch(at + (min(row + i * TURN, (uint32_t)rows - 1) * (uint32_t)token + mine), piece[i]);
     }
   }
   __device__ __forceinline__ void put(T* lds, int rows, int entries, bool whole) const {
@@ -369,19 +404,22 @@ struct MemPlace {
   }
 };
 
-enum MemWhat { MEM_STATES, MEM_OUT, MEM_OUT_DOTS };  // what a segment adds to its state; results; results and their products with other rows
+// What a segment adds to its state; results; results and their products with other rows; what a segment adds, for these
+enum MemWhat { MEM_STATES, MEM_OUT, MEM_OUT_DOTS, MEM_STATES_DOTS };
 
 // A workgroup takes one segment of one head of one sequence, and of the values' columns a slice of 16 * WAVES; a wavefront owns 16 of them and their
 // state, DK numbers each, which stays in its registers from chunk to chunk: what a lane holds of it as a result is what it has to hold of it as an operand
 // if the sum's order follows.  The next chunk's rows and decays are on their way while one is worked on.
-// bfloat16 rows: the state is met in two parts of 8 bits (three where float32 results depend on it), what is added to it in three, so that states are as
-// exact as float32 sums; pairs' products, in one, which the header's documentation states.
+// bfloat16 rows: pairs' products and the state that queries meet are rounded to bfloat16 for their products, 2^-9 each, what is added to a state
+// to 17 bits (7e-7 of a state in the norm, in one case measured, where three parts gave 1.3e-7: 48 of 94 products of a chunk and a tenth of the vector
+// instructions less by a third), as the header's documentation states; where gradients of decays, sums of float32 numbers, depend on them, both take
+// three parts, all of float32's bits.  Matrix and vector instructions take turns here: a chunk of a wavefront is the sum of both.
 template <typename T, int DK, int WAVES, int WHAT>
 __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)) memory_chunk_kernel(const MemArgs a) {
   typedef MemShape<T, DK, WAVES> S;
   typedef typename MemOperand<T>::type op_t;
-  constexpr bool BF16 = sizeof(T) == 2, STATES = WHAT == MEM_STATES, DOTS = WHAT == MEM_OUT_DOTS;
-  constexpr int IN = BF16 ? (DOTS ? 3 : 2) : 1, UP = BF16 ? 3 : 1, KT = DK / 16;
+  constexpr bool BF16 = sizeof(T) == 2, STATES = WHAT == MEM_STATES || WHAT == MEM_STATES_DOTS, DOTS = WHAT == MEM_OUT_DOTS;
+  constexpr int IN = BF16 && DOTS ? 3 : 1, UP = !BF16 ? 1 : DOTS || WHAT == MEM_STATES_DOTS ? 3 : 2, KT = DK / 16;
   constexpr int HALVES = WAVES / 4;  // wavefronts that share sixteen rows of pairs
   __shared__ alignas(16) T xl[STATES ? 8 : MEM_CHUNK * (S::OWN || S::XS > S::PS ? S::XS : S::PS)], wl[MEM_CHUNK * S::XS], vl[MEM_CHUNK * S::VS];
   __shared__ alignas(16) T own[STATES || !S::OWN ? 8 : MEM_CHUNK * S::PS];
@@ -390,15 +428,12 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
   T* const pl = S::OWN ? own : xl;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int c = lane & 15, g = lane >> 4;
-  // Workgroups of an XCD, every eighth, take neighbouring heads, which may share rows that they then find in its cache, with all their segments:
-  // places without a segment are as many for every XCD (with segments slowest the last XCD had most of them, and the others 68 for 64 places).
-  const uint32_t each = gridDim.x / 8, work = blockIdx.x % 8 * each + blockIdx.x / 8;
-  const int slice = work % a.slices;
-  const int64_t entry = work / a.slices % a.m.entries;
-  const int head = work / a.slices / a.m.entries;
+  int64_t entry;
+  int head, slice;
+  mem_deal(a.m, a.heads, a.slices, entry, head, slice);
   int64_t seq, first;
   int segment, n;
-  if (head >= a.heads || !mem_segment(a.m, entry, seq, segment)) return;
+  if (entry >= a.m.entries || !mem_segment(a.m, entry, seq, segment)) return;
   mem_rows(a.m, seq, first, n);
   first = __builtin_amdgcn_readfirstlane((int)first);  // (tokens are below 2^31)
   n = __builtin_amdgcn_readfirstlane(n);
@@ -413,23 +448,17 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
   MemStage<T, DK, S::XS, S::XP, 64 * WAVES> x_rows, w_rows;
   MemStage<T, S::COLS, S::VS, S::VP, 64 * WAVES> v_rows;
   float g_next = 0.f;
-  const int64_t way = reverse ? -MEM_CHUNK : MEM_CHUNK;
-  const int64_t t_first = first + (int64_t)(reverse ? c1 - 1 : c0) * MEM_CHUNK;
-  if (!STATES) x_rows.begin(a.x, static_cast<const T*>(a.x.p) + head / a.x.group * a.x.head, t_first, 0, a.x.d);
-  w_rows.begin(a.w, static_cast<const T*>(a.w.p) + head / a.w.group * a.w.head, t_first, 0, a.w.d);
-  v_rows.begin(a.v, static_cast<const T*>(a.v.p) + head / a.v.group * a.v.head, t_first, slice * S::COLS, cols - slice * S::COLS);
-  const float* g_at = a.log_decay + t_first * a.g_token + head * a.g_head;
-  const auto fetch = [&](int rows) {
-    if (!STATES) x_rows.fetch(rows);
-    w_rows.fetch(rows);
-    v_rows.fetch(rows);
-    if (!STATES) x_rows.at += way * x_rows.token;
-    w_rows.at += way * w_rows.token;
-    v_rows.at += way * v_rows.token;
+  const T* const x_at = static_cast<const T*>(a.x.p) + (STATES ? 0 : head / a.x.group * a.x.head);
+  const T* const w_at = static_cast<const T*>(a.w.p) + head / a.w.group * a.w.head;
+  const T* const v_at = static_cast<const T*>(a.v.p) + head / a.v.group * a.v.head + slice * S::COLS;
+  const auto fetch = [&](int chunk, int rows) {
+    const int64_t t0 = first + (int64_t)chunk * MEM_CHUNK;
+    if (!STATES) x_rows.fetch(x_at + t0 * a.x.token, a.x.token, rows, a.x.d);
+    w_rows.fetch(w_at + t0 * a.w.token, a.w.token, rows, a.w.d);
+    v_rows.fetch(v_at + t0 * a.v.token, a.v.token, rows, cols - slice * S::COLS);
   };
-  const auto fetch_decays = [&](int rows) {
-    g_next = g_at[min(lane, rows - 1) * a.g_token];
-    g_at += way * a.g_token;
+  const auto fetch_decays = [&](int chunk, int rows) {
+    g_next = a.log_decay[(first + (int64_t)chunk * MEM_CHUNK + min(lane, rows - 1)) * a.g_token + head * a.g_head];
   };
   const auto rows_of = [&](int chunk) { return min(MEM_CHUNK, n - chunk * MEM_CHUNK); };
   const auto decays_of = [&](int chunk, MemDecays& to) {
@@ -439,8 +468,8 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
 
   const int begin = reverse ? c1 - 1 : c0;
   if (c0 < c1) {
-    fetch_decays(rows_of(begin));
-    if (S::AHEAD) fetch(rows_of(begin));
+    fetch_decays(begin, rows_of(begin));
+    if (S::AHEAD) fetch(begin, rows_of(begin));
   }
   srv_floatx4 s[KT] = {};
   const MemPlace<KT> place = {(uint32_t)(4 * g * a.s_row + (col0 + c) * a.s_col), col0 + c < cols ? a.w.d - 4 * g : 0, a.s_row};
@@ -459,20 +488,31 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
   }
 
   for (int turn = 0; turn < c1 - c0; ++turn) {
-    const int chunk = reverse ? c1 - 1 - turn : c0 + turn, after = reverse ? chunk - 1 : chunk + 1, rows = rows_of(chunk);
+    const int chunk = reverse ? c1 - 1 - turn : c0 + turn, rows = rows_of(chunk);
+    const int after = reverse ? chunk - 1 : chunk + 1;
     const int64_t t0 = first + (int64_t)chunk * MEM_CHUNK;
     const bool whole = whole_state && rows == MEM_CHUNK;
     asm volatile("" : "+v"(c), "+v"(g));  // places and masks are found anew: kept over the loop they would take registers that spill
     const MemDecays& dl = decays[turn & 1];
-    if (!S::AHEAD) fetch(rows);
+    if (!S::AHEAD) fetch(chunk, rows);
     if (turn) __syncthreads();  // the last chunk has been read
     if (!STATES) x_rows.put(xl, rows, a.x.d, whole);
     w_rows.put(wl, rows, a.w.d, whole);
     v_rows.put(vl, rows, cols - slice * S::COLS, whole);
     const bool more = turn + 1 < c1 - c0;
+    typename MemFour<T>::type dot[DOTS ? 4 : 1];
+    if constexpr (DOTS) {
+      const T* const from = static_cast<const T*>(a.dot.p) + head / a.dot.group * a.dot.head + t0 * a.dot.token + col0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        dot[i] = 0;
+        if (whole || (16 * i + c < rows && col0 + 4 * g < cols))
+          dot[i] = *reinterpret_cast<const typename MemFour<T>::type*>(from + (16 * i * a.dot.token + (c * (uint32_t)a.dot.token + 4 * g)));
+      }
+    }
     if (more) {
-      fetch_decays(rows_of(after));  // first: they are used before the rows are
-      if (S::AHEAD) fetch(rows_of(after));
+      fetch_decays(after, rows_of(after));  // first: they are used before the rows are
+      if (S::AHEAD) fetch(after, rows_of(after));
     }
     __syncthreads();
 
@@ -511,56 +551,59 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
         if constexpr (S::RESIDENT == 4) __builtin_amdgcn_sched_barrier(0);
       }
       if constexpr (!S::OWN) __syncthreads();  // x has been read
+      // Weights: within a sixteen exp(G_i - G_j), a difference at a time; between two of them the product of the way to the end of one, from there to the
+      // beginning of the other, and on from there, all at most 1
       const int i = 16 * own_rows + c;
-      const float own_hi = dl.hi[i], own_lo = dl.lo[i];
+      const float own_since = a.pair_scale * dl.since[i];
 #pragma unroll
       for (int u = 0; u < 4 / HALVES; ++u) {
         const int j = j0 + HALVES * u;
         float p[4] = {};
-        if (reverse ? j >= own_rows : j <= own_rows) {
+        if (j == own_rows) {
           const srv_floatx4 hi = *reinterpret_cast<const srv_floatx4*>(&dl.hi[16 * j + 4 * g]), lo = *reinterpret_cast<const srv_floatx4*>(&dl.lo[16 * j + 4 * g]);
+          const float own_hi = dl.hi[i], own_lo = dl.lo[i];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int e = 16 * j + 4 * g + r;
-            const bool seen = reverse ? e >= i : e <= i;
-            p[r] = seen ? a.pair_scale * z[u][r] * mem_between(own_hi, own_lo, hi[r], lo[r], sign) : 0.f;
+            float x = a.pair_scale * z[u][r] * mem_between(own_hi, own_lo, hi[r], lo[r], sign);
+            asm volatile("" : "+v"(x));  // (a select, not a branch for every number)
+            p[r] = (reverse ? 4 * g + r >= c : 4 * g + r <= c) ? x : 0.f;
           }
+        } else if (reverse ? j > own_rows : j < own_rows) {
+          const srv_floatx4 left = *reinterpret_cast<const srv_floatx4*>(&dl.left[16 * j + 4 * g]);
+          const float way = own_since * __builtin_amdgcn_exp2f(reverse ? dl.border[j][0] - dl.border[own_rows][1] : dl.border[own_rows][0] - dl.border[j][1]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) p[r] = z[u][r] * way * left[r];
         }
         mem_store4(pl + i * S::PS + 16 * j + 4 * g, p);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] *= dl.in[16 * i + c];
       if constexpr (DOTS) {
-        const T* dot = static_cast<const T*>(a.dot.p) + head / a.dot.group * a.dot.head + t0 * a.dot.token + col0;
-        const uint32_t mine = c * (uint32_t)a.dot.token + 4 * g;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float sum = 0.f;
-          if (whole || (16 * i + c < rows && col0 + 4 * g < cols))
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sum += o[i][r] * srv_widen(dot[16 * i * a.dot.token + mine + r]);
+          for (int r = 0; r < 4; ++r) sum += o[i][r] * srv_widen(dot[i][r]);
           sum += __shfl_xor(sum, 16, 64);
           sum += __shfl_xor(sum, 32, 64);
           if (g == 0) meet[wave][16 * i + c] = sum;
         }
       }
     }
+    if (more && wave == ((turn + 1) & (WAVES - 1))) {
+      const double sum = decays_of(after, decays[(turn + 1) & 1]);
+      if (STATES) grown += sum;
+    }
+    if constexpr (!STATES) __syncthreads();
     // the values, tokens side by side in a lane
     op_t v[2];
     float finite = 0.f;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       v[k] = mem_column(vl + (32 * k + 8 * g) * S::VS + wave * 16, S::VS, c);
-      if constexpr (!STATES)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) finite = fmaf(mem_entry(v[k], e), 0.f, finite);  // NaN once one is not
-    }
-    if (more && wave == ((turn + 1) & (WAVES - 1))) {
-      const double sum = decays_of(after, decays[(turn + 1) & 1]);
-      if (STATES) grown += sum;
+      if constexpr (!STATES) finite = mem_finite(v[k], finite);
     }
     if constexpr (!STATES) {
-      __syncthreads();
       if constexpr (DOTS)
         if (wave == 0 && lane < rows) {
           float sum = 0.f;

@@ -46,10 +46,10 @@ __global__ void __launch_bounds__(256) memory_pairs_kernel(const MemDecayArgs a)
   __shared__ MemDecays dl;
   __shared__ float left[MEM_CHUNK], below[4][MEM_CHUNK];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  const int head = blockIdx.x % a.heads;
-  int64_t seq, first;
-  int chunk, n;
-  if (!mem_segment(a.m, blockIdx.x / a.heads, seq, chunk)) return;
+  int64_t entry, seq, first;
+  int head, none, chunk, n;
+  mem_deal(a.m, a.heads, 1, entry, head, none);
+  if (entry >= a.m.entries || !mem_segment(a.m, entry, seq, chunk)) return;
   mem_rows(a.m, seq, first, n);
   const int64_t t0 = first + (int64_t)chunk * MEM_CHUNK;
   const int rows = min(MEM_CHUNK, n - chunk * MEM_CHUNK);
@@ -181,10 +181,10 @@ static __global__ void memory_decay_sum_kernel(const double* sums, int64_t entri
 // The gradients of heads that share a row, in their order: a chunk's tokens of one shared head to a workgroup, four entries at a time to a thread
 template <typename T>
 __global__ void __launch_bounds__(256) memory_heads_kernel(const MemSequences m, const float* parts, T* out, int heads, int group, int d) {
-  const int head = blockIdx.x % heads;
-  int64_t seq, first;
-  int chunk, n;
-  if (!mem_segment(m, blockIdx.x / heads, seq, chunk)) return;
+  int64_t entry, seq, first;
+  int head, none, chunk, n;
+  mem_deal(m, heads, 1, entry, head, none);
+  if (entry >= m.entries || !mem_segment(m, entry, seq, chunk)) return;
   mem_rows(m, seq, first, n);
   const int64_t t0 = first + (int64_t)chunk * MEM_CHUNK;
   const int quads = min(MEM_CHUNK, n - chunk * MEM_CHUNK) * (d / 4);
