@@ -46,26 +46,32 @@ __device__ __forceinline__ void mem_rows(const MemSequences& m, int64_t s, int64
   const int64_t end = min((int64_t)m.cu_q[s + 1], m.tokens);
   n = (int)max(min(end - first, (int64_t)m.max_q), (int64_t)0);
 }
-__device__ __forceinline__ int mem_segments(const MemSequences& m, int64_t s) {
-  int64_t first;
-  int n;
-  mem_rows(m, s, first, n);
+__device__ __forceinline__ int mem_segments(const MemSequences& m, int n) {
   const int chunks = (int)(((int64_t)n + MEM_CHUNK - 1) / MEM_CHUNK);
   return max(1, (chunks + m.segment - 1) / m.segment);
 }
 
-// Segment number `at` of all: its sequence, and which of that one's segments it is; false if there are fewer.  Each wavefront adds up the
-// sequences for itself, a run of them to a lane.
-__device__ __forceinline__ bool mem_segment(const MemSequences& m, int64_t at, int64_t& seq, int& segment) {
+// Segment number `at` of all: its sequence with that one's rows, and which of its segments it is, the same for all lanes; false if there are fewer.  Each
+// wavefront adds up the sequences for itself, a run of them to a lane; where a run is one, what the lanes have read is all that it takes.
+__device__ __forceinline__ bool mem_segment(const MemSequences& m, int64_t at, int64_t& seq, int& segment, int64_t& first, int& n) {
   if (m.entries == m.sequences) {
+    if (at >= m.sequences) return false;
     seq = at;
     segment = 0;
-    return at < m.sequences;
+    mem_rows(m, at, first, n);
+    first = __builtin_amdgcn_readfirstlane((int)first);  // (tokens are below 2^31)
+    n = __builtin_amdgcn_readfirstlane(n);
+    return true;
   }
   const int lane = threadIdx.x & 63;
-  const int64_t run = (m.sequences + 63) / 64, first = min(lane * run, m.sequences), last = min(first + run, m.sequences);
+  const int64_t run = (m.sequences + 63) / 64, own_first = min(lane * run, m.sequences), own_last = min(own_first + run, m.sequences);
   uint32_t own = 0;
-  for (int64_t s = first; s < last; ++s) own += mem_segments(m, s);
+  int64_t row = 0;
+  int rows = 0;
+  for (int64_t s = own_first; s < own_last; ++s) {
+    mem_rows(m, s, row, rows);
+    own += mem_segments(m, rows);
+  }
   uint32_t sum = own;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -76,10 +82,18 @@ __device__ __forceinline__ bool mem_segment(const MemSequences& m, int64_t at, i
   const int who = __builtin_ctzll(__builtin_amdgcn_ballot_w64(at < sum));
   uint32_t before = __builtin_amdgcn_readlane(sum - own, who);
   int64_t s = who * run;
-  for (;; ++s) {
-    const uint32_t n = __builtin_amdgcn_readfirstlane(mem_segments(m, s));
-    if (at < before + n) break;
-    before += n;
+  if (run > 1) {
+    for (;; ++s) {
+      mem_rows(m, s, row, rows);
+      const uint32_t count = __builtin_amdgcn_readfirstlane(mem_segments(m, rows));
+      if (at < before + count) break;
+      before += count;
+    }
+    first = __builtin_amdgcn_readfirstlane((int)row);
+    n = __builtin_amdgcn_readfirstlane(rows);
+  } else {
+    first = __builtin_amdgcn_readlane((int)row, who);
+    n = __builtin_amdgcn_readlane(rows, who);
   }
   seq = s;
   segment = (int)(at - before);
@@ -433,11 +447,7 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
   mem_deal(a.m, a.heads, a.slices, entry, head, slice);
   int64_t seq, first;
   int segment, n;
-  if (entry >= a.m.entries || !mem_segment(a.m, entry, seq, segment)) return;
-  mem_rows(a.m, seq, first, n);
-  first = __builtin_amdgcn_readfirstlane((int)first);  // (tokens are below 2^31)
-  n = __builtin_amdgcn_readfirstlane(n);
-  segment = __builtin_amdgcn_readfirstlane(segment);
+  if (entry >= a.m.entries || !mem_segment(a.m, entry, seq, segment, first, n)) return;
   const int chunks = (int)(((int64_t)n + MEM_CHUNK - 1) / MEM_CHUNK), segments = max(1, (chunks + a.m.segment - 1) / a.m.segment);
   const int c0 = segment * a.m.segment, c1 = min(c0 + a.m.segment, chunks);
   const bool reverse = a.reverse;
@@ -703,13 +713,16 @@ static __global__ void __launch_bounds__(256) memory_scan_kernel(const MemArgs a
   const int head = blockIdx.x / blocks % a.heads, e = (blockIdx.x % blocks * 256 + threadIdx.x) * 4;
   const int64_t seq = blockIdx.x / blocks / a.heads;
   int64_t entry = 0, first;
-  for (int64_t s = threadIdx.x & 63; s < seq; s += 64) entry += mem_segments(a.m, s);
+  int n;
+  for (int64_t s = threadIdx.x & 63; s < seq; s += 64) {
+    mem_rows(a.m, s, first, n);
+    entry += mem_segments(a.m, n);
+  }
 #pragma unroll
   for (int o = 32; o; o >>= 1) entry += __shfl_xor(entry, o, 64);
   if (e >= a.dk * a.dv) return;
-  int n;
   mem_rows(a.m, seq, first, n);
-  const int segments = (int)min((int64_t)mem_segments(a.m, seq), a.m.entries - entry);  // (fewer only where cu_q does not ascend)
+  const int segments = (int)min((int64_t)mem_segments(a.m, n), a.m.entries - entry);  // (fewer only where cu_q does not ascend)
   const int64_t row = mem_begin(a.states, seq, n), size = (int64_t)a.heads * a.dk * a.dv;
   srv_floatx4 now = {};
   if (row >= 0) now = *reinterpret_cast<const srv_floatx4*>(a.states.in + row * size + (int64_t)head * a.dk * a.dv + e);
