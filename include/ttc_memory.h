@@ -25,8 +25,8 @@ extern "C" {
  * Sequences are packed as in ttc_attention: sequence s has the rows cu_q[s] .. cu_q[s+1]-1, rows behind the last are left as they are.
  * dk and dv are multiples of 8 from 8 to 256; rows of tokens are at most 2^23 - 1 entries apart.
  * States, sums and decays are float32 or wider.  bfloat16 rows, sequences of more than four tokens: what queries meet of the state, and the
- * products of queries and keys of one chunk of 64 tokens, are rounded to bfloat16 for their products (2^-9 of each), what is added to a state to
- * 17 significant bits; nothing else but the results is rounded to less than float32's 24.
+ * products of queries and keys of one chunk of 64 tokens, are rounded to bfloat16 for their products (2^-9 of each); nothing else but the
+ * results is rounded to less than float32's 24 bits.
  * A token's NaN or infinity reaches its own and later tokens' results, and no earlier ones (an infinity may become NaN there). */
 typedef struct {
   int64_t sequences, tokens;   /* tokens: rows of q, k, v, out; below 2^31                                 */

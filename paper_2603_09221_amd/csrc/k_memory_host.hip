@@ -84,8 +84,8 @@ hipError_t run_chunks(MemArgs p, bool bf16, int what, hipStream_t st) {
 }
 
 // What the segments add to their states, and from that what each finds
-hipError_t run_starts(const MemArgs& p, bool bf16, int what, hipStream_t st) {
-  if (const hipError_t e = run_chunks(p, bf16, what, st); e != hipSuccess) return e;
+hipError_t run_starts(const MemArgs& p, bool bf16, hipStream_t st) {
+  if (const hipError_t e = run_chunks(p, bf16, MEM_STATES, st); e != hipSuccess) return e;
   const int64_t blocks = (p.dk * p.dv / 4 + 255) / 256;
   hipLaunchKernelGGL(memory_scan_kernel, dim3((uint32_t)(p.m.sequences * p.heads * blocks)), dim3(256), 0, st, p);
   return hipGetLastError();
@@ -116,7 +116,7 @@ hipError_t launch_linear_attention(const ttc_linear_attention_t& a, int cus, voi
   if (p.m.entries != p.m.sequences) {
     p.added = static_cast<float*>(workspace);
     p.faded = p.added + p.m.entries * a.heads * a.dk * a.dv;
-    if (const hipError_t e = run_starts(p, bf16, MEM_STATES, st); e != hipSuccess) return e;
+    if (const hipError_t e = run_starts(p, bf16, st); e != hipSuccess) return e;
     p.starts = p.added;
   }
   return run_chunks(p, bf16, MEM_OUT, st);
@@ -198,11 +198,11 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
   if (segmented) {
     base.added = place(plan.added);
     base.faded = place(plan.faded);
-    if ((e = run_starts(base, bf16, MEM_STATES_DOTS, st)) != hipSuccess) return e;
+    if ((e = run_starts(base, bf16, st)) != hipSuccess) return e;
     base.starts = base.added;
     back.added = place(plan.added_r);
     back.faded = place(plan.faded_r);
-    if ((e = run_starts(back, bf16, MEM_STATES_DOTS, st)) != hipSuccess) return e;
+    if ((e = run_starts(back, bf16, st)) != hipSuccess) return e;
     back.starts = back.added;
   }
   const auto result = [&](MemArgs& p, void* out, uint64_t parts, int heads, int d) {

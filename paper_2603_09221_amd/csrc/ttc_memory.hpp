@@ -182,16 +182,20 @@ __device__ __forceinline__ float mem_finite(const mem_float8& v, float so_far) {
   return so_far;
 }
 
-// Eight float32 numbers as a sum of PARTS operands, the largest part first.  One or two parts are rounded to nearest: 8 or 17 significant bits, 2^-9 or 2^-18
-// of a number at most; three are cut off and hold all 24.  (An infinity leaves NaN in the second, as does a number beyond the largest bfloat16.)
+// Eight float32 numbers as a sum of PARTS operands, the largest part first.  One part is rounded to nearest, 2^-9 of a number at
+// most; three are cut off and hold all 24 bits.  (An infinity leaves NaN in the second, as does a number beyond the largest bfloat16.)
 template <int PARTS>
 __device__ __forceinline__ void mem_split(const float (&x)[8], srv_bf16x8 (&part)[PARTS]) {
-  float rest[8];
+  static_assert(PARTS == 1 || PARTS == 3);
+  if constexpr (PARTS == 1) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) rest[i] = x[i];
+    for (int i = 0; i < 8; ++i) part[0][i] = static_cast<__bf16>(x[i]);
+  } else {
+    float rest[8];
 #pragma unroll
-  for (int k = 0; k < PARTS; ++k) {
-    if constexpr (PARTS == 3) {
+    for (int i = 0; i < 8; ++i) rest[i] = x[i];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
       srv_uintx4 p;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -201,12 +205,6 @@ __device__ __forceinline__ void mem_split(const float (&x)[8], srv_bf16x8 (&part
         rest[2 * i + 1] -= __uint_as_float(hi & 0xffff0000u);
       }
       part[k] = __builtin_bit_cast(srv_bf16x8, p);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) part[k][i] = static_cast<__bf16>(rest[i]);
-      if (k + 1 < PARTS)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) rest[i] -= (float)part[k][i];
     }
   }
 }
@@ -418,22 +416,22 @@ struct MemPlace {
   }
 };
 
-// What a segment adds to its state; results; results and their products with other rows; what a segment adds, for these
-enum MemWhat { MEM_STATES, MEM_OUT, MEM_OUT_DOTS, MEM_STATES_DOTS };
+// What a segment adds to its state; results; results and their products with other rows
+enum MemWhat { MEM_STATES, MEM_OUT, MEM_OUT_DOTS };
 
 // A workgroup takes one segment of one head of one sequence, and of the values' columns a slice of 16 * WAVES; a wavefront owns 16 of them and their
 // state, DK numbers each, which stays in its registers from chunk to chunk: what a lane holds of it as a result is what it has to hold of it as an operand
 // if the sum's order follows.  The next chunk's rows and decays are on their way while one is worked on.
-// bfloat16 rows: pairs' products and the state that queries meet are rounded to bfloat16 for their products, 2^-9 each, what is added to a state
-// to 17 bits (7e-7 of a state in the norm, in one case measured, where three parts gave 1.3e-7: 48 of 94 products of a chunk and a tenth of the vector
-// instructions less by a third), as the header's documentation states; where gradients of decays, sums of float32 numbers, depend on them, both take
-// three parts, all of float32's bits.  Matrix and vector instructions take turns here: a chunk of a wavefront is the sum of both.
+// bfloat16 rows: pairs' products and the state that queries meet are rounded to bfloat16 for their products, 2^-9 each, as the header's documentation
+// states; where gradients of decays, sums of float32 numbers, depend on what a token reads, the state has three parts, all of float32's bits, and so has
+// always what is added to it (two, 17 bits, left a state of 16384 tokens 1.6e-6 off in the norm; three leave 1.3e-7).  Matrix and vector instructions take
+// turns here: a chunk of a wavefront is the sum of both.
 template <typename T, int DK, int WAVES, int WHAT>
 __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)) memory_chunk_kernel(const MemArgs a) {
   typedef MemShape<T, DK, WAVES> S;
   typedef typename MemOperand<T>::type op_t;
-  constexpr bool BF16 = sizeof(T) == 2, STATES = WHAT == MEM_STATES || WHAT == MEM_STATES_DOTS, DOTS = WHAT == MEM_OUT_DOTS;
-  constexpr int IN = BF16 && DOTS ? 3 : 1, UP = !BF16 ? 1 : DOTS || WHAT == MEM_STATES_DOTS ? 3 : 2, KT = DK / 16;
+  constexpr bool BF16 = sizeof(T) == 2, STATES = WHAT == MEM_STATES, DOTS = WHAT == MEM_OUT_DOTS;
+  constexpr int IN = BF16 && DOTS ? 3 : 1, UP = BF16 ? 3 : 1, KT = DK / 16;
   constexpr int HALVES = WAVES / 4;  // wavefronts that share sixteen rows of pairs
   __shared__ alignas(16) T xl[STATES ? 8 : MEM_CHUNK * (S::OWN || S::XS > S::PS ? S::XS : S::PS)], wl[MEM_CHUNK * S::XS], vl[MEM_CHUNK * S::VS];
   __shared__ alignas(16) T own[STATES || !S::OWN ? 8 : MEM_CHUNK * S::PS];
