@@ -449,7 +449,8 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
   const int chunks = (int)(((int64_t)n + MEM_CHUNK - 1) / MEM_CHUNK), segments = max(1, (chunks + a.m.segment - 1) / a.m.segment);
   const int c0 = segment * a.m.segment, c1 = min(c0 + a.m.segment, chunks);
   const bool reverse = a.reverse;
-  const float sign = reverse ? -1.f : 1.f;
+  const int order = reverse ? -1 : 1;  // (a factor, where a choice would be a branch)
+  const float sign = (float)order;
   if (STATES && segment == (reverse ? 0 : segments - 1)) return;  // nobody finds what this one leaves
   const int col0 = slice * S::COLS + wave * 16, cols = a.v.d;
 
@@ -551,10 +552,9 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
 #pragma unroll
         for (int u = 0; u < 4 / HALVES; ++u) {
           const int j = j0 + HALVES * u;
-          if (reverse ? j >= own_rows : j <= own_rows) {
-            const T* key = wl + (16 * j + c) * S::XS + 32 * k + 8 * g;
-            z[u] = mem_mma(mem_operand(key, key + 4), x, z[u]);
-          }
+          if (HALVES == 1 && order * (j - own_rows) > 0) continue;  // (of two wavefronts to sixteen rows both have something to do)
+          const T* key = wl + (16 * j + c) * S::XS + 32 * k + 8 * g;
+          z[u] = mem_mma(mem_operand(key, key + 4), x, z[u]);
         }
         if constexpr (S::RESIDENT == 4) __builtin_amdgcn_sched_barrier(0);
       }
@@ -574,11 +574,11 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
           for (int r = 0; r < 4; ++r) {
             float x = a.pair_scale * z[u][r] * mem_between(own_hi, own_lo, hi[r], lo[r], sign);
             asm volatile("" : "+v"(x));  // (a select, not a branch for every number)
-            p[r] = (reverse ? 4 * g + r >= c : 4 * g + r <= c) ? x : 0.f;
+            p[r] = order * (4 * g + r - c) <= 0 ? x : 0.f;
           }
-        } else if (reverse ? j > own_rows : j < own_rows) {
+        } else if (order * (j - own_rows) < 0) {
           const srv_floatx4 left = *reinterpret_cast<const srv_floatx4*>(&dl.left[16 * j + 4 * g]);
-          const float way = own_since * __builtin_amdgcn_exp2f(reverse ? dl.border[j][0] - dl.border[own_rows][1] : dl.border[own_rows][0] - dl.border[j][1]);
+          const float way = own_since * __builtin_amdgcn_exp2f(dl.border[max(j, own_rows)][0] - dl.border[min(j, own_rows)][1]);
 #pragma unroll
           for (int r = 0; r < 4; ++r) p[r] = z[u][r] * way * left[r];
         }
@@ -633,14 +633,19 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
           clean[k] = y[0];
         }
       }
+      const auto pairs = [&](int i, int k) {
+        const T* row = pl + (16 * i + c) * S::PS + 32 * k + 8 * g;
+        o[i] = mem_mma(clean[k], mem_operand(row, row + 4), o[i]);
+      };
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-          if (reverse ? 2 * k + 1 >= i : 2 * k <= i) {
-            const T* row = pl + (16 * i + c) * S::PS + 32 * k + 8 * g;
-            o[i] = mem_mma(clean[k], mem_operand(row, row + 4), o[i]);
-          }
+      for (int i = 0; i < 4; ++i) pairs(i, i / 2);
+      if (reverse) {
+        pairs(0, 1);
+        pairs(1, 1);
+      } else {
+        pairs(2, 0);
+        pairs(3, 0);
+      }
       if (bad)
         for (int j = 0; j < rows; ++j)
 #pragma unroll
@@ -648,7 +653,7 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               const float y = srv_widen(vl[j * S::VS + wave * 16 + 4 * g + r]);
-              const bool seen = reverse ? j >= 16 * i + c : j <= 16 * i + c;
+              const bool seen = order * (j - (16 * i + c)) <= 0;
               if (seen && !isfinite(y)) o[i][r] += srv_widen(pl[(16 * i + c) * S::PS + j]) * y;
             }
       const int64_t out_at = t0 * a.out_token + head * a.out_head + col0;
