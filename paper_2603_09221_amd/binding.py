@@ -935,9 +935,14 @@ def ttc_kv_place(past, new_tokens, block_table, page, tokens, *, pages, free=Non
     out = dict(out) if out else {}
     at = {}
     for name, n in sizes.items():
-        if out.get(name) is None:
-            out[name] = _new(past, (n,), PLACE_OUTPUTS[name], stream)
-        at[name] = _vector(out[name], n, PLACE_OUTPUTS[name], name)
+        if out.get(name) is not None:
+            at[name] = _vector(out[name], n, PLACE_OUTPUTS[name], name)
+    for dtype in (torch.int32, torch.int64):  # of each type the new tensors are parts of one: an allocation apiece is half of the call
+        names = [name for name in sizes if name not in at and PLACE_OUTPUTS[name] is dtype]
+        if names:
+            parts = _new(past, (sum(sizes[name] for name in names),), dtype, stream).split([sizes[name] for name in names])
+            for name, part in zip(names, parts):
+                out[name], at[name] = part, part.data_ptr()
     _same_device(past, new_tokens, block_table, free, free_count, *(out[name] for name in sizes))
     _here(past, stream)
     _check(load().ttc_kv_place(KvPlace(sequences, tokens, pages, page, width, before, new, block_table.data_ptr(), table_stride, listed,
