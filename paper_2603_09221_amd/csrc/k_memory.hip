@@ -5,7 +5,7 @@
 namespace ttc {
 
 template <typename T, int WAVES>
-static void chunks(const MemArgs& a, int what, uint32_t grid, hipStream_t st) {
+static void chunks(const MemTwo& a, int what, uint32_t grid, hipStream_t st) {
   switch (what) {
     case MEM_STATES: hipLaunchKernelGGL((memory_chunk_kernel<T, TTC_D, WAVES, MEM_STATES>), dim3(grid), dim3(64 * WAVES), 0, st, a); break;
     case MEM_OUT: hipLaunchKernelGGL((memory_chunk_kernel<T, TTC_D, WAVES, MEM_OUT>), dim3(grid), dim3(64 * WAVES), 0, st, a); break;
@@ -14,7 +14,7 @@ static void chunks(const MemArgs& a, int what, uint32_t grid, hipStream_t st) {
 }
 
 template <>
-hipError_t launch_memory_chunks<TTC_D>(const MemArgs& a, bool bf16, int columns, int what, uint32_t grid, hipStream_t st) {
+hipError_t launch_memory_chunks<TTC_D>(const MemTwo& a, bool bf16, int columns, int what, uint32_t grid, hipStream_t st) {
   if (columns == 128) {
     if (bf16) chunks<unsigned short, 8>(a, what, grid, st);
 #if TTC_D <= 128

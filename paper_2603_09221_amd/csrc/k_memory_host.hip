@@ -4,9 +4,9 @@
 
 namespace ttc {
 
-template <> hipError_t launch_memory_chunks<64>(const MemArgs&, bool, int, int, uint32_t, hipStream_t);
-template <> hipError_t launch_memory_chunks<128>(const MemArgs&, bool, int, int, uint32_t, hipStream_t);
-template <> hipError_t launch_memory_chunks<256>(const MemArgs&, bool, int, int, uint32_t, hipStream_t);
+template <> hipError_t launch_memory_chunks<64>(const MemTwo&, bool, int, int, uint32_t, hipStream_t);
+template <> hipError_t launch_memory_chunks<128>(const MemTwo&, bool, int, int, uint32_t, hipStream_t);
+template <> hipError_t launch_memory_chunks<256>(const MemTwo&, bool, int, int, uint32_t, hipStream_t);
 template <> hipError_t launch_memory_step<64>(const MemArgs&, bool, uint32_t, hipStream_t);
 template <> hipError_t launch_memory_step<128>(const MemArgs&, bool, uint32_t, hipStream_t);
 template <> hipError_t launch_memory_step<256>(const MemArgs&, bool, uint32_t, hipStream_t);
@@ -74,20 +74,23 @@ MemArgs forward_args(const ttc_linear_attention_t& a) {
   return p;
 }
 
-hipError_t run_chunks(MemArgs p, bool bf16, int what, hipStream_t st) {
-  const int rows = p.w.d;
-  const int columns = columns_of(rows, p.v.d, bf16);
-  p.slices = slices_of(rows, p.v.d, bf16);
-  const uint32_t grid = dealt(p.m, p.heads, p.slices);
+// One call, or two of the same sequences, heads and sizes
+hipError_t run_chunks(const MemArgs& a, const MemArgs* b, bool bf16, int what, hipStream_t st) {
+  const int rows = a.w.d, columns = columns_of(rows, a.v.d, bf16);
+  MemTwo p = {{a, b ? *b : a}, 0};
+  p.of[0].slices = p.of[1].slices = slices_of(rows, a.v.d, bf16);
+  p.split = dealt(a.m, a.heads, p.of[0].slices);
+  const uint32_t grid = b ? 2 * p.split : p.split;
   return rows <= 64 ? launch_memory_chunks<64>(p, bf16, columns, what, grid, st)
                     : rows <= 128 ? launch_memory_chunks<128>(p, bf16, columns, what, grid, st) : launch_memory_chunks<256>(p, bf16, columns, what, grid, st);
 }
 
 // What the segments add to their states, and from that what each finds
-hipError_t run_starts(const MemArgs& p, bool bf16, hipStream_t st) {
-  if (const hipError_t e = run_chunks(p, bf16, MEM_STATES, st); e != hipSuccess) return e;
-  const int64_t blocks = (p.dk * p.dv / 4 + 255) / 256;
-  hipLaunchKernelGGL(memory_scan_kernel, dim3((uint32_t)(p.m.sequences * p.heads * blocks)), dim3(256), 0, st, p);
+hipError_t run_starts(const MemArgs& a, const MemArgs* b, bool bf16, hipStream_t st) {
+  if (const hipError_t e = run_chunks(a, b, bf16, MEM_STATES, st); e != hipSuccess) return e;
+  const int64_t blocks = (a.dk * a.dv / 4 + 255) / 256;
+  MemTwo p = {{a, b ? *b : a}, (uint32_t)(a.m.sequences * a.heads * blocks)};
+  hipLaunchKernelGGL(memory_scan_kernel, dim3(b ? 2 * p.split : p.split), dim3(256), 0, st, p);
   return hipGetLastError();
 }
 
@@ -116,10 +119,10 @@ hipError_t launch_linear_attention(const ttc_linear_attention_t& a, int cus, voi
   if (p.m.entries != p.m.sequences) {
     p.added = static_cast<float*>(workspace);
     p.faded = p.added + p.m.entries * a.heads * a.dk * a.dv;
-    if (const hipError_t e = run_starts(p, bf16, st); e != hipSuccess) return e;
+    if (const hipError_t e = run_starts(p, nullptr, bf16, st); e != hipSuccess) return e;
     p.starts = p.added;
   }
-  return run_chunks(p, bf16, MEM_OUT, st);
+  return run_chunks(p, nullptr, bf16, MEM_OUT, st);
 }
 
 namespace {
@@ -198,11 +201,10 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
   if (segmented) {
     base.added = place(plan.added);
     base.faded = place(plan.faded);
-    if ((e = run_starts(base, bf16, st)) != hipSuccess) return e;
-    base.starts = base.added;
     back.added = place(plan.added_r);
     back.faded = place(plan.faded_r);
-    if ((e = run_starts(back, bf16, st)) != hipSuccess) return e;
+    if ((e = run_starts(base, &back, bf16, st)) != hipSuccess) return e;
+    base.starts = base.added;
     back.starts = back.added;
   }
   const auto result = [&](MemArgs& p, void* out, uint64_t parts, int heads, int d) {
@@ -214,7 +216,7 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
   };
   MemArgs dv = back;
   result(dv, b.gv, 0, f.heads, f.dv);
-  if ((e = run_chunks(dv, bf16, MEM_OUT, st)) != hipSuccess) return e;
+  if ((e = run_chunks(dv, nullptr, bf16, MEM_OUT, st)) != hipSuccess) return e;
   MemArgs dk = back;
   dk.x = v;
   dk.w = gout;
@@ -225,7 +227,6 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
   dk.dot = k;
   dk.dots = place(plan.b);
   result(dk, b.gk, plan.gk, f.heads_qk, f.dk);
-  if ((e = run_chunks(dk, bf16, MEM_OUT_DOTS, st)) != hipSuccess) return e;
   MemArgs dq = base;
   dq.x = gout;
   dq.w = v;
@@ -235,18 +236,19 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
   dq.dot = q;
   dq.dots = place(plan.a);
   result(dq, b.gq, plan.gq, f.heads_qk, f.dk);
-  if ((e = run_chunks(dq, bf16, MEM_OUT_DOTS, st)) != hipSuccess) return e;
+  if ((e = run_chunks(dk, &dq, bf16, MEM_OUT_DOTS, st)) != hipSuccess) return e;
   if (group > 1) {
     MemSequences m = plan.chunks;
     m.blocks = blocks_of(m.entries, f.heads_qk);
-    const dim3 grid(dealt(m, f.heads_qk, 1));
-    for (int i = 0; i < 2; ++i) {
-      const float* parts = place(i ? plan.gk : plan.gq);
-      void* out = i ? b.gk : b.gq;
-      if (bf16) hipLaunchKernelGGL((memory_heads_kernel<unsigned short>), grid, dim3(256), 0, st, m, parts, static_cast<unsigned short*>(out), f.heads_qk, group, f.dk);
-      else hipLaunchKernelGGL((memory_heads_kernel<float>), grid, dim3(256), 0, st, m, parts, static_cast<float*>(out), f.heads_qk, group, f.dk);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
+    const uint32_t split = dealt(m, f.heads_qk, 1);
+    const auto run = [&](auto type) {
+      typedef decltype(type) T;
+      hipLaunchKernelGGL((memory_heads_kernel<T>), dim3(2 * split), dim3(256), 0, st, m, place(plan.gq), static_cast<T*>(b.gq), place(plan.gk),
+                         static_cast<T*>(b.gk), split, f.heads_qk, group, f.dk);
+    };
+    if (bf16) run((unsigned short)0);
+    else run(0.f);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   MemDecayArgs d = {};
   d.m = plan.chunks;

@@ -26,10 +26,10 @@ struct MemSequences {
   int32_t blocks;      // of heads: what the XCDs take in turn is a segment of one block's heads (mem_deal)
 };
 
-// Workgroup b's segment and head, of `per_head` workgroups for each.  Every eighth workgroup lies on one XCD.  An XCD takes whole segments, of all heads
+// The segment and head of workgroup b, of `per_head` workgroups for each.  Every eighth workgroup lies on one XCD.  An XCD takes whole segments, of all heads
 // or of a block of them: rows that heads share are in its cache.  Places without a segment come last.
-__device__ __forceinline__ void mem_deal(const MemSequences& m, int heads, uint32_t per_head, int64_t& entry, int& head, int& rest) {
-  const uint32_t inner = heads / m.blocks * per_head, turn = blockIdx.x / 8, item = turn / inner * 8 + blockIdx.x % 8, in = turn % inner;
+__device__ __forceinline__ void mem_deal(const MemSequences& m, uint32_t b, int heads, uint32_t per_head, int64_t& entry, int& head, int& rest) {
+  const uint32_t inner = heads / m.blocks * per_head, turn = b / 8, item = turn / inner * 8 + b % 8, in = turn % inner;
   entry = item / m.blocks;
   head = item % m.blocks * (heads / m.blocks) + in / per_head;
   rest = in % per_head;
@@ -280,6 +280,13 @@ struct MemArgs {
   float* dots;                  // (slices, heads, tokens)
 };
 
+// Two calls of the same sizes in one launch (a gradient's, of tokens in both orders: what one leaves idle is the other's); the first `split` workgroups, a
+// multiple of eight, are the first one's
+struct MemTwo {
+  MemArgs of[2];
+  uint32_t split;
+};
+
 // Decays of a chunk, a token to a lane, added up in float64, so that the differences of sums are as exact as the decays themselves; powers of two
 struct MemDecays {
   float hi[MEM_CHUNK], lo[MEM_CHUNK];   // G / ln 2 as a sum of two
@@ -427,7 +434,9 @@ enum MemWhat { MEM_STATES, MEM_OUT, MEM_OUT_DOTS };
 // always what is added to it (two, 17 bits, left a state of 16384 tokens 1.6e-6 off in the norm; three leave 1.3e-7).  Matrix and vector instructions take
 // turns here: a chunk of a wavefront is the sum of both.
 template <typename T, int DK, int WAVES, int WHAT>
-__global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)) memory_chunk_kernel(const MemArgs a) {
+__global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)) memory_chunk_kernel(const MemTwo two) {
+  const bool second = blockIdx.x >= two.split;
+  const MemArgs& a = two.of[second];
   typedef MemShape<T, DK, WAVES> S;
   typedef typename MemOperand<T>::type op_t;
   constexpr bool BF16 = sizeof(T) == 2, STATES = WHAT == MEM_STATES, DOTS = WHAT == MEM_OUT_DOTS;
@@ -442,7 +451,7 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
   int c = lane & 15, g = lane >> 4;
   int64_t entry;
   int head, slice;
-  mem_deal(a.m, a.heads, a.slices, entry, head, slice);
+  mem_deal(a.m, second ? blockIdx.x - two.split : blockIdx.x, a.heads, a.slices, entry, head, slice);
   int64_t seq, first;
   int segment, n;
   if (entry >= a.m.entries || !mem_segment(a.m, entry, seq, segment, first, n)) return;
@@ -711,10 +720,13 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
 }
 
 // The segments' states: what each adds becomes what each finds, four numbers of one head's state to a thread.
-static __global__ void __launch_bounds__(256) memory_scan_kernel(const MemArgs a) {
+static __global__ void __launch_bounds__(256) memory_scan_kernel(const MemTwo two) {
+  const bool second = blockIdx.x >= two.split;
+  const MemArgs& a = two.of[second];
+  const uint32_t b = second ? blockIdx.x - two.split : blockIdx.x;
   const int quads = a.dk * a.dv / 4, blocks = (quads + 255) / 256;
-  const int head = blockIdx.x / blocks % a.heads, e = (blockIdx.x % blocks * 256 + threadIdx.x) * 4;
-  const int64_t seq = blockIdx.x / blocks / a.heads;
+  const int head = b / blocks % a.heads, e = (b % blocks * 256 + threadIdx.x) * 4;
+  const int64_t seq = b / blocks / a.heads;
   int64_t entry = 0, first;
   int n;
   for (int64_t s = threadIdx.x & 63; s < seq; s += 64) {

@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(256, 4) memory_pairs_kernel(const MemDecayArgs
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
   int64_t entry, seq, first;
   int head, none, chunk, n;
-  mem_deal(a.m, a.heads, 1, entry, head, none);
+  mem_deal(a.m, blockIdx.x, a.heads, 1, entry, head, none);
   if (entry >= a.m.entries || !mem_segment(a.m, entry, seq, chunk, first, n)) return;
   const int64_t t0 = first + (int64_t)chunk * MEM_CHUNK;
   const int rows = min(MEM_CHUNK, n - chunk * MEM_CHUNK);
@@ -212,10 +212,13 @@ static __global__ void memory_decay_sum_kernel(const double* sums, int64_t entri
 
 // The gradients of heads that share a row, in their order: a chunk's tokens of one shared head to a workgroup, four entries at a time to a thread
 template <typename T>
-__global__ void __launch_bounds__(256) memory_heads_kernel(const MemSequences m, const float* parts, T* out, int heads, int group, int d) {
+__global__ void __launch_bounds__(256) memory_heads_kernel(const MemSequences m, const float* parts0, T* out0, const float* parts1, T* out1, uint32_t split, int heads, int group, int d) {
+  const bool second = blockIdx.x >= split;  // (two in one launch, as MemTwo)
+  const float* const parts = second ? parts1 : parts0;
+  T* const out = second ? out1 : out0;
   int64_t entry, seq, first;
   int head, none, chunk, n;
-  mem_deal(m, heads, 1, entry, head, none);
+  mem_deal(m, second ? blockIdx.x - split : blockIdx.x, heads, 1, entry, head, none);
   if (entry >= m.entries || !mem_segment(m, entry, seq, chunk, first, n)) return;
   const int64_t t0 = first + (int64_t)chunk * MEM_CHUNK;
   const int quads = min(MEM_CHUNK, n - chunk * MEM_CHUNK) * (d / 4);

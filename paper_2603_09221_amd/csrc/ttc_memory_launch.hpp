@@ -17,7 +17,8 @@ hipError_t launch_residual_norm_backward(const ttc_residual_norm_backward_t& b, 
 
 // rows of x and w of up to D entries; columns of a workgroup (64 or 128); what: a MemWhat
 struct MemArgs;
-template <int D> hipError_t launch_memory_chunks(const MemArgs& a, bool bf16, int columns, int what, uint32_t grid, hipStream_t st);
+struct MemTwo;
+template <int D> hipError_t launch_memory_chunks(const MemTwo& a, bool bf16, int columns, int what, uint32_t grid, hipStream_t st);
 template <int D> hipError_t launch_memory_step(const MemArgs& a, bool bf16, uint32_t grid, hipStream_t st);
 
 }  // namespace ttc
