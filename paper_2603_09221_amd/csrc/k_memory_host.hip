@@ -138,7 +138,7 @@ BackwardPlan plan_backward(const ttc_linear_attention_backward_t& b, int cus) {
   const ttc_linear_attention_t& f = b.forward;
   BackwardPlan p = {};
   p.slices = slices_of(f.dv, f.dk, f.dtype == TTC_BF16);
-  p.m = sequences_of(f, segment_of(f, p.slices, cus));
+  p.m = sequences_of(f, segment_of(f, 2 * p.slices, cus));  // (two calls in a launch: 255 us where segments for one each take 287)
   p.chunks = sequences_of(f, 1);
   uint64_t at = 0;
   const auto take = [&](uint64_t& place, uint64_t bytes) {

@@ -57,7 +57,7 @@ __device__ __forceinline__ float mem_sixteen(float x) {
 template <typename T>
 __global__ void __launch_bounds__(256, 4) memory_pairs_kernel(const MemDecayArgs a) {
   typedef typename MemOperand<T>::type op_t;
-  constexpr int STEPS = sizeof(T) == 2 ? 2 : 1;  // operands of 32 entries in a block
+  constexpr int STEPS = sizeof(T) == 2 ? 4 : 1;  // operands of 32 entries in a block: what registers hold
   __shared__ alignas(16) MemDecays dl;
   __shared__ alignas(16) float left[MEM_CHUNK], below[4][MEM_CHUNK];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
