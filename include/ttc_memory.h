@@ -24,7 +24,7 @@ extern "C" {
  * as -200, which leaves nothing of a state: -inf begins anew).  Head h has query and key head h / (heads / heads_qk).
  * Sequences are packed as in ttc_attention: sequence s has the rows cu_q[s] .. cu_q[s+1]-1, rows behind the last are left as they are.
  * dk and dv are multiples of 8 from 8 to 256; rows of tokens are at most 2^23 - 1 entries apart.
- * States, sums and decays are float32 or wider.  bfloat16 rows, sequences of more than four tokens: what queries meet of the state, and the
+ * States, sums and decays are float32 or wider.  bfloat16 rows, max_q more than 6: what queries meet of the state, and the
  * products of queries and keys of one chunk of 64 tokens, are rounded to bfloat16 for their products (2^-9 of each); nothing else but the
  * results is rounded to less than float32's 24 bits.
  * A token's NaN or infinity reaches its own and later tokens' results, and no earlier ones (an infinity may become NaN there). */

@@ -51,6 +51,17 @@ def test_against_oracle(lengths, heads, heads_qk, dk, dv, dtype, constant):
     check(q, k, v, g, cu, out["out"], out["state"])
 
 
+@pytest.mark.parametrize("most", [5, 6, 7, 15, 16, 17])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_few_tokens_on_both_sides_of_the_rules(most, dtype):
+    """Sequences that one kernel goes through token by token and the other in chunks."""
+    lengths = [most, 0, 1, most - 2, 3]
+    q, k, v, g, cu = attention_inputs(lengths, 4, 2, 64, 72, dtype, seed=most)
+    first = torch.randn((5, 4, 64, 72), generator=torch.Generator().manual_seed(most)).to(q.device)
+    out = binding.ttc_linear_attention(q, k, v, g, cu_q=cu, max_q=most, state=first, want_state=True)
+    check(q, k, v, g, cu, out["out"], out["state"], host(first))
+
+
 @pytest.mark.parametrize("dk,dv", [(64, 64), (128, 128), (256, 256), (24, 200)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_single_tokens_with_rows_of_a_pool(dk, dv, dtype):
