@@ -4,14 +4,17 @@
 
 namespace ttc {
 
-constexpr int NORM_THREADS = 2048;  // of a compute unit, forward
+// Threads of a compute unit: forward all that fit (16384 rows of 4096 bfloat16: 117 us; 121 with 2048, 123 with 1024); backward those that their registers
+// leave room for at once, as every workgroup leaves a part of each sum (8192 rows of 4096: 136 us; 146 with 1024, 167 with 2048).
+constexpr int NORM_THREADS = 4096, NORM_THREADS_BACKWARD = 512;
 
 static bool row16(const void* p, int64_t stride, int32_t dtype) {
   const int64_t bytes = dtype == TTC_BF16 ? 2 : 4;
   return (uint64_t)p % 16 == 0 && stride * bytes % 16 == 0;
 }
 
-// The fewest threads that hold a row in eights: more eights to a thread take registers that the wavefronts in flight lack
+// A thread to every eight features as far as a workgroup goes: more eights to a thread take registers that the wavefronts in flight lack (two: 123 us
+// forward where one takes 121, 256 us backward where one takes 136)
 template <typename F>
 static void norm_shape(int features, F&& f) {
   if (features <= 512) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
@@ -43,7 +46,7 @@ static int norm_grid(const ttc_residual_norm_t& n, int cus) {
   int grid = 0;
   norm_shape(n.features, [&](auto lanes, auto pieces) {
     typedef NormShape<decltype(lanes)::value, decltype(pieces)::value> S;
-    const int64_t rows = (n.tokens + S::ROWS - 1) / S::ROWS, most = (int64_t)cus * (1024 / S::THREADS);
+    const int64_t rows = (n.tokens + S::ROWS - 1) / S::ROWS, each = NORM_THREADS_BACKWARD / S::THREADS, most = cus * (each ? each : 1);
     grid = (int)(rows < most ? rows : most);
   });
   return grid;

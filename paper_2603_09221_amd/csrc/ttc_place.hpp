@@ -7,7 +7,8 @@
 namespace ttc {
 
 constexpr int PLACE_THREADS = 1024;       // sequences that are added up at once
-constexpr int64_t PLACE_ALONE = 4096;     // tokens that the one workgroup places itself
+// Tokens that the one workgroup places itself: 64 sequences with 2048 in 5.9 us, 9.1 with a second launch; with 4096 in 8.2 and 8.8, with 8192 in 12.7 and 8.9
+constexpr int64_t PLACE_ALONE = 4096;
 constexpr int PLACE_TOKENS = 4;           // tokens of a thread of place_tokens_kernel
 
 // Inclusive sums over the workgroup's threads; every thread also gets the whole.  `waves`: 16 numbers of LDS, free again on return.
