@@ -151,19 +151,19 @@ __device__ __forceinline__ mem_float8 mem_operand(const float* p, const float* q
   const srv_floatx4 a = *reinterpret_cast<const srv_floatx4*>(p), b = *reinterpret_cast<const srv_floatx4*>(q);
   return {{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
 }
-// Column c of the eight rows from `p` on, `step` numbers apart; p: column 0 of 16 in LDS.  Of bfloat16 sixteen lanes read four rows of sixteen
-// numbers, four to a lane, and get a column's four each.
-__device__ __forceinline__ srv_bf16x8 mem_column(const unsigned short* p, int step, int c) {
+// Column c of the eight rows 4 g .. 4 g + 3 and 16 + 4 g .. 16 + 4 g + 3, `step` numbers apart; p: column 0 of 16 of row 0 in LDS.  Of bfloat16 sixteen
+// lanes read four rows of sixteen numbers, four to a lane, and get a column's four each.
+__device__ __forceinline__ srv_bf16x8 mem_column(const unsigned short* p, int step, int g, int c) {
   typedef __bf16 four_t __attribute__((ext_vector_type(4)));
   typedef __attribute__((address_space(3))) four_t* lds_t;
-  const unsigned short* q = p + (c >> 2) * step + (c & 3) * 4;
-  const four_t a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_t)q), b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_t)(q + 4 * step));
+  const unsigned short* q = p + (4 * g + (c >> 2)) * step + (c & 3) * 4;
+  const four_t a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_t)q), b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_t)(q + 16 * step));
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
-__device__ __forceinline__ mem_float8 mem_column(const float* p, int step, int c) {
+__device__ __forceinline__ mem_float8 mem_column(const float* p, int step, int g, int c) {
   mem_float8 x;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x.x[i] = p[i * step + c];
+  for (int i = 0; i < 8; ++i) x.x[i] = p[(4 * g + i + (i < 4 ? 0 : 12)) * step + c];
   return x;
 }
 __device__ __forceinline__ float mem_entry(const srv_bf16x8& v, int i) { return (float)v[i]; }
@@ -233,10 +233,21 @@ __device__ __forceinline__ void mem_fetch(const float* p, MemEight<float>& to) {
   to.x[0] = *reinterpret_cast<const mem_floatx4*>(p);
   to.x[1] = *reinterpret_cast<const mem_floatx4*>(p + 4);
 }
-__device__ __forceinline__ void mem_put(unsigned short* p, const MemEight<unsigned short>& x) { *reinterpret_cast<srv_u16x8*>(p) = x.x; }
+// to LDS, the second four `apart` from the first
+template <int APART>
+__device__ __forceinline__ void mem_put(unsigned short* p, const MemEight<unsigned short>& x) {
+  if constexpr (APART == 4) {
+    *reinterpret_cast<srv_u16x8*>(p) = x.x;
+  } else {
+    const srv_uintx4 u = __builtin_bit_cast(srv_uintx4, x.x);
+    *reinterpret_cast<srv_uintx2*>(p) = srv_uintx2{u[0], u[1]};
+    *reinterpret_cast<srv_uintx2*>(p + APART) = srv_uintx2{u[2], u[3]};
+  }
+}
+template <int APART>
 __device__ __forceinline__ void mem_put(float* p, const MemEight<float>& x) {
   *reinterpret_cast<srv_floatx4*>(p) = x.x[0];
-  *reinterpret_cast<srv_floatx4*>(p + 4) = x.x[1];
+  *reinterpret_cast<srv_floatx4*>(p + APART) = x.x[1];
 }
 // four numbers to a row of any alignment
 __device__ __forceinline__ void mem_out4(unsigned short* p, const srv_floatx4& x) {
@@ -343,11 +354,14 @@ __device__ __forceinline__ float mem_between(float a_hi, float a_lo, float b_hi,
 
 template <typename T, int DK, int WAVES>
 struct MemShape {
-  static constexpr int PAD = 16 / sizeof(T);
+  // Rows of bfloat16 an odd multiple of 32 bytes apart: the columns that 32 lanes read at once lie on as many banks, and so do the 16 bytes of rows that 16
+  // do.  (Of 16 bytes, with the eight rows of a column's share one behind the other: LDS was busy for 53 % of a long prompt's cycles instead of 41 %, 148 us
+  // instead of 137.)  Of float32 numbers what 64 lanes read of columns lies on 64 banks with 16 bytes more.
+  static constexpr int PAD = sizeof(T) == 2 ? 16 : 4;
   static constexpr int COLS = 16 * WAVES;
   static constexpr int XS = DK + PAD, VS = COLS + PAD, PS = MEM_CHUNK + PAD;  // rows in LDS
   // the pairs' products have a place of their own unless LDS is too small for it: then that of x, for one more barrier
-  static constexpr bool OWN = (2 * MEM_CHUNK * XS + MEM_CHUNK * VS + MEM_CHUNK * PS) * sizeof(T) <= 150 * 1024;
+  static constexpr bool OWN = MEM_CHUNK * (2 * XS + VS + PS) * sizeof(T) <= 150 * 1024;
   static constexpr int XP = DK / 8 / WAVES, VP = 2;  // pieces of eight that a thread brings
   // wavefronts of a SIMD that registers are kept for: two workgroups on a compute unit, where LDS has room for them; two at least, for with all 512
   // registers of one the compiler puts sums into accumulation registers and reads some of them too early behind a branch (the build looks for that)
@@ -355,9 +369,13 @@ struct MemShape {
   static constexpr bool AHEAD = sizeof(T) == 2 || DK * 8 <= 128 * WAVES;  // registers for the next chunk's rows
 };
 
+// Where entry e, a multiple of four, of a row of x lies in LDS: 16 b + 4 g + r at 8 g + 4 b + r of every 32, so that what a lane reads to meet a state's numbers
+// lies side by side
+__device__ __forceinline__ uint32_t mem_place(uint32_t e) { return (e & ~31u) + (e & 12) * 2 + (e & 16) / 4; }
+
 // 64 rows on their way to LDS: zeros behind the last row and behind the last entry.  Those places are read from the last row and entry that
 // are there, so that no load waits for a branch.
-template <typename T, int D, int STEP, int PIECES, int THREADS>
+template <typename T, int D, int STEP, int PIECES, int THREADS, bool PLACED = false>
 struct MemStage {
   static constexpr int ROW = D / 8, TURN = THREADS / ROW;  // pieces of a row, rows of one turn of the workgroup
   static_assert(PIECES * TURN == MEM_CHUNK);
@@ -376,15 +394,16 @@ struct MemStage {
     }
   }
   __device__ __forceinline__ void put(T* lds, int rows, int entries, bool whole) const {
-    T* p = lds + threadIdx.x / ROW * STEP + threadIdx.x % ROW * 8;
+    constexpr int APART = PLACED ? 8 : 4;
+    T* p = lds + threadIdx.x / ROW * STEP + (PLACED ? mem_place(threadIdx.x % ROW * 8) : threadIdx.x % ROW * 8);
     if (whole) {
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) mem_put(p + i * TURN * STEP, piece[i]);
+      for (int i = 0; i < PIECES; ++i) mem_put<APART>(p + i * TURN * STEP, piece[i]);
     } else {
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
         const bool there = (int)(threadIdx.x % ROW) * 8 < entries && (int)(threadIdx.x / ROW) + i * TURN < rows;
-        mem_put(p + i * TURN * STEP, there ? piece[i] : MemEight<T>{});
+        mem_put<APART>(p + i * TURN * STEP, there ? piece[i] : MemEight<T>{});
       }
     }
   }
@@ -463,7 +482,8 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
   if (STATES && segment == (reverse ? 0 : segments - 1)) return;  // nobody finds what this one leaves
   const int col0 = slice * S::COLS + wave * 16, cols = a.v.d;
 
-  MemStage<T, DK, S::XS, S::XP, 64 * WAVES> x_rows, w_rows;
+  MemStage<T, DK, S::XS, S::XP, 64 * WAVES, true> x_rows;
+  MemStage<T, DK, S::XS, S::XP, 64 * WAVES> w_rows;
   MemStage<T, S::COLS, S::VS, S::VP, 64 * WAVES> v_rows;
   float g_next = 0.f;
   const T* const x_at = static_cast<const T*>(a.x.p) + (STATES ? 0 : head / a.x.group * a.x.head);
@@ -544,8 +564,8 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
         mem_split<IN>(x, part);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const T* row = xl + (16 * i + c) * S::XS + 16 * k + 4 * g;
-          const op_t y = mem_operand(row, row + 16);
+          const T* row = xl + (16 * i + c) * S::XS + 16 * k + 8 * g;
+          const op_t y = mem_operand(row, row + 4);
 #pragma unroll
           for (int p = IN - 1; p >= 0; --p) o[i] = mem_mma(part[p], y, o[i]);
         }
@@ -556,8 +576,8 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
       srv_floatx4 z[4 / HALVES] = {};
 #pragma unroll
       for (int k = 0; k < DK / 32; ++k) {
-        const T* row = xl + (16 * own_rows + c) * S::XS + 32 * k + 8 * g;
-        const op_t x = mem_operand(row, row + 4);
+        const T* row = xl + (16 * own_rows + c) * S::XS + 32 * k + mem_place(8 * g);
+        const op_t x = mem_operand(row, row + 8);
 #pragma unroll
         for (int u = 0; u < 4 / HALVES; ++u) {
           const int j = j0 + HALVES * u;
@@ -591,7 +611,7 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
 #pragma unroll
           for (int r = 0; r < 4; ++r) p[r] = z[u][r] * way * left[r];
         }
-        mem_store4(pl + i * S::PS + 16 * j + 4 * g, p);
+        mem_store4(pl + i * S::PS + mem_place(16 * j + 4 * g), p);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] *= dl.in[16 * i + c];
@@ -617,7 +637,7 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
     float finite = 0.f;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      v[k] = mem_column(vl + (32 * k + 8 * g) * S::VS + wave * 16, S::VS, c);
+      v[k] = mem_column(vl + 32 * k * S::VS + wave * 16, S::VS, g, c);
       if constexpr (!STATES) finite = mem_finite(v[k], finite);
     }
     if constexpr (!STATES) {
@@ -663,7 +683,7 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
             for (int r = 0; r < 4; ++r) {
               const float y = srv_widen(vl[j * S::VS + wave * 16 + 4 * g + r]);
               const bool seen = order * (j - (16 * i + c)) <= 0;
-              if (seen && !isfinite(y)) o[i][r] += srv_widen(pl[(16 * i + c) * S::PS + j]) * y;
+              if (seen && !isfinite(y)) o[i][r] += srv_widen(pl[(16 * i + c) * S::PS + mem_place(j & ~3) + (j & 3)]) * y;
             }
       const int64_t out_at = t0 * a.out_token + head * a.out_head + col0;
       const uint32_t mine = c * (uint32_t)a.out_token + 4 * g;
@@ -681,7 +701,7 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
     for (int k = 0; k < KT; ++k) s[k] *= fade;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const srv_floatx4 u0 = *reinterpret_cast<const srv_floatx4*>(&dl.up[32 * h + 8 * g]), u1 = *reinterpret_cast<const srv_floatx4*>(&dl.up[32 * h + 8 * g + 4]);
+      const srv_floatx4 u0 = *reinterpret_cast<const srv_floatx4*>(&dl.up[32 * h + 4 * g]), u1 = *reinterpret_cast<const srv_floatx4*>(&dl.up[32 * h + 16 + 4 * g]);
       op_t up[UP];
       float x[8];
 #pragma unroll
@@ -689,7 +709,7 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
       mem_split<UP>(x, up);
 #pragma unroll
       for (int k = 0; k < KT; ++k) {
-        const op_t w = mem_column(wl + (32 * h + 8 * g) * S::XS + 16 * k, S::XS, c);
+        const op_t w = mem_column(wl + 32 * h * S::XS + 16 * k, S::XS, g, c);
 #pragma unroll
         for (int p = UP - 1; p >= 0; --p) s[k] = mem_mma(w, up[p], s[k]);
       }
