@@ -21,9 +21,10 @@ extern "C" {
  * Every head of every sequence has a state S of (dk, dv) float32 numbers.  Token t lets it fade, adds its key and value, and asks:
  *     S_t = exp(g_t) S_{t-1} + k_t v_t^T,     out_t = scale * S_t^T q_t.
  * g is the log decay, in float32, at most 0 (a positive one lets the state grow; numbers may then pass the largest float32; one below -200 counts
- * as -200, which leaves nothing of a state: -inf begins anew).  Head h has query and key head h / (heads / heads_qk).
+ * as -200, which leaves nothing of a finite state: -inf begins anew).  Head h has query and key head h / (heads / heads_qk).
  * Sequences are packed as in ttc_attention: sequence s has the rows cu_q[s] .. cu_q[s+1]-1, rows behind the last are left as they are.
- * dk and dv are multiples of 8 from 8 to 256; rows of tokens are at most 2^23 - 1 entries apart.
+ * dk and dv are multiples of 8 from 8 to 256; rows of tokens are at most 2^23 - 1 entries apart (in gradients
+ * heads * max(dk, dv) too).  A launch counts 2^32 threads: (tokens / 64 + sequences) * heads below 2^23 with sequences * heads below 2^20 are always taken.
  * States, sums and decays are float32 or wider.  bfloat16 rows, max_q more than 6: what queries meet of the state, and the
  * products of queries and keys of one chunk of 64 tokens, are rounded to bfloat16 for their products (2^-9 of each); nothing else but the
  * results is rounded to less than float32's 24 bits.

@@ -29,9 +29,16 @@ int blocks_of(int64_t entries, int heads) {
   while (n < heads && (entries * n < 16 || heads % n)) ++n;
   return n;
 }
-MemSequences sequences_of(const ttc_linear_attention_t& a, int segment) {
-  MemSequences m = {a.sequences, a.tokens, a.cu_q, a.max_q, segment, a.sequences, 1};
-  if ((int64_t)segment * MEM_CHUNK < a.max_q) m.entries += a.tokens / ((int64_t)segment * MEM_CHUNK);
+// Sequences in segments.  A sequence has places for as many as the longest has, or, where that takes more than `wider` times as many, sequences have what they
+// need, which every workgroup has to add up (gradients of 8192 times 72 tokens, 8 heads: 14.7 ms so).
+MemSequences sequences_of(const ttc_linear_attention_t& a, int segment, int wider) {
+  const int64_t rows = (int64_t)segment * MEM_CHUNK, longest = a.max_q < a.tokens ? a.max_q : a.tokens;
+  const int64_t each = longest <= rows ? 1 : (longest + rows - 1) / rows, tight = each == 1 ? a.sequences : a.sequences + a.tokens / rows;
+  MemSequences m = {a.sequences, a.tokens, a.cu_q, a.max_q, segment, tight, 0, 1};
+  if (each == 1 || ((double)a.sequences * each <= (double)tight * wider && (double)a.sequences * each * a.heads < 8388608.)) {  // (threads of a launch: 2^32)
+    m.entries = a.sequences * each;
+    m.each = (int32_t)each;
+  }
   m.blocks = blocks_of(m.entries, a.heads);
   return m;
 }
@@ -104,7 +111,7 @@ uint64_t round16(uint64_t n) { return (n + 15) & ~15ull; }
 
 uint64_t linear_attention_workspace(const ttc_linear_attention_t& a, int cus) {
   if (a.max_q <= step_most(a.dtype == TTC_BF16)) return 0;
-  const MemSequences m = sequences_of(a, segment_of(a, slices_of(a.dk, a.dv, a.dtype == TTC_BF16), cus));
+  const MemSequences m = sequences_of(a, segment_of(a, slices_of(a.dk, a.dv, a.dtype == TTC_BF16), cus), 1);
   if (m.entries == m.sequences) return 0;
   return (uint64_t)m.entries * a.heads * a.dk * a.dv * 4 + round16((uint64_t)m.entries * a.heads * 4);
 }
@@ -113,13 +120,12 @@ hipError_t launch_linear_attention(const ttc_linear_attention_t& a, int cus, voi
   const bool bf16 = a.dtype == TTC_BF16;
   MemArgs p = forward_args(a);
   if (a.max_q <= step_most(bf16)) {
-    p.m = sequences_of(a, 1);
-    p.m.entries = a.sequences;
+    p.m = sequences_of(a, 1, 1);
     p.slices = (a.dv + 63) / 64;
     const uint32_t grid = (uint32_t)(a.sequences * a.heads * p.slices);
     return a.dk <= 64 ? launch_memory_step<64>(p, bf16, grid, st) : a.dk <= 128 ? launch_memory_step<128>(p, bf16, grid, st) : launch_memory_step<256>(p, bf16, grid, st);
   }
-  p.m = sequences_of(a, segment_of(a, slices_of(a.dk, a.dv, a.dtype == TTC_BF16), cus));
+  p.m = sequences_of(a, segment_of(a, slices_of(a.dk, a.dv, a.dtype == TTC_BF16), cus), 1);
   if (p.m.entries != p.m.sequences) {
     p.added = static_cast<float*>(workspace);
     p.faded = p.added + p.m.entries * a.heads * a.dk * a.dv;
@@ -142,8 +148,8 @@ BackwardPlan plan_backward(const ttc_linear_attention_backward_t& b, int cus) {
   const ttc_linear_attention_t& f = b.forward;
   BackwardPlan p = {};
   p.slices = slices_of(f.dv, f.dk, f.dtype == TTC_BF16);
-  p.m = sequences_of(f, segment_of(f, 2 * p.slices, cus));  // (two calls are in a launch: 255 us where segments for one each take 287)
-  p.chunks = sequences_of(f, 1);
+  p.m = sequences_of(f, segment_of(f, 2 * p.slices, cus), 1);  // (two calls are in a launch: 255 us where segments for one each take 287)
+  p.chunks = sequences_of(f, 1, 8);
   uint64_t at = 0;
   const auto take = [&](uint64_t& place, uint64_t bytes) {
     place = at;

@@ -12,14 +12,17 @@ bool aligned(const void* p, uint64_t n) { return (uint64_t)p % n == 0; }
 bool known_dtype(int32_t t) { return t == TTC_F32 || t == TTC_BF16; }
 uint64_t bytes_of(int32_t t) { return t == TTC_BF16 ? 2 : 4; }
 
-// Sizes and numbers, which the workspace depends on
-ttc_status_t check_sizes(const ttc_linear_attention_t& a) {
+// Sizes and numbers, which the workspace depends on; calls: in one launch
+ttc_status_t check_sizes(const ttc_linear_attention_t& a, int calls) {
   if (a.sequences < 0 || a.tokens < 0 || a.heads < 1 || a.heads_qk < 1 || a.heads % a.heads_qk || !known_dtype(a.dtype) || a.max_q < 0 || !isfinite(a.scale))
     return TTC_ERR_INVALID_ARG;
   if (!a.cu_q && a.tokens != a.sequences) return TTC_ERR_INVALID_ARG;
   if (a.dk < 8 || a.dk > 256 || a.dk % 8 || a.dv < 8 || a.dv > 256 || a.dv % 8) return TTC_ERR_UNSUPPORTED;
-  // workgroups of a launch, and a workspace that can be counted: at most one for every head and 64 tokens, times four slices
-  if (a.tokens > 0x7fffffffll || a.sequences > 0x7fffffffll || ((double)a.tokens / 64 + a.sequences) * a.heads * 64 >= 2147483648.) return TTC_ERR_UNSUPPORTED;
+  // a launch has less than 2^32 threads: 512 for every head of 64 tokens, and for every 64 columns of a sequence's heads 256 in each call (of an odd number of
+  // 64 columns as many as for the next even one)
+  const double launch = 4294967296., slices = ((a.dk > a.dv ? a.dk : a.dv) + 63) / 64;
+  if (a.tokens > 0x7fffffffll || a.sequences > 0x7fffffffll || ((double)a.tokens / 64 + a.sequences + 8) * a.heads * 512 >= launch ||
+      calls * ((double)a.sequences + 8) * a.heads * (slices + 1) * 256 >= launch) return TTC_ERR_UNSUPPORTED;
   // 64 rows of a chunk lie within 2^31 bytes
   for (int64_t step : {a.q_token, a.k_token, a.v_token, a.out_token})
     if (a.tokens > 1 && (step < 0 || step >= (1 << 23))) return TTC_ERR_UNSUPPORTED;
@@ -69,8 +72,10 @@ ttc_status_t check_norm_backward(const ttc_residual_norm_backward_t* b) {
 
 ttc_status_t check_backward(const ttc_linear_attention_backward_t* b) {
   if (!b) return TTC_ERR_INVALID_ARG;
-  if (const ttc_status_t s = check_sizes(b->forward); s != TTC_OK) return s;
-  return check_pointers(b->forward);
+  const ttc_linear_attention_t& f = b->forward;
+  if (const ttc_status_t s = check_sizes(f, 2); s != TTC_OK) return s;
+  if (f.tokens > 1 && (int64_t)f.heads * (f.dk > f.dv ? f.dk : f.dv) >= (1 << 23)) return TTC_ERR_UNSUPPORTED;  // the results' rows
+  return check_pointers(f);
 }
 
 }  // namespace
@@ -78,12 +83,12 @@ ttc_status_t check_backward(const ttc_linear_attention_backward_t* b) {
 extern "C" {
 
 size_t ttc_linear_attention_workspace_bytes(const ttc_linear_attention_t* a) {
-  return a && check_sizes(*a) == TTC_OK ? ttc::linear_attention_workspace(*a, ttc::compute_units()) : 0;
+  return a && check_sizes(*a, 1) == TTC_OK ? ttc::linear_attention_workspace(*a, ttc::compute_units()) : 0;
 }
 
 ttc_status_t ttc_linear_attention(const ttc_linear_attention_t* a, void* workspace, size_t workspace_bytes, void* hip_stream) {
   if (!a) return TTC_ERR_INVALID_ARG;
-  if (const ttc_status_t s = check_sizes(*a); s != TTC_OK) return s;
+  if (const ttc_status_t s = check_sizes(*a, 1); s != TTC_OK) return s;
   if (const ttc_status_t s = check_pointers(*a); s != TTC_OK) return s;
   if (a->tokens && (!a->out || !aligned(a->out, bytes_of(a->dtype)) || a->out == a->q || a->out == a->k || a->out == a->v)) return TTC_ERR_INVALID_ARG;
   if (!a->sequences || (!a->state_out && (!a->tokens || !a->max_q))) return TTC_OK;

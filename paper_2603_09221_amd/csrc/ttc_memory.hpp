@@ -22,7 +22,8 @@ struct MemSequences {
   const int32_t* cu_q;
   int32_t max_q;
   int32_t segment;     // chunks of a segment
-  int64_t entries;     // segments of all sequences at most; every sequence has one
+  int64_t entries;     // places for segments; every sequence has one at least
+  int32_t each;        // of a sequence, as many as the longest has; 0: sequences have as many as they need, one behind the other
   int32_t blocks;      // of heads: what the XCDs take in turn is a segment of one block's heads (mem_deal)
 };
 
@@ -51,17 +52,18 @@ __device__ __forceinline__ int mem_segments(const MemSequences& m, int n) {
   return max(1, (chunks + m.segment - 1) / m.segment);
 }
 
-// Segment number `at` of all: its sequence with that one's rows, and which of its segments it is, the same for all lanes; false if there are fewer.  Each
-// wavefront adds up the sequences for itself, a run of them to a lane; where a run is one, what the lanes have read is all that it takes.
+// The segment at place `at`: its sequence with that one's rows, and which of its segments it is, the same for all lanes; false if there is none.  Where
+// sequences have no places of their own each wavefront adds them up for itself, a run of them to a lane; if a run is one, what the lanes have read is all
+// that it takes.
 __device__ __forceinline__ bool mem_segment(const MemSequences& m, int64_t at, int64_t& seq, int& segment, int64_t& first, int& n) {
-  if (m.entries == m.sequences) {
-    if (at >= m.sequences) return false;
-    seq = at;
-    segment = 0;
-    mem_rows(m, at, first, n);
+  if (m.each) {
+    if (at >= m.entries) return false;
+    seq = (uint32_t)at / (uint32_t)m.each;
+    segment = (int)((uint32_t)at % (uint32_t)m.each);
+    mem_rows(m, seq, first, n);
     first = __builtin_amdgcn_readfirstlane((int)first);  // (tokens are below 2^31)
     n = __builtin_amdgcn_readfirstlane(n);
-    return true;
+    return segment < mem_segments(m, n);
   }
   const int lane = threadIdx.x & 63;
   const int64_t run = (m.sequences + 63) / 64, own_first = min(lane * run, m.sequences), own_last = min(own_first + run, m.sequences);
@@ -749,12 +751,16 @@ static __global__ void __launch_bounds__(256) memory_scan_kernel(const MemTwo tw
   const int64_t seq = b / blocks / a.heads;
   int64_t entry = 0, first;
   int n;
-  for (int64_t s = threadIdx.x & 63; s < seq; s += 64) {
-    mem_rows(a.m, s, first, n);
-    entry += mem_segments(a.m, n);
-  }
+  if (a.m.each) {
+    entry = seq * a.m.each;
+  } else {
+    for (int64_t s = threadIdx.x & 63; s < seq; s += 64) {
+      mem_rows(a.m, s, first, n);
+      entry += mem_segments(a.m, n);
+    }
 #pragma unroll
-  for (int o = 32; o; o >>= 1) entry += __shfl_xor(entry, o, 64);
+    for (int o = 32; o; o >>= 1) entry += __shfl_xor(entry, o, 64);
+  }
   if (e >= a.dk * a.dv) return;
   mem_rows(a.m, seq, first, n);
   const int segments = (int)min((int64_t)mem_segments(a.m, n), a.m.entries - entry);  // (fewer only where cu_q does not ascend)

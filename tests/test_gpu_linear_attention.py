@@ -197,6 +197,13 @@ def test_many_sequences():
     check(q, k, v, g, cu, got["out"], got["state"])
 
 
+def test_many_sequences_of_one_length():
+    lengths = [130] * 70
+    q, k, v, g, cu = attention_inputs(lengths, 1, 1, 16, 16, torch.float32, seed=9)
+    got = binding.ttc_linear_attention(q, k, v, g, cu_q=cu, max_q=130, want_state=True)
+    check(q, k, v, g, cu, got["out"], got["state"])
+
+
 def test_no_tokens_leave_states_as_they_are():
     state = torch.randn((3, 2, 16, 24), device=DEV)
     q, v, g = torch.zeros((0, 2, 16), device=DEV), torch.zeros((0, 2, 24), device=DEV), torch.zeros((0, 2), device=DEV)

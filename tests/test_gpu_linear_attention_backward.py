@@ -74,6 +74,14 @@ def test_many_heads_and_sequences_without_segments():
     check([t[:cu[3]] for t in x[:4]] + [cu[:4]], gout[:cu[3]], first[few], glast[few], part)
 
 
+@pytest.mark.parametrize("lengths", [[70] * 90, [(i * 7) % 5 if i % 3 else 0 for i in range(150)] + [900] + [0] * 20 + [66]])
+def test_many_sequences(lengths):
+    """More sequences than a wavefront has lanes, alike and far from it."""
+    x, gout, first, glast = gradient_inputs(lengths, 2, 2, 16, 24, torch.float32, False, 5, True)
+    got = binding.ttc_linear_attention_backward(*x[:4], gout, cu_q=x[4], max_q=max(lengths), state=first, grad_state=glast)
+    check(x, gout, first, glast, got)
+
+
 def test_single_tokens_and_no_tokens():
     x, gout, first, glast = gradient_inputs([1] * 9, 2, 2, 64, 64, torch.float32, False, 4, True)
     got = binding.ttc_linear_attention_backward(*x[:4], gout, state=first, grad_state=glast)

@@ -106,6 +106,15 @@ def test_linear_attention_workspace(lib):
     assert lib.ttc_linear_attention_workspace_bytes(linear(heads=3)) == 0
 
 
+def test_linear_attention_refuses_what_a_launch_does_not_count(lib):
+    for change in (dict(tokens=1 << 28, max_q=1 << 28, heads=1, heads_qk=1), dict(tokens=1 << 26, max_q=1 << 25)):
+        assert lib.ttc_linear_attention(linear(**change), None, 0, None) == WORKSPACE, change
+    for change in (dict(tokens=1 << 30, max_q=1 << 30), dict(sequences=1 << 22), dict(heads=1 << 23), dict(sequences=1 << 20, dk=256, dv=256)):
+        assert lib.ttc_linear_attention(linear(**change), FAKE, 1 << 62, None) == UNSUPPORTED, change
+    # a gradient's results are contiguous, whatever the strides of what it is given
+    assert lib.ttc_linear_attention_backward(backward(dict(heads=1 << 16, heads_qk=1 << 16)), FAKE, 1 << 62, None) == UNSUPPORTED
+
+
 def backward(change_forward={}, **kw):
     return _fill(binding.LinearAttentionBackward(linear(**change_forward), FAKE, 512, 128, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE), kw)
 
