@@ -189,3 +189,32 @@ def test_replays_of_the_examples_layer_equal_eager_steps():
         want = made.forward(new, b.cache, at["slots"], at["positions"], b.pages, b.length, states=b.states)
         torch.cuda.synchronize()
         assert torch.equal(got, want) and torch.equal(a.cache, b.cache) and torch.equal(a.length, b.length) and torch.equal(a.states, b.states)
+
+
+def test_rows_beyond_what_32_bits_count():
+    """Rows of one wide tensor, the last of them more than 2^32 entries behind the first, give the bits of the same rows side by side."""
+    tokens, step, heads, d = 33000, 1 << 17, 2, 64
+    wide = torch.empty((tokens, step), dtype=torch.bfloat16, device=DEV)
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    near = torch.randn((tokens, 5 * heads * d), generator=gen, device=DEV).bfloat16()
+    near[:, heads * d:2 * heads * d] *= d ** -0.5
+    wide[:, :5 * heads * d] = near
+    g = -torch.rand((tokens, heads), generator=gen, device=DEV)
+    at = dict(cu_q=torch.tensor([0, 1, 900, tokens - 70, tokens], dtype=torch.int32, device=DEV), max_q=tokens)
+    results = []
+    for x in (near, wide):
+        q, k, v, gout, gate = (x[:, i * heads * d:(i + 1) * heads * d] for i in range(5))
+        by_heads = [t.unflatten(1, (heads, d)) for t in (q, k, v, gout)]
+        place = torch.zeros_like(x[:, 5 * heads * d:6 * heads * d]) if x is near else wide[:, 5 * heads * d:6 * heads * d].zero_()
+        got = binding.ttc_linear_attention(*by_heads[:3], g, out={"out": place.unflatten(1, (heads, d))} if x is wide else None, want_state=True, **at)
+        back = binding.ttc_linear_attention_backward(*by_heads[:3], g, by_heads[3], **at)
+        norm = binding.ttc_residual_norm(q, residual=k, gate=gate, post="rms", groups=heads, pre="layer", out={"r": place} if x is wide else None)
+        grads = binding.ttc_residual_norm_backward(q, residual=k, gate=gate, post="rms", groups=heads, pre="layer", grad_h=v, grad_r=gout)
+        results.append([got["state"]] + [norm["r"].clone(), norm["h"]] + list(back.values()) + list(grads.values()))
+        if x is near:
+            out = got["out"].clone()
+        else:
+            again = binding.ttc_linear_attention(*by_heads[:3], g, out={"out": place.unflatten(1, (heads, d))}, **at)["out"]
+            assert torch.equal(again.flatten(1), out.flatten(1))
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
