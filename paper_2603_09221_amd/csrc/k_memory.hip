@@ -9,6 +9,7 @@ static void chunks(const MemTwo& a, int what, uint32_t grid, hipStream_t st) {
   switch (what) {
     case MEM_STATES: hipLaunchKernelGGL((memory_chunk_kernel<T, TTC_D, WAVES, MEM_STATES>), dim3(grid), dim3(64 * WAVES), 0, st, a); break;
     case MEM_OUT: hipLaunchKernelGGL((memory_chunk_kernel<T, TTC_D, WAVES, MEM_OUT>), dim3(grid), dim3(64 * WAVES), 0, st, a); break;
+    case MEM_OUT_PAIRS: hipLaunchKernelGGL((memory_chunk_kernel<T, TTC_D, WAVES, MEM_OUT_PAIRS>), dim3(grid), dim3(64 * WAVES), 0, st, a); break;
     case MEM_OUT_DOTS: hipLaunchKernelGGL((memory_chunk_kernel<T, TTC_D, WAVES, MEM_OUT_DOTS>), dim3(grid), dim3(64 * WAVES), 0, st, a); break;
   }
 }

@@ -140,7 +140,7 @@ namespace {
 // Places in the workspace of a backward pass, in bytes from its beginning
 struct BackwardPlan {
   MemSequences m, chunks;
-  int slices;           // of dq's and dk's columns
+  int slices, pair_slices;  // of dq's and dk's columns, of dv's
   uint64_t added, faded, added_r, faded_r, a, b, pairs, gstate, sums, gq, gk, bytes;
 };
 
@@ -148,6 +148,7 @@ BackwardPlan plan_backward(const ttc_linear_attention_backward_t& b, int cus) {
   const ttc_linear_attention_t& f = b.forward;
   BackwardPlan p = {};
   p.slices = slices_of(f.dv, f.dk, f.dtype == TTC_BF16);
+  p.pair_slices = slices_of(f.dk, f.dv, f.dtype == TTC_BF16);
   p.m = sequences_of(f, segment_of(f, 2 * p.slices, cus), 1);  // (two calls are in a launch: 255 us where segments for one each take 287)
   p.chunks = sequences_of(f, 1, 8);
   uint64_t at = 0;
@@ -164,7 +165,7 @@ BackwardPlan plan_backward(const ttc_linear_attention_backward_t& b, int cus) {
   }
   take(p.a, (uint64_t)p.slices * f.heads * f.tokens * 4);
   take(p.b, (uint64_t)p.slices * f.heads * f.tokens * 4);
-  take(p.pairs, (uint64_t)f.heads * f.tokens * 4);
+  take(p.pairs, (uint64_t)p.pair_slices * f.heads * f.tokens * 4);
   if (f.state_in && !b.gstate) take(p.gstate, f.sequences * f.heads * state);
   if (!f.g_token) take(p.sums, (uint64_t)p.m.entries * f.heads * 8);
   if (f.heads != f.heads_qk) {
@@ -226,7 +227,9 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
   };
   MemArgs dv = back;
   result(dv, b.gv, 0, f.heads, f.dv);
-  if ((e = run_chunks(dv, nullptr, bf16, MEM_OUT, st)) != hipSuccess) return e;
+  dv.dot = v;
+  dv.dots = place(plan.pairs);
+  if ((e = run_chunks(dv, nullptr, bf16, MEM_OUT_PAIRS, st)) != hipSuccess) return e;
   MemArgs dk = back;
   dk.x = v;
   dk.w = gout;
@@ -261,19 +264,12 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   MemDecayArgs d = {};
-  d.m = plan.chunks;
-  d.q = q;
-  d.k = k;
-  d.v = v;
-  d.gout = gout;
+  d.m = plan.m;
   d.heads = f.heads;
   d.dk = f.dk;
   d.dv = f.dv;
   d.slices = plan.slices;
-  d.scale = f.scale;
-  d.log_decay = f.log_decay;
-  d.g_token = f.g_token;
-  d.g_head = f.g_head;
+  d.pair_slices = plan.pair_slices;
   d.pairs = place(plan.pairs);
   d.a = place(plan.a);
   d.b = place(plan.b);
@@ -283,11 +279,6 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
   d.sums = f.g_token ? nullptr : reinterpret_cast<double*>(ws + plan.sums);
   d.found = base.starts;
   d.found_r = back.starts;
-  const dim3 grid(dealt(d.m, f.heads, 1));
-  if (bf16) hipLaunchKernelGGL((memory_pairs_kernel<unsigned short>), grid, dim3(256), 0, st, d);
-  else hipLaunchKernelGGL((memory_pairs_kernel<float>), grid, dim3(256), 0, st, d);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  d.m = plan.m;
   hipLaunchKernelGGL(memory_decay_kernel, dim3((uint32_t)(plan.m.entries * f.heads)), dim3(MEM_SUM_THREADS), 0, st, d);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (!f.g_token) hipLaunchKernelGGL(memory_decay_sum_kernel, dim3((f.heads + 63) / 64), dim3(64), 0, st, d.sums, plan.m.entries, f.heads, b.glog_decay);

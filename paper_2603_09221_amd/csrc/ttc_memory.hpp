@@ -261,6 +261,31 @@ __device__ __forceinline__ void mem_out4(float* p, const srv_floatx4& x) { *rein
 // and from one
 template <typename T> struct MemFour { typedef T type __attribute__((ext_vector_type(4), aligned(sizeof(T)))); };
 
+// eight numbers of a row in memory, or zeros in their place
+__device__ __forceinline__ srv_bf16x8 mem_global(const unsigned short* p, bool wanted) {
+  MemEight<unsigned short> x;
+  mem_fetch(p, x);
+  return wanted ? __builtin_bit_cast(srv_bf16x8, x.x) : srv_bf16x8{};
+}
+__device__ __forceinline__ mem_float8 mem_global(const float* p, bool wanted) {
+  MemEight<float> x;
+  mem_fetch(p, x);
+  if (!wanted) x = {};
+  return {{x.x[0][0], x.x[0][1], x.x[0][2], x.x[0][3], x.x[1][0], x.x[1][1], x.x[1][2], x.x[1][3]}};
+}
+
+// The sum over sixteen lanes side by side, in each of them
+template <int CTRL>
+__device__ __forceinline__ float mem_dpp_add(float x) {
+  return x + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float mem_sixteen(float x) {
+  x = mem_dpp_add<0xb1>(x);     // the neighbour's
+  x = mem_dpp_add<0x4e>(x);     // of two
+  x = mem_dpp_add<0x141>(x);    // mirrored: of four
+  return mem_dpp_add<0x140>(x); // of eight
+}
+
 // ---- the kernel of chunks ---------------------------------------------------------------------------------------------------
 
 struct MemRows {
@@ -289,8 +314,8 @@ struct MemArgs {
   float* faded;                 // (entries, heads): and the factor on what it finds
   int32_t s_row, s_col;         // of a state's numbers, in elements
   int32_t dk, dv;               // rows and columns of a state as it is stored
-  MemRows dot;                  // rows whose product with what a token reads of the state is wanted (p NULL: not)
-  float* dots;                  // (slices, heads, tokens)
+  MemRows dot;                  // MEM_OUT_DOTS: rows whose products with what the tokens read of the state are wanted; MEM_OUT_PAIRS: those of a pair's second factor
+  float* dots;                  // (slices, heads, tokens): these products, or sums of pairs
 };
 
 // Two calls of the same sizes in one launch (a gradient's, of tokens in both orders: what one leaves idle is the other's); the first `split` workgroups, a
@@ -444,8 +469,8 @@ struct MemPlace {
   }
 };
 
-// What a segment adds to its state; results; results and their products with other rows
-enum MemWhat { MEM_STATES, MEM_OUT, MEM_OUT_DOTS };
+// What a segment adds to its state; results; results and their products with other rows; results and sums of the pairs' products with others'
+enum MemWhat { MEM_STATES, MEM_OUT, MEM_OUT_DOTS, MEM_OUT_PAIRS };
 
 // A workgroup takes one segment of one head of one sequence, and of the values' columns a slice of 16 * WAVES; a wavefront owns 16 of them and their
 // state, DK numbers each, which stays in its registers from chunk to chunk: what a lane holds of it as a result is what it has to hold of it as an operand
@@ -461,12 +486,13 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
   typedef MemShape<T, DK, WAVES> S;
   typedef typename MemOperand<T>::type op_t;
   constexpr bool BF16 = sizeof(T) == 2, STATES = WHAT == MEM_STATES, DOTS = WHAT == MEM_OUT_DOTS;
+  constexpr bool PAIRS = WHAT == MEM_OUT_PAIRS;
   constexpr int IN = BF16 && DOTS ? 3 : 1, UP = BF16 ? 3 : 1, KT = DK / 16;
   constexpr int HALVES = WAVES / 4;  // wavefronts that share sixteen rows of pairs
   __shared__ alignas(16) T xl[STATES ? 8 : MEM_CHUNK * (S::OWN || S::XS > S::PS ? S::XS : S::PS)], wl[MEM_CHUNK * S::XS], vl[MEM_CHUNK * S::VS];
   __shared__ alignas(16) T own[STATES || !S::OWN ? 8 : MEM_CHUNK * S::PS];
   __shared__ alignas(16) MemDecays decays[2];
-  __shared__ alignas(16) float meet[WAVES][MEM_CHUNK];
+  __shared__ alignas(16) float meet[8][MEM_CHUNK];
   T* const pl = S::OWN ? own : xl;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int c = lane & 15, g = lane >> 4;
@@ -575,6 +601,16 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
       }
       // pairs: a wavefront has the products of sixteen rows with those, or with every other sixteen of those, that they see
       const int own_rows = wave & 3, j0 = HALVES == 1 ? 0 : wave >> 2;
+      op_t second[PAIRS ? S::COLS / 32 : 1];
+      if constexpr (PAIRS) {
+        const T* const from = static_cast<const T*>(a.dot.p) + head / a.dot.group * a.dot.head + t0 * a.dot.token + slice * S::COLS;
+        const uint32_t row = min(16 * own_rows + c, rows - 1) * (uint32_t)a.dot.token;
+#pragma unroll
+        for (int k = 0; k < S::COLS / 32; ++k) {
+          const bool there = slice * S::COLS + 32 * k + 8 * g < cols;
+          second[k] = mem_global(from + (row + (there ? 32 * k + 8 * g : 0)), there);
+        }
+      }
       srv_floatx4 z[4 / HALVES] = {};
 #pragma unroll
       for (int k = 0; k < DK / 32; ++k) {
@@ -594,6 +630,7 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
       // beginning of the other, and on from there, all at most 1
       const int i = 16 * own_rows + c;
       const float own_since = a.pair_scale * dl.since[i];
+      float all = 0.f;  // (with PAIRS) of the row
 #pragma unroll
       for (int u = 0; u < 4 / HALVES; ++u) {
         const int j = j0 + HALVES * u;
@@ -614,6 +651,33 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
           for (int r = 0; r < 4; ++r) p[r] = z[u][r] * way * left[r];
         }
         mem_store4(pl + i * S::PS + mem_place(16 * j + 4 * g), p);
+        if constexpr (PAIRS) {
+          // times the second factor; a pair of one token with itself belongs to no sum
+          srv_floatx4 sums = {};
+          if (order * (j - own_rows) <= 0) {
+            srv_floatx4 y = {};
+#pragma unroll
+            for (int k = 0; k < S::COLS / 32; ++k) {
+              const T* value = vl + (16 * j + c) * S::VS + 32 * k + 8 * g;
+              y = mem_mma(mem_operand(value, value + 4), second[k], y);
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int e = 16 * j + 4 * g + r;
+              float x = p[r] * y[r];
+              asm volatile("" : "+v"(x));
+              x = order * (e - i) < 0 && max(e, i) < rows ? x : 0.f;
+              all += x;
+              sums[r] = mem_sixteen(x);
+            }
+          }
+          if (c == 0) *reinterpret_cast<srv_floatx4*>(&meet[own_rows][16 * j + 4 * g]) = sums;
+        }
+      }
+      if constexpr (PAIRS) {
+        all += __shfl_xor(all, 16, 64);
+        all += __shfl_xor(all, 32, 64);
+        if (g == 0) meet[4 + j0][i] = all;
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[i] *= dl.in[16 * i + c];
@@ -649,6 +713,15 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
 #pragma unroll
           for (int w = 0; w < WAVES; ++w) sum += meet[w][lane];
           a.dots[((int64_t)slice * a.heads + head) * a.m.tokens + t0 + lane] = sum;
+        }
+      if constexpr (PAIRS)
+        if (wave == (turn & (WAVES - 1))) {  // rows are the pairs' earlier tokens, columns the later ones
+          double step = meet[4][lane];
+          if (HALVES == 2) step += meet[5][lane];
+#pragma unroll
+          for (int w = 0; w < 4; ++w) step -= meet[w][lane];
+          const double sum = mem_sums(step) - step;
+          if (lane < rows) a.dots[((int64_t)slice * a.heads + head) * a.m.tokens + t0 + lane] = (float)sum;
         }
       const bool bad = __builtin_amdgcn_ballot_w64(finite != 0.f) != 0;
       op_t clean[2];

@@ -13,12 +13,8 @@ namespace ttc {
 
 struct MemDecayArgs {
   MemSequences m;
-  MemRows q, k, v, gout;
-  int32_t heads, dk, dv, slices;
-  float scale;
-  const float* log_decay;
-  int64_t g_token, g_head;
-  float* pairs;                 // (heads, tokens)
+  int32_t heads, dk, dv, slices, pair_slices;
+  const float* pairs;           // (pair_slices, heads, tokens): sum_{j < t <= i} m_ij of a chunk's pairs
   const float *a, *b;           // (slices, heads, tokens)
   MemStates begin;              // of the forward call
   const float* gstate;          // (sequences, heads, dk, dv), where a sequence began with a state
@@ -26,109 +22,6 @@ struct MemDecayArgs {
   float* out;                   // (tokens, heads), or
   double* sums;                 // (entries, heads): sums over tokens instead
 };
-
-// eight numbers of a row in memory, or zeros in their place
-__device__ __forceinline__ srv_bf16x8 mem_global(const unsigned short* p, bool wanted) {
-  MemEight<unsigned short> x;
-  mem_fetch(p, x);
-  return wanted ? __builtin_bit_cast(srv_bf16x8, x.x) : srv_bf16x8{};
-}
-__device__ __forceinline__ mem_float8 mem_global(const float* p, bool wanted) {
-  MemEight<float> x;
-  mem_fetch(p, x);
-  if (!wanted) x = {};
-  return {{x.x[0][0], x.x[0][1], x.x[0][2], x.x[0][3], x.x[1][0], x.x[1][1], x.x[1][2], x.x[1][3]}};
-}
-
-// The sum over sixteen lanes side by side, in each of them
-template <int CTRL>
-__device__ __forceinline__ float mem_dpp_add(float x) {
-  return x + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true));
-}
-__device__ __forceinline__ float mem_sixteen(float x) {
-  x = mem_dpp_add<0xb1>(x);     // the neighbour's
-  x = mem_dpp_add<0x4e>(x);     // of two
-  x = mem_dpp_add<0x141>(x);    // mirrored: of four
-  return mem_dpp_add<0x140>(x); // of eight
-}
-
-// sum_{j < t <= i} m_ij for the tokens t of one chunk of one head: its steps are column sums below and row sums left of the diagonal.  A wavefront has sixteen
-// rows and the tiles of sixteen columns up to the diagonal, its operands from memory as they are; a block of entries of all of them is under way at once.
-template <typename T>
-__global__ void __launch_bounds__(256, 4) memory_pairs_kernel(const MemDecayArgs a) {
-  typedef typename MemOperand<T>::type op_t;
-  constexpr int STEPS = sizeof(T) == 2 ? 4 : 1;  // operands of 32 entries in a block: what registers hold
-  __shared__ alignas(16) MemDecays dl;
-  __shared__ alignas(16) float left[MEM_CHUNK], below[4][MEM_CHUNK];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
-  int64_t entry, seq, first;
-  int head, none, chunk, n;
-  mem_deal(a.m, blockIdx.x, a.heads, 1, entry, head, none);
-  if (entry >= a.m.entries || !mem_segment(a.m, entry, seq, chunk, first, n)) return;
-  const int64_t t0 = first + (int64_t)chunk * MEM_CHUNK;
-  const int rows = min(MEM_CHUNK, n - chunk * MEM_CHUNK);
-  if (rows <= 0) return;
-  if (wave == 0) {
-    mem_decays(lane < rows ? a.log_decay[(t0 + lane) * a.g_token + head * a.g_head] : 0.f, lane, false, 1.f, 1.f, dl);
-  }
-  srv_floatx4 z[2][4] = {};
-  const int i = 16 * wave + c;
-  // rows behind the last are read from it (their products have no place in a sum)
-  const auto products = [&](const MemRows& late, const MemRows& early, srv_floatx4 (&to)[4]) {
-    const T* x = static_cast<const T*>(late.p) + head / late.group * late.head + t0 * late.token + min(i, rows - 1) * (uint32_t)late.token;
-    const T* y = static_cast<const T*>(early.p) + head / early.group * early.head + t0 * early.token;
-    uint32_t at[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) at[j] = min(16 * j + c, rows - 1) * (uint32_t)early.token;
-    for (int e0 = 0; e0 < late.d; e0 += 32 * STEPS) {
-      op_t own[STEPS], other[STEPS][4];
-#pragma unroll
-      for (int s = 0; s < STEPS; ++s) {
-        const int e = e0 + 32 * s + 8 * g;
-        const bool there = e < late.d;
-        own[s] = mem_global(x + (there ? e : 0), there);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (j <= wave) other[s][j] = mem_global(y + (at[j] + (there ? e : 0)), there);
-      }
-#pragma unroll
-      for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (j <= wave) to[j] = mem_mma(other[s][j], own[s], to[j]);
-    }
-  };
-  products(a.q, a.k, z[0]);
-  products(a.gout, a.v, z[1]);
-  __syncthreads();
-  const float own_hi = dl.hi[i], own_lo = dl.lo[i];
-  float row = 0.f;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    srv_floatx4 sums = {};
-    if (j <= wave) {
-      const srv_floatx4 hi = *reinterpret_cast<const srv_floatx4*>(&dl.hi[16 * j + 4 * g]), lo = *reinterpret_cast<const srv_floatx4*>(&dl.lo[16 * j + 4 * g]);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float x = a.scale * z[0][j][r] * z[1][j][r] * mem_between(own_hi, own_lo, hi[r], lo[r], 1.f);
-        asm volatile("" : "+v"(x));  // (a select, not a branch for every number)
-        x = i < rows && 16 * j + 4 * g + r < i ? x : 0.f;
-        row += x;
-        sums[r] = mem_sixteen(x);
-      }
-    }
-    if (c == 0) *reinterpret_cast<srv_floatx4*>(&below[wave][16 * j + 4 * g]) = sums;
-  }
-  row += __shfl_xor(row, 16, 64);
-  row += __shfl_xor(row, 32, 64);
-  if (g == 0) left[i] = row;
-  __syncthreads();
-  if (wave == 0) {
-    const double step = (double)((below[0][lane] + below[1][lane]) + (below[2][lane] + below[3][lane])) - left[lane];
-    const double sum = mem_sums(step) - step;
-    if (lane < rows) a.pairs[head * a.m.tokens + t0 + lane] = (float)sum;
-  }
-}
 
 constexpr int MEM_SUM_THREADS = 1024;
 
@@ -190,7 +83,8 @@ static __global__ void __launch_bounds__(MEM_SUM_THREADS) memory_decay_kernel(co
       all += x;
     }
     if (real) {
-      const double grad = a.pairs[t] + now + (sum - step);
+      double grad = now + (sum - step);
+      for (int s = 0; s < a.pair_slices; ++s) grad += a.pairs[s * a.heads * a.m.tokens + t];
       if (a.out) a.out[(first + at + tid) * a.heads + head] = (float)grad;
       total += grad;
     }
