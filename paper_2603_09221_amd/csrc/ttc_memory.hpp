@@ -584,21 +584,37 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
 
     srv_floatx4 o[4] = {};
     if constexpr (!STATES) {
-      // what the tokens read of the state
+      const auto from_state = [&] {  // what the tokens read of the state
 #pragma unroll
-      for (int k = 0; k < KT; k += 2) {
-        op_t part[IN];
-        const float x[8] = {s[k][0], s[k][1], s[k][2], s[k][3], s[k + 1][0], s[k + 1][1], s[k + 1][2], s[k + 1][3]};
-        mem_split<IN>(x, part);
+        for (int k = 0; k < KT; k += 2) {
+          op_t part[IN];
+          const float x[8] = {s[k][0], s[k][1], s[k][2], s[k][3], s[k + 1][0], s[k + 1][1], s[k + 1][2], s[k + 1][3]};
+          mem_split<IN>(x, part);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const T* row = xl + (16 * i + c) * S::XS + 16 * k + 8 * g;
-          const op_t y = mem_operand(row, row + 4);
+          for (int i = 0; i < 4; ++i) {
+            const T* row = xl + (16 * i + c) * S::XS + 16 * k + 8 * g;
+            const op_t y = mem_operand(row, row + 4);
 #pragma unroll
-          for (int p = IN - 1; p >= 0; --p) o[i] = mem_mma(part[p], y, o[i]);
+            for (int p = IN - 1; p >= 0; --p) o[i] = mem_mma(part[p], y, o[i]);
+          }
+          if constexpr (S::RESIDENT == 4) __builtin_amdgcn_sched_barrier(0);  // reads that go ahead take registers: spilled ones cost more
         }
-        if constexpr (S::RESIDENT == 4) __builtin_amdgcn_sched_barrier(0);  // reads that go ahead take registers: spilled ones cost more
-      }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] *= dl.in[16 * i + c];
+        if constexpr (DOTS) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum += o[i][r] * srv_widen(dot[i][r]);
+            sum += __shfl_xor(sum, 16, 64);
+            sum += __shfl_xor(sum, 32, 64);
+            if (g == 0) meet[wave][16 * i + c] = sum;
+          }
+        }
+      };
+      // Pairs first where they have their place beside x: their sums need no registers then that what is read of the state has
+      if constexpr (!S::OWN) from_state();
       // pairs: a wavefront has the products of sixteen rows with those, or with every other sixteen of those, that they see
       const int own_rows = wave & 3, j0 = HALVES == 1 ? 0 : wave >> 2;
       op_t second[PAIRS ? S::COLS / 32 : 1];
@@ -679,19 +695,7 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
         all += __shfl_xor(all, 32, 64);
         if (g == 0) meet[4 + j0][i] = all;
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] *= dl.in[16 * i + c];
-      if constexpr (DOTS) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float sum = 0.f;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) sum += o[i][r] * srv_widen(dot[i][r]);
-          sum += __shfl_xor(sum, 16, 64);
-          sum += __shfl_xor(sum, 32, 64);
-          if (g == 0) meet[wave][16 * i + c] = sum;
-        }
-      }
+      if constexpr (S::OWN) from_state();
     }
     if (more && wave == ((turn + 1) & (WAVES - 1))) {
       const double sum = decays_of(after, decays[(turn + 1) & 1]);
