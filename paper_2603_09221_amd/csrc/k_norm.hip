@@ -8,11 +8,6 @@ namespace ttc {
 // leave room for at once, as every workgroup leaves a part of each sum (8192 rows of 4096: 136 us; 146 with 1024, 167 with 2048).
 constexpr int NORM_THREADS = 4096, NORM_THREADS_BACKWARD = 512;
 
-static bool row16(const void* p, int64_t stride, int32_t dtype) {
-  const int64_t bytes = dtype == TTC_BF16 ? 2 : 4;
-  return (uint64_t)p % 16 == 0 && stride * bytes % 16 == 0;
-}
-
 // A thread to every eight features as far as a workgroup goes: more eights to a thread take registers that the wavefronts in flight lack (two: 123 us
 // forward where one takes 121, 256 us backward where one takes 136)
 template <typename F>
@@ -29,14 +24,13 @@ hipError_t launch_residual_norm(const ttc_residual_norm_t& n, int cus, hipStream
   NormArgs a = {};
   a.n = n;
   a.group = n.features / n.groups;
-  a.vec = row16(n.y, n.y_token, n.dtype) << ROW_Y | row16(n.gate, n.gate_token, n.dtype) << ROW_GATE |
-          row16(n.residual, n.residual_token, n.dtype) << ROW_RESIDUAL | row16(n.r, n.r_token, n.dtype) << ROW_R | row16(n.h, n.h_token, n.dtype) << ROW_H;
   norm_shape(n.features, [&](auto lanes, auto pieces) {
     typedef NormShape<decltype(lanes)::value, decltype(pieces)::value> S;
-    const int64_t rows = (n.tokens + S::ROWS - 1) / S::ROWS, most = (int64_t)cus * (NORM_THREADS / S::THREADS);
+    const int threads = S::threads(n.features);
+    const int64_t rows = (n.tokens + S::ROWS - 1) / S::ROWS, most = (int64_t)cus * (NORM_THREADS / threads);
     const dim3 grid((uint32_t)(rows < most ? rows : most));
-    if (n.dtype == TTC_BF16) hipLaunchKernelGGL((residual_norm_kernel<unsigned short, lanes(), pieces()>), grid, dim3(S::THREADS), 0, st, a);
-    else hipLaunchKernelGGL((residual_norm_kernel<float, lanes(), pieces()>), grid, dim3(S::THREADS), 0, st, a);
+    if (n.dtype == TTC_BF16) hipLaunchKernelGGL((residual_norm_kernel<unsigned short, lanes(), pieces()>), grid, dim3(threads), 0, st, a);
+    else hipLaunchKernelGGL((residual_norm_kernel<float, lanes(), pieces()>), grid, dim3(threads), 0, st, a);
   });
   return hipGetLastError();
 }
@@ -46,7 +40,7 @@ static int norm_grid(const ttc_residual_norm_t& n, int cus) {
   int grid = 0;
   norm_shape(n.features, [&](auto lanes, auto pieces) {
     typedef NormShape<decltype(lanes)::value, decltype(pieces)::value> S;
-    const int64_t rows = (n.tokens + S::ROWS - 1) / S::ROWS, each = NORM_THREADS_BACKWARD / S::THREADS, most = cus * (each ? each : 1);
+    const int64_t rows = (n.tokens + S::ROWS - 1) / S::ROWS, each = NORM_THREADS_BACKWARD / S::threads(n.features), most = cus * (each ? each : 1);
     grid = (int)(rows < most ? rows : most);
   });
   return grid;
@@ -75,11 +69,6 @@ hipError_t launch_residual_norm_backward(const ttc_residual_norm_backward_t& b, 
   a.group = n.features / n.groups;
   a.gr = b.gr; a.gh = b.gh; a.gr_token = b.gr_token; a.gh_token = b.gh_token;
   a.gy = b.gy; a.ggate = b.ggate; a.gresidual = b.gresidual;
-  const auto rows = [&](const void* in, int64_t stride, const void* result) {  // one bit for what is read and its gradient
-    return row16(in, stride, n.dtype) && row16(result, n.features, n.dtype);
-  };
-  a.vec = rows(n.y, n.y_token, b.gy) << ROW_Y | rows(n.gate, n.gate_token, b.ggate) << ROW_GATE |
-          rows(n.residual, n.residual_token, b.gresidual) << ROW_RESIDUAL | row16(b.gr, b.gr_token, n.dtype) << ROW_R | row16(b.gh, b.gh_token, n.dtype) << ROW_H;
   const int grid = norm_grid(n, cus);
   NormParts sum = {};
   float* out[5];
@@ -98,8 +87,8 @@ hipError_t launch_residual_norm_backward(const ttc_residual_norm_backward_t& b, 
   sum.chunks = (n.features + 63) / 64;
   if (grid) norm_shape(n.features, [&](auto lanes, auto pieces) {
     typedef NormShape<decltype(lanes)::value, decltype(pieces)::value> S;
-    if (n.dtype == TTC_BF16) hipLaunchKernelGGL((residual_norm_backward_kernel<unsigned short, lanes(), pieces()>), dim3(grid), dim3(S::THREADS), 0, st, a);
-    else hipLaunchKernelGGL((residual_norm_backward_kernel<float, lanes(), pieces()>), dim3(grid), dim3(S::THREADS), 0, st, a);
+    if (n.dtype == TTC_BF16) hipLaunchKernelGGL((residual_norm_backward_kernel<unsigned short, lanes(), pieces()>), dim3(grid), dim3(S::threads(n.features)), 0, st, a);
+    else hipLaunchKernelGGL((residual_norm_backward_kernel<float, lanes(), pieces()>), dim3(grid), dim3(S::threads(n.features)), 0, st, a);
   });
   if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (vectors) hipLaunchKernelGGL(norm_parts_kernel, dim3(vectors * sum.chunks), dim3(64 * NORM_PARTS_WAVES), 0, st, sum);

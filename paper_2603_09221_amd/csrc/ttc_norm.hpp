@@ -15,13 +15,13 @@ struct NormArgs {
   void *gy, *ggate, *gresidual;
   float* part[5];     // sums over a workgroup's rows: post_gain, post_offset, residual_gain, pre_gain, pre_offset
   int32_t group;      // features of a group
-  uint8_t vec;        // rows of 16-byte alignment: bits by NormRow
 };
-enum NormRow { ROW_Y, ROW_GATE, ROW_RESIDUAL, ROW_R, ROW_H };  // gr as r, gh as h
 
+// From 256 lanes on a workgroup has one row, and no more wavefronts than that has features for
 template <int LANES, int PIECES>
 struct NormShape {
   static constexpr int THREADS = LANES < 256 ? 256 : LANES;
+  static int threads(int features) { return LANES < 256 || PIECES > 1 ? THREADS : (features + 511) / 512 * 64; }
   static constexpr int ROWS = THREADS / LANES;  // of a workgroup at once
 };
 
@@ -69,10 +69,17 @@ struct NormSums {
         for (int i = 0; i < N; ++i) meet[turn][threadIdx.x >> 6][i] = x[i];
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        x[i] = 0.f;
+      for (int i = 0; i < N; ++i) x[i] = 0.f;
+      if constexpr (LANES == 1024) {  // one after the other: read ahead, 16 pairs take registers that are not there
+#pragma unroll 2
+        for (uint32_t w = 0; w < blockDim.x / 64; ++w)
 #pragma unroll
-        for (int w = 0; w < LANES / 64; ++w) x[i] += meet[turn][threadIdx.x / LANES * (LANES / 64) + w][i];
+          for (int i = 0; i < N; ++i) x[i] += meet[turn][w][i];
+      } else {
+#pragma unroll
+        for (int w = 0; w < LANES / 64; ++w)
+#pragma unroll
+          for (int i = 0; i < N; ++i) x[i] += meet[turn][threadIdx.x / LANES * (LANES / 64) + w][i];
       }
       turn ^= 1;
     }
@@ -133,23 +140,25 @@ struct NormSums {
 
 // ---- rows ---------------------------------------------------------------------------------------------------------------
 
-// eight features as they lie in memory
+// Eight features as they lie in memory, in accesses of 16 bytes whatever the row's alignment: device memory takes them at that of a number
 template <typename T> struct NormEight;
 template <> struct NormEight<unsigned short> { srv_u16x8 x; };
 template <> struct NormEight<float> { srv_floatx4 x[2]; };
+typedef unsigned short norm_u16x8 __attribute__((ext_vector_type(8), aligned(2)));
+typedef float norm_floatx4 __attribute__((ext_vector_type(4), aligned(4)));
 
-__device__ __forceinline__ void norm_fetch(const unsigned short* p, int e, int features, bool vec, NormEight<unsigned short>& to) {
-  if (vec && e + 8 <= features) {
-    to.x = __builtin_nontemporal_load(reinterpret_cast<const srv_u16x8*>(p + e));
+__device__ __forceinline__ void norm_fetch(const unsigned short* p, int e, int features, NormEight<unsigned short>& to) {
+  if (e + 8 <= features) {
+    to.x = __builtin_nontemporal_load(reinterpret_cast<const norm_u16x8*>(p + e));
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k) to.x[k] = e + k < features ? p[e + k] : 0;
   }
 }
-__device__ __forceinline__ void norm_fetch(const float* p, int e, int features, bool vec, NormEight<float>& to) {
-  if (vec && e + 8 <= features) {
-    to.x[0] = __builtin_nontemporal_load(reinterpret_cast<const srv_floatx4*>(p + e));
-    to.x[1] = __builtin_nontemporal_load(reinterpret_cast<const srv_floatx4*>(p + e + 4));
+__device__ __forceinline__ void norm_fetch(const float* p, int e, int features, NormEight<float>& to) {
+  if (e + 8 <= features) {
+    to.x[0] = __builtin_nontemporal_load(reinterpret_cast<const norm_floatx4*>(p + e));
+    to.x[1] = __builtin_nontemporal_load(reinterpret_cast<const norm_floatx4*>(p + e + 4));
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k) to.x[k / 4][k % 4] = e + k < features ? p[e + k] : 0.f;
@@ -158,10 +167,20 @@ __device__ __forceinline__ void norm_fetch(const float* p, int e, int features, 
 __device__ __forceinline__ float norm_entry(const NormEight<unsigned short>& v, int k) { return srv_widen(v.x[k]); }
 __device__ __forceinline__ float norm_entry(const NormEight<float>& v, int k) { return v.x[k / 4][k % 4]; }
 
+__device__ __forceinline__ void norm_put(unsigned short* p, const float (&x)[8]) {
+  srv_u16x8 v;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) v[k] = srv_narrow<unsigned short>(x[k]);
+  __builtin_nontemporal_store(norm_u16x8(v), reinterpret_cast<norm_u16x8*>(p));
+}
+__device__ __forceinline__ void norm_put(float* p, const float (&x)[8]) {
+  __builtin_nontemporal_store(norm_floatx4{x[0], x[1], x[2], x[3]}, reinterpret_cast<norm_floatx4*>(p));
+  __builtin_nontemporal_store(norm_floatx4{x[4], x[5], x[6], x[7]}, reinterpret_cast<norm_floatx4*>(p + 4));
+}
 template <typename T>
-__device__ __forceinline__ void norm_store(T* row, int e, int features, bool vec, const float (&x)[8]) {
+__device__ __forceinline__ void norm_store(T* row, int e, int features, const float (&x)[8]) {
   if (e + 8 <= features) {
-    srv_stream8(row + e, vec, x);
+    norm_put(row + e, x);
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
@@ -265,42 +284,56 @@ __device__ __forceinline__ void norm_act(int act, float x, float& y, float& slop
   }
 }
 
+// 16384 rows of 4096 bfloat16 with everything: 117 us, 5.7 TB/s.
 template <typename T, int LANES, int PIECES>
 __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_norm_kernel(const NormArgs a) {
   typedef NormShape<LANES, PIECES> S;
   __shared__ float meet[2][16][2];
   __shared__ float pieces[S::THREADS * PIECES];
+  if (LANES >= 256 && threadIdx.x < 64) (&meet[0][0][0])[threadIdx.x] = 0.f;  // those of wavefronts that are not there
+  if (LANES >= 256) __syncthreads();
   NormSums<LANES, PIECES> sums = {meet, pieces};
   const int at = threadIdx.x % LANES, c = a.n.features;
   const int64_t step = (int64_t)gridDim.x * S::ROWS;
+  // what belongs to the features, and the next row, as far as registers go: kept for all rows and under way beside one, else read anew
+  constexpr bool KEEP = PIECES == 1;
   float post_gain[PIECES][8], post_offset[PIECES][8], by[PIECES][8], pre_gain[PIECES][8], pre_offset[PIECES][8];
-#pragma unroll
-  for (int i = 0; i < PIECES; ++i) {
+  const auto vectors = [&](int i) {
     const int e = (i * LANES + at) * 8;
     norm_vector(a.n.post ? a.n.post_gain : nullptr, 1.f, e, c, post_gain[i]);
     norm_vector(a.n.post ? a.n.post_offset : nullptr, 0.f, e, c, post_offset[i]);
     norm_vector(a.n.residual_gain, 1.f, e, c, by[i]);
-    norm_vector(a.n.pre_gain, 1.f, e, c, pre_gain[i]);
-    norm_vector(a.n.pre_offset, 0.f, e, c, pre_offset[i]);
 #pragma unroll
     for (int k = 0; k < 8; ++k) by[i][k] *= a.n.scale;
-  }
+  };
+  const auto vectors_after = [&](int i) {
+    const int e = (i * LANES + at) * 8;
+    norm_vector(a.n.pre_gain, 1.f, e, c, pre_gain[i]);
+    norm_vector(a.n.pre_offset, 0.f, e, c, pre_offset[i]);
+  };
+  if (KEEP)
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      vectors(i);
+      vectors_after(i);
+    }
   NormEight<T> y[PIECES], gate[PIECES], residual[PIECES];
   const auto fetch = [&](int64_t t) {  // (behind the last row: the last once more, for nothing)
     t = t < a.n.tokens ? t : a.n.tokens - 1;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const int e = (i * LANES + at) * 8;
-      norm_fetch(static_cast<const T*>(a.n.y) + t * a.n.y_token, e, c, a.vec >> ROW_Y & 1, y[i]);
-      if (a.n.gate) norm_fetch(static_cast<const T*>(a.n.gate) + t * a.n.gate_token, e, c, a.vec >> ROW_GATE & 1, gate[i]);
-      if (a.n.residual) norm_fetch(static_cast<const T*>(a.n.residual) + t * a.n.residual_token, e, c, a.vec >> ROW_RESIDUAL & 1, residual[i]);
+      norm_fetch(static_cast<const T*>(a.n.y) + t * a.n.y_token, e, c, y[i]);
+      if (a.n.gate) norm_fetch(static_cast<const T*>(a.n.gate) + t * a.n.gate_token, e, c, gate[i]);
+      if (a.n.residual) norm_fetch(static_cast<const T*>(a.n.residual) + t * a.n.residual_token, e, c, residual[i]);
     }
   };
   int64_t first = (int64_t)blockIdx.x * S::ROWS;
-  fetch(first + threadIdx.x / LANES);
+  if (KEEP) fetch(first + threadIdx.x / LANES);
   for (; first < a.n.tokens; first += step) {
     const int64_t t = first + threadIdx.x / LANES;
     const bool real = t < a.n.tokens;
+    if (!KEEP) fetch(t);
     float x[PIECES][8], g[PIECES][8], r[PIECES][8], inverse[PIECES];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i)
@@ -310,11 +343,12 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
         if (a.n.gate) g[i][k] = norm_entry(gate[i], k);
         r[i][k] = a.n.residual ? norm_entry(residual[i], k) : 0.f;
       }
-    if (first + step < a.n.tokens) fetch(t + step);
+    if (KEEP && first + step < a.n.tokens) fetch(t + step);
     if (a.n.post) norm_unit<LANES, PIECES>(x, a.n.post, a.n.post_eps, a, true, inverse, sums);
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const int e = (i * LANES + at) * 8;
+      if (!KEEP) vectors(i);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         float z = x[i][k] * post_gain[i][k] + post_offset[i][k], act, slope;
@@ -324,61 +358,73 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
         }
         x[i][k] = r[i][k] + by[i][k] * z;  // (0 behind the last feature: so are all its terms)
       }
-      if (real && a.n.r) norm_store(static_cast<T*>(a.n.r) + t * a.n.r_token, e, c, a.vec >> ROW_R & 1, x[i]);
+      if (real && a.n.r) norm_store(static_cast<T*>(a.n.r) + t * a.n.r_token, e, c, x[i]);
     }
     if (!a.n.pre) continue;
     norm_unit<LANES, PIECES>(x, a.n.pre, a.n.pre_eps, a, false, inverse, sums);
     if (!real) continue;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
+      if (!KEEP) vectors_after(i);
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[i][k] = x[i][k] * pre_gain[i][k] + pre_offset[i][k];
-      norm_store(static_cast<T*>(a.n.h) + t * a.n.h_token, (i * LANES + at) * 8, c, a.vec >> ROW_H & 1, x[i]);
+      norm_store(static_cast<T*>(a.n.h) + t * a.n.h_token, (i * LANES + at) * 8, c, x[i]);
     }
   }
 }
 
 // The sums over tokens stay in registers; a workgroup leaves one part of each for norm_parts_kernel, and which rows make a part depends on the
-// sizes alone.
+// sizes alone.  8192 rows of 4096 bfloat16 with everything: 125 us, 4.3 TB/s, on 8 wavefronts a compute unit, which is what 214 registers leave room for.
 template <typename T, int LANES, int PIECES>
 __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_norm_backward_kernel(const NormArgs a) {
   typedef NormShape<LANES, PIECES> S;
   constexpr int WIDTH = LANES * PIECES * 8;
   __shared__ float meet[2][16][2];
   __shared__ float pieces[S::ROWS > 1 ? S::ROWS * WIDTH : S::THREADS * PIECES];
+  if (LANES >= 256 && threadIdx.x < 64) (&meet[0][0][0])[threadIdx.x] = 0.f;  // those of wavefronts that are not there
+  if (LANES >= 256) __syncthreads();
   NormSums<LANES, PIECES> sums = {meet, pieces};
   const int at = threadIdx.x % LANES, c = a.n.features, post = a.n.post, pre = a.n.pre;
   const int64_t step = (int64_t)gridDim.x * S::ROWS;
   float total_of[5][PIECES][8] = {};
+  // As above.  With more than 512 threads a thread has 128 registers, and what belongs to the features would be spilled by all: 4096 rows of 8192 bfloat16 327 us,
+  // 680 with all of it kept (435 where the second use reads it once more than the compiler wants to; 415 with 512 threads of two eights each).
+  constexpr bool KEEP = LANES <= 512;
   float post_gain[PIECES][8], post_offset[PIECES][8], by[PIECES][8], pre_gain[PIECES][8];
-#pragma unroll
-  for (int i = 0; i < PIECES; ++i) {
+  const auto vectors = [&](int i) {
     const int e = (i * LANES + at) * 8;
     norm_vector(post ? a.n.post_gain : nullptr, 1.f, e, c, post_gain[i]);
     norm_vector(post ? a.n.post_offset : nullptr, 0.f, e, c, post_offset[i]);
     norm_vector(a.n.residual_gain, 1.f, e, c, by[i]);
-    norm_vector(a.n.pre_gain, 1.f, e, c, pre_gain[i]);
-  }
+  };
+  const auto vectors_after = [&](int i) { norm_vector(a.n.pre_gain, 1.f, (i * LANES + at) * 8, c, pre_gain[i]); };
+  if (KEEP)
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      vectors(i);
+      vectors_after(i);
+    }
   NormEight<T> y[PIECES], gate[PIECES], residual[PIECES], gr[PIECES], gh[PIECES];
   const auto fetch = [&](int64_t t) {  // (behind the last row: the last once more, for nothing)
     t = t < a.n.tokens ? t : a.n.tokens - 1;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const int e = (i * LANES + at) * 8;
-      norm_fetch(static_cast<const T*>(a.n.y) + t * a.n.y_token, e, c, a.vec >> ROW_Y & 1, y[i]);
-      if (a.n.gate) norm_fetch(static_cast<const T*>(a.n.gate) + t * a.n.gate_token, e, c, a.vec >> ROW_GATE & 1, gate[i]);
-      if (a.gr) norm_fetch(static_cast<const T*>(a.gr) + t * a.gr_token, e, c, a.vec >> ROW_R & 1, gr[i]);
+      norm_fetch(static_cast<const T*>(a.n.y) + t * a.n.y_token, e, c, y[i]);
+      if (a.n.gate) norm_fetch(static_cast<const T*>(a.n.gate) + t * a.n.gate_token, e, c, gate[i]);
+      if (a.gr) norm_fetch(static_cast<const T*>(a.gr) + t * a.gr_token, e, c, gr[i]);
       if (pre) {
-        norm_fetch(static_cast<const T*>(a.gh) + t * a.gh_token, e, c, a.vec >> ROW_H & 1, gh[i]);
-        if (a.n.residual) norm_fetch(static_cast<const T*>(a.n.residual) + t * a.n.residual_token, e, c, a.vec >> ROW_RESIDUAL & 1, residual[i]);
+        norm_fetch(static_cast<const T*>(a.gh) + t * a.gh_token, e, c, gh[i]);
+        if (a.n.residual) norm_fetch(static_cast<const T*>(a.n.residual) + t * a.n.residual_token, e, c, residual[i]);
       }
     }
   };
   int64_t first = (int64_t)blockIdx.x * S::ROWS;
-  fetch(first + threadIdx.x / LANES);
+  if (KEEP) fetch(first + threadIdx.x / LANES);
   for (; first < a.n.tokens; first += step) {
     const int64_t t = first + threadIdx.x / LANES;
     const bool real = t < a.n.tokens;
+    if (!KEEP) fetch(t);
     float x[PIECES][8], act[PIECES][8], slope[PIECES][8], total[PIECES][8], g[PIECES][8], r[PIECES][8], inverse[PIECES];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i)
@@ -392,7 +438,7 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
           r[i][k] = a.n.residual ? norm_entry(residual[i], k) : 0.f;
         }
       }
-    if (first + step < a.n.tokens) fetch(t + step);
+    if (KEEP && first + step < a.n.tokens) fetch(t + step);
     if (post) norm_unit<LANES, PIECES>(x, post, a.n.post_eps, a, true, inverse, sums);
     if (a.n.gate)
 #pragma unroll
@@ -403,6 +449,7 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
       float unit_inverse[PIECES];
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
+        if (!KEEP) vectors(i);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           const float z = x[i][k] * post_gain[i][k] + post_offset[i][k];
@@ -411,13 +458,15 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
       }
       norm_unit<LANES, PIECES>(r, pre, a.n.pre_eps, a, false, unit_inverse, sums);
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i)
+      for (int i = 0; i < PIECES; ++i) {
+        if (!KEEP) vectors_after(i);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           total_of[3][i][k] += g[i][k] * r[i][k];
           if (a.part[4]) total_of[4][i][k] += g[i][k];
           g[i][k] *= pre_gain[i][k];
         }
+      }
       norm_unit_backward<LANES, PIECES>(g, r, unit_inverse, pre, a, false, sums);
 #pragma unroll
       for (int i = 0; i < PIECES; ++i)
@@ -427,8 +476,9 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const int e = (i * LANES + at) * 8;
-      if (real && a.gresidual) norm_store(static_cast<T*>(a.gresidual) + t * c, e, c, a.vec >> ROW_RESIDUAL & 1, total[i]);
+      if (real && a.gresidual) norm_store(static_cast<T*>(a.gresidual) + t * c, e, c, total[i]);
       float ggate[8];
+      if (!KEEP) vectors(i);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const float z = x[i][k] * post_gain[i][k] + post_offset[i][k];
@@ -440,12 +490,12 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
         if (a.part[1]) total_of[1][i][k] += gz;
         total[i][k] = gz * post_gain[i][k];
       }
-      if (real && a.ggate) norm_store(static_cast<T*>(a.ggate) + t * c, e, c, a.vec >> ROW_GATE & 1, ggate);
+      if (real && a.ggate) norm_store(static_cast<T*>(a.ggate) + t * c, e, c, ggate);
     }
     if (post) norm_unit_backward<LANES, PIECES>(total, x, inverse, post, a, true, sums);
     if (real && a.gy)
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i) norm_store(static_cast<T*>(a.gy) + t * c, (i * LANES + at) * 8, c, a.vec >> ROW_Y & 1, total[i]);
+      for (int i = 0; i < PIECES; ++i) norm_store(static_cast<T*>(a.gy) + t * c, (i * LANES + at) * 8, c, total[i]);
   }
 #pragma unroll
   for (int v = 0; v < 5; ++v)
