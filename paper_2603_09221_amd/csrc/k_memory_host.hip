@@ -14,16 +14,16 @@ template <> hipError_t launch_memory_step<256>(const MemArgs&, bool, uint32_t, h
 namespace {
 
 // Tokens of a sequence up to which memory_step_kernel takes it.  256 sequences, 16 heads of 128 x 128, step / chunks in us: bfloat16 with 4 tokens 104 / 121,
-// 6: 120 / 121, 8: 139 / 124; float32, whose chunks are matrix instructions of an eighth of the rate, with 8: 134 / 313, 12: 164 / 315.  A few small heads: alike.
+// 6: 120 / 121, 8: 138 / 123; float32, whose chunks are matrix instructions of an eighth of the rate, with 8: 132 / 318, 12: 164 / 319.  A few small heads: alike.
 int step_most(bool bf16) { return bf16 ? 6 : 16; }
 
-// Columns of a workgroup, and workgroups to the columns of a state: 128, for rows and pairs' products are shared by more (16384 tokens of 32 heads 211 us, with
+// Columns of a workgroup, and workgroups to the columns of a state: 128, for rows and pairs' products are shared by more (16384 tokens of 32 heads 208 us, with
 // 64 columns 263).  float32 rows of more than 128 entries leave LDS room for 64.
 int columns_of(int rows, int cols, bool bf16) { return cols > 64 && (bf16 || rows <= 128) ? 128 : 64; }
 int slices_of(int rows, int cols, bool bf16) { return (cols + columns_of(rows, cols, bf16) - 1) / columns_of(rows, cols, bf16); }
 
-// Blocks of heads: one where there are segments for the XCDs to take in turn, two for each, else the fewest that make as many (512 tokens of 64 heads: 41 us,
-// with one block 53; 64 tokens: 14.6 and 17.2)
+// Blocks of heads: one where there are segments for the XCDs to take in turn, two for each, else the fewest that make as many (512 tokens of 64 heads: 39 us,
+// with one block 50; 64 tokens: 14.7 and 17.1)
 int blocks_of(int64_t entries, int heads) {
   int n = 1;
   while (n < heads && (entries * n < 16 || heads % n)) ++n;
@@ -49,10 +49,10 @@ uint32_t dealt(const MemSequences& m, int heads, int per_head) {
 
 // Chunks of a segment: all of a sequence where sequences, heads and slices give every compute unit the two workgroups that LDS has room for, else the
 // fewest with which there are no more than two a unit, for a third waits until another is done.  Of sequences of different lengths (the host knows how many
-// tokens they have) half a segment each is taken to be left over.  One sequence of 16384 tokens, 32 heads, bfloat16: 211 us; 251, 233 and 232 with one, three
-// and four workgroups a unit; twelve of up to 1500 tokens, 16 heads, float32: 104; 154, 116, 114; gradients of four times 2048 tokens, 16 heads: 253; 352,
-// 300, 287.  At least two chunks, for a state is as much to write and to read as a chunk's rows: gradients of three of up to 1999 tokens, 8 heads, float32:
-// 152 us, as with one; 180 and 158 with three and four.
+// tokens they have) half a segment each is taken to be left over.  One sequence of 16384 tokens, 32 heads, bfloat16: 208 us; 243, 230 and 227 with one, three
+// and four workgroups a unit; twelve of up to 1500 tokens, 16 heads, float32: 104; 154, 116, 114; gradients of four times 2048 tokens, 16 heads: 224; 284,
+// 253, 240.  At least two chunks, for a state is as much to write and to read as a chunk's rows: gradients of three of up to 1999 tokens, 8 heads, float32:
+// 140 us, as with one; 173 and 155 with three and four.
 int segment_of(const ttc_linear_attention_t& a, int slices, int cus) {
   const int64_t longest = a.max_q < a.tokens ? a.max_q : a.tokens;
   const int chunks = (int)((longest + MEM_CHUNK - 1) / MEM_CHUNK);
@@ -149,7 +149,7 @@ BackwardPlan plan_backward(const ttc_linear_attention_backward_t& b, int cus) {
   BackwardPlan p = {};
   p.slices = slices_of(f.dv, f.dk, f.dtype == TTC_BF16);
   p.pair_slices = slices_of(f.dk, f.dv, f.dtype == TTC_BF16);
-  p.m = sequences_of(f, segment_of(f, 2 * p.slices, cus), 1);  // (two calls are in a launch: 255 us where segments for one each take 287)
+  p.m = sequences_of(f, segment_of(f, 2 * p.slices, cus), 1);  // (two calls are in a launch: 224 us for four times 2048 tokens; 241 with segments for one)
   p.chunks = sequences_of(f, 1, 8);
   uint64_t at = 0;
   const auto take = [&](uint64_t& place, uint64_t bytes) {
