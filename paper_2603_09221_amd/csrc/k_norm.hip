@@ -87,8 +87,13 @@ hipError_t launch_residual_norm_backward(const ttc_residual_norm_backward_t& b, 
   sum.chunks = (n.features + 63) / 64;
   if (grid) norm_shape(n.features, [&](auto lanes, auto pieces) {
     typedef NormShape<decltype(lanes)::value, decltype(pieces)::value> S;
-    if (n.dtype == TTC_BF16) hipLaunchKernelGGL((residual_norm_backward_kernel<unsigned short, lanes(), pieces()>), dim3(grid), dim3(S::threads(n.features)), 0, st, a);
-    else hipLaunchKernelGGL((residual_norm_backward_kernel<float, lanes(), pieces()>), dim3(grid), dim3(S::threads(n.features)), 0, st, a);
+    constexpr bool wide = lanes() > 512;  // where registers are short
+    const auto run = [&](auto type, auto offsets) {
+      hipLaunchKernelGGL((residual_norm_backward_kernel<decltype(type), lanes(), pieces(), decltype(offsets)::value>), dim3(grid), dim3(S::threads(n.features)), 0, st, a);
+    };
+    const bool any = n.post_offset || a.part[1] || a.part[4];
+    if (n.dtype == TTC_BF16) any || !wide ? run((unsigned short)0, std::true_type{}) : run((unsigned short)0, std::integral_constant<bool, !wide>{});
+    else any || !wide ? run(0.f, std::true_type{}) : run(0.f, std::integral_constant<bool, !wide>{});
   });
   if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   if (vectors) hipLaunchKernelGGL(norm_parts_kernel, dim3(vectors * sum.chunks), dim3(64 * NORM_PARTS_WAVES), 0, st, sum);

@@ -1,7 +1,7 @@
 // What the gradients of linear attention need beside memory_chunk_kernel's: those of the log decays, and sums over heads that share a query.
 //
 // With <R_t, S_t> the product of a state and of the loss's gradient with respect to it, dl/dg_t = exp(g_t) <R_t, S_{t-1}>: what tokens before t
-// put in, as far as tokens from t on read it.  Pairs of one chunk are added up one by one (no difference of large sums):
+// put in, as far as tokens from t on read it.  Pairs of one chunk are added up one by one (MEM_OUT_PAIRS; no difference of large sums):
 //     dl/dg_t = sum_{j < t <= i} m_ij + I + sum_{s < t} (b_s - a_s),      m_ij = scale exp(G_i - G_j) (q_i . k_j) (dout_i . v_j),
 // the last sum over the earlier tokens of the segment: a_s is q_s times what dq_s has from the state before its chunk, b_s is k_s times what dk_s
 // has from the state's gradient behind its chunk, I = <R, S> where the segment begins.  Sums over tokens are float64; their terms' errors of

@@ -21,8 +21,9 @@ struct NormArgs {
 template <int LANES, int PIECES>
 struct NormShape {
   static constexpr int THREADS = LANES < 256 ? 256 : LANES;
-  static int threads(int features) { return LANES < 256 || PIECES > 1 ? THREADS : (features + 511) / 512 * 64; }
   static constexpr int ROWS = THREADS / LANES;  // of a workgroup at once
+  __device__ static __forceinline__ int row() { return LANES <= 256 ? threadIdx.x / LANES : 0; }  // (a number for all threads where there is one: addresses are, too)
+  static int threads(int features) { return LANES < 256 || PIECES > 1 ? THREADS : (features + 511) / 512 * 64; }
 };
 
 template <int CTRL, int ROWS = 0xf>
@@ -293,7 +294,7 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
   if (LANES >= 256 && threadIdx.x < 64) (&meet[0][0][0])[threadIdx.x] = 0.f;  // those of wavefronts that are not there
   if (LANES >= 256) __syncthreads();
   NormSums<LANES, PIECES> sums = {meet, pieces};
-  const int at = threadIdx.x % LANES, c = a.n.features;
+  const int at = LANES <= 256 ? threadIdx.x % LANES : threadIdx.x, c = a.n.features;
   const int64_t step = (int64_t)gridDim.x * S::ROWS;
   // what belongs to the features, and the next row, as far as registers go: kept for all rows and under way beside one, else read anew
   constexpr bool KEEP = PIECES == 1;
@@ -329,9 +330,9 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
     }
   };
   int64_t first = (int64_t)blockIdx.x * S::ROWS;
-  if (KEEP) fetch(first + threadIdx.x / LANES);
+  if (KEEP) fetch(first + S::row());
   for (; first < a.n.tokens; first += step) {
-    const int64_t t = first + threadIdx.x / LANES;
+    const int64_t t = first + S::row();
     const bool real = t < a.n.tokens;
     if (!KEEP) fetch(t);
     float x[PIECES][8], g[PIECES][8], r[PIECES][8], inverse[PIECES];
@@ -375,7 +376,8 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
 
 // The sums over tokens stay in registers; a workgroup leaves one part of each for norm_parts_kernel, and which rows make a part depends on the
 // sizes alone.  8192 rows of 4096 bfloat16 with everything: 125 us, 4.3 TB/s, on 8 wavefronts a compute unit, which is what 214 registers leave room for.
-template <typename T, int LANES, int PIECES>
+// OFFSETS: there are some, or their gradients are wanted
+template <typename T, int LANES, int PIECES, bool OFFSETS>
 __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_norm_backward_kernel(const NormArgs a) {
   typedef NormShape<LANES, PIECES> S;
   constexpr int WIDTH = LANES * PIECES * 8;
@@ -384,17 +386,19 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
   if (LANES >= 256 && threadIdx.x < 64) (&meet[0][0][0])[threadIdx.x] = 0.f;  // those of wavefronts that are not there
   if (LANES >= 256) __syncthreads();
   NormSums<LANES, PIECES> sums = {meet, pieces};
-  const int at = threadIdx.x % LANES, c = a.n.features, post = a.n.post, pre = a.n.pre;
+  int at = LANES <= 256 ? threadIdx.x % LANES : threadIdx.x;
+  const int c = a.n.features, post = a.n.post, pre = a.n.pre;
   const int64_t step = (int64_t)gridDim.x * S::ROWS;
   float total_of[5][PIECES][8] = {};
-  // As above.  With more than 512 threads a thread has 128 registers, and what belongs to the features would be spilled by all: 4096 rows of 8192 bfloat16 327 us,
-  // 680 with all of it kept (435 where the second use reads it once more than the compiler wants to; 415 with 512 threads of two eights each).
+  // As above.  With more than 512 threads a thread has 128 registers, and what belongs to the features would be spilled by all: 4096 rows of 8192 bfloat16 199 us
+  // without offsets, 680 with all of it kept (415 with 512 threads of two eights each).  With two eights a gate is computed where it is needed, twice: 2048 rows
+  // of 16384 603 us, 1005 with both its numbers kept.
   constexpr bool KEEP = LANES <= 512;
   float post_gain[PIECES][8], post_offset[PIECES][8], by[PIECES][8], pre_gain[PIECES][8];
   const auto vectors = [&](int i) {
     const int e = (i * LANES + at) * 8;
     norm_vector(post ? a.n.post_gain : nullptr, 1.f, e, c, post_gain[i]);
-    norm_vector(post ? a.n.post_offset : nullptr, 0.f, e, c, post_offset[i]);
+    norm_vector(OFFSETS && post ? a.n.post_offset : nullptr, 0.f, e, c, post_offset[i]);
     norm_vector(a.n.residual_gain, 1.f, e, c, by[i]);
   };
   const auto vectors_after = [&](int i) { norm_vector(a.n.pre_gain, 1.f, (i * LANES + at) * 8, c, pre_gain[i]); };
@@ -420,11 +424,14 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
     }
   };
   int64_t first = (int64_t)blockIdx.x * S::ROWS;
-  if (KEEP) fetch(first + threadIdx.x / LANES);
+  if (KEEP) fetch(first + S::row());
   for (; first < a.n.tokens; first += step) {
-    const int64_t t = first + threadIdx.x / LANES;
+    const int64_t t = first + S::row();
     const bool real = t < a.n.tokens;
-    if (!KEEP) fetch(t);
+    if (!KEEP) {
+      if (PIECES > 1) asm volatile("" : "+v"(at));  // places are found anew: kept, they would take registers that spill
+      fetch(t);
+    }
     float x[PIECES][8], act[PIECES][8], slope[PIECES][8], total[PIECES][8], g[PIECES][8], r[PIECES][8], inverse[PIECES];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i)
@@ -432,6 +439,7 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
       for (int k = 0; k < 8; ++k) {
         x[i][k] = norm_entry(y[i], k);
         act[i][k] = a.n.gate ? norm_entry(gate[i], k) : 1.f;
+        if (!KEEP) slope[i][k] = 0.f;  // (without a gate nobody reads it, but 43 registers are spilled instead of 27)
         total[i][k] = a.gr && real ? norm_entry(gr[i], k) : 0.f;
         if (pre) {
           g[i][k] = real ? norm_entry(gh[i], k) : 0.f;
@@ -440,16 +448,24 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
       }
     if (KEEP && first + step < a.n.tokens) fetch(t + step);
     if (post) norm_unit<LANES, PIECES>(x, post, a.n.post_eps, a, true, inverse, sums);
-    if (a.n.gate)
+    const auto gates = [&](int i) {  // from the row as it came, where that is what is kept
+      if (a.n.gate)
 #pragma unroll
-      for (int i = 0; i < PIECES; ++i)
+        for (int k = 0; k < 8; ++k) norm_act(a.n.act, PIECES == 1 ? act[i][k] : norm_entry(gate[i], k), act[i][k], slope[i][k]);
+    };
+    if constexpr (KEEP) {  // (the same, but for what the compiler makes of it: 338 us for 29484 rows of 1138, 422 through the lambda; wide rows the other way)
+      if (a.n.gate)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) norm_act(a.n.act, act[i][k], act[i][k], slope[i][k]);
+        for (int k = 0; k < 8; ++k) norm_act(a.n.act, act[0][k], act[0][k], slope[0][k]);
+    } else if (PIECES == 1) {
+      gates(0);
+    }
     if (pre) {
       float unit_inverse[PIECES];
 #pragma unroll
       for (int i = 0; i < PIECES; ++i) {
         if (!KEEP) vectors(i);
+        if (PIECES > 1) gates(i);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           const float z = x[i][k] * post_gain[i][k] + post_offset[i][k];
@@ -463,7 +479,7 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
           total_of[3][i][k] += g[i][k] * r[i][k];
-          if (a.part[4]) total_of[4][i][k] += g[i][k];
+          if (OFFSETS && a.part[4]) total_of[4][i][k] += g[i][k];
           g[i][k] *= pre_gain[i][k];
         }
       }
@@ -479,6 +495,7 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
       if (real && a.gresidual) norm_store(static_cast<T*>(a.gresidual) + t * c, e, c, total[i]);
       float ggate[8];
       if (!KEEP) vectors(i);
+      if (PIECES > 1) gates(i);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const float z = x[i][k] * post_gain[i][k] + post_offset[i][k];
@@ -487,7 +504,7 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
         if (a.n.gate) ggate[k] = d * by[i][k] * z * slope[i][k];
         const float gz = d * by[i][k] * act[i][k];
         total_of[0][i][k] += gz * x[i][k];
-        if (a.part[1]) total_of[1][i][k] += gz;
+        if (OFFSETS && a.part[1]) total_of[1][i][k] += gz;
         total[i][k] = gz * post_gain[i][k];
       }
       if (real && a.ggate) norm_store(static_cast<T*>(a.ggate) + t * c, e, c, ggate);
@@ -499,7 +516,7 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
   }
 #pragma unroll
   for (int v = 0; v < 5; ++v)
-    if (a.part[v]) {
+    if ((OFFSETS || v % 3 != 1) && a.part[v]) {
       if constexpr (S::ROWS > 1) {
         float* mine = pieces + threadIdx.x / LANES * WIDTH;
         __syncthreads();

@@ -90,6 +90,27 @@ def test_against_oracle(tokens, features, groups, dtype, post, pre, activation, 
             assert (off <= (64 + tokens) * U * size.sum(0) + 1e-38).all(), name
 
 
+@pytest.mark.parametrize("features", [4096, 5000, 8192, 16384])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_many_wide_rows(features, dtype):
+    """Several rows to a workgroup; and gains without offsets, which are those with offsets of 0: an addition of 0 rounds nothing, so that only the
+    order of roundings could differ (64 half steps, as against the oracle)."""
+    test_against_oracle(530, features, 1, dtype, "rms", "rms", "silu", True, True)
+    x = inputs(530, features, dtype, "rms", "layer", True, True, True, seed=2)
+    gen = torch.Generator().manual_seed(3)
+    gr, gh = (torch.randn((530, features), generator=gen).to(dtype).to(DEV) for _ in range(2))
+    kw = dict(post="rms", pre="layer", grad_r=gr, grad_h=gh)
+    zeros = {**x, "post_offset": torch.zeros_like(x["post_gain"]), "pre_offset": torch.zeros_like(x["post_gain"])}
+    want = binding.ttc_residual_norm_backward(**zeros, **kw)
+    got = binding.ttc_residual_norm_backward(**{**x, "post_offset": None, "pre_offset": None}, **kw)
+    assert set(want) - set(got) == {"gpost_offset", "gpre_offset"}
+    for name in ("gy", "ggate", "gresidual"):
+        near(got[name], host(want[name]), dtype, np.abs(host(gr)) + 8 * np.abs(host(gh)))
+    for name in ("gpost_gain", "gresidual_gain", "gpre_gain"):
+        off, size = np.abs(host(got[name]) - host(want[name])), 530 * 8 * (np.abs(host(gr)).max() + 8 * np.abs(host(gh)).max())
+        assert (off <= 64 * U * size).all(), name
+
+
 def test_parts_and_no_parts():
     """Only h, only r, nothing but a copy; gradients with grad_r left out."""
     x = inputs(5, 256, torch.float32, "rms", "rms", True, True, True)
