@@ -14,6 +14,7 @@
 namespace ttc {
 
 constexpr int MEM_CHUNK = 64;      // tokens of a chunk: a lane each where decays are added up
+constexpr int MEM_FEW = 32;        // tokens of a chunk that leave room for a second part of the pairs' products
 
 // ---- sequences and their segments ---------------------------------------------------------------------------------------------
 
@@ -476,7 +477,8 @@ enum MemWhat { MEM_STATES, MEM_OUT, MEM_OUT_DOTS, MEM_OUT_PAIRS };
 // state, DK numbers each, which stays in its registers from chunk to chunk: what a lane holds of it as a result is what it has to hold of it as an operand
 // if the sum's order follows.  The next chunk's rows and decays are on their way while one is worked on.
 // bfloat16 rows: pairs' products and the state that queries meet are rounded to bfloat16 for their products, 2^-9 each, as the header's documentation
-// states; where gradients of decays, sums of float32 numbers, depend on what a token reads, the state has three parts, all of float32's bits, and so has
+// states; with four wavefronts a chunk of 32 tokens or fewer has the place of the other 32 for what the first rounding of pairs leaves, for with a few tokens one
+// rounding can be a whole result's (with eight registers are short: 205 us instead of 151 for 16384 tokens; a second part for all takes LDS and 5 to 20 %); where gradients of decays, sums of float32 numbers, depend on what a token reads, the state has three parts, all of float32's bits, and so has
 // always what is added to it (two, 17 bits, left a state of 16384 tokens 1.6e-6 off in the norm; three leave 1.3e-7).
 // MEM_OUT_PAIRS: where the rows of results are keys and values (dv), a pair's product times that of the value and the result's gradient is its share of the
 // decays' gradients between the two tokens: added up by rows and by columns here, where all but one operand is in LDS (a kernel of its own took 38 us of
@@ -562,7 +564,7 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
     const int chunk = reverse ? c1 - 1 - turn : c0 + turn, rows = rows_of(chunk);
     const int after = reverse ? chunk - 1 : chunk + 1;
     const int64_t t0 = first + (int64_t)chunk * MEM_CHUNK;
-    const bool whole = whole_state && rows == MEM_CHUNK;
+    const bool whole = whole_state && rows == MEM_CHUNK, few = BF16 && WAVES == 4 && rows <= MEM_FEW;
     asm volatile("" : "+v"(c), "+v"(g));  // places and masks are found anew: kept over the loop they would take registers that spill
     const MemDecays& dl = decays[turn & 1];
     if (!S::AHEAD) fetch(chunk, rows);
@@ -671,7 +673,13 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
 #pragma unroll
           for (int r = 0; r < 4; ++r) p[r] = z[u][r] * way * left[r];
         }
-        mem_store4(pl + i * S::PS + mem_place(16 * j + 4 * g), p);
+        if (!few || own_rows < 2) mem_store4(pl + i * S::PS + mem_place(16 * j + 4 * g), p);
+        if (few && own_rows < 2) {
+          float rest[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) rest[r] = p[r] - srv_widen(srv_narrow<T>(p[r]));
+          mem_store4(pl + (i + 32) * S::PS + mem_place(16 * j + 4 * g), rest);
+        }
         if constexpr (PAIRS) {
           // times the second factor; a pair of one token with itself belongs to no sum
           srv_floatx4 sums = {};
@@ -750,14 +758,23 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
         const T* row = pl + (16 * i + c) * S::PS + 32 * k + 8 * g;
         o[i] = mem_mma(clean[k], mem_operand(row, row + 4), o[i]);
       };
+      if (few) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) pairs(i, i / 2);
-      if (reverse) {
-        pairs(0, 1);
-        pairs(1, 1);
+        for (int i = 0; i < 2; ++i) {
+          const T* row = pl + (16 * i + 32 + c) * S::PS + 8 * g;
+          o[i] = mem_mma(clean[0], mem_operand(row, row + 4), o[i]);
+          pairs(i, 0);
+        }
       } else {
-        pairs(2, 0);
-        pairs(3, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) pairs(i, i / 2);
+        if (reverse) {
+          pairs(0, 1);
+          pairs(1, 1);
+        } else {
+          pairs(2, 0);
+          pairs(3, 0);
+        }
       }
       if (bad)
         for (int j = 0; j < rows; ++j)
