@@ -311,7 +311,7 @@ struct MemArgs {
   MemStates rule;               // whose beginning says where the last state is 0 (gstate); in NULL: no rule
   int32_t ruled;
   const float* starts;          // of the segments: (entries, heads, dk, dv), or NULL: a sequence is one segment
-  float* added;                 // likewise, what a segment adds to a state that it finds as zeros (mem_state_kernel)
+  float* added;                 // likewise, what a segment adds to a state that it finds as zeros (MEM_STATES)
   float* faded;                 // (entries, heads): and the factor on what it finds
   int32_t s_row, s_col;         // of a state's numbers, in elements
   int32_t dk, dv;               // rows and columns of a state as it is stored
@@ -331,7 +331,7 @@ struct MemDecays {
   float hi[MEM_CHUNK], lo[MEM_CHUNK];   // G / ln 2 as a sum of two
   float in[MEM_CHUNK], up[MEM_CHUNK];
   float since[MEM_CHUNK], left[MEM_CHUNK];  // factors from the beginning, and to the end, of a token's sixteen (the other way round from the last token on)
-  float border[4][2];                   // G / ln 2 where a sixteen begins and ends
+  float across[4];                      // what lies across a sixteen, from its beginning to its end, / ln 2
   float whole;
 };
 
@@ -369,10 +369,7 @@ __device__ __forceinline__ double mem_decays(float g, int lane, bool reverse, fl
   const float after = __builtin_amdgcn_exp2f((float)(sum - begin)), ahead = __builtin_amdgcn_exp2f((float)(end - sum));
   to.since[lane] = reverse ? ahead : after;
   to.left[lane] = reverse ? after : ahead;
-  if ((lane & 15) == 0) {
-    to.border[lane >> 4][0] = (float)begin;
-    to.border[lane >> 4][1] = (float)end;
-  }
+  if ((lane & 15) == 0) to.across[lane >> 4] = (float)(end - begin);  // not what two rounded sums differ by: sums are thousands where 16 tokens forget all
   return whole;
 }
 // sign: -1 where the first is the earlier one
@@ -649,8 +646,8 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
         if constexpr (S::RESIDENT == 4) __builtin_amdgcn_sched_barrier(0);
       }
       if constexpr (!S::OWN) __syncthreads();  // x has been read
-      // Weights: within a sixteen exp(G_i - G_j), a difference at a time; between two of them the product of the way to the end of one, from there to the
-      // beginning of the other, and on from there, all at most 1
+      // Weights: within a sixteen exp(G_i - G_j), a difference at a time; between two of them the product of the way to the end of one, across the
+      // sixteens from there to the beginning of the other, and on from there, all at most 1
       const int i = 16 * own_rows + c;
       const float own_since = a.pair_scale * dl.since[i];
       float all = 0.f;  // (with PAIRS) of the row
@@ -669,7 +666,9 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
           }
         } else if (order * (j - own_rows) < 0) {
           const srv_floatx4 left = *reinterpret_cast<const srv_floatx4*>(&dl.left[16 * j + 4 * g]);
-          const float way = own_since * __builtin_amdgcn_exp2f(dl.border[max(j, own_rows)][0] - dl.border[min(j, own_rows)][1]);
+          const int before = min(j, own_rows), behind = max(j, own_rows);
+          const float between = (before < 1 && behind > 1 ? dl.across[1] : 0.f) + (before < 2 && behind > 2 ? dl.across[2] : 0.f);
+          const float way = own_since * __builtin_amdgcn_exp2f(between);
 #pragma unroll
           for (int r = 0; r < 4; ++r) p[r] = z[u][r] * way * left[r];
         }

@@ -1,0 +1,73 @@
+"""Linear attention where tokens forget much and those behind them nothing, forward and backward, against the float64 oracle.
+
+The weight between two tokens is exp of the decays between them, and of those alone: what the tokens before both have forgotten is in
+neither's way.  Where all of 16 or 31 tokens forget strongly, the sums of decays from a chunk's beginning are thousands of times the difference
+that counts.  Bounds are those of the other tests of linear attention: none counts a rounding for such a sum."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import memory_oracle as oracle
+from paper_2603_09221_amd import binding
+from tests import test_gpu_linear_attention as forward
+from tests import test_gpu_linear_attention_backward as backward
+from tests.memory_inputs import attention_inputs, host
+
+pytestmark = pytest.mark.gpu
+CHUNK = 64
+
+
+def strong_tokens(length, count, per_chunk=(0, 2)):
+    """The first `count` tokens of the first and the third chunk, and what lies between the second's sixteens 0 and 2."""
+    at = torch.zeros(length, dtype=torch.bool)
+    for c in per_chunk:
+        at[c * CHUNK:c * CHUNK + count] = True
+    at[CHUNK + 3:CHUNK + 12] = True
+    return at
+
+
+@pytest.mark.parametrize("decay", [-20.0, -200.0, -float("inf")])
+@pytest.mark.parametrize("count", [16, 31])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_tokens_behind_those_that_forget(decay, count, dtype):
+    length = 3 * CHUNK + 59
+    q, k, v, g, cu = attention_inputs([length], 2, 2, 64, 64, dtype, seed=count, rate=1e-3)
+    g[strong_tokens(length, count).to(g.device)] = decay
+    got = binding.ttc_linear_attention(q, k, v, g, cu_q=cu, max_q=length, want_state=True)
+    forward.check(q, k, v, g, cu, got["out"], got["state"])
+
+
+def check_gradients(x, gout, first, glast, got):
+    """backward.check, but that first states' gradients below 2^-149, float32's smallest number, are 0 or that: a bound relative to exp(-200) of something
+    is nothing that a float32 result could keep."""
+    q, k, v, g, cu = x
+    want = oracle.linear_attention_gradients(*[host(t) for t in (q, k, v)], host(g), [int(i) for i in cu], q.shape[2] ** -0.5, *[host(t) for t in (gout, first, glast)])[4]
+    state, none = host(got["gstate"]), np.abs(want) < 2.0 ** -149
+    assert (np.abs(state[none]) <= 2.0 ** -149).all()
+    backward.check(x, gout, first, glast, {**got, "gstate": torch.from_numpy(np.where(none, want, state))})
+
+
+@pytest.mark.parametrize("decay", [-20.0, -200.0, -float("inf")])
+@pytest.mark.parametrize("count", [16, 31])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradients_of_tokens_behind_those_that_forget(decay, count, dtype):
+    length = 3 * CHUNK + 59
+    x, gout, first, glast = backward.gradient_inputs([length], 2, 2, 64, 64, dtype, False, count, True)
+    g = x[3]
+    g.mul_(1e-3)
+    g[strong_tokens(length, count).to(g.device)] = decay
+    got = binding.ttc_linear_attention_backward(*x[:4], gout, cu_q=x[4], max_q=length, state=first, grad_state=glast)
+    check_gradients(x, gout, first, glast, got)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_decays_that_heads_have_for_good(dtype):
+    """One that forgets all, one that forgets much, one a little, one nothing."""
+    length = 2 * CHUNK + 40
+    x, gout, first, glast = backward.gradient_inputs([length], 4, 2, 64, 64, dtype, True, 3, True)
+    x[3].copy_(torch.tensor([-200.0, -20.0, -0.05, 0.0]))
+    q, k, v, g, cu = x
+    got = binding.ttc_linear_attention(q, k, v, g, cu_q=cu, max_q=length, state=first, want_state=True)
+    forward.check(q, k, v, g, cu, got["out"], got["state"], first.double().cpu().numpy())
+    got = binding.ttc_linear_attention_backward(q, k, v, g, gout, cu_q=cu, max_q=length, state=first, grad_state=glast)
+    backward.check(x, gout, first, glast, got)
