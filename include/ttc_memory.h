@@ -25,9 +25,9 @@ extern "C" {
  * Sequences are packed as in ttc_attention: sequence s has the rows cu_q[s] .. cu_q[s+1]-1, rows behind the last are left as they are.
  * dk and dv are multiples of 8 from 8 to 256; rows of tokens are at most 2^23 - 1 entries apart (in gradients
  * heads * max(dk, dv) too).  A launch counts 2^32 threads: (tokens / 64 + sequences) * heads below 2^23 with sequences * heads below 2^20 are always taken.
- * States, sums and decays are float32 or wider.  bfloat16 rows, max_q more than 6: what queries meet of the state, and the
- * products of queries and keys of one chunk of 64 tokens, are rounded to bfloat16 for their products (2^-9 of each; with
- * max_q at most 32 the products of queries and keys to 2^-18); nothing else but the results is rounded to less than float32's 24 bits.
+ * States, sums and decays are float32 or wider.  bfloat16 rows, in gradients and where max_q is more than 6: what queries meet of the state, and the
+ * products of queries and keys of one chunk of 64 tokens, are sums of two bfloat16 numbers for their products (2^-16 of each is lost); nothing
+ * else but the results, gradients of decays included, is rounded to less than float32's 24 bits.
  * A token's NaN or infinity reaches its own and later tokens' results, and no earlier ones (an infinity may become NaN there). */
 typedef struct {
   int64_t sequences, tokens;   /* tokens: rows of q, k, v, out; below 2^31                                 */

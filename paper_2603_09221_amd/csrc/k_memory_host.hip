@@ -13,15 +13,15 @@ template <> hipError_t launch_memory_step<256>(const MemArgs&, bool, uint32_t, h
 
 namespace {
 
-// Tokens of a sequence up to which memory_step_kernel takes it.  256 sequences, 16 heads of 128 x 128, step / chunks in us: bfloat16 with 4 tokens 104 / 121,
-// 6: 120 / 121, 8: 138 / 123; float32, whose chunks are matrix instructions of an eighth of the rate, with 8: 132 / 318, 12: 164 / 319.  A few small heads: alike.
+// Tokens of a sequence up to which memory_step_kernel takes it.  256 sequences, 16 heads of 128 x 128, step / chunks in us: bfloat16 with 4 tokens 107 / 133,
+// 6: 124 / 140, 8: 143 / 137; float32, whose chunks are matrix instructions of an eighth of the rate, with 8: 140 / 319, 16: 202 / 323.  64 sequences, 32 heads
+// of 64: 21 / 32 with 6 and 36 / 60 with 16.
 int step_most(bool bf16) { return bf16 ? 6 : 16; }
 
-// Columns of a workgroup, and workgroups to the columns of a state: 128, for rows and pairs' products are shared by more (16384 tokens of 32 heads 208 us, with
-// 64 columns 263).  float32 rows of more than 128 entries leave LDS room for 64, and
-// bfloat16 sequences of at most 32 tokens take 64, whose kernel has a second part of their pairs' products.
-int columns_of(int rows, int cols, bool bf16, int most) { return cols > 64 && (bf16 ? most > MEM_FEW : rows <= 128) ? 128 : 64; }
-int slices_of(int rows, int cols, bool bf16, int most) { return (cols + columns_of(rows, cols, bf16, most) - 1) / columns_of(rows, cols, bf16, most); }
+// Columns of a workgroup, and workgroups to the columns of a state: 128, for rows and pairs' products are shared by more (16384 tokens of 32 heads 228 us, with
+// 64 columns 289).  float32 rows of more than 128 entries leave LDS room for 64.
+int columns_of(int rows, int cols, bool bf16) { return cols > 64 && (bf16 || rows <= 128) ? 128 : 64; }
+int slices_of(int rows, int cols, bool bf16) { return (cols + columns_of(rows, cols, bf16) - 1) / columns_of(rows, cols, bf16); }
 
 // Blocks of heads: one where there are segments for the XCDs to take in turn, two for each, else the fewest that make as many (512 tokens of 64 heads: 39 us,
 // with one block 50; 64 tokens: 14.7 and 17.1)
@@ -50,10 +50,10 @@ uint32_t dealt(const MemSequences& m, int heads, int per_head) {
 
 // Chunks of a segment: all of a sequence where sequences, heads and slices give every compute unit the two workgroups that LDS has room for, else the
 // fewest with which there are no more than two a unit, for a third waits until another is done.  Of sequences of different lengths (the host knows how many
-// tokens they have) half a segment each is taken to be left over.  One sequence of 16384 tokens, 32 heads, bfloat16: 208 us; 243, 230 and 227 with one, three
-// and four workgroups a unit; twelve of up to 1500 tokens, 16 heads, float32: 104; 154, 116, 114; gradients of four times 2048 tokens, 16 heads: 224; 284,
-// 253, 240.  At least two chunks, for a state is as much to write and to read as a chunk's rows: gradients of three of up to 1999 tokens, 8 heads, float32:
-// 140 us, as with one; 173 and 155 with three and four.
+// tokens they have) half a segment each is taken to be left over.  One sequence of 16384 tokens, 32 heads, bfloat16: 228 us; 269, 252 and 247 with one, three
+// and four workgroups a unit; twelve of up to 1500 tokens, 16 heads, float32: 104; 153, 115, 113; gradients of four times 2048 tokens, 16 heads: 230; 301,
+// 262, 244.  At least two chunks, for a state is as much to write and to read as a chunk's rows: gradients of three of up to 1999 tokens, 8 heads, float32:
+// 139 us, as with one; 171 and 153 with three and four.
 int segment_of(const ttc_linear_attention_t& a, int slices, int cus) {
   const int64_t longest = a.max_q < a.tokens ? a.max_q : a.tokens;
   const int chunks = (int)((longest + MEM_CHUNK - 1) / MEM_CHUNK);
@@ -88,9 +88,9 @@ MemArgs forward_args(const ttc_linear_attention_t& a) {
 
 // One call, or two of the same sequences, heads and sizes
 hipError_t run_chunks(const MemArgs& a, const MemArgs* b, bool bf16, int what, hipStream_t st) {
-  const int rows = a.w.d, columns = columns_of(rows, a.v.d, bf16, a.m.max_q);
+  const int rows = a.w.d, columns = columns_of(rows, a.v.d, bf16);
   MemTwo p = {{a, b ? *b : a}, 0};
-  p.of[0].slices = p.of[1].slices = slices_of(rows, a.v.d, bf16, a.m.max_q);
+  p.of[0].slices = p.of[1].slices = slices_of(rows, a.v.d, bf16);
   p.split = dealt(a.m, a.heads, p.of[0].slices);
   const uint32_t grid = b ? 2 * p.split : p.split;
   return rows <= 64 ? launch_memory_chunks<64>(p, bf16, columns, what, grid, st)
@@ -112,7 +112,7 @@ uint64_t round16(uint64_t n) { return (n + 15) & ~15ull; }
 
 uint64_t linear_attention_workspace(const ttc_linear_attention_t& a, int cus) {
   if (a.max_q <= step_most(a.dtype == TTC_BF16)) return 0;
-  const MemSequences m = sequences_of(a, segment_of(a, slices_of(a.dk, a.dv, a.dtype == TTC_BF16, a.max_q), cus), 1);
+  const MemSequences m = sequences_of(a, segment_of(a, slices_of(a.dk, a.dv, a.dtype == TTC_BF16), cus), 1);
   if (m.entries == m.sequences) return 0;
   return (uint64_t)m.entries * a.heads * a.dk * a.dv * 4 + round16((uint64_t)m.entries * a.heads * 4);
 }
@@ -126,7 +126,7 @@ hipError_t launch_linear_attention(const ttc_linear_attention_t& a, int cus, voi
     const uint32_t grid = (uint32_t)(a.sequences * a.heads * p.slices);
     return a.dk <= 64 ? launch_memory_step<64>(p, bf16, grid, st) : a.dk <= 128 ? launch_memory_step<128>(p, bf16, grid, st) : launch_memory_step<256>(p, bf16, grid, st);
   }
-  p.m = sequences_of(a, segment_of(a, slices_of(a.dk, a.dv, a.dtype == TTC_BF16, a.max_q), cus), 1);
+  p.m = sequences_of(a, segment_of(a, slices_of(a.dk, a.dv, a.dtype == TTC_BF16), cus), 1);
   if (p.m.entries != p.m.sequences) {
     p.added = static_cast<float*>(workspace);
     p.faded = p.added + p.m.entries * a.heads * a.dk * a.dv;
@@ -148,9 +148,9 @@ struct BackwardPlan {
 BackwardPlan plan_backward(const ttc_linear_attention_backward_t& b, int cus) {
   const ttc_linear_attention_t& f = b.forward;
   BackwardPlan p = {};
-  p.slices = slices_of(f.dv, f.dk, f.dtype == TTC_BF16, f.max_q);
-  p.pair_slices = slices_of(f.dk, f.dv, f.dtype == TTC_BF16, f.max_q);
-  p.m = sequences_of(f, segment_of(f, 2 * p.slices, cus), 1);  // (two calls are in a launch: 224 us for four times 2048 tokens; 241 with segments for one)
+  p.slices = slices_of(f.dv, f.dk, f.dtype == TTC_BF16);
+  p.pair_slices = slices_of(f.dk, f.dv, f.dtype == TTC_BF16);
+  p.m = sequences_of(f, segment_of(f, 2 * p.slices, cus), 1);  // (two calls are in a launch: 230 us for four times 2048 tokens; 245 with segments for one)
   p.chunks = sequences_of(f, 1, 8);
   uint64_t at = 0;
   const auto take = [&](uint64_t& place, uint64_t bytes) {

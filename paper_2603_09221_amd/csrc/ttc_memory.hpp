@@ -14,7 +14,6 @@
 namespace ttc {
 
 constexpr int MEM_CHUNK = 64;      // tokens of a chunk: a lane each where decays are added up
-constexpr int MEM_FEW = 32;        // tokens of a chunk that leave room for a second part of the pairs' products
 
 // ---- sequences and their segments ---------------------------------------------------------------------------------------------
 
@@ -185,14 +184,17 @@ __device__ __forceinline__ float mem_finite(const mem_float8& v, float so_far) {
   return so_far;
 }
 
-// Eight float32 numbers as a sum of PARTS operands, the largest part first.  One part is rounded to nearest, 2^-9 of a number at
+// Eight float32 numbers as a sum of PARTS operands, the largest part first.  One and two parts are rounded to nearest, 2^-8 and 2^-16 of a number at
 // most; three are cut off and hold all 24 bits.  (An infinity leaves NaN in the second, as does a number beyond the largest bfloat16.)
 template <int PARTS>
 __device__ __forceinline__ void mem_split(const float (&x)[8], srv_bf16x8 (&part)[PARTS]) {
-  static_assert(PARTS == 1 || PARTS == 3);
-  if constexpr (PARTS == 1) {
+  static_assert(PARTS >= 1 && PARTS <= 3);
+  if constexpr (PARTS < 3) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) part[0][i] = static_cast<__bf16>(x[i]);
+    if constexpr (PARTS == 2)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) part[1][i] = static_cast<__bf16>(x[i] - (float)part[0][i]);
   } else {
     float rest[8];
 #pragma unroll
@@ -381,12 +383,14 @@ template <typename T, int DK, int WAVES>
 struct MemShape {
   // Rows of bfloat16 an odd multiple of 32 bytes apart: the columns that 32 lanes read at once lie on as many banks, and so do the 16 bytes of rows that 16
   // do.  (Of 16 bytes, with the eight rows of a column's share one behind the other: LDS was busy for 53 % of a long prompt's cycles instead of 41 %, 148 us
-  // instead of 137.)  Of float32 numbers what 64 lanes read of columns lies on 64 banks with 16 bytes more.
+  // instead of 137.)  Of float32 numbers what 64 lanes read of columns lies on 64 banks with 16 bytes more.  Pairs' products are read by rows alone, with 16
+  // bytes more; 16 less than the others, heads of 64 then have three workgroups of four wavefronts on a unit (64 x 32 tokens of 32 heads 34 us, else 39).
   static constexpr int PAD = sizeof(T) == 2 ? 16 : 4;
   static constexpr int COLS = 16 * WAVES;
-  static constexpr int XS = DK + PAD, VS = COLS + PAD, PS = MEM_CHUNK + PAD;  // rows in LDS
+  static constexpr int XS = DK + PAD, VS = COLS + PAD, PS = MEM_CHUNK + 16 / (int)sizeof(T);  // rows in LDS
+  static constexpr int PARTS = sizeof(T) == 2 ? 2 : 1;  // of the pairs' products, one behind the other
   // the pairs' products have a place of their own unless LDS is too small for it: then that of x, for one more barrier
-  static constexpr bool OWN = MEM_CHUNK * (2 * XS + VS + PS) * sizeof(T) <= 150 * 1024;
+  static constexpr bool OWN = MEM_CHUNK * (2 * XS + VS + PARTS * PS) * sizeof(T) <= 150 * 1024;
   static constexpr int XP = DK / 8 / WAVES, VP = 2;  // pieces of eight that a thread brings
   // wavefronts of a SIMD that registers are kept for: two workgroups on a compute unit, where LDS has room for them; two at least, for with all 512
   // registers of one the compiler puts sums into accumulation registers and reads some of them too early behind a branch (the build looks for that)
@@ -473,10 +477,10 @@ enum MemWhat { MEM_STATES, MEM_OUT, MEM_OUT_DOTS, MEM_OUT_PAIRS };
 // A workgroup takes one segment of one head of one sequence, and of the values' columns a slice of 16 * WAVES; a wavefront owns 16 of them and their
 // state, DK numbers each, which stays in its registers from chunk to chunk: what a lane holds of it as a result is what it has to hold of it as an operand
 // if the sum's order follows.  The next chunk's rows and decays are on their way while one is worked on.
-// bfloat16 rows: pairs' products and the state that queries meet are rounded to bfloat16 for their products, 2^-9 each, as the header's documentation
-// states; with four wavefronts a chunk of 32 tokens or fewer has the place of the other 32 for what the first rounding of pairs leaves, for with a few tokens one
-// rounding can be a whole result's (with eight registers are short: 205 us instead of 151 for 16384 tokens; a second part for all takes LDS and 5 to 20 %); where gradients of decays, sums of float32 numbers, depend on what a token reads, the state has three parts, all of float32's bits, and so has
-// always what is added to it (two, 17 bits, left a state of 16384 tokens 1.6e-6 off in the norm; three leave 1.3e-7).
+// bfloat16 rows: pairs' products and the state that queries meet have two bfloat16 parts for their products, 2^-16 of each off, as the header's documentation
+// states: results are then as near as their own rounding lets them (16384 tokens 0.00166 in the norm, with one part each 0.00235; two take 228 us, one 209).
+// Where gradients of decays, sums of float32 numbers, depend on what a token reads, the state has three parts, all of float32's bits, and so has
+// always what is added to it (two left a state of 16384 tokens 1.6e-6 off in the norm; three leave 1.3e-7).
 // MEM_OUT_PAIRS: where the rows of results are keys and values (dv), a pair's product times that of the value and the result's gradient is its share of the
 // decays' gradients between the two tokens: added up by rows and by columns here, where all but one operand is in LDS (a kernel of its own took 38 us of
 // 250 for four times 2048 tokens of 16 heads of 128, this takes 17).
@@ -491,12 +495,12 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
   typedef typename MemOperand<T>::type op_t;
   constexpr bool BF16 = sizeof(T) == 2, STATES = WHAT == MEM_STATES, DOTS = WHAT == MEM_OUT_DOTS;
   constexpr bool PAIRS = WHAT == MEM_OUT_PAIRS;
-  constexpr int IN = BF16 && DOTS ? 3 : 1, UP = BF16 ? 3 : 1, KT = DK / 16;
+  constexpr int IN = !BF16 ? 1 : DOTS ? 3 : 2, UP = BF16 ? 3 : 1, KT = DK / 16;
   constexpr int HALVES = WAVES / 4;  // wavefronts that share sixteen rows of pairs
   __shared__ alignas(16) T xl[STATES ? 8 : MEM_CHUNK * (S::OWN || S::XS > S::PS ? S::XS : S::PS)], wl[MEM_CHUNK * S::XS], vl[MEM_CHUNK * S::VS];
-  __shared__ alignas(16) T own[STATES || !S::OWN ? 8 : MEM_CHUNK * S::PS];
+  __shared__ alignas(16) T own[STATES || !S::OWN ? 8 : S::PARTS * MEM_CHUNK * S::PS];
   __shared__ alignas(16) MemDecays decays[2];
-  __shared__ alignas(16) float meet[8][MEM_CHUNK];
+  __shared__ alignas(16) float meet[WAVES == 4 ? 5 : 8][MEM_CHUNK];
   T* const pl = S::OWN ? own : xl;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int c = lane & 15, g = lane >> 4;
@@ -561,7 +565,7 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
     const int chunk = reverse ? c1 - 1 - turn : c0 + turn, rows = rows_of(chunk);
     const int after = reverse ? chunk - 1 : chunk + 1;
     const int64_t t0 = first + (int64_t)chunk * MEM_CHUNK;
-    const bool whole = whole_state && rows == MEM_CHUNK, few = BF16 && WAVES == 4 && rows <= MEM_FEW;
+    const bool whole = whole_state && rows == MEM_CHUNK;
     asm volatile("" : "+v"(c), "+v"(g));  // places and masks are found anew: kept over the loop they would take registers that spill
     const MemDecays& dl = decays[turn & 1];
     if (!S::AHEAD) fetch(chunk, rows);
@@ -672,12 +676,13 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
 #pragma unroll
           for (int r = 0; r < 4; ++r) p[r] = z[u][r] * way * left[r];
         }
-        if (!few || own_rows < 2) mem_store4(pl + i * S::PS + mem_place(16 * j + 4 * g), p);
-        if (few && own_rows < 2) {
+        T* const to = pl + i * S::PS + mem_place(16 * j + 4 * g);
+        mem_store4(to, p);
+        if constexpr (S::PARTS == 2) {
           float rest[4];
 #pragma unroll
           for (int r = 0; r < 4; ++r) rest[r] = p[r] - srv_widen(srv_narrow<T>(p[r]));
-          mem_store4(pl + (i + 32) * S::PS + mem_place(16 * j + 4 * g), rest);
+          mem_store4(to + MEM_CHUNK * S::PS, rest);
         }
         if constexpr (PAIRS) {
           // times the second factor; a pair of one token with itself belongs to no sum
@@ -754,26 +759,20 @@ __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)
         }
       }
       const auto pairs = [&](int i, int k) {
-        const T* row = pl + (16 * i + c) * S::PS + 32 * k + 8 * g;
-        o[i] = mem_mma(clean[k], mem_operand(row, row + 4), o[i]);
+#pragma unroll
+        for (int part = S::PARTS - 1; part >= 0; --part) {
+          const T* row = pl + (part * MEM_CHUNK + 16 * i + c) * S::PS + 32 * k + 8 * g;
+          o[i] = mem_mma(clean[k], mem_operand(row, row + 4), o[i]);
+        }
       };
-      if (few) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const T* row = pl + (16 * i + 32 + c) * S::PS + 8 * g;
-          o[i] = mem_mma(clean[0], mem_operand(row, row + 4), o[i]);
-          pairs(i, 0);
-        }
+      for (int i = 0; i < 4; ++i) pairs(i, i / 2);
+      if (reverse) {
+        pairs(0, 1);
+        pairs(1, 1);
       } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) pairs(i, i / 2);
-        if (reverse) {
-          pairs(0, 1);
-          pairs(1, 1);
-        } else {
-          pairs(2, 0);
-          pairs(3, 0);
-        }
+        pairs(2, 0);
+        pairs(3, 0);
       }
       if (bad)
         for (int j = 0; j < rows; ++j)
