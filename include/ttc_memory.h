@@ -62,7 +62,8 @@ ttc_status_t ttc_linear_attention(const ttc_linear_attention_t *attention, void 
 
 /* Gradients of a loss from dl/dout and dl/dS of the sequences' last states.  `forward` describes the forward call; its out, state_out are
  * not used.  gq, gk sum over the heads that share them; a glog_decay for g_token = 0 sums over all tokens (else it is one per token and
- * head).  gstate: with respect to the states that the sequences began with, 0 where a sequence began with zeros by rule. */
+ * head).  gstate: with respect to the states that the sequences began with, 0 where a sequence began with zeros by rule.  No result may
+ * overlap another or anything that is read (TTC_ERR_INVALID_ARG): rows are read again after results have been written. */
 typedef struct {
   ttc_linear_attention_t forward;
   const void *gout;            /* (tokens, heads, dv) of dtype by gout_token, gout_head                     */

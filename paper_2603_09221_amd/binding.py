@@ -1103,7 +1103,8 @@ def ttc_linear_attention_backward(q, k, v, log_decay, grad_out, *, cu_q=None, ma
                                   scale=None, out=None, workspace=None, stream=None):
     """{"gq", "gk", "gv", "glog_decay"} of a loss with the gradient grad_out (tokens, heads, dv) with respect to ttc_linear_attention's out, and
     grad_state (sequences, heads, dk, dv) with respect to the sequences' last states (None: zeros); with `state` also "gstate" (sequences, heads,
-    dk, dv), with respect to what each began with.  glog_decay is float32, of log_decay's shape; rows that no sequence has are not written."""
+    dk, dv), with respect to what each began with.  glog_decay is float32, of log_decay's shape; rows that no sequence has are not written.
+    `out` may carry tensors under these names, none of them in the place of another or of anything given."""
     lib = load()
     a = _linear_attention(q, k, v, log_decay, cu_q, max_q, state, state_row, kv_len, scale, True)
     gout_token, gout_head = _heads_strides(grad_out, "grad_out", v.shape, v.dtype)

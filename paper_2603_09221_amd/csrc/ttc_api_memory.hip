@@ -12,6 +12,32 @@ bool aligned(const void* p, uint64_t n) { return (uint64_t)p % n == 0; }
 bool known_dtype(int32_t t) { return t == TTC_F32 || t == TTC_BF16; }
 uint64_t bytes_of(int32_t t) { return t == TTC_BF16 ? 2 : 4; }
 
+// Memory that a call reads or writes: `count` rows of `width` bytes, `step` bytes apart
+struct Rows {
+  uint64_t at;
+  int64_t count, step;
+  uint64_t width;
+};
+
+Rows whole(const void* p, uint64_t bytes) { return {(uint64_t)p, p && bytes ? 1 : 0, 0, bytes}; }
+// of tokens, with the space between their heads; strides in entries of `size` bytes
+Rows rows_of(const void* p, int64_t tokens, int64_t token, int64_t heads, int64_t head, int64_t entries, uint64_t size) {
+  uint64_t at = (uint64_t)p;
+  if (head < 0) at += (heads - 1) * head * (int64_t)size;
+  if (token < 0 && tokens > 1) at += (tokens - 1) * token * (int64_t)size;
+  return {at, p ? tokens : 0, (token < 0 ? -token : token) * (int64_t)size, ((heads - 1) * (head < 0 ? -head : head) + entries) * size};
+}
+// Whether `one` block of memory and rows have a byte in common
+bool meet(const Rows& one, const Rows& r) {
+  if (!one.count || r.count < 1) return false;
+  const uint64_t end = one.at + one.width;
+  if (r.count == 1 || (uint64_t)r.step <= r.width) return one.at < r.at + (r.count - 1) * r.step + r.width && r.at < end;
+  if (r.at >= end) return false;
+  const uint64_t behind = r.at + r.width;  // of the first row; the first row that ends behind one.at is the only one to look at
+  const uint64_t row = one.at < behind ? 0 : (one.at - behind) / r.step + 1;
+  return row < (uint64_t)r.count && r.at + row * r.step < end;
+}
+
 // Sizes and numbers, which the workspace depends on; calls: in one launch
 ttc_status_t check_sizes(const ttc_linear_attention_t& a, int calls) {
   if (a.sequences < 0 || a.tokens < 0 || a.heads < 1 || a.heads_qk < 1 || a.heads % a.heads_qk || !known_dtype(a.dtype) || a.max_q < 0 || !isfinite(a.scale))
@@ -78,6 +104,27 @@ ttc_status_t check_backward(const ttc_linear_attention_backward_t* b) {
   return check_pointers(f);
 }
 
+// A result in the place of something that a later launch of the call reads, or of another result
+bool backward_overlaps(const ttc_linear_attention_backward_t& b) {
+  const ttc_linear_attention_t& f = b.forward;
+  const uint64_t n = bytes_of(f.dtype), state = (uint64_t)f.heads * f.dk * f.dv * 4;
+  const Rows result[5] = {whole(b.gq, (uint64_t)f.tokens * f.heads_qk * f.dk * n), whole(b.gk, (uint64_t)f.tokens * f.heads_qk * f.dk * n),
+                          whole(b.gv, (uint64_t)f.tokens * f.heads * f.dv * n), whole(b.glog_decay, (uint64_t)(f.g_token ? f.tokens : 1) * f.heads * 4),
+                          whole(b.gstate, f.sequences * state)};
+  const Rows read[10] = {rows_of(f.q, f.tokens, f.q_token, f.heads_qk, f.q_head, f.dk, n), rows_of(f.k, f.tokens, f.k_token, f.heads_qk, f.k_head, f.dk, n),
+                         rows_of(f.v, f.tokens, f.v_token, f.heads, f.v_head, f.dv, n), rows_of(b.gout, f.tokens, b.gout_token, f.heads, b.gout_head, f.dv, n),
+                         rows_of(f.log_decay, f.tokens, f.g_token, f.heads, f.g_head, 1, 4), whole(f.state_in, f.state_rows * state),
+                         whole(b.gstate_out, f.sequences * state), whole(f.cu_q, (f.sequences + 1) * 4), whole(f.state_row, f.sequences * 4),
+                         whole(f.kv_len, f.sequences * 4)};
+  for (int i = 0; i < 5; ++i) {
+    for (const Rows& r : read)
+      if (meet(result[i], r)) return true;
+    for (int k = 0; k < i; ++k)
+      if (meet(result[i], result[k])) return true;
+  }
+  return false;
+}
+
 }  // namespace
 
 extern "C" {
@@ -111,6 +158,7 @@ ttc_status_t ttc_linear_attention_backward(const ttc_linear_attention_backward_t
   if (f.tokens > 1 && (b->gout_token < 0 || b->gout_token >= (1 << 23))) return TTC_ERR_UNSUPPORTED;
   const uint64_t need = ttc::linear_attention_backward_workspace(*b, ttc::compute_units());
   if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return TTC_ERR_WORKSPACE;
+  if (backward_overlaps(*b)) return TTC_ERR_INVALID_ARG;
   return ttc::launch_linear_attention_backward(*b, ttc::compute_units(), workspace, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? TTC_OK : TTC_ERR_DEVICE;
 }
 

@@ -1,0 +1,67 @@
+"""Results of memory layers' gradients that would lie where the call still reads: refused before the device is touched, by addresses that nobody reads."""
+import pytest
+
+from paper_2603_09221_amd import binding
+from tests.test_memory_boundary import INVALID, lib  # noqa: F401  (a fixture)
+
+FINE = (0, 4)     # ok, or no device
+
+# 600 tokens, 4 heads over 2 of 64 x 128 in bfloat16; every tensor in a part of 16 MB of its own
+AT = {name: (i + 1) << 24 for i, name in enumerate(("q", "k", "v", "gout", "log_decay", "state_in", "gstate_out", "cu_q", "state_row", "kv_len", "gq", "gk", "gv",
+                                                    "glog_decay", "gstate", "workspace"))}
+TOKENS, HEADS, HEADS_QK, DK, DV = 600, 4, 2, 64, 128
+SIZE = dict(gq=TOKENS * HEADS_QK * DK * 2, gk=TOKENS * HEADS_QK * DK * 2, gv=TOKENS * HEADS * DV * 2, glog_decay=TOKENS * HEADS * 4,
+            gstate=2 * HEADS * DK * DV * 4)
+READ = dict(q=SIZE["gq"], k=SIZE["gk"], v=SIZE["gv"], gout=SIZE["gv"], log_decay=SIZE["glog_decay"], state_in=3 * SIZE["gstate"] // 2, gstate_out=SIZE["gstate"],
+            cu_q=12, state_row=8, kv_len=8)
+
+
+def call(lib, strides={}, **at):
+    a = {**AT, **at}
+    f = binding.LinearAttention(sequences=2, tokens=TOKENS, heads=HEADS, heads_qk=HEADS_QK, dk=DK, dv=DV, dtype=1, max_q=500, scale=0.1, q_token=128, q_head=64,
+                                k_token=128, k_head=64, v_token=512, v_head=128, g_token=4, g_head=1, state_rows=3,
+                                **{k: a[k] for k in ("q", "k", "v", "log_decay", "cu_q", "state_in", "state_row", "kv_len")})
+    b = binding.LinearAttentionBackward(forward=f, gout_token=512, gout_head=128, **{k: a[k] for k in ("gout", "gstate_out", "gq", "gk", "gv", "glog_decay", "gstate")})
+    for name, value in strides.items():
+        setattr(b.forward if hasattr(f, name) else b, name, value)
+    return lib.ttc_linear_attention_backward(b, a["workspace"], 1 << 40, None)
+
+
+@pytest.mark.parametrize("result", SIZE)
+@pytest.mark.parametrize("read", READ)
+def test_results_in_the_place_of_what_is_read(lib, result, read):  # noqa: F811
+    last = READ[read] // 16 * 16 - (16 if READ[read] >= 16 and READ[read] % 16 == 0 else 0)
+    for at in (AT[read], AT[read] + last, AT[read] - SIZE[result] + 16):     # the same, its last bytes, its first
+        assert call(lib, **{result: at}) == INVALID
+
+
+@pytest.mark.parametrize("one", SIZE)
+@pytest.mark.parametrize("two", SIZE)
+def test_results_in_each_others_place(lib, one, two):  # noqa: F811
+    if one != two:
+        assert call(lib, **{one: AT[two] + 16}) == INVALID
+
+
+def test_rows_far_apart(lib):  # noqa: F811
+    """A result between two rows of a strided tensor is no overlap; a byte of either row is.  (Without sequences nothing is launched, but places are
+    checked; where there is no device that is what is said then.)"""
+    wide = 1 << 20      # entries: rows 2 MB apart, of 1 KB
+    v = AT["workspace"] + (1 << 40)
+    width, step = DV * HEADS * 2, 2 * wide
+    for row in (0, 5, TOKENS - 2):
+        first, last = v + row * step + width, v + (row + 1) * step - SIZE["gq"]
+        for at, want in ((first, True), (last, True), (first - 2, False), (last + 2, False)):
+            assert call(lib, dict(v_token=wide, sequences=0), v=v, gq=at) in (FINE if want else (INVALID,)), (row, at)
+    for at, want in ((v - SIZE["gq"], True), (v - SIZE["gq"] + 2, False), (v + (TOKENS - 1) * step + width, True), (v + (TOKENS - 1) * step + width - 2, False)):
+        assert call(lib, dict(v_token=wide, sequences=0), v=v, gq=at) in (FINE if want else (INVALID,))
+
+
+def test_rows_of_one_buffer(lib):  # noqa: F811
+    """Queries, keys and values where a fused projection left them, heads side by side or tokens side by side; results behind it, or in it."""
+    for strides, end in ((dict(q_token=768, k_token=768, v_token=768), TOKENS * 768 * 2),
+                         (dict(q_token=64, q_head=64 * TOKENS, k_token=64, k_head=64 * TOKENS, v_token=128, v_head=128 * TOKENS), TOKENS * 768 * 2)):
+        base = 1 << 41
+        first = base + (256 if strides["q_token"] == 768 else 64 * TOKENS * HEADS_QK * 2)
+        where = dict(q=base, k=first, v=2 * first - base)
+        for at, want in ((base + end, True), (base + end - 2, False), (base - SIZE["gv"], True), (base - SIZE["gv"] + 2, False)):
+            assert call(lib, {**strides, "sequences": 0}, gv=at, **where) in (FINE if want else (INVALID,))
