@@ -105,7 +105,8 @@ typedef struct {
 ttc_status_t ttc_residual_norm(const ttc_residual_norm_t *norm, void *hip_stream);
 
 /* Gradients of a loss from dl/dr and dl/dh.  `forward` describes the forward call; its r and h are not used.  Any result may be NULL; a vector's
- * is summed over the tokens, in an order that depends on the sizes alone.  workspace as above. */
+ * is summed over the tokens, in an order that depends on the sizes alone.  workspace as above.  gy, ggate, gresidual may be y, gate, residual, gr
+ * or gh where these are contiguous; they may not overlap them otherwise, nor another result, nor a vector (TTC_ERR_INVALID_ARG). */
 typedef struct {
   ttc_residual_norm_t forward;
   const void *gr, *gh;         /* (tokens, features) of dtype by the strides below; gr may be NULL (zeros), gh is NULL exactly where pre is none */

@@ -1199,7 +1199,8 @@ def ttc_residual_norm_backward(y, *, grad_r=None, grad_h=None, residual=None, ga
                                workspace=None, stream=None):
     """{"gy", "ggate", "gresidual", "gpost_gain", "gpost_offset", "gresidual_gain", "gpre_gain", "gpre_offset"}, each where the forward call has
     what it belongs to, of a loss with the gradients grad_r (None: zeros) and grad_h with respect to ttc_residual_norm's results.  ggate is each
-    token's, also of a gate that is the same for all."""
+    token's, also of a gate that is the same for all.  `out` may carry tensors under these names: gy, ggate and gresidual may be contiguous y, gate,
+    residual, grad_r or grad_h themselves."""
     lib = load()
     n, vectors = _residual_norm(y, residual, gate, activation, post, post_gain, post_offset, groups, post_eps, scale, residual_gain, pre, pre_gain,
                                 pre_offset, pre_eps)

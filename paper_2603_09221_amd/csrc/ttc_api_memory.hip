@@ -104,6 +104,28 @@ ttc_status_t check_backward(const ttc_linear_attention_backward_t* b) {
   return check_pointers(f);
 }
 
+// A result in the place of another, or of rows or vectors that are read, unless the rows are the same: a thread writes its part of a row after it read it
+bool norm_backward_overlaps(const ttc_residual_norm_backward_t& b) {
+  const ttc_residual_norm_t& n = b.forward;
+  const uint64_t e = bytes_of(n.dtype), vector = (uint64_t)n.features * 4, rows = (uint64_t)n.tokens * n.features * e;
+  const Rows result[8] = {whole(b.gy, rows), whole(b.ggate, rows), whole(b.gresidual, rows), whole(b.gpost_gain, vector), whole(b.gpost_offset, vector),
+                          whole(b.gresidual_gain, vector), whole(b.gpre_gain, vector), whole(b.gpre_offset, vector)};
+  const void* const given[5] = {n.y, n.gate, n.residual, b.gr, b.gh};
+  const int64_t stride[5] = {n.y_token, n.gate_token, n.residual_token, b.gr_token, b.gh_token};
+  for (int i = 0; i < 8; ++i) {
+    for (int k = 0; k < i; ++k)
+      if (meet(result[i], result[k])) return true;
+    if (i >= 3) continue;  // (vectors are written by a launch that reads the workspace alone)
+    for (int k = 0; k < 5; ++k) {
+      const bool same = result[i].at == (uint64_t)given[k] && (n.tokens < 2 || stride[k] == n.features);
+      if (!same && meet(result[i], rows_of(given[k], n.tokens, stride[k], 1, 0, n.features, e))) return true;
+    }
+    for (const float* v : {n.post_gain, n.post_offset, n.residual_gain, n.pre_gain, n.pre_offset})
+      if (meet(result[i], whole(v, vector))) return true;
+  }
+  return false;
+}
+
 // A result in the place of something that a later launch of the call reads, or of another result
 bool backward_overlaps(const ttc_linear_attention_backward_t& b) {
   const ttc_linear_attention_t& f = b.forward;
@@ -184,6 +206,7 @@ ttc_status_t ttc_residual_norm_backward(const ttc_residual_norm_backward_t* b, v
   if (const ttc_status_t s = check_norm_backward(b); s != TTC_OK) return s;
   const uint64_t need = ttc::norm_backward_workspace(*b, ttc::compute_units());
   if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return TTC_ERR_WORKSPACE;
+  if (norm_backward_overlaps(*b)) return TTC_ERR_INVALID_ARG;
   return ttc::launch_residual_norm_backward(*b, ttc::compute_units(), workspace, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? TTC_OK : TTC_ERR_DEVICE;
 }
 

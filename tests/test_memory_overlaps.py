@@ -65,3 +65,42 @@ def test_rows_of_one_buffer(lib):  # noqa: F811
         where = dict(q=base, k=first, v=2 * first - base)
         for at, want in ((base + end, True), (base + end - 2, False), (base - SIZE["gv"], True), (base - SIZE["gv"] + 2, False)):
             assert call(lib, {**strides, "sequences": 0}, gv=at, **where) in (FINE if want else (INVALID,))
+
+
+# the norms' gradients: 37 rows of 96 in float32 (0) or bfloat16 (1)
+NORM_ROWS, FEATURES = 37, 96
+NORM_READ = ("y", "gate", "residual", "gr", "gh")
+VECTORS = binding.NORM_VECTORS
+NORM_AT = {name: (i + 1) << 24 for i, name in enumerate(NORM_READ + VECTORS + ("gy", "ggate", "gresidual") + tuple("g" + v for v in VECTORS) + ("workspace",))}
+
+
+def norm_call(lib, dtype, strides={}, tokens=NORM_ROWS, **at):
+    a = {**NORM_AT, **at}
+    f = binding.ResidualNorm(tokens=tokens, features=FEATURES, groups=1, dtype=dtype, post=1, pre=2, act=2, post_eps=1e-5, pre_eps=1e-5, scale=1.0,
+                             **{k: a[k] for k in ("y", "gate", "residual") + VECTORS}, **{k + "_token": strides.get(k, FEATURES) for k in ("y", "gate", "residual")})
+    b = binding.ResidualNormBackward(forward=f, **{k: a[k] for k in ("gr", "gh", "gy", "ggate", "gresidual") + tuple("g" + v for v in VECTORS)},
+                                     **{k + "_token": strides.get(k, FEATURES) for k in ("gr", "gh")})
+    return lib.ttc_residual_norm_backward(b, a["workspace"], 1 << 40, None)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("result", ["gy", "ggate", "gresidual"])
+def test_norms_results_in_the_place_of_what_is_read(lib, result, dtype):  # noqa: F811
+    size = (4, 2)[dtype]
+    for read in NORM_READ:
+        for at in (1, -1, FEATURES, 1 - NORM_ROWS * FEATURES, NORM_ROWS * FEATURES - 1):
+            assert norm_call(lib, dtype, **{result: NORM_AT[read] + at * size}) == INVALID, (read, at)
+        for stride in (0, -FEATURES, FEATURES + 8, 2 * FEATURES):
+            assert norm_call(lib, dtype, {read: stride}, **{result: NORM_AT[read]}) == INVALID, (read, stride)
+    for vector in VECTORS:
+        assert norm_call(lib, dtype, **{result: NORM_AT[vector]}) == INVALID
+        assert norm_call(lib, dtype, **{result: NORM_AT[vector] + 4 * FEATURES - 4}) == INVALID
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_norms_results_in_each_others_place(lib, dtype):  # noqa: F811
+    names = ["gy", "ggate", "gresidual"] + ["g" + v for v in VECTORS]
+    for one in names:
+        for two in names:
+            if one != two:
+                assert norm_call(lib, dtype, **{one: NORM_AT[two] + 4}) == INVALID, (one, two)
