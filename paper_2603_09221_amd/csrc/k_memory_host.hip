@@ -274,6 +274,9 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
   d.pairs = place(plan.pairs);
   d.a = place(plan.a);
   d.b = place(plan.b);
+  d.log_decay = f.log_decay;
+  d.g_token = f.g_token;
+  d.g_head = f.g_head;
   d.begin = begin;
   d.gstate = gstate;
   d.out = f.g_token ? b.glog_decay : nullptr;

@@ -5,7 +5,7 @@
 //     dl/dg_t = sum_{j < t <= i} m_ij + I + sum_{s < t} (b_s - a_s),      m_ij = scale exp(G_i - G_j) (q_i . k_j) (dout_i . v_j),
 // the last sum over the earlier tokens of the segment: a_s is q_s times what dq_s has from the state before its chunk, b_s is k_s times what dk_s
 // has from the state's gradient behind its chunk, I = <R, S> where the segment begins.  Sums over tokens are float64; their terms' errors of
-// 2^-24 add up from one such beginning to the next.
+// 2^-24 add up from one such beginning to the next.  A token whose exp(g) is 0 in float32 has the gradient 0, which the sum's terms would only come near to.
 #pragma once
 #include "ttc_memory.hpp"
 
@@ -16,6 +16,8 @@ struct MemDecayArgs {
   int32_t heads, dk, dv, slices, pair_slices;
   const float* pairs;           // (pair_slices, heads, tokens): sum_{j < t <= i} m_ij of a chunk's pairs
   const float *a, *b;           // (slices, heads, tokens)
+  const float* log_decay;
+  int64_t g_token, g_head;
   MemStates begin;              // of the forward call
   const float* gstate;          // (sequences, heads, dk, dv), where a sequence began with a state
   const float *found, *found_r; // (entries, heads, dk, dv): the segments' states from before, and their gradients from behind
@@ -24,6 +26,7 @@ struct MemDecayArgs {
 };
 
 constexpr int MEM_SUM_THREADS = 1024;
+constexpr float MEM_FORGETS = -104.f;  // its exponential is less than half of float32's smallest number
 
 // One head of one segment: 1024 tokens at a time.  Two states a segment are what it reads: 31 MB in 9.4 us for four times 2048 tokens of 16 heads of 128.
 static __global__ void __launch_bounds__(MEM_SUM_THREADS) memory_decay_kernel(const MemDecayArgs a) {
@@ -85,6 +88,7 @@ static __global__ void __launch_bounds__(MEM_SUM_THREADS) memory_decay_kernel(co
     if (real) {
       double grad = now + (sum - step);
       for (int s = 0; s < a.pair_slices; ++s) grad += a.pairs[s * a.heads * a.m.tokens + t];
+      if (a.log_decay[(first + at + tid) * a.g_token + head * a.g_head] < MEM_FORGETS) grad *= 0.0;  // (NaN stays)
       if (a.out) a.out[(first + at + tid) * a.heads + head] = (float)grad;
       total += grad;
     }

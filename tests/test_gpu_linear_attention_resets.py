@@ -71,3 +71,50 @@ def test_decays_that_heads_have_for_good(dtype):
     forward.check(q, k, v, g, cu, got["out"], got["state"], first.double().cpu().numpy())
     got = binding.ttc_linear_attention_backward(q, k, v, g, gout, cu_q=cu, max_q=length, state=first, grad_state=glast)
     backward.check(x, gout, first, glast, got)
+
+
+@pytest.mark.parametrize("decay", [-104.5, -200.0, -float("inf")])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("length", [40, 4 * CHUNK + 9])
+def test_a_decay_that_leaves_nothing_has_no_gradient(decay, dtype, length):
+    """dl/dg = exp(g) <R, S> is 0 where exp(g) is 0 in float32, below -104 (2^-150): not what is left of terms that cancel."""
+    x, gout, first, glast = backward.gradient_inputs([length, 30], 2, 1, 64, 64, dtype, False, 11, True)
+    q, k, v, g, cu = x
+    none = torch.zeros(g.shape, dtype=torch.bool)
+    none[::7, 0] = none[5::CHUNK, 1] = none[length:length + 1] = True
+    g[none.to(g.device)] = decay
+    got = binding.ttc_linear_attention_backward(q, k, v, g, gout, cu_q=cu, max_q=length, state=first, grad_state=glast)
+    check_gradients(x, gout, first, glast, got)
+    assert not got["glog_decay"].cpu()[none].any() and got["glog_decay"].cpu()[~none].all()
+    fixed = torch.tensor([decay, -0.1], device=g.device)
+    got = binding.ttc_linear_attention_backward(q, k, v, fixed, gout, cu_q=cu, max_q=length, state=first, grad_state=glast)["glog_decay"]
+    assert got[0] == 0 and got[1] != 0
+
+
+@pytest.mark.parametrize("length", [3, CHUNK, 150, 600])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_no_number_reaches_gradients_that_do_not_depend_on_it(length, dtype):
+    """NaN and infinities in a token's query, key, value or result's gradient: other heads', other sequences' and the tokens' on the other side keep their
+    bits; of the decays' gradients, which are sums along a sequence, other heads' and other sequences'."""
+    x, gout, first, glast = backward.gradient_inputs([length, 20], 2, 2, 64, 64, dtype, False, 12, True)
+    q, k, v, g, cu = x
+    call = lambda: binding.ttc_linear_attention_backward(q, k, v, g, gout, cu_q=cu, max_q=max(length, 20), state=first, grad_state=glast)
+    want = call()
+    at = length * 2 // 3
+    before, own, after = slice(0, at), slice(at, at + 1), slice(at + 1, length)
+    keeps = {"q": dict(gq=(before, own, after), gk=(after,), gv=(after,)), "k": dict(gq=(before,), gk=(before, own, after), gv=(before, after)),
+             "v": dict(gq=(before,), gk=(before, after), gv=(before, own, after)), "gout": dict(gq=(before, after), gk=(after,), gv=(after,))}
+    for value in (float("nan"), float("inf"), -float("inf")):
+        for name, t in (("q", q), ("k", k), ("v", v), ("gout", gout)):
+            keep = t[at].clone()
+            t[at, 0, 5] = value
+            got = call()
+            t[at] = keep
+            for result in ("gq", "gk", "gv", "glog_decay"):
+                assert torch.equal(got[result][:, 1], want[result][:, 1]) and torch.equal(got[result][length:], want[result][length:]), (name, result)
+            assert torch.equal(got["gstate"][1], want["gstate"][1]) and torch.equal(got["gstate"][0, 1], want["gstate"][0, 1])
+            for result, parts in keeps[name].items():
+                for part in parts:
+                    assert torch.equal(got[result][part, 0], want[result][part, 0]), (name, result, part)
+            if name in ("k", "v"):
+                assert torch.equal(got["gstate"], want["gstate"])
