@@ -207,7 +207,7 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
   back.v = gout;
   hipError_t e;
   if (!f.sequences) {
-    if (!f.g_token) hipLaunchKernelGGL(memory_decay_sum_kernel, dim3((f.heads + 63) / 64), dim3(64), 0, st, nullptr, 0, f.heads, b.glog_decay);
+    if (!f.g_token) hipLaunchKernelGGL(memory_decay_sum_kernel, dim3(f.heads), dim3(256), 0, st, nullptr, 0, f.heads, b.glog_decay);
     return hipGetLastError();
   }
   if (segmented) {
@@ -285,7 +285,7 @@ hipError_t launch_linear_attention_backward(const ttc_linear_attention_backward_
   d.found_r = back.starts;
   hipLaunchKernelGGL(memory_decay_kernel, dim3((uint32_t)(plan.m.entries * f.heads)), dim3(MEM_SUM_THREADS), 0, st, d);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (!f.g_token) hipLaunchKernelGGL(memory_decay_sum_kernel, dim3((f.heads + 63) / 64), dim3(64), 0, st, d.sums, plan.m.entries, f.heads, b.glog_decay);
+  if (!f.g_token) hipLaunchKernelGGL(memory_decay_sum_kernel, dim3(f.heads), dim3(256), 0, st, d.sums, plan.m.entries, f.heads, b.glog_decay);
   return hipGetLastError();
 }
 

@@ -118,3 +118,14 @@ def test_no_number_reaches_gradients_that_do_not_depend_on_it(length, dtype):
                     assert torch.equal(got[result][part, 0], want[result][part, 0]), (name, result, part)
             if name in ("k", "v"):
                 assert torch.equal(got["gstate"], want["gstate"])
+
+
+@pytest.mark.parametrize("heads,heads_qk", [(1, 1), (6, 3)])
+@pytest.mark.parametrize("lengths", [[i % 4 for i in range(700)], [3] * 257, [1], [70] * 300])
+def test_a_decay_for_good_over_many_sequences(lengths, heads, heads_qk):
+    """Its gradient is the sum of those of all tokens: of as many segments as there are sequences, and more; the same bits every time."""
+    x, gout, first, glast = backward.gradient_inputs(lengths, heads, heads_qk, 16, 24, torch.float32, True, 14, True)
+    call = lambda: binding.ttc_linear_attention_backward(*x[:4], gout, cu_q=x[4], max_q=max(lengths), state=first, grad_state=glast)
+    got = call()
+    backward.check(x, gout, first, glast, got)
+    assert torch.equal(call()["glog_decay"], got["glog_decay"])
