@@ -4,12 +4,12 @@
 
 namespace ttc {
 
-// Threads of a compute unit: forward all that fit (16384 rows of 4096 bfloat16: 117 us; 121 with 2048, 123 with 1024); backward those that their registers
-// leave room for at once, as every workgroup leaves a part of each sum (8192 rows of 4096: 136 us; 146 with 1024, 167 with 2048).
+// Threads of a compute unit: forward all that fit (16384 rows of 4096 bfloat16: 117 us; 120 with 2048, 123 with 1024); backward those that their registers
+// leave room for at once, as every workgroup leaves a part of each sum (8192 rows of 4096: 130 us; 141 with 1024, 162 with 2048).
 constexpr int NORM_THREADS = 4096, NORM_THREADS_BACKWARD = 512;
 
-// A thread to every eight features as far as a workgroup goes: more eights to a thread take registers that the wavefronts in flight lack (two: 123 us
-// forward where one takes 121, 256 us backward where one takes 136)
+// A thread to every eight features as far as a workgroup goes: more eights to a thread take registers that the wavefronts in flight lack (two: 188 us
+// forward where one takes 117, 301 us backward where one takes 130)
 template <typename F>
 static void norm_shape(int features, F&& f) {
   if (features <= 512) f(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});

@@ -266,7 +266,8 @@ __device__ __forceinline__ void norm_unit_backward(float (&g)[PIECES][8], const 
 }
 
 // act(x) and its derivative, from exp(-|x|), which never overflows; c = 1 - s comes without a cancellation.  Beyond 200 all is 0 or 1 in
-// float32, and infinities there would meet zeros; NaN stays.  The exponential is (1 + |x|) 2^-24 of itself off, the reciprocal a step.
+// float32, and infinities there would meet zeros; NaN stays.  The exponential is a power of two of |x| / ln 2, whose rounding, |x| 2^-24, is made up for
+// by 2^d = 1 + d ln 2; it is two steps off then, the reciprocal one.
 __device__ __forceinline__ void norm_act(int act, float x, float& y, float& slope) {
   if (act == TTC_GATE_IDENTITY) {
     y = x;
@@ -274,7 +275,11 @@ __device__ __forceinline__ void norm_act(int act, float x, float& y, float& slop
     return;
   }
   const float low = x < -200.f ? -200.f : x, near = low > 200.f ? 200.f : low;
-  const float e = __builtin_amdgcn_exp2f(fabsf(near) * -1.44269504088896340736f), d = __builtin_amdgcn_rcpf(1.f + e), f = e * d;
+  constexpr double LOG2E = 1.44269504088896340736;
+  constexpr float hi = (float)LOG2E, lo = (float)(LOG2E - hi);
+  const float size = fabsf(near), power = size * -hi, rest = fmaf(size, -lo, fmaf(size, -hi, -power));
+  const float rough = __builtin_amdgcn_exp2f(power), e = fmaf(rough, rest * 0.693147180559945309417f, rough);
+  const float d = __builtin_amdgcn_rcpf(1.f + e), f = e * d;
   const float s = x < 0.f ? f : d, c = x < 0.f ? d : f;
   if (act == TTC_GATE_SIGMOID) {
     y = s;
@@ -375,7 +380,7 @@ __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_
 }
 
 // The sums over tokens stay in registers; a workgroup leaves one part of each for norm_parts_kernel, and which rows make a part depends on the
-// sizes alone.  8192 rows of 4096 bfloat16 with everything: 125 us, 4.3 TB/s, on 8 wavefronts a compute unit, which is what 214 registers leave room for.
+// sizes alone.  8192 rows of 4096 bfloat16 with everything: 130 us, 4.1 TB/s, on 8 wavefronts a compute unit, which is what 221 registers leave room for.
 // OFFSETS: there are some, or their gradients are wanted
 template <typename T, int LANES, int PIECES, bool OFFSETS>
 __global__ void __launch_bounds__((NormShape<LANES, PIECES>::THREADS)) residual_norm_backward_kernel(const NormArgs a) {
