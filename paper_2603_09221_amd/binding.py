@@ -696,6 +696,15 @@ def _int32(**numbers):
             raise ValueError(f"{name}: {value} does not fit in 32 bits")
 
 
+def _results(out, names):
+    """A copy of `out`, whose tensors all go by names of the call's results: one that is not written must not come back as if it were."""
+    out = dict(out) if out else {}
+    for name, t in out.items():
+        if t is not None and name not in names:
+            raise ValueError(f"out: this call has no result {name!r}")
+    return out
+
+
 def _here(t, stream):
     """The last check before a launch, which goes to the current device (or the stream's): that device holds the tensors."""
     _on_gpu(t)
@@ -932,7 +941,7 @@ def ttc_kv_place(past, new_tokens, block_table, page, tokens, *, pages, free=Non
     sizes = {"cu_q": sequences + 1, "kv_len": sequences, "positions": tokens, "slots": tokens, "sequence": tokens}
     if free is not None:
         sizes.update(free_count=1, missing=1)
-    out = dict(out) if out else {}
+    out = _results(out, sizes)
     at = {}
     for name, n in sizes.items():
         if out.get(name) is not None:
@@ -1072,10 +1081,8 @@ def ttc_linear_attention(q, k, v, log_decay, *, cu_q=None, max_q=None, state=Non
     sequence.  scale defaults to dk^-1/2."""
     lib = load()
     a = _linear_attention(q, k, v, log_decay, cu_q, max_q, state, state_row, kv_len, scale, False)
-    y = last = None
-    if out:
-        y, last = out.get("out"), out.get("state")
-    out = dict(out) if out else {}
+    out = _results(out, ("out", "state"))
+    y, last = out.get("out"), out.get("state")
     if y is None:
         y = out["out"] = _new_like(v, stream)
         a.out_token, a.out_head = a.heads * a.dv, a.dv
@@ -1114,7 +1121,7 @@ def ttc_linear_attention_backward(q, k, v, log_decay, grad_out, *, cu_q=None, ma
     shapes = {"gq": (q.shape, q.dtype), "gk": (q.shape, q.dtype), "gv": (v.shape, q.dtype), "glog_decay": (log_decay.shape, torch.float32)}
     if state is not None:
         shapes["gstate"] = (each, torch.float32)
-    out = dict(out) if out else {}
+    out = _results(out, shapes)
     for name, (shape, dtype) in shapes.items():
         if out.get(name) is None:
             out[name] = _new(q, shape, dtype, stream)
@@ -1178,7 +1185,7 @@ def ttc_residual_norm(y, *, residual=None, gate=None, activation="silu", post=No
     residual itself."""
     n, _ = _residual_norm(y, residual, gate, activation, post, post_gain, post_offset, groups, post_eps, scale, residual_gain, pre, pre_gain, pre_offset,
                           pre_eps)
-    out = dict(out) if out else {}
+    out = _results(out, ("r",) if pre is None else ("r", "h"))
     for name in ("r", "h") if pre is not None else ("r",):
         if out.get(name) is None:
             out[name] = _new_like(y, stream) if y.is_contiguous() else _new(y, y.shape, y.dtype, stream)
@@ -1209,7 +1216,7 @@ def ttc_residual_norm_backward(y, *, grad_r=None, grad_h=None, residual=None, ga
     gr_token, gh_token = (0 if t is None else _rows_stride(t, name, y.shape, y.dtype) for name, t in (("grad_r", grad_r), ("grad_h", grad_h)))
     rows = {"gy": y, "ggate": gate, "gresidual": residual}
     wanted = [name for name, t in rows.items() if t is not None] + ["g" + name for name, t in vectors.items() if t is not None]
-    out = dict(out) if out else {}
+    out = _results(out, wanted)
     for name in wanted:
         shape, dtype = (y.shape, y.dtype) if name in rows else (y.shape[1:], torch.float32)
         if out.get(name) is None:
