@@ -24,7 +24,8 @@ extern "C" {
  * as -200, which leaves nothing of a finite state: -inf begins anew).  Head h has query and key head h / (heads / heads_qk).
  * Sequences are packed as in ttc_attention: sequence s has the rows cu_q[s] .. cu_q[s+1]-1, rows behind the last are left as they are.
  * dk and dv are multiples of 8 from 8 to 256; rows of tokens are at most 2^23 - 1 entries apart (in gradients
- * heads * max(dk, dv) too).  A launch counts 2^32 threads: (tokens / 64 + sequences) * heads below 2^23 with sequences * heads below 2^20 are always taken.
+ * heads * max(dk, dv) too).  A launch counts 2^32 threads: (tokens / 64 + sequences + 8) * heads below 2^23 with
+ * (sequences + 8) * heads below 2^20 are always taken.
  * States, sums and decays are float32 or wider.  bfloat16 rows, in gradients and where max_q is more than 6: what queries meet of the state, and the
  * products of queries and keys of one chunk of 64 tokens, are sums of two bfloat16 numbers for their products (2^-16 of each is lost); nothing
  * else but the results, gradients of decays included, is rounded to less than float32's 24 bits.
