@@ -65,7 +65,7 @@ ttc_status_t ttc_linear_attention(const ttc_linear_attention_t *attention, void 
  * not used.  gq, gk sum over the heads that share them; a glog_decay for g_token = 0 sums over all tokens (else it is one per token and
  * head).  gstate: with respect to the states that the sequences began with, 0 where a sequence began with zeros by rule.
  * A decay below -104, which leaves nothing of a state in float32, has the gradient 0; the others are sums over a sequence's tokens, 2^-24 of their terms off, and a
- * token's NaN or infinity may reach those of all tokens of its sequence and head (of gq, gk, gv those that depend on it).  No result may
+ * token's NaN or infinity may reach those of all tokens of its sequence and head (of gq, gk, gv those that depend on it; a decay's NaN any of them).  No result may
  * overlap another or anything that is read (TTC_ERR_INVALID_ARG): rows are read again after results have been written. */
 typedef struct {
   ttc_linear_attention_t forward;

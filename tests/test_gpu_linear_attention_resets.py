@@ -129,3 +129,34 @@ def test_a_decay_for_good_over_many_sequences(lengths, heads, heads_qk):
     got = call()
     backward.check(x, gout, first, glast, got)
     assert torch.equal(call()["glog_decay"], got["glog_decay"])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradients_of_strong_and_weak_decays_beside_each_other(dtype):
+    """-150 at every ninth token of one head, nothing fades in the second, a third forgets now and then and nothing else fades."""
+    length = 4 * CHUNK + 20
+    x, gout, first, glast = backward.gradient_inputs([length], 3, 3, 64, 64, dtype, False, 15, True)
+    g = x[3]
+    g[:, 0] = -1e-3
+    g[::9, 0] = -150.0
+    g[:, 1:] = 0.0
+    g[17::50, 2] = -float("inf")
+    got = binding.ttc_linear_attention_backward(*x[:4], gout, cu_q=x[4], max_q=length, state=first, grad_state=glast)
+    check_gradients(x, gout, first, glast, got)
+
+
+@pytest.mark.parametrize("length", [40, 3 * CHUNK + 7])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_decay_that_is_nan(length, dtype):
+    """It reaches its own and later tokens of its head forward; of the gradients no other head's and no other sequence's, and no query's before it."""
+    x, gout, first, glast = backward.gradient_inputs([length, 30], 2, 2, 64, 64, dtype, False, 16, True)
+    q, k, v, g, cu = x
+    call = lambda: binding.ttc_linear_attention_backward(q, k, v, g, gout, cu_q=cu, max_q=length, state=first, grad_state=glast)
+    want, at = call(), length // 2
+    g[at, 0] = float("nan")
+    got = call()
+    for result in ("gq", "gk", "gv", "glog_decay"):
+        assert torch.equal(got[result][:, 1], want[result][:, 1]) and torch.equal(got[result][length:], want[result][length:]), result
+    assert torch.equal(got["gq"][:at], want["gq"][:at]) and torch.isnan(got["gq"][at:length, 0]).all()
+    assert torch.isnan(got["gk"][:at, 0]).all() and torch.isnan(got["gv"][:at, 0]).all() and torch.isnan(got["glog_decay"][at, 0])
+    assert torch.equal(got["gstate"][1], want["gstate"][1]) and torch.equal(got["gstate"][0, 1], want["gstate"][0, 1])
