@@ -484,8 +484,8 @@ enum MemWhat { MEM_STATES, MEM_OUT, MEM_OUT_DOTS, MEM_OUT_PAIRS };
 // MEM_OUT_PAIRS: where the rows of results are keys and values (dv), a pair's product times that of the value and the result's gradient is its share of the
 // decays' gradients between the two tokens: added up by rows and by columns here, where all but one operand is in LDS (a kernel of its own took 38 us of
 // 250 for four times 2048 tokens of 16 heads of 128, this takes 17).
-// 16384 tokens of 32 heads of 128 x 128 over 8 of queries and keys, bfloat16: 135 us, in which the matrix instructions are busy for 26 % of the cycles, the vector
-// instructions for 40 %, LDS for 41 %: a workgroup's phases between its barriers need them by turns, and only two workgroups share a unit.
+// 16384 tokens of 32 heads of 128 x 128 over 8 of queries and keys, bfloat16: 164 us, in which the matrix instructions are busy for 29 % of the cycles, the vector
+// instructions for 46 %, LDS for 40 %: a workgroup's phases between its barriers need them by turns, and only two workgroups share a unit.
 // Twelve sequences of up to 1500 tokens, 16 heads of 64 x 64, float32: 75 us, matrix instructions 35 %.
 template <typename T, int DK, int WAVES, int WHAT>
 __global__ void __launch_bounds__(64 * WAVES, (MemShape<T, DK, WAVES>::RESIDENT)) memory_chunk_kernel(const MemTwo two) {
